@@ -43,8 +43,8 @@ def _sources():
 
 
 def _deps():
-    return _sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + [os.path.join(INCLUDE, "isjl_sim.h"),
-                                                                 os.path.abspath(__file__)]
+    return _sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(INCLUDE, "*.h")) + [
+        os.path.abspath(__file__)]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -1,0 +1,195 @@
+// kv.cu -- the C ABI of the decode step (include/isjl_kv.h): handle, checks, launches.
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <new>
+
+#include "kv_internal.cuh"
+
+struct isjl_kv {
+    isjl_kv_config cfg;
+    int sms = 0, shift = 0, grid = 0;
+    // one allocation: the status word, then the workspaces of assign and attend
+    unsigned char *d_work = nullptr;
+    int32_t *d_status = nullptr;
+    int32_t *d_first_take = nullptr, *d_first_back = nullptr;
+    uint32_t *d_arrived = nullptr;
+    float2 *d_part_ml = nullptr;
+    float *d_part_o = nullptr;
+    cudaStream_t last_stream = nullptr;
+    bool ran = false;
+};
+
+namespace {
+
+constexpr size_t kAlign = 256;
+size_t rounded(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0; }
+
+bool cache_ok(const isjl_kv_cache *c) {
+    if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return false;
+    for (int i = 0; i < 3; ++i)
+        if (!stride_ok(c->k_stride[i]) || !stride_ok(c->v_stride[i])) return false;
+    return true;
+}
+
+isjl_status launched(isjl_kv *kv, cudaError_t e, cudaStream_t st) {
+    if (e != cudaSuccess) return ISJL_ERR_CUDA;
+    kv->last_stream = st;
+    kv->ran = true;
+    return ISJL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
+    if (!out) return ISJL_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!cfg || cfg->n_blocks < 1 || cfg->block_size < 8 || cfg->block_size > 256 ||
+        (cfg->block_size & (cfg->block_size - 1)) != 0 || cfg->n_kv_heads < 1 || cfg->n_q_heads < cfg->n_kv_heads ||
+        cfg->n_q_heads > 1024 || cfg->n_q_heads % cfg->n_kv_heads != 0 ||
+        (cfg->head_dim != 64 && cfg->head_dim != 128 && cfg->head_dim != 256) ||
+        (cfg->type != ISJL_KV_BF16 && cfg->type != ISJL_KV_FP16) || cfg->max_rows < 1 || cfg->max_rows > (1 << 20))
+        return ISJL_ERR_INVALID_ARG;
+    isjl_kv *kv = new (std::nothrow) isjl_kv();
+    if (!kv) return ISJL_ERR_OOM;
+    kv->cfg = *cfg;
+    while ((1 << kv->shift) < cfg->block_size) ++kv->shift;
+    int device = 0;
+    const int queries = cfg->max_rows < ISJL_KV_MAX_ROWS ? cfg->max_rows : ISJL_KV_MAX_ROWS;
+    if (cudaGetDevice(&device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
+        isjl::attend_grid(cfg->head_dim, cfg->type, queries, kv->sms, &kv->grid) != cudaSuccess || kv->grid < 1) {
+        cudaGetLastError();
+        delete kv;
+        return ISJL_ERR_CUDA;
+    }
+    const size_t rows = rounded(sizeof(int32_t) * ((size_t)cfg->max_rows + 1));
+    const size_t arrived = rounded(sizeof(uint32_t) * kv->grid);
+    const size_t ml = rounded(sizeof(float2) * 32 * kv->grid), o = sizeof(float) * 32 * cfg->head_dim * (size_t)kv->grid;
+    const size_t zeroed = kAlign + arrived;
+    const size_t total = zeroed + 2 * rows + ml + o;
+    if (cudaMalloc(reinterpret_cast<void **>(&kv->d_work), total) != cudaSuccess) {
+        cudaGetLastError();
+        delete kv;
+        return ISJL_ERR_OOM;
+    }
+    unsigned char *p = kv->d_work;
+    kv->d_status = reinterpret_cast<int32_t *>(p);
+    p += kAlign;
+    kv->d_arrived = reinterpret_cast<uint32_t *>(p);
+    p += arrived;
+    kv->d_first_take = reinterpret_cast<int32_t *>(p);
+    p += rows;
+    kv->d_first_back = reinterpret_cast<int32_t *>(p);
+    p += rows;
+    kv->d_part_ml = reinterpret_cast<float2 *>(p);
+    p += ml;
+    kv->d_part_o = reinterpret_cast<float *>(p);
+    // calls may come on any stream: the zeros have to be there before create returns
+    if (cudaMemset(kv->d_work, 0, zeroed) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+        cudaGetLastError();
+        cudaFree(kv->d_work);
+        delete kv;
+        return ISJL_ERR_CUDA;
+    }
+    *out = kv;
+    return ISJL_OK;
+}
+
+void isjl_kv_destroy(isjl_kv *kv) {
+    if (!kv) return;
+    cudaDeviceSynchronize();
+    cudaFree(kv->d_work);
+    delete kv;
+}
+
+isjl_status isjl_kv_assign(isjl_kv *kv, const isjl_kv_assign_args *a, void *stream) {
+    if (!kv || !a || a->n_rows < 0 || a->n_rows > kv->cfg.max_rows || a->table_width < 1 ||
+        ((int64_t)a->table_width << kv->shift) > INT32_MAX || a->max_tokens < 1 || a->prefix_len < 0 ||
+        (int64_t)a->prefix_len + ((int64_t)a->table_width << kv->shift) > INT32_MAX ||
+        !a->free_list || !a->n_free || !a->n_free_out || !a->starts || !a->slots || !a->positions || !a->rows || !a->visible ||
+        (a->n_rows > 0 && (!a->lens || !a->new_tokens || !a->table || !a->lens_out || !a->granted)))
+        return ISJL_ERR_INVALID_ARG;
+    isjl::AssignArgs g;
+    std::memset(&g, 0, sizeof(g));
+    g.a = *a;
+    g.n_blocks = kv->cfg.n_blocks;
+    g.shift = kv->shift;
+    g.first_take = kv->d_first_take;
+    g.first_back = kv->d_first_back;
+    g.status = kv->d_status;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return launched(kv, isjl::launch_assign(g, kv->sms, st), st);
+}
+
+isjl_status isjl_kv_append(isjl_kv *kv, const isjl_kv_append_args *a, const isjl_kv_cache *cache, void *stream) {
+    if (!kv || !a || !cache_ok(cache) || a->n_tokens < 0 || a->rot < 0 || a->rot > kv->cfg.head_dim || a->rot % 16 != 0 ||
+        (a->interleaved != 0 && a->interleaved != 1) || !(a->eps >= 0.f) || !std::isfinite(a->eps))
+        return ISJL_ERR_INVALID_ARG;
+    if (a->n_tokens == 0) return ISJL_OK;
+    const int64_t q_row = (int64_t)kv->cfg.n_q_heads * kv->cfg.head_dim;
+    const int64_t row = q_row + 2 * (int64_t)kv->cfg.n_kv_heads * kv->cfg.head_dim;
+    if (!a->qkv || !a->q_out || !a->slots || !aligned16(a->qkv) || !aligned16(a->q_out) || !aligned16(a->q_weight) ||
+        !aligned16(a->k_weight) || a->qkv_stride < row || a->qkv_stride % 8 != 0 || a->q_out_stride < q_row ||
+        a->q_out_stride % 8 != 0 || (a->rot > 0 && (!a->rope || !a->positions || a->n_positions < 1 || !aligned16(a->rope))) ||
+        (a->q_out == a->qkv && a->q_out_stride != a->qkv_stride))
+        return ISJL_ERR_INVALID_ARG;
+    isjl::AppendArgs g;
+    std::memset(&g, 0, sizeof(g));
+    g.a = *a;
+    g.cache = *cache;
+    g.n_q_heads = kv->cfg.n_q_heads;
+    g.n_kv_heads = kv->cfg.n_kv_heads;
+    g.shift = kv->shift;
+    g.n_slots = (int64_t)kv->cfg.n_blocks << kv->shift;
+    g.status = kv->d_status;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return launched(kv, isjl::launch_append(g, kv->cfg.head_dim, kv->cfg.type, kv->sms, st), st);
+}
+
+isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl_kv_cache *cache, void *stream) {
+    const int most = !kv ? 0 : kv->cfg.max_rows < ISJL_KV_MAX_ROWS ? kv->cfg.max_rows : ISJL_KV_MAX_ROWS;
+    if (!kv || !a || !cache_ok(cache) || a->n < 0 || a->n > most || a->table_width < 1 || a->n_table_rows < 0 ||
+        a->n_prefix_blocks < 0 || ((int64_t)(a->table_width + (int64_t)a->n_prefix_blocks) << kv->shift) > INT32_MAX ||
+        (a->n_prefix_blocks > 0 && !a->prefix) || a->window < 0 || a->sinks < 0 || !(a->scale > 0.f) || !std::isfinite(a->scale))
+        return ISJL_ERR_INVALID_ARG;
+    if (a->n == 0) return ISJL_OK;
+    if (!a->q || !a->out || !a->lens || !a->table || !aligned16(a->q) || !aligned16(a->out) ||
+        (!a->rows && a->n > a->n_table_rows))
+        return ISJL_ERR_INVALID_ARG;
+    for (int i = 0; i < 2; ++i)
+        if (!stride_ok(a->q_stride[i]) || !stride_ok(a->out_stride[i])) return ISJL_ERR_INVALID_ARG;
+    isjl::AttendArgs g;
+    std::memset(&g, 0, sizeof(g));
+    g.a = *a;
+    if (a->window == 0) g.a.sinks = 0;
+    g.cache = *cache;
+    g.n_blocks = kv->cfg.n_blocks;
+    g.shift = kv->shift;
+    g.n_kv_heads = kv->cfg.n_kv_heads;
+    g.group = kv->cfg.n_q_heads / kv->cfg.n_kv_heads;
+    g.part_o = kv->d_part_o;
+    g.part_ml = kv->d_part_ml;
+    g.arrived = kv->d_arrived;
+    g.status = kv->d_status;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return launched(kv, isjl::launch_attend(g, kv->cfg.head_dim, kv->cfg.type, kv->grid, st), st);
+}
+
+isjl_status isjl_kv_status(isjl_kv *kv) {
+    if (!kv) return ISJL_ERR_INVALID_ARG;
+    if (!kv->ran) return ISJL_OK;
+    int32_t word = 0;
+    if (cudaMemcpyAsync(&word, kv->d_status, sizeof(word), cudaMemcpyDeviceToHost, kv->last_stream) != cudaSuccess ||
+        cudaMemsetAsync(kv->d_status, 0, sizeof(word), kv->last_stream) != cudaSuccess ||
+        cudaStreamSynchronize(kv->last_stream) != cudaSuccess)
+        return ISJL_ERR_CUDA;
+    return word ? ISJL_ERR_INVALID_ARG : ISJL_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,134 @@
+// kv_append.cu -- norms, position rotation and cache write of new tokens (isjl_kv_append).
+//
+// A head of D values is D / 8 threads of 8 values (16 bytes) each.  A thread keeps its place in the head and
+// goes over the token's heads, so that the angles and weights of that place are loaded once per token; the
+// sum of squares and the other half of a rotated pair come from the head's other threads by shuffles.  All
+// arithmetic is in 32 bits with one rounding at the end.  Bound by memory: 4 bytes a value.
+#include "kv_internal.cuh"
+
+namespace isjl {
+namespace {
+
+constexpr int kThreads = 128;
+
+template <typename T>
+__device__ __forceinline__ void load8(const void *p, float (&x)[8]) {
+    const uint4 w = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = Half<T>::unpack(u[i]);
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+
+template <int D, typename T>
+__global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendArgs g) {
+    constexpr int kLanes = D / 8, kHeads = kThreads / kLanes;   // threads of a head, heads at a time
+    const isjl_kv_append_args &a = g.a;
+    const int t = blockIdx.x, c = threadIdx.x % kLanes, part = threadIdx.x / kLanes;
+    const int hq = g.n_q_heads, hkv = g.n_kv_heads, heads = hq + 2 * hkv, half = a.rot / 2;
+    int64_t slot = a.slots[t];
+    int position = 0;
+    if (slot >= 0) {
+        position = a.rot ? a.positions[t] : 0;
+        if (slot >= g.n_slots || position < 0 || (a.rot && position >= a.n_positions)) {
+            if (threadIdx.x == 0) report(g.status);
+            slot = -1;
+        }
+    }
+    T *q_out = static_cast<T *>(a.q_out) + t * a.q_out_stride;
+    if (slot < 0) {
+        for (int i = threadIdx.x; i < hq * kLanes; i += kThreads)
+            reinterpret_cast<uint4 *>(q_out)[i] = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    const T *x_in = static_cast<const T *>(a.qkv) + t * a.qkv_stride;
+    const int64_t block = slot >> g.shift, place = slot & ((1 << g.shift) - 1);
+    T *k_out = static_cast<T *>(g.cache.k) + block * g.cache.k_stride[0] + place * g.cache.k_stride[1];
+    T *v_out = static_cast<T *>(g.cache.v) + block * g.cache.v_stride[0] + place * g.cache.v_stride[1];
+
+    // values 8 c .. 8 c + 7 of a head: their angles, and where their pairs are
+    const bool turns = 8 * c < a.rot;
+    float cosv[8], sinv[8];
+    const bool second = !a.interleaved && 8 * c >= half;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { cosv[i] = 1.f; sinv[i] = 0.f; }
+    if (turns) {
+        const float *angle = a.rope + (int64_t)position * a.rot;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int j = a.interleaved ? 4 * c + i / 2 : 8 * c + i - (second ? half : 0);
+            cosv[i] = angle[j];
+            sinv[i] = angle[half + j];
+        }
+    }
+    const int partner = turns && !a.interleaved ? (second ? c - half / 8 : c + half / 8) : c;
+    const int lane = threadIdx.x & 31, from = lane - (lane % kLanes) + partner;
+
+    // the same number of turns for every thread, so that whole warps take part in the shuffles
+    for (int h0 = 0; h0 < heads; h0 += kHeads) {
+        const int h = h0 + part;
+        const bool live = h < heads;
+        float x[8];
+        if (live) load8<T>(x_in + h * D + 8 * c, x);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        const bool is_v = h >= hq + hkv, is_k = !is_v && h >= hq;
+        const void *weight = is_v ? nullptr : is_k ? a.k_weight : a.q_weight;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
+#pragma unroll
+        for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
+        if (weight) {
+            float w[8];
+            load8<T>(static_cast<const T *>(weight) + 8 * c, w);
+            const float r = rsqrtf(sum * (1.f / D) + a.eps);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] *= r * w[i];
+        }
+        float y[8];
+        if (a.interleaved) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                y[i] = x[i] * cosv[i] - x[i + 1] * sinv[i];
+                y[i + 1] = x[i + 1] * cosv[i] + x[i] * sinv[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float other = __shfl_sync(~0u, x[i], from);
+                y[i] = x[i] * cosv[i] + (second ? other : -other) * sinv[i];
+            }
+        }
+        if (!live) continue;
+        uint4 w;
+        if (is_v || !turns) w = make_uint4(Half<T>::pack(x[0], x[1]), Half<T>::pack(x[2], x[3]),
+                                           Half<T>::pack(x[4], x[5]), Half<T>::pack(x[6], x[7]));
+        else w = make_uint4(Half<T>::pack(y[0], y[1]), Half<T>::pack(y[2], y[3]), Half<T>::pack(y[4], y[5]),
+                            Half<T>::pack(y[6], y[7]));
+        T *to = is_v ? v_out + (h - hq - hkv) * g.cache.v_stride[2]
+                     : is_k ? k_out + (h - hq) * g.cache.k_stride[2] : q_out + (int64_t)h * D;
+        *reinterpret_cast<uint4 *>(to + 8 * c) = w;
+    }
+}
+
+template <int D>
+cudaError_t launch_dim(const AppendArgs &g, int type, cudaStream_t st) {
+    if (type == ISJL_KV_BF16) append_kernel<D, __nv_bfloat16><<<g.a.n_tokens, kThreads, 0, st>>>(g);
+    else append_kernel<D, __half><<<g.a.n_tokens, kThreads, 0, st>>>(g);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_append(const AppendArgs &g, int head_dim, int type, int sms, cudaStream_t st) {
+    (void)sms;
+    return head_dim == 64 ? launch_dim<64>(g, type, st)
+         : head_dim == 128 ? launch_dim<128>(g, type, st) : launch_dim<256>(g, type, st);
+}
+
+}  // namespace isjl

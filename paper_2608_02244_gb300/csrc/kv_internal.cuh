@@ -1,0 +1,102 @@
+// kv_internal.cuh -- what the decode-step entry points (kv.cu) and their kernels share.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "isjl_kv.h"
+
+namespace isjl {
+
+// the 16-bit types of a cache: packing with one rounding, and the tensor instruction
+template <typename T>
+struct Half;
+
+template <>
+struct Half<__nv_bfloat16> {
+    using Pair = __nv_bfloat162;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<uint32_t *>(&v);
+    }
+    static __device__ __forceinline__ float2 unpack(uint32_t w) {
+        return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162 *>(&w));
+    }
+    // d += a (16 x 16, row) * b (16 x 8, column)
+    static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+                     "{%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+};
+
+template <>
+struct Half<__half> {
+    using Pair = __half2;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<uint32_t *>(&v);
+    }
+    static __device__ __forceinline__ float2 unpack(uint32_t w) {
+        return __half22float2(*reinterpret_cast<__half2 *>(&w));
+    }
+    static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+                     "{%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ void report(int32_t *status) { atomicOr(status, 1); }
+
+// ---- assign (kv_assign.cu)
+struct AssignArgs {
+    isjl_kv_assign_args a;
+    int32_t n_blocks, shift;      // block_size = 1 << shift
+    int32_t *first_take;          // [n_rows + 1] new blocks taken before each row, and in all
+    int32_t *first_back;          // [n_rows + 1] blocks given back before each row, and in all
+    int32_t *status;
+};
+cudaError_t launch_assign(const AssignArgs &a, int sms, cudaStream_t st);
+
+// ---- append (kv_append.cu)
+struct AppendArgs {
+    isjl_kv_append_args a;
+    isjl_kv_cache cache;
+    int32_t n_q_heads, n_kv_heads, shift;
+    int64_t n_slots;
+    int32_t *status;
+};
+cudaError_t launch_append(const AppendArgs &a, int head_dim, int type, int sms, cudaStream_t st);
+
+// ---- attend (kv_attend.cu)
+struct AttendArgs {
+    isjl_kv_attend_args a;
+    isjl_kv_cache cache;
+    int32_t n_blocks, shift, n_kv_heads, group;
+    int32_t own_first;            // 1: prefix tokens are done by others and merged, 0: read here
+    int32_t splits;               // pieces of the prefix part to merge (own_first)
+    const float *prefix_o;        // [splits][n][n_q_heads][head_dim], sums of exp2(s - m) v
+    const float2 *prefix_ml;      // [splits][n][n_q_heads], m and the sum of exp2(s - m)
+    float *part_o;                // [grid][2][16][head_dim] pieces of (query, key head) items
+    float2 *part_ml;              // [grid][2][16]
+    uint32_t *arrived;            // [grid], zero between calls
+    int32_t *status;
+};
+size_t attend_smem(int head_dim, int n);
+// blocks of one full wave for calls of up to max_rows queries
+cudaError_t attend_grid(int head_dim, int type, int max_rows, int sms, int *grid);
+cudaError_t launch_attend(const AttendArgs &a, int head_dim, int type, int grid, cudaStream_t st);
+
+}  // namespace isjl
