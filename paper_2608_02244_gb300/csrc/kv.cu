@@ -4,7 +4,7 @@
 #include <cstring>
 #include <new>
 
-#include "kv_internal.cuh"
+#include "kv_tma.cuh"
 
 struct isjl_kv {
     isjl_kv_config cfg;
@@ -16,6 +16,9 @@ struct isjl_kv {
     uint32_t *d_arrived = nullptr;
     float2 *d_part_ml = nullptr;
     float *d_part_o = nullptr;
+    float2 *d_prefix_ml = nullptr;       // null: this shape has no prefix kernel
+    float *d_prefix_o = nullptr;
+    void *encoder = nullptr;
     cudaStream_t last_stream = nullptr;
     bool ran = false;
 };
@@ -26,7 +29,8 @@ constexpr size_t kAlign = 256;
 size_t rounded(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0; }
+// what a copy's map can hold: less than 2^40 bytes
+bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0 && s < ((int64_t)1 << 39); }
 
 bool cache_ok(const isjl_kv_cache *c) {
     if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return false;
@@ -43,6 +47,35 @@ isjl_status launched(isjl_kv *kv, cudaError_t e, cudaStream_t st) {
 }
 
 }  // namespace
+
+namespace isjl {
+
+void *tensor_map_encoder() {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess) {
+        cudaGetLastError();
+        return nullptr;
+    }
+    return fn;
+}
+
+bool encode_cache(void *encoder, CUtensorMap *map, void *p, const int64_t *stride, int rows, int n_blocks, int shift, int n_kv_heads,
+                  int head_dim, int type) {
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    const cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)1 << shift, (cuuint64_t)n_kv_heads, (cuuint64_t)n_blocks};
+    const cuuint64_t strides[3] = {2 * (cuuint64_t)stride[1], 2 * (cuuint64_t)stride[2], 2 * (cuuint64_t)stride[0]};
+    const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, steps[4] = {1, 1, 1, 1};
+    return reinterpret_cast<Encode>(encoder)(
+               map, type == ISJL_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, p, dims, strides, box,
+               steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace isjl
 
 extern "C" {
 
@@ -72,7 +105,15 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
     const size_t arrived = rounded(sizeof(uint32_t) * kv->grid);
     const size_t ml = rounded(sizeof(float2) * 32 * kv->grid), o = sizeof(float) * 32 * cfg->head_dim * (size_t)kv->grid;
     const size_t zeroed = kAlign + arrived;
-    const size_t total = zeroed + 2 * rows + ml + o;
+    // pieces of the prefix part: an item of 256 rows lies in at most sms / items + 2 blocks
+    const bool shares = cfg->head_dim <= 128 && cfg->n_q_heads / cfg->n_kv_heads <= 128;
+    const size_t pieces = shares ? (size_t)kv->sms * 256 + 2 * (size_t)queries * cfg->n_q_heads : 0;
+    const size_t prefix_ml = rounded(sizeof(float2) * pieces), prefix_o = sizeof(float) * cfg->head_dim * pieces;
+    if (!(kv->encoder = isjl::tensor_map_encoder())) {
+        delete kv;
+        return ISJL_ERR_CUDA;
+    }
+    const size_t total = zeroed + 2 * rows + ml + rounded(o) + prefix_ml + prefix_o;
     if (cudaMalloc(reinterpret_cast<void **>(&kv->d_work), total) != cudaSuccess) {
         cudaGetLastError();
         delete kv;
@@ -90,6 +131,11 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
     kv->d_part_ml = reinterpret_cast<float2 *>(p);
     p += ml;
     kv->d_part_o = reinterpret_cast<float *>(p);
+    p += rounded(o);
+    if (shares) {
+        kv->d_prefix_ml = reinterpret_cast<float2 *>(p);
+        kv->d_prefix_o = reinterpret_cast<float *>(p + prefix_ml);
+    }
     // calls may come on any stream: the zeros have to be there before create returns
     if (cudaMemset(kv->d_work, 0, zeroed) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
         cudaGetLastError();
@@ -178,7 +224,30 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
     g.arrived = kv->d_arrived;
     g.status = kv->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return launched(kv, isjl::launch_attend(g, kv->cfg.head_dim, kv->cfg.type, kv->grid, st), st);
+    if (kv->d_prefix_o && a->n_prefix_blocks > 0 && a->window == 0) {
+        isjl::PrefixArgs p;
+        std::memset(&p, 0, sizeof(p));
+        p.tokens = a->n_prefix_blocks << kv->shift;
+        p.line = isjl::prefix_line(a->n, g.group, g.n_kv_heads, p.tokens, kv->sms);
+        p.q = a->q;
+        p.q_stride[0] = a->q_stride[0];
+        p.q_stride[1] = a->q_stride[1];
+        p.prefix = a->prefix;
+        p.part_o = kv->d_prefix_o;
+        p.part_ml = kv->d_prefix_ml;
+        p.status = kv->d_status;
+        p.scale = a->scale;
+        p.n = a->n;
+        p.n_blocks = g.n_blocks;
+        p.shift = g.shift;
+        p.n_kv_heads = g.n_kv_heads;
+        p.group = g.group;
+        g.line = p.line;
+        g.prefix_o = kv->d_prefix_o;
+        g.prefix_ml = kv->d_prefix_ml;
+        if (isjl::launch_prefix(p, *cache, kv->encoder, kv->cfg.head_dim, kv->cfg.type, st) != cudaSuccess) return ISJL_ERR_CUDA;
+    }
+    return launched(kv, isjl::launch_attend(g, kv->encoder, kv->cfg.head_dim, kv->cfg.type, kv->grid, st), st);
 }
 
 isjl_status isjl_kv_status(isjl_kv *kv) {
@@ -189,7 +258,7 @@ isjl_status isjl_kv_status(isjl_kv *kv) {
         cudaMemsetAsync(kv->d_status, 0, sizeof(word), kv->last_stream) != cudaSuccess ||
         cudaStreamSynchronize(kv->last_stream) != cudaSuccess)
         return ISJL_ERR_CUDA;
-    return word ? ISJL_ERR_INVALID_ARG : ISJL_OK;
+    return word & 2 ? ISJL_ERR_INTERNAL : word ? ISJL_ERR_INVALID_ARG : ISJL_OK;
 }
 
 }  // extern "C"

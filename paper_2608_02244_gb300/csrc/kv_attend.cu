@@ -9,7 +9,7 @@
 // are the 16 rows of a tensor instruction.  At an item's end the four warps join through shared memory, and
 // an item cut by the run's ends is joined by the last of its blocks to arrive, in their order, so that the
 // result does not depend on the order of arrival.
-#include "kv_internal.cuh"
+#include "kv_tma.cuh"
 
 namespace isjl {
 namespace {
@@ -22,20 +22,13 @@ template <int D>
 struct Shape {
     static constexpr int kStages = D == 64 ? 6 : 3;
     static constexpr int kBlocks = D == 256 ? 1 : 2;               // per SM
-    static constexpr int kRowBytes = 2 * D;
-    static constexpr int kSideBytes = kSlice * kRowBytes;          // keys (or values) of a slice
+    static constexpr int kHalves = D / 64;                         // rows of 128 bytes hold 64 values
+    static constexpr int kHalfBytes = kSlice * 128;
+    static constexpr int kSideBytes = kHalves * kHalfBytes;        // keys (or values) of a slice
     static constexpr int kRing = kWarps * kStages * 2 * kSideBytes;
-    static constexpr int kJoin = 2 * 16 * (D / 2) * 4;
-    static constexpr int kChunks = D / 8;                          // 16-byte pieces of a row
-    static constexpr int kPasses = kSlice * kChunks / 32;          // copies of a lane per side
+    static constexpr int kJoinRow = D + 8;                         // padded: 8 rows of a warp's store on all banks
+    static constexpr int kJoin = 2 * 8 * kJoinRow * 4;
 };
-
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void copy16(uint32_t to, const void *from, bool real) {
-    const int bytes = real ? 16 : 0;      // 0: the 16 bytes become zeros and nothing is read
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-}
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -63,7 +56,7 @@ __device__ __forceinline__ Sight sight(const AttendArgs &g, int t) {
     const int32_t prefix = a.n_prefix_blocks << g.shift;
     const bool bad = x > 0 && s.row >= 0 && (s.row >= a.n_table_rows || ((x - 1) >> g.shift) >= a.table_width);
     if (bad) report(g.status);
-    s.end = x <= 0 || s.row < 0 || bad ? 0 : x + (g.own_first ? 0 : prefix);
+    s.end = x <= 0 || s.row < 0 || bad ? 0 : x + (g.line.blocks ? 0 : prefix);
     s.lo = a.window && s.end > a.window ? s.end - a.window : 0;
     s.head = min((min(a.sinks, s.lo) + kTile - 1) / kTile, s.lo / kTile);
     s.tiles = max(1, s.head + (s.end + kTile - 1) / kTile - s.lo / kTile);
@@ -81,21 +74,28 @@ struct Place {
 };
 
 template <int D, typename T>
-__global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(const __grid_constant__ AttendArgs g) {
+__global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks)
+attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
     using S = Shape<D>;
     extern __shared__ __align__(1024) unsigned char smem[];
-    float *join = reinterpret_cast<float *>(smem + S::kRing);                        // [2][16][D / 2]
+    float *join = reinterpret_cast<float *>(smem + S::kRing);                        // [2][8][kJoinRow]
     float2 *stats = reinterpret_cast<float2 *>(smem + S::kRing + S::kJoin);          // [kWarps][16]
     float2 *row_stat = stats + kWarps * 16;                                          // [16]
     int32_t *before = reinterpret_cast<int32_t *>(row_stat + 16);                    // [n + 1] tiles before a query
     __shared__ int32_t warp_sum[kWarps];
     __shared__ int32_t last_one;
+    __shared__ __align__(8) uint64_t bars[kWarps * S::kStages];
 
     const isjl_kv_attend_args &a = g.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n = a.n, parts = (g.group + 15) / 16, H = g.n_kv_heads * parts, hq = g.n_kv_heads * g.group;
     const float scale = a.scale * kLog2e;
 
+    const uint32_t bar0 = smem_addr(bars) + warp * S::kStages * 8;
+    if (lane == 0) {
+        for (int i = 0; i < S::kStages; ++i) bar_init(bar0 + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     // ---- tiles before each query
     {
         const int per = (n + kThreads - 1) / kThreads;
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
 
     // ---- the ring
     const uint32_t ring = smem_addr(smem) + warp * S::kStages * 2 * S::kSideBytes;
-    const int32_t prefix_blocks = g.own_first ? 0 : a.n_prefix_blocks;
+    const int32_t prefix_blocks = g.line.blocks ? 0 : a.n_prefix_blocks;
     // block numbers of the slice's first and second 8 tokens, kNone where nothing of them is visible.  They
     // are asked for one tile ahead of the copies that use them, and looked at only there.
     auto blocks_of = [&](const Place &p, int32_t &b0, int32_t &b1) {
@@ -170,26 +170,29 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
             (k ? b1 : b0) = b;
         }
     };
-    const int chunk = lane % S::kChunks, row0 = lane / S::kChunks;
-    constexpr int kRowsPass = 32 / S::kChunks;
+    // one copy for the slice's rows of a block (16, or 8 of each of two blocks) and 64 of their values
     auto load = [&](const Place &p, int stage, int32_t b0, int32_t b1) {
-        if ((b0 != kNone && (uint32_t)b0 >= (uint32_t)g.n_blocks) || (b1 != kNone && (uint32_t)b1 >= (uint32_t)g.n_blocks))
-            report(g.status);
-        const int32_t x = tile_start(p.s, p.tile) + warp * kSlice;
+        const uint32_t bar = bar0 + 8 * stage;
+        if (b0 == kNone && b1 == kNone) {              // nothing to come: the stage's turn passes all the same
+            bar_arrive(bar);
+            return;
+        }
+        const int32_t slot = (tile_start(p.s, p.tile) + warp * kSlice) & ((1 << g.shift) - 1);
         const int kv = p.h / parts;
-        const T *kb = static_cast<const T *>(g.cache.k) + kv * g.cache.k_stride[2] + chunk * 8;
-        const T *vb = static_cast<const T *>(g.cache.v) + kv * g.cache.v_stride[2] + chunk * 8;
         const uint32_t to = ring + stage * 2 * S::kSideBytes;
-        const int32_t mask = (1 << g.shift) - 1;
+        bar_expect(bar, 2 * S::kSideBytes);
+        if (g.shift > 3 && b0 == kNone) b0 = b1;       // both halves are of one block
+        if ((uint32_t)b0 >= (uint32_t)g.n_blocks) { if (b0 != kNone) report(g.status); b0 = g.n_blocks; }   // beyond the cache: zeros
+        if (g.shift == 3 && (uint32_t)b1 >= (uint32_t)g.n_blocks) { if (b1 != kNone) report(g.status); b1 = g.n_blocks; }
 #pragma unroll
-        for (int i = 0; i < S::kPasses; ++i) {
-            const int r = i * kRowsPass + row0;
-            const int32_t y = x + r, b = i < S::kPasses / 2 ? b0 : b1;
-            const bool real = (uint32_t)b < (uint32_t)g.n_blocks && y < p.s.end && (y >= p.s.lo || y < a.sinks);
-            const int64_t bb = real ? b : 0, ss = real ? (y & mask) : 0;
-            const uint32_t at = to + r * S::kRowBytes + ((chunk ^ (r & 7)) << 4);
-            copy16(at, kb + bb * g.cache.k_stride[0] + ss * g.cache.k_stride[1], real);
-            copy16(at + S::kSideBytes, vb + bb * g.cache.v_stride[0] + ss * g.cache.v_stride[1], real);
+        for (int half = 0; half < S::kHalves; ++half) {
+            const uint32_t at = to + half * S::kHalfBytes;
+            tma_load(at, &kmap, bar, half * 64, slot, kv, b0);
+            tma_load(at + S::kSideBytes, &vmap, bar, half * 64, slot, kv, b0);
+            if (g.shift == 3) {
+                tma_load(at + 1024, &kmap, bar, half * 64, 0, kv, b1);
+                tma_load(at + S::kSideBytes + 1024, &vmap, bar, half * 64, 0, kv, b1);
+            }
         }
     };
 
@@ -198,14 +201,20 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
     int32_t b0, b1;
     blocks_of(ahead, b0, b1);
     auto feed = [&](int stage) {
-        if (fa < f1) {
-            load(ahead, stage, b0, b1);
-            if (++fa < f1) {
-                advance(ahead);
-                blocks_of(ahead, b0, b1);
+        if (fa >= f1) return;
+        if (lane == 0) load(ahead, stage, b0, b1);
+        if (++fa < f1) {
+            advance(ahead);
+            blocks_of(ahead, b0, b1);
+            if (ahead.tile == 0) {                     // the next item's queries
+                const int kv = ahead.h / parts, first = kv * g.group + (ahead.h - kv * parts) * 16;
+                const int live = min(16, (kv + 1) * g.group - first);
+                const T *qt = static_cast<const T *>(a.q) + ahead.t * a.q_stride[0] + first * a.q_stride[1];
+                if (warp == 0)
+                    for (int i = lane; i < live * (D / 64); i += 32)
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(qt + i / (D / 64) * a.q_stride[1] + i % (D / 64) * 64));
             }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
     for (int i = 0; i < S::kStages - 1; ++i) feed(i);
@@ -230,6 +239,28 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
             for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
         m[0] = m[1] = -INFINITY;
         l[0] = l[1] = 0.f;
+        if (!g.line.blocks || here.tile != 0 || here.s.end == 0) return;
+        // the prefix's pieces are where the item starts from, one warp each
+        const int item = kv * g.line.pairs + here.t / g.line.tokens_of_tile / 2;
+        const int pieces = g.line.last_block(item) - g.line.first_block(item) + 1;
+        for (int k = warp; k < pieces; k += kWarps) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (r + 8 * j >= live) continue;
+                const int64_t at = ((int64_t)k * n + here.t) * hq + first + r + 8 * j;
+                const float2 ml = g.prefix_ml[at];
+                const float next = fmaxf(m[j], ml.x), ref = next == -INFINITY ? 0.f : next;
+                const float fix = ex2(m[j] - ref), w = ex2(ml.x - ref);
+                m[j] = next;
+                l[j] = l[j] * fix + ((lane & 3) == 0 ? ml.y * w : 0.f);
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    const float2 v = *reinterpret_cast<const float2 *>(g.prefix_o + at * D + i * 8 + c);
+                    o[i][2 * j] = o[i][2 * j] * fix + v.x * w;
+                    o[i][2 * j + 1] = o[i][2 * j + 1] * fix + v.y * w;
+                }
+            }
+        }
     };
 
     auto compute = [&](int stage) {
@@ -240,11 +271,11 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
         {
             // lanes 0-7: tokens 0-7 low half of 16 values, 8-15: high half, 16-23: tokens 8-15 low, 24-31: high
             const int r = (lane & 7) + (lane >> 4) * 8, up = (lane >> 3) & 1;
-            const uint32_t at = base + r * S::kRowBytes;
+            const uint32_t at = base + r * 128, turn = (up ^ (r & 7)) << 4;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 uint32_t b[4];
-                ldsm4(b, at + (((2 * k + up) ^ (r & 7)) << 4));
+                ldsm4(b, at + (k / 4) * S::kHalfBytes + (turn ^ ((k % 4) << 5)));
                 Half<T>::mma(s[0], q[k], b[0], b[1]);
                 Half<T>::mma(s[1], q[k], b[2], b[3]);
             }
@@ -258,6 +289,14 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
                     const int32_t y = x + i * 8 + c + j;
                     if (y >= here.s.end || (y < here.s.lo && y >= a.sinks)) s[i][j] = s[i][2 + j] = -INFINITY;
                 }
+            // a weight of 0 does not silence an infinite or undefined value: what is not seen becomes 0
+            for (int i = lane; i < kSlice * S::kHalves * 8; i += 32) {
+                const int r = (i / 8) % kSlice;
+                if (x + r >= here.s.end || (x + r < here.s.lo && x + r >= a.sinks))
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + S::kSideBytes + (i / 8) * 128 + (i % 8) * 16), "r"(0) : "memory");
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before the next copy to this stage
+            __syncwarp();
         }
         float top[2];
 #pragma unroll
@@ -298,11 +337,11 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
                                Half<T>::pack(p[1][0], p[1][1]), Half<T>::pack(p[1][2], p[1][3])};
         {
             const int r = (lane & 7) + ((lane >> 3) & 1) * 8, up = lane >> 4;
-            const uint32_t at = base + S::kSideBytes + r * S::kRowBytes;
+            const uint32_t at = base + S::kSideBytes + r * 128, turn = (up ^ (r & 7)) << 4;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 uint32_t b[4];
-                ldsm4t(b, at + (((2 * k + up) ^ (r & 7)) << 4));
+                ldsm4t(b, at + (k / 4) * S::kHalfBytes + (turn ^ ((k % 4) << 5)));
                 Half<T>::mma(o[2 * k], w, b[0], b[1]);
                 Half<T>::mma(o[2 * k + 1], w, b[2], b[3]);
             }
@@ -315,9 +354,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
         const int live = min(16, (kv + 1) * g.group - first);
         const int64_t i0 = (int64_t)before[t] * H + (int64_t)here.h * here.s.tiles, i1 = i0 + here.s.tiles;
         const int64_t c0 = ((i0 + 1) * C - 1) / W, c1 = (i1 * C - 1) / W;         // its first and last block
-        const bool nothing = here.s.end == 0;
-        const int splits = nothing ? 0 : g.splits;
-        const bool whole = c0 == c1 && splits == 0;
+        const bool whole = c0 == c1;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             l[j] += __shfl_xor_sync(~0u, l[j], 1);
@@ -329,6 +366,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int r = (lane >> 2) + 8 * j;
+            if (8 * j >= live) break;
             float top = -INFINITY, sum = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stats[w * 16 + r].x);
@@ -342,36 +380,36 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
         T *out = static_cast<T *>(a.out) + t * a.out_stride[0] + first * a.out_stride[1];
         const int rr = lane >> 2, cc = (lane & 3) * 2;
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-            constexpr int kHalf = D / 2;
-            auto put = [&](bool add) {
-                float *to = join + (warp & 1) * 16 * kHalf;
+        for (int j = 0; j < 2; ++j) {                 // rows 8 j .. 8 j + 7
+            if (8 * j >= live) break;
+            float *to = join + (warp & 1) * 8 * S::kJoinRow + rr * S::kJoinRow + cc;
+            if (j) __syncthreads();                   // the first rows have been read
+            if (warp >= 2) {
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
+                for (int i = 0; i < D / 8; ++i)
+                    *reinterpret_cast<float2 *>(to + i * 8) = make_float2(o[i][2 * j] * mine[j], o[i][2 * j + 1] * mine[j]);
+            }
+            __syncthreads();
+            if (warp < 2) {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        float2 *at = reinterpret_cast<float2 *>(to + (rr + 8 * j) * kHalf + i * 8 + cc);
-                        float2 v = make_float2(o[hf * (D / 16) + i][2 * j] * mine[j], o[hf * (D / 16) + i][2 * j + 1] * mine[j]);
-                        if (add) { const float2 u = *at; v.x += u.x; v.y += u.y; }
-                        *at = v;
-                    }
+                for (int i = 0; i < D / 8; ++i) {
+                    float2 *at = reinterpret_cast<float2 *>(to + i * 8);
+                    const float2 u = *at;
+                    *at = make_float2(fmaf(o[i][2 * j], mine[j], u.x), fmaf(o[i][2 * j + 1], mine[j], u.y));
                 }
-            };
-            if (hf) __syncthreads();          // the first half has been read
-            if (warp >= 2) put(false);
+            }
             __syncthreads();
-            if (warp < 2) put(true);
-            __syncthreads();
-            for (int i = threadIdx.x; i < live * kHalf / 2; i += kThreads) {
-                const int r = i / (kHalf / 2), d = (i % (kHalf / 2)) * 2;
-                const float2 u = *reinterpret_cast<const float2 *>(join + r * kHalf + d);
-                const float2 v = *reinterpret_cast<const float2 *>(join + (16 + r) * kHalf + d);
-                float2 sum = make_float2(u.x + v.x, u.y + v.y);
+            for (int i = threadIdx.x; i < min(8, live - 8 * j) * (D / 4); i += kThreads) {
+                const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+                const float4 u = *reinterpret_cast<const float4 *>(join + r * S::kJoinRow + d);
+                const float4 v = *reinterpret_cast<const float4 *>(join + (8 + r) * S::kJoinRow + d);
+                const float4 sum = make_float4(u.x + v.x, u.y + v.y, u.z + v.z, u.w + v.w);
                 if (whole) {
-                    const float total = row_stat[r].y, inv = total > 0.f || total != total ? 1.f / total : 0.f;
-                    *reinterpret_cast<uint32_t *>(out + r * a.out_stride[1] + hf * kHalf + d) = Half<T>::pack(sum.x * inv, sum.y * inv);
+                    const float total = row_stat[8 * j + r].y, inv = total > 0.f || total != total ? 1.f / total : 0.f;
+                    *reinterpret_cast<uint2 *>(out + (8 * j + r) * a.out_stride[1] + d) =
+                        make_uint2(Half<T>::pack(sum.x * inv, sum.y * inv), Half<T>::pack(sum.z * inv, sum.w * inv));
                 } else {
-                    *reinterpret_cast<float2 *>(g.part_o + (mypart + r) * D + hf * kHalf + d) = sum;
+                    *reinterpret_cast<float4 *>(g.part_o + (mypart + 8 * j + r) * D + d) = sum;
                 }
             }
         }
@@ -388,6 +426,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
         __threadfence();
         __syncthreads();
         if (threadIdx.x == 0) {
+            // c0's count is that of the one item that begins in c0 and ends beyond it
             const uint32_t all = (uint32_t)(c1 - c0);
             const uint32_t seen = atomicAdd(g.arrived + c0, 1u);
             last_one = seen == all;
@@ -398,12 +437,10 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
         __threadfence();
         const int pieces = (int)(c1 - c0) + 1;
         auto piece = [&](int k) { return ((c0 + k) * 2 + (k == 0 ? 1 : 0)) * 16; };
-        auto prefix_at = [&](int k, int r) { return ((int64_t)k * n + t) * hq + first + r; };
         for (int i = threadIdx.x; i < live * (D / 4); i += kThreads) {
             const int r = i / (D / 4), d = (i % (D / 4)) * 4;
             float top = -INFINITY;
             for (int k = 0; k < pieces; ++k) top = fmaxf(top, __ldcg(&g.part_ml[piece(k) + r]).x);
-            for (int k = 0; k < splits; ++k) top = fmaxf(top, __ldcg(&g.prefix_ml[prefix_at(k, r)]).x);
             const float ref = top == -INFINITY ? 0.f : top;
             float total = 0.f;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -415,8 +452,6 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
                 sum.z += v.z * w;
                 sum.w += v.w * w;
             };
-            for (int k = 0; k < splits; ++k)
-                add(__ldcg(&g.prefix_ml[prefix_at(k, r)]), __ldcg(reinterpret_cast<const float4 *>(g.prefix_o + prefix_at(k, r) * D + d)));
 #pragma unroll 4
             for (int k = 0; k < pieces; ++k)
                 add(__ldcg(&g.part_ml[piece(k) + r]), __ldcg(reinterpret_cast<const float4 *>(g.part_o + (piece(k) + r) * D + d)));
@@ -429,25 +464,27 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks) attend_kernel(con
     };
 
     int stage = 0;
+    uint32_t phase = 0;
+    bool stuck = false;
     begin_item();
     for (int64_t f = f0; f < f1; ++f) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
-        __syncwarp();
+        __syncwarp();                                   // all have read the stage that is fed now
         feed(stage == 0 ? S::kStages - 1 : stage - 1);
+        if (!stuck && !bar_wait(bar0 + 8 * stage, phase)) stuck = true;
         compute(stage);
-        stage = stage + 1 == S::kStages ? 0 : stage + 1;
+        if (++stage == S::kStages) { stage = 0; phase ^= 1; }
         if (here.tile + 1 == here.s.tiles || f + 1 == f1) end_item();
         if (f + 1 < f1) {
             advance(here);
             if (here.tile == 0) begin_item();
         }
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (stuck) atomicOr(g.status, 2);
 }
 
 template <int D, typename T>
-cudaError_t launch_of(const AttendArgs &g, int grid, cudaStream_t st) {
-    attend_kernel<D, T><<<grid, kThreads, attend_smem(D, g.a.n), st>>>(g);
+cudaError_t launch_of(const AttendArgs &g, const CUtensorMap &k, const CUtensorMap &v, int grid, cudaStream_t st) {
+    attend_kernel<D, T><<<grid, kThreads, attend_smem(D, g.a.n), st>>>(g, k, v);
     return cudaGetLastError();
 }
 
@@ -480,12 +517,17 @@ cudaError_t attend_grid(int head_dim, int type, int max_rows, int sms, int *grid
          : head_dim == 128 ? grid_of<128, __half>(max_rows, sms, grid) : grid_of<256, __half>(max_rows, sms, grid);
 }
 
-cudaError_t launch_attend(const AttendArgs &g, int head_dim, int type, int grid, cudaStream_t st) {
+cudaError_t launch_attend(const AttendArgs &g, void *encoder, int head_dim, int type, int grid, cudaStream_t st) {
+    CUtensorMap k, v;
+    const int rows = g.shift == 3 ? 8 : kSlice;
+    if (!encode_cache(encoder, &k, g.cache.k, g.cache.k_stride, rows, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||
+        !encode_cache(encoder, &v, g.cache.v, g.cache.v_stride, rows, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type))
+        return cudaErrorInvalidValue;
     if (type == ISJL_KV_BF16)
-        return head_dim == 64 ? launch_of<64, __nv_bfloat16>(g, grid, st)
-             : head_dim == 128 ? launch_of<128, __nv_bfloat16>(g, grid, st) : launch_of<256, __nv_bfloat16>(g, grid, st);
-    return head_dim == 64 ? launch_of<64, __half>(g, grid, st)
-         : head_dim == 128 ? launch_of<128, __half>(g, grid, st) : launch_of<256, __half>(g, grid, st);
+        return head_dim == 64 ? launch_of<64, __nv_bfloat16>(g, k, v, grid, st)
+             : head_dim == 128 ? launch_of<128, __nv_bfloat16>(g, k, v, grid, st) : launch_of<256, __nv_bfloat16>(g, k, v, grid, st);
+    return head_dim == 64 ? launch_of<64, __half>(g, k, v, grid, st)
+         : head_dim == 128 ? launch_of<128, __half>(g, k, v, grid, st) : launch_of<256, __half>(g, k, v, grid, st);
 }
 
 }  // namespace isjl

@@ -17,6 +17,7 @@ struct Half;
 
 template <>
 struct Half<__nv_bfloat16> {
+    static constexpr bool kIsBf16 = true;
     using Pair = __nv_bfloat162;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -36,6 +37,7 @@ struct Half<__nv_bfloat16> {
 
 template <>
 struct Half<__half> {
+    static constexpr bool kIsBf16 = false;
     using Pair = __half2;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         __half2 v = __floats2half2_rn(lo, hi);
@@ -80,15 +82,41 @@ struct AppendArgs {
 };
 cudaError_t launch_append(const AppendArgs &a, int head_dim, int type, int sms, cudaStream_t st);
 
+// ---- a shared prefix computed once for the batch (kv_prefix.cu)
+
+// The line of (key head, pair of row tiles, token tile); a row tile holds the queries of whole tokens.
+struct PrefixLine {
+    int32_t tokens_of_tile, pairs, items, tiles;   // items: key heads x pairs, `tiles` token tiles each
+    int32_t blocks, pieces;                        // 0 blocks: there is no such part
+    __host__ __device__ int64_t work() const { return (int64_t)items * tiles; }
+    // the first and last block that an item's run of the line belongs to
+    __host__ __device__ int first_block(int item) const { return (int)((((int64_t)item * tiles + 1) * blocks - 1) / work()); }
+    __host__ __device__ int last_block(int item) const { return (int)((((int64_t)item + 1) * tiles * blocks - 1) / work()); }
+};
+
+struct PrefixArgs {
+    PrefixLine line;
+    const void *q;
+    int64_t q_stride[2];
+    const int32_t *prefix;
+    float *part_o;                // [pieces][n][n_q_heads][head_dim], sums of exp2(s - m) v
+    float2 *part_ml;              // [pieces][n][n_q_heads], m and the sum of exp2(s - m)
+    int32_t *status;
+    float scale;
+    int32_t n, tokens, n_blocks, shift, n_kv_heads, group;
+};
+void *tensor_map_encoder();       // null if the driver has none
+PrefixLine prefix_line(int n, int group, int n_kv_heads, int tokens, int sms);
+cudaError_t launch_prefix(const PrefixArgs &g, const isjl_kv_cache &cache, void *encoder, int head_dim, int type, cudaStream_t st);
+
 // ---- attend (kv_attend.cu)
 struct AttendArgs {
     isjl_kv_attend_args a;
     isjl_kv_cache cache;
     int32_t n_blocks, shift, n_kv_heads, group;
-    int32_t own_first;            // 1: prefix tokens are done by others and merged, 0: read here
-    int32_t splits;               // pieces of the prefix part to merge (own_first)
-    const float *prefix_o;        // [splits][n][n_q_heads][head_dim], sums of exp2(s - m) v
-    const float2 *prefix_ml;      // [splits][n][n_q_heads], m and the sum of exp2(s - m)
+    PrefixLine line;              // blocks > 0: the prefix's tokens are done by kv_prefix.cu and merged here
+    const float *prefix_o;
+    const float2 *prefix_ml;
     float *part_o;                // [grid][2][16][head_dim] pieces of (query, key head) items
     float2 *part_ml;              // [grid][2][16]
     uint32_t *arrived;            // [grid], zero between calls
@@ -97,6 +125,6 @@ struct AttendArgs {
 size_t attend_smem(int head_dim, int n);
 // blocks of one full wave for calls of up to max_rows queries
 cudaError_t attend_grid(int head_dim, int type, int max_rows, int sms, int *grid);
-cudaError_t launch_attend(const AttendArgs &a, int head_dim, int type, int grid, cudaStream_t st);
+cudaError_t launch_attend(const AttendArgs &a, void *encoder, int head_dim, int type, int grid, cudaStream_t st);
 
 }  // namespace isjl
