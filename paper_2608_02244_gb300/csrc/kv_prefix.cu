@@ -40,13 +40,21 @@ __device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t leading, uint3
            ((uint64_t)((stride >> 4) & 0x3fff) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-__device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((int)add) : "memory");
+// operands by the low word and the (common) high word of their descriptors
+__device__ __forceinline__ void mma_smem(uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t what, bool add) {
+    asm volatile("{\n.reg .pred p;\n.reg .b64 x, y;\nmov.b64 x, {%1, %3};\nmov.b64 y, {%2, %3};\nsetp.ne.b32 p, %5, 0;\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, p;\n}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(what), "r"((int)add) : "memory");
 }
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((int)add) : "memory");
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t what, bool add) {
+    asm volatile("{\n.reg .pred p;\n.reg .b64 y;\nmov.b64 y, {%2, %3};\nsetp.ne.b32 p, %5, 0;\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(what), "r"((int)add) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t mine;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(mine));
+    return mine != 0;
 }
 __device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -72,7 +80,7 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
 // barriers, in 8-byte words after the tiles
-enum { kFull = 0, kEmpty = 8, kScores = 16, kWeights = 18, kSums = 20, kQueries = 22, kBars = 24 };
+enum { kFull = 0, kEmpty = 8, kScores = 16, kWeights = 18, kSums = 20, kQueries = 22, kRest = 24, kBars = 26 };
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -101,6 +109,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
         for (int i = 0; i < 2; ++i) {
             bar_init(bar(kScores + i), 1);
             bar_init(bar(kWeights + i), 128);
+            bar_init(bar(kRest + i), 128);
             bar_init(bar(kSums + i), 1);
             bar_init(bar(kQueries + i), 128);
         }
@@ -131,12 +140,20 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
         const float scale = g.scale * kLog2e;
         uint32_t step = 0;
         int item_no = 0;
+        int stage = 0;                             // of the tile's keys; its values are in the next one
         bool ok = true;
         for (int64_t f = f0; f < f1 && ok;) {
             const int item = (int)(f / ln.tiles), j0 = (int)(f - (int64_t)item * ln.tiles);
             const int count = (int)min((int64_t)ln.tiles - j0, f1 - f), head = item / ln.pairs, pair = item % ln.pairs;
             f += count;
-            if (group == 1 && !two_of(pair)) continue;
+            const bool two = two_of(pair);
+            if (group == 1 && !two) {
+                stage = (stage + 2 * count) % S::kStages;
+                continue;
+            }
+            // The last group to use a tile frees its stages: when it sees its scores, the products of the keys are
+            // done, and those of the tile before's values, which were issued earlier.
+            const bool frees = (group == 1) == two && (threadIdx.x & 127) == 0;
             const int token = (2 * pair + group) * ln.tokens_of_tile + row / g.group, member = row % g.group;
             const bool live = row < ln.tokens_of_tile * g.group && token < g.n;
             const int q_head = head * g.group + member;
@@ -158,6 +175,12 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                 ok = __all_sync(~0u, bar_wait(bar(kScores + group), step & 1, failed));
                 if (!ok) break;
                 fence_after();
+                if (frees) {
+                    bar_arrive(bar(kEmpty + stage));
+                    if (j > 0) bar_arrive(bar(kEmpty + (stage == 0 ? S::kStages - 1 : stage - 1)));
+                }
+                stage += 2;
+                if (stage >= S::kStages) stage -= S::kStages;
                 uint32_t s[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_load(s[c], s_at + 32 * c);
@@ -206,16 +229,17 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                         p[i] = Half<T>::pack(x, y);
                     }
                     tmem_store(s_at + 32 * h, p);
+                    tmem_store_wait();
+                    fence_before();
+                    bar_arrive(bar((h ? kRest : kWeights) + group));      // the product starts with the first half
                 }
                 total += (part[0] + part[1]) + (part[2] + part[3]);
-                tmem_store_wait();
-                fence_before();
-                bar_arrive(bar(kWeights + group));
             }
             ok = ok && __all_sync(~0u, bar_wait(bar(kSums + group), item_no & 1, failed));
             if (!ok) break;
             fence_after();
             ++item_no;
+            if (frees) bar_arrive(bar(kEmpty + (stage == 0 ? S::kStages - 1 : stage - 1)));
             const int64_t at = ((int64_t)(blockIdx.x - ln.first_block(item)) * g.n + token) * (g.n_kv_heads * g.group) + q_head;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -236,85 +260,117 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
             // ---- keys and values: one copy for each cache block (or part of one) of a tile and 64 of its values
             const int rows = min(1 << g.shift, kKeys), pieces = kKeys / rows;      // pieces: 1 .. 16
             const uint32_t piece_bytes = rows * 128;
-            int load = 0;
+            // this lane's part of a tile: piece lane % pieces, and every 32 / pieces-th half
+            const int piece = lane % pieces;
+            auto block_of = [&](int j) {
+                const int token = j * kKeys + piece * rows;
+                return token < g.tokens ? g.prefix[token >> g.shift] : g.n_blocks;       // beyond the prefix: zeros
+            };
+            int load = 0, stage = 0;
+            uint32_t turn = 0;
             bool ok = true;
-            for (int64_t f = f0; f < f1 && ok; ++f) {
-                const int item = (int)(f / ln.tiles), j = (int)(f - (int64_t)item * ln.tiles), head = item / ln.pairs;
-                // this lane's part: piece lane % pieces, and every 32 / pieces-th half
-                const int piece = lane % pieces, token = j * kKeys + piece * rows;
-                int block = g.n_blocks, slot = 0;                      // beyond the cache: zeros
-                if (token < g.tokens) {
-                    block = g.prefix[token >> g.shift];
-                    slot = token & ((1 << g.shift) - 1);
-                    if ((uint32_t)block >= (uint32_t)g.n_blocks) { report(g.status); block = g.n_blocks; }
-                }
-                for (int side = 0; side < 2 && ok; ++side, ++load) {
-                    const int stage = load % S::kStages, turn = load / S::kStages;
-                    ok = turn == 0 || bar_wait(bar(kEmpty + stage), (turn - 1) & 1, failed);
-                    ok = __all_sync(~0u, ok);
-                    if (!ok) break;
-                    if (lane == 0) bar_expect(bar(kFull + stage), S::kTileBytes);
-                    __syncwarp();
-                    for (int half = lane / pieces; half < S::kHalves; half += 32 / pieces)
-                        tma_load(ring + stage * S::kTileBytes + half * S::kHalfBytes + piece * piece_bytes, side ? &vmap : &kmap,
-                                 bar(kFull + stage), half * 64, slot, head, block);
+            for (int64_t f = f0; f < f1 && ok;) {
+                const int item = (int)(f / ln.tiles), j0 = (int)(f - (int64_t)item * ln.tiles), head = item / ln.pairs;
+                const int count = (int)min((int64_t)ln.tiles - j0, f1 - f);
+                f += count;
+                int coming = block_of(j0);                             // asked for one tile ahead
+                for (int j = j0; j < j0 + count && ok; ++j) {
+                    int block = coming;
+                    const int slot = (j * kKeys + piece * rows) & ((1 << g.shift) - 1);
+                    if (j + 1 < j0 + count) coming = block_of(j + 1);
+                    if ((uint32_t)block > (uint32_t)g.n_blocks) { report(g.status); block = g.n_blocks; }
+                    for (int side = 0; side < 2; ++side) {
+                        ok = __all_sync(~0u, load < S::kStages || bar_wait(bar(kEmpty + stage), turn ^ 1, failed));
+                        if (!ok) break;
+                        if (lane == 0) bar_expect(bar(kFull + stage), S::kTileBytes);
+                        __syncwarp();
+                        for (int half = lane / pieces; half < S::kHalves; half += 32 / pieces)
+                            tma_load(ring + stage * S::kTileBytes + half * S::kHalfBytes + piece * piece_bytes, side ? &vmap : &kmap,
+                                     bar(kFull + stage), half * 64, slot, head, block);
+                        ++load;
+                        if (++stage == S::kStages) { stage = 0; turn ^= 1; }
+                    }
                 }
             }
             // nothing is left in flight, also after a failure
             for (int i = max(0, load - S::kStages); i < load; ++i) bar_wait(bar(kFull + i % S::kStages), (i / S::kStages) & 1, nullptr);
         } else if (warp == kIssueWarp) {
-            if (lane == 0) {
-                int load = 0;
-                uint32_t step[2] = {0, 0}, begun[2] = {0, 0};       // weights taken, items begun so far of each row tile
-                bool ok = true;
-                auto scores = [&](int i, int stage) {
-                    const uint32_t a = q_at + i * S::kTileBytes, b = ring + stage * S::kTileBytes;
-    #pragma unroll
+            // The whole warp runs this loop, so that addresses stay uniform, and one thread of it issues: with the
+            // products of 64 cycles each, their issue has to take less.
+            const bool one = elect_one();
+            uint32_t step[2] = {0, 0}, begun[2] = {0, 0};       // weights taken, items begun so far of each row tile
+            bool ok = tmem_base == 0;                            // all columns are ours: they begin at 0
+            // operands differ in their address field alone: low word plus 16-byte steps
+            const uint32_t q_lo = (uint32_t)operand(q_at, 16, 1024), k_lo = (uint32_t)operand(ring, 16, 1024);
+            const uint32_t v_lo = (uint32_t)operand(ring, S::kHalfBytes, 1024);
+            constexpr uint32_t high = (1024 >> 4) | (1u << 14) | (2u << 29);
+            auto scores = [&](int i, int stage) {
+                const uint32_t a = q_lo + i * (S::kTileBytes >> 4), b = k_lo + stage * (S::kTileBytes >> 4);
+                if (one) {
+#pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off = (k / 4) * S::kHalfBytes + (k % 4) * 32;
-                        mma_smem(tmem + i * 128, operand(a + off, 16, 1024), operand(b + off, 16, 1024), kFirst, k > 0);
+                        const uint32_t off = ((k / 4) * S::kHalfBytes + (k % 4) * 32) >> 4;
+                        mma_smem(i * 128, a + off, b + off, high, kFirst, k > 0);
                     }
                     commit(bar(kScores + i));
-                };
-                auto sums = [&](int i, int stage, bool add) {
-                    const uint32_t b = ring + stage * S::kTileBytes;
-    #pragma unroll
-                    for (int k = 0; k < kKeys / 16; ++k)
-                        mma_tmem(tmem + 256 + i * 128, tmem + i * 128 + k * 8, operand(b + k * 2048, S::kHalfBytes, 1024), kSecond, add || k > 0);
-                };
-                auto full = [&](int l) { return bar_wait(bar(kFull + l % S::kStages), (l / S::kStages) & 1, failed); };
-                for (int64_t f = f0; f < f1 && ok;) {
-                    const int item = (int)(f / ln.tiles), j0 = (int)(f - (int64_t)item * ln.tiles);
-                    const int count = (int)min((int64_t)ln.tiles - j0, f1 - f), groups = two_of(item % ln.pairs) ? 2 : 1;
-                    ok = full(load);
-                    for (int i = 0; i < groups && ok; ++i) {
-                        ok = bar_wait(bar(kQueries + i), begun[i] & 1, failed);
-                        if (!ok) break;
-                        ++begun[i];
-                        fence_after();
-                        scores(i, load % S::kStages);
-                    }
-                    if (!ok) break;
-                    commit(bar(kEmpty + load % S::kStages));
-                    for (int j = 0; j < count && ok; ++j, load += 2) {
-                        const int v = load + 1, next = load + 2;
-                        const bool more = j + 1 < count;
-                        ok = full(v) && (!more || full(next));
-                        for (int i = 0; i < groups && ok; ++i) {
-                            ok = bar_wait(bar(kWeights + i), step[i] & 1, failed);
-                            if (!ok) break;
-                            ++step[i];
-                            fence_after();
-                            sums(i, v % S::kStages, j > 0);
-                            if (i + 1 == groups) commit(bar(kEmpty + v % S::kStages));
-                            if (more) scores(i, next % S::kStages);
-                            else commit(bar(kSums + i));
-                        }
-                        if (ok && more) commit(bar(kEmpty + next % S::kStages));
-                    }
-                    f += count;
                 }
+            };
+            auto sums = [&](int i, int stage, int half, bool add) {
+                const uint32_t b = v_lo + stage * (S::kTileBytes >> 4), a = i * 128, d = 256 + i * 128;
+                constexpr int kSteps = kKeys / 32;
+                if (one) {
+#pragma unroll
+                    for (int k = 0; k < kSteps; ++k)
+                        mma_tmem(d, a + (half * kSteps + k) * 8, b + (half * kSteps + k) * (2048 >> 4), high, kSecond, add || half + k > 0);
+                }
+            };
+            auto wait = [&](int b, uint32_t phase) { ok = ok && __all_sync(~0u, bar_wait(bar(b), phase, failed)); };
+            int k_at = 0, v_at = 1;                              // stages of the tile's keys and values, and their turns
+            uint32_t k_turn = 0, v_turn = 0;
+            auto next = [&](int &at, uint32_t &turn) {
+                at += 2;
+                if (at >= S::kStages) { at -= S::kStages; turn ^= 1; }
+            };
+            for (int64_t f = f0; f < f1 && ok;) {
+                const int item = (int)(f / ln.tiles), j0 = (int)(f - (int64_t)item * ln.tiles);
+                const int count = (int)min((int64_t)ln.tiles - j0, f1 - f), groups = two_of(item % ln.pairs) ? 2 : 1;
+                wait(kFull + k_at, k_turn);
+                for (int i = 0; i < groups && ok; ++i) {
+                    wait(kQueries + i, begun[i]++ & 1);
+                    if (!ok) break;
+                    fence_after();
+                    scores(i, k_at);
+                }
+                if (!ok) break;
+                next(k_at, k_turn);
+                for (int j = 0; j < count && ok; ++j) {
+                    const bool more = j + 1 < count;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (i >= groups) break;
+                        
+                        // one wait for weights and (before the first row tile's) copies: a lane for each barrier
+                        const bool copies = lane == 1 && i == 0;
+                        wait(copies ? kFull + v_at : kWeights + i, copies ? v_turn : step[i] & 1);
+                        if (!ok) break;
+                        fence_after();
+                        
+                        sums(i, v_at, 0, j > 0);
+                        wait(copies && more ? kFull + k_at : kRest + i, copies && more ? k_turn : step[i] & 1);
+                        ++step[i];
+                        if (!ok) break;
+                        fence_after();
+                        sums(i, v_at, 1, true);
+                        if (more) scores(i, k_at);
+                        else if (one) commit(bar(kSums + i));
+                        
+                    }
+                    next(v_at, v_turn);
+                    if (more) next(k_at, k_turn);
+                }
+                f += count;
             }
+            if (!ok) *failed = 1;
             __syncwarp();
         }
     }
