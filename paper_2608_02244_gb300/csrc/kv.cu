@@ -102,8 +102,9 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
         return ISJL_ERR_CUDA;
     }
     const size_t rows = rounded(sizeof(int32_t) * ((size_t)cfg->max_rows + 1));
-    const size_t arrived = rounded(sizeof(uint32_t) * kv->grid);
-    const size_t ml = rounded(sizeof(float2) * 32 * kv->grid), o = sizeof(float) * 32 * cfg->head_dim * (size_t)kv->grid;
+    const size_t warps = (size_t)kv->grid * isjl::kAttendWarps;
+    const size_t arrived = rounded(sizeof(uint32_t) * warps);
+    const size_t ml = rounded(sizeof(float2) * 32 * warps), o = sizeof(float) * 32 * cfg->head_dim * warps;
     const size_t zeroed = kAlign + arrived;
     // pieces of the prefix part: an item of 256 rows lies in at most sms / items + 2 blocks
     const bool shares = cfg->head_dim <= 128 && cfg->n_q_heads / cfg->n_kv_heads <= 128;

@@ -1,33 +1,32 @@
 // kv_attend.cu -- attention of single queries over paged tokens (isjl_kv_attend).
 //
 // A step reads every visible key and value once and does 4 D operations a query head with each: bound by
-// memory.  The work is a line of tiles of 64 tokens: for each query, each key head (and each 16 of its query
-// heads), its visible tiles in order, the first tokens' before the window's.  Every block of the grid gets an
-// equal run of that line wherever requests end, so ragged batches keep all SMs loading to the end.  A warp
-// takes 16 tokens of each tile through a ring of its own of asynchronous copies (no block barrier while an
-// item lasts), with the running maximum and sum of a softmax over its tokens; the query heads of a key head
-// are the 16 rows of a tensor instruction.  At an item's end the four warps join through shared memory, and
-// an item cut by the run's ends is joined by the last of its blocks to arrive, in their order, so that the
-// result does not depend on the order of arrival.
+// memory.  The work is a line of slices of 32 tokens: for each query, each key head (and each 16 of its query
+// heads), its visible slices in order, the first tokens' before the window's.  Every warp of the grid gets an
+// equal run of that line wherever requests end, so ragged batches keep all SMs loading to the end.  A warp's
+// slices come by TMA through a ring of its own and no warp waits for another: the running maximum and sum of
+// the softmax, the sums and an item's result are the warp's own, and while one is between items the others
+// keep the memory busy.  The query heads of a key head are the 16 rows of a tensor instruction.  An item cut
+// by the runs' ends leaves pieces, which the last of their owners to arrive joins in their order, so that the
+// result does not depend on the order of arrival; pieces of neighbouring warps are joined in shared memory first.
 #include "kv_tma.cuh"
 
 namespace isjl {
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kSlice = 16, kTile = kWarps * kSlice;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr int32_t kNone = INT32_MIN;
+constexpr int kWarps = kAttendWarps, kThreads = 32 * kWarps, kSlice = 32;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <int D>
 struct Shape {
-    static constexpr int kStages = D == 64 ? 6 : 3;
+    static constexpr int kStages = D == 64 ? 6 : 3;                // of a warp's ring: keys or values of a slice
     static constexpr int kBlocks = D == 256 ? 1 : 2;               // per SM
     static constexpr int kHalves = D / 64;                         // rows of 128 bytes hold 64 values
     static constexpr int kHalfBytes = kSlice * 128;
-    static constexpr int kSideBytes = kHalves * kHalfBytes;        // keys (or values) of a slice
-    static constexpr int kRing = kWarps * kStages * 2 * kSideBytes;
+    static constexpr int kStageBytes = kHalves * kHalfBytes;
+    static constexpr int kRing = kWarps * kStages * kStageBytes;
     static constexpr int kJoinRow = D + 8;                         // padded: 8 rows of a warp's store on all banks
-    static constexpr int kJoin = 2 * 8 * kJoinRow * 4;
+    static_assert(kWarps * 16 * kJoinRow * 4 <= kRing, "the joined pieces take the ring's place");
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
@@ -43,8 +42,8 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t at) {
 // what a query sees: tokens end - window .. end - 1 and 0 .. sinks - 1, counted from the first token that
 // this kernel reads (the prefix's, or the own ones' where the prefix is done elsewhere)
 struct Sight {
-    int32_t end, lo, head;     // head: tiles with first tokens that lie before the window's first tile
-    int32_t tiles;             // at least 1: an item without tokens still has a result
+    int32_t end, lo, head;     // head: slices with first tokens that lie before the window's first slice
+    int32_t slices;            // at least 1: an item without tokens still has a result
     int32_t row;
 };
 
@@ -58,18 +57,19 @@ __device__ __forceinline__ Sight sight(const AttendArgs &g, int t) {
     if (bad) report(g.status);
     s.end = x <= 0 || s.row < 0 || bad ? 0 : x + (g.line.blocks ? 0 : prefix);
     s.lo = a.window && s.end > a.window ? s.end - a.window : 0;
-    s.head = min((min(a.sinks, s.lo) + kTile - 1) / kTile, s.lo / kTile);
-    s.tiles = max(1, s.head + (s.end + kTile - 1) / kTile - s.lo / kTile);
+    s.head = min((min(a.sinks, s.lo) + kSlice - 1) / kSlice, s.lo / kSlice);
+    s.slices = max(1, s.head + (s.end + kSlice - 1) / kSlice - s.lo / kSlice);
     return s;
 }
 
-__device__ __forceinline__ int32_t tile_start(const Sight &s, int tile) {
-    return (tile < s.head ? tile : s.lo / kTile + tile - s.head) * kTile;
+// first token of a query's slice
+__device__ __forceinline__ int32_t slice_start(const Sight &s, int i) {
+    return (i < s.head ? i : s.lo / kSlice + i - s.head) * kSlice;
 }
 
-// place on the line of tiles
+// place on the line of slices
 struct Place {
-    int t, h, tile;
+    int t, h, i;
     Sight s;
 };
 
@@ -78,12 +78,11 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks)
 attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
     using S = Shape<D>;
     extern __shared__ __align__(1024) unsigned char smem[];
-    float *join = reinterpret_cast<float *>(smem + S::kRing);                        // [2][8][kJoinRow]
-    float2 *stats = reinterpret_cast<float2 *>(smem + S::kRing + S::kJoin);          // [kWarps][16]
-    float2 *row_stat = stats + kWarps * 16;                                          // [16]
-    int32_t *before = reinterpret_cast<int32_t *>(row_stat + 16);                    // [n + 1] tiles before a query
+    float2 *stats = reinterpret_cast<float2 *>(smem + S::kRing);                     // [kWarps][16]
+    int32_t *before = reinterpret_cast<int32_t *>(stats + kWarps * 16);              // [n + 1] slices before a query
     __shared__ int32_t warp_sum[kWarps];
-    __shared__ int32_t last_one;
+    __shared__ int64_t cut[kWarps];           // where on the line the item begins that a warp's run leaves cut, or -1
+    __shared__ int32_t complete[kWarps];
     __shared__ __align__(8) uint64_t bars[kWarps * S::kStages];
 
     const isjl_kv_attend_args &a = g.a;
@@ -96,13 +95,13 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         for (int i = 0; i < S::kStages; ++i) bar_init(bar0 + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    // ---- tiles before each query
+    // ---- slices before each query
     {
         const int per = (n + kThreads - 1) / kThreads;
         const int begin = min(n, (int)threadIdx.x * per), end = min(n, begin + per);
         int32_t sum = 0;
         for (int t = begin; t < end; ++t) {
-            const int32_t k = sight(g, t).tiles;
+            const int32_t k = sight(g, t).slices;
             before[t] = k;
             sum += k;
         }
@@ -125,95 +124,76 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         __syncthreads();
     }
     const int64_t W = (int64_t)before[n] * H;
-    const int64_t C = min((int64_t)gridDim.x, W);
-    const int64_t me = blockIdx.x;
-    if (me >= C) return;
-    const int64_t f0 = W * me / C, f1 = W * (me + 1) / C;
+    const int64_t C = min((int64_t)gridDim.x * kWarps, W);               // warps with work
+    const int64_t me = (int64_t)blockIdx.x * kWarps + warp;
+    if ((int64_t)blockIdx.x * kWarps >= C) return;
+    const int64_t f0 = me < C ? W * me / C : W, f1 = me < C ? W * (me + 1) / C : W;
 
-    auto place_at = [&](int64_t f) {
-        Place p;
-        int lo = 0, hi = n;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if ((int64_t)before[mid] * H <= f) lo = mid; else hi = mid;
-        }
-        p.t = lo;
-        p.s = sight(g, lo);
-        const int32_t rest = (int32_t)(f - (int64_t)before[lo] * H);
-        p.h = rest / p.s.tiles;
-        p.tile = rest - p.h * p.s.tiles;
-        return p;
-    };
     auto advance = [&](Place &p) {
-        if (++p.tile < p.s.tiles) return;
-        p.tile = 0;
+        if (++p.i < p.s.slices) return;
+        p.i = 0;
         if (++p.h < H) return;
         p.h = 0;
         if (++p.t < n) p.s = sight(g, p.t);
     };
 
-    // ---- the ring
-    const uint32_t ring = smem_addr(smem) + warp * S::kStages * 2 * S::kSideBytes;
+    // ---- the ring: keys and values of a slice, one stage each.  A lane has one copy of a stage: the rows of one
+    // of the slice's blocks (or of the slice, in a larger block) and 64 of their values.
+    const uint32_t ring = smem_addr(smem) + warp * S::kStages * S::kStageBytes;
     const int32_t prefix_blocks = g.line.blocks ? 0 : a.n_prefix_blocks;
-    // block numbers of the slice's first and second 8 tokens, kNone where nothing of them is visible.  They
-    // are asked for one tile ahead of the copies that use them, and looked at only there.
-    auto blocks_of = [&](const Place &p, int32_t &b0, int32_t &b1) {
-        const int32_t x = tile_start(p.s, p.tile) + warp * kSlice;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int32_t y = x + 8 * k;
-            int32_t b = kNone;
-            if (y < p.s.end && (y + 8 > p.s.lo || y < a.sinks)) {
-                const int32_t j = y >> g.shift;
-                b = j < prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - prefix_blocks)];
-            }
-            (k ? b1 : b0) = b;
-        }
-    };
-    // one copy for the slice's rows of a block (16, or 8 of each of two blocks) and 64 of their values
-    auto load = [&](const Place &p, int stage, int32_t b0, int32_t b1) {
-        const uint32_t bar = bar0 + 8 * stage;
-        if (b0 == kNone && b1 == kNone) {              // nothing to come: the stage's turn passes all the same
-            bar_arrive(bar);
-            return;
-        }
-        const int32_t slot = (tile_start(p.s, p.tile) + warp * kSlice) & ((1 << g.shift) - 1);
-        const int kv = p.h / parts;
-        const uint32_t to = ring + stage * 2 * S::kSideBytes;
-        bar_expect(bar, 2 * S::kSideBytes);
-        if (g.shift > 3 && b0 == kNone) b0 = b1;       // both halves are of one block
-        if ((uint32_t)b0 >= (uint32_t)g.n_blocks) { if (b0 != kNone) report(g.status); b0 = g.n_blocks; }   // beyond the cache: zeros
-        if (g.shift == 3 && (uint32_t)b1 >= (uint32_t)g.n_blocks) { if (b1 != kNone) report(g.status); b1 = g.n_blocks; }
-#pragma unroll
-        for (int half = 0; half < S::kHalves; ++half) {
-            const uint32_t at = to + half * S::kHalfBytes;
-            tma_load(at, &kmap, bar, half * 64, slot, kv, b0);
-            tma_load(at + S::kSideBytes, &vmap, bar, half * 64, slot, kv, b0);
-            if (g.shift == 3) {
-                tma_load(at + 1024, &kmap, bar, half * 64, 0, kv, b1);
-                tma_load(at + S::kSideBytes + 1024, &vmap, bar, half * 64, 0, kv, b1);
-            }
-        }
+    const int rows_shift = min(g.shift, 5), half = lane % S::kHalves, piece = lane / S::kHalves;
+    const bool copies = piece < (kSlice >> rows_shift);
+    const uint32_t copy_at = ring + half * S::kHalfBytes + ((piece << rows_shift) << 7);
+    // the number of this lane's block, asked for one slice ahead of the copies that use it and looked at only there
+    constexpr int32_t kNone = INT32_MIN;
+    auto block_of = [&](const Place &p) {
+        const int32_t y = slice_start(p.s, p.i) + (piece << rows_shift);
+        if (!copies || y >= p.s.end || (y + (1 << rows_shift) <= p.s.lo && y >= a.sinks)) return kNone;   // nothing is seen of it
+        const int32_t j = y >> g.shift;
+        return j < prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - prefix_blocks)];
     };
 
-    Place ahead = place_at(f0), here = ahead;
-    int64_t fa = f0;
-    int32_t b0, b1;
-    blocks_of(ahead, b0, b1);
+    Place here;
+    here.t = here.h = here.i = 0;
+    if (f0 < f1) {
+        int lo = 0, hi = n;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((int64_t)before[mid] * H <= f0) lo = mid; else hi = mid;
+        }
+        here.t = lo;
+        here.s = sight(g, lo);
+        const int32_t rest = (int32_t)(f0 - (int64_t)before[lo] * H);
+        here.h = rest / here.s.slices;
+        here.i = rest - here.h * here.s.slices;
+    }
+    Place ahead = here;
+    int64_t ahead_left = f1 - f0;                      // slices whose values are still to be asked for
+    bool ahead_values = false;                         // what is next: keys or values
+    int32_t ahead_block = f0 < f1 ? block_of(ahead) : kNone;
     auto feed = [&](int stage) {
-        if (fa >= f1) return;
-        if (lane == 0) load(ahead, stage, b0, b1);
-        if (++fa < f1) {
-            advance(ahead);
-            blocks_of(ahead, b0, b1);
-            if (ahead.tile == 0) {                     // the next item's queries
-                const int kv = ahead.h / parts, first = kv * g.group + (ahead.h - kv * parts) * 16;
-                const int live = min(16, (kv + 1) * g.group - first);
-                const T *qt = static_cast<const T *>(a.q) + ahead.t * a.q_stride[0] + first * a.q_stride[1];
-                if (warp == 0)
-                    for (int i = lane; i < live * (D / 64); i += 32)
-                        asm volatile("prefetch.global.L2 [%0];" ::"l"(qt + i / (D / 64) * a.q_stride[1] + i % (D / 64) * 64));
-            }
+        if (ahead_left == 0) return;
+        const uint32_t bar = bar0 + 8 * stage;
+        int32_t block = ahead_block;
+        if ((uint32_t)block >= (uint32_t)g.n_blocks) {                 // beyond the cache: zeros
+            if (block != kNone) report(g.status);
+            block = g.n_blocks;
+        }
+        if (lane == 0) bar_expect(bar, S::kStageBytes);
+        if (copies)
+            tma_load(copy_at + stage * S::kStageBytes, ahead_values ? &vmap : &kmap, bar, half * 64,
+                     slice_start(ahead.s, ahead.i) & ((1 << g.shift) - 1) & ~((1 << rows_shift) - 1), ahead.h / parts, block);
+        ahead_values = !ahead_values;
+        if (ahead_values) return;
+        if (--ahead_left == 0) return;
+        advance(ahead);
+        ahead_block = block_of(ahead);
+        if (ahead.i == 0) {                            // the next item's queries
+            const int kv = ahead.h / parts, from = kv * g.group + (ahead.h - kv * parts) * 16;
+            const int rows = min(16, (kv + 1) * g.group - from);
+            const T *qt = static_cast<const T *>(a.q) + ahead.t * a.q_stride[0] + from * a.q_stride[1];
+            for (int i = lane; i < rows * (D / 64); i += 32)
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(qt + i / (D / 64) * a.q_stride[1] + i % (D / 64) * 64));
         }
     };
 #pragma unroll
@@ -221,11 +201,44 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
 
     uint32_t q[D / 16][4];
     float o[D / 8][4], m[2], l[2];
+    int first = 0, live = 0;                           // query heads of the item
+    const int r = lane >> 2, c = (lane & 3) * 2;       // this lane's rows r and r + 8, its columns 8 i + c and + 1
     auto begin_item = [&]() {
-        const int kv = here.h / parts, first = kv * g.group + (here.h - kv * parts) * 16;
-        const int live = min(16, (kv + 1) * g.group - first);
+        const int kv = here.h / parts;
+        first = kv * g.group + (here.h - kv * parts) * 16;
+        live = min(16, (kv + 1) * g.group - first);
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+        m[0] = m[1] = -INFINITY;
+        l[0] = l[1] = 0.f;
+        if (g.line.blocks && here.i == 0 && here.s.end > 0) {
+            // the prefix's pieces are where the item starts from
+            const int item = kv * g.line.pairs + here.t / g.line.tokens_of_tile / 2;
+            const int pieces = g.line.last_block(item) - g.line.first_block(item) + 1;
+            const int64_t step = (int64_t)n * hq;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (r + 8 * j >= live) continue;
+                const int64_t at = (int64_t)here.t * hq + first + r + 8 * j;
+                for (int k = 0; k < pieces; ++k) {
+                    const float2 ml = g.prefix_ml[at + k * step];
+                    const float next = fmaxf(m[j], ml.x), ref = next == -INFINITY ? 0.f : next;
+                    const float fix = ex2(m[j] - ref), w = ex2(ml.x - ref);
+                    m[j] = next;
+                    l[j] = l[j] * fix + ((lane & 3) == 0 ? ml.y * w : 0.f);
+                    const float *from = g.prefix_o + (at + k * step) * D + c;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        const float2 v = *reinterpret_cast<const float2 *>(from + i * 8);
+                        o[i][2 * j] = o[i][2 * j] * fix + v.x * w;
+                        o[i][2 * j + 1] = o[i][2 * j + 1] * fix + v.y * w;
+                    }
+                }
+            }
+        }
         const T *qt = static_cast<const T *>(a.q) + here.t * a.q_stride[0] + first * a.q_stride[1];
-        const int r = lane >> 2, c = (lane & 3) * 2;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
 #pragma unroll
@@ -233,77 +246,57 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
                 const int row = r + (j & 1) * 8, col = k * 16 + c + (j >> 1) * 8;
                 q[k][j] = row < live ? *reinterpret_cast<const uint32_t *>(qt + row * a.q_stride[1] + col) : 0u;
             }
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
-        m[0] = m[1] = -INFINITY;
-        l[0] = l[1] = 0.f;
-        if (!g.line.blocks || here.tile != 0 || here.s.end == 0) return;
-        // the prefix's pieces are where the item starts from, one warp each
-        const int item = kv * g.line.pairs + here.t / g.line.tokens_of_tile / 2;
-        const int pieces = g.line.last_block(item) - g.line.first_block(item) + 1;
-        for (int k = warp; k < pieces; k += kWarps) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (r + 8 * j >= live) continue;
-                const int64_t at = ((int64_t)k * n + here.t) * hq + first + r + 8 * j;
-                const float2 ml = g.prefix_ml[at];
-                const float next = fmaxf(m[j], ml.x), ref = next == -INFINITY ? 0.f : next;
-                const float fix = ex2(m[j] - ref), w = ex2(ml.x - ref);
-                m[j] = next;
-                l[j] = l[j] * fix + ((lane & 3) == 0 ? ml.y * w : 0.f);
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
-                    const float2 v = *reinterpret_cast<const float2 *>(g.prefix_o + at * D + i * 8 + c);
-                    o[i][2 * j] = o[i][2 * j] * fix + v.x * w;
-                    o[i][2 * j + 1] = o[i][2 * j + 1] * fix + v.y * w;
-                }
-            }
-        }
     };
 
-    auto compute = [&](int stage) {
-        const int32_t x = tile_start(here.s, here.tile) + warp * kSlice;
-        if (x >= here.s.end || (x + kSlice <= here.s.lo && x >= a.sinks)) return;   // nothing visible
-        const uint32_t base = ring + stage * 2 * S::kSideBytes;
-        float s[2][4] = {};
+    int stage = 0;
+    uint32_t phase = 0;
+    bool stuck = false;
+    // the next stage of the ring, when it has come; the one before it, which all have read by now, is fed
+    auto next_stage = [&]() {
+        __syncwarp();
+        feed(stage == 0 ? S::kStages - 1 : stage - 1);
+        if (!stuck && !bar_wait(bar0 + 8 * stage, phase)) stuck = true;
+        const uint32_t at = ring + stage * S::kStageBytes;
+        if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+        return at;
+    };
+
+    auto slice = [&]() {
+        const int32_t x = slice_start(here.s, here.i);
+        const uint32_t keys = next_stage();
+        float s[4][4] = {};
         {
             // lanes 0-7: tokens 0-7 low half of 16 values, 8-15: high half, 16-23: tokens 8-15 low, 24-31: high
-            const int r = (lane & 7) + (lane >> 4) * 8, up = (lane >> 3) & 1;
-            const uint32_t at = base + r * 128, turn = (up ^ (r & 7)) << 4;
+            const int row = (lane & 7) + (lane >> 4) * 8, up = (lane >> 3) & 1;
+            const uint32_t at = keys + row * 128, turn = (up ^ (row & 7)) << 4;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                uint32_t b[4];
-                ldsm4(b, at + (k / 4) * S::kHalfBytes + (turn ^ ((k % 4) << 5)));
-                Half<T>::mma(s[0], q[k], b[0], b[1]);
-                Half<T>::mma(s[1], q[k], b[2], b[3]);
-            }
-        }
-        const int c = (lane & 3) * 2;
-        if (x + kSlice > here.s.end || x < here.s.lo) {
+            for (int k = 0; k < D / 16; ++k)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int32_t y = x + i * 8 + c + j;
-                    if (y >= here.s.end || (y < here.s.lo && y >= a.sinks)) s[i][j] = s[i][2 + j] = -INFINITY;
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t b[4];
+                    ldsm4(b, at + h * 2048 + (k / 4) * S::kHalfBytes + (turn ^ ((k % 4) << 5)));
+                    Half<T>::mma(s[2 * h], q[k], b[0], b[1]);
+                    Half<T>::mma(s[2 * h + 1], q[k], b[2], b[3]);
                 }
-            // a weight of 0 does not silence an infinite or undefined value: what is not seen becomes 0
-            for (int i = lane; i < kSlice * S::kHalves * 8; i += 32) {
-                const int r = (i / 8) % kSlice;
-                if (x + r >= here.s.end || (x + r < here.s.lo && x + r >= a.sinks))
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + S::kSideBytes + (i / 8) * 128 + (i % 8) * 16), "r"(0) : "memory");
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before the next copy to this stage
-            __syncwarp();
+        }
+        const bool edge = x + kSlice > here.s.end || x < here.s.lo;
+        auto hidden = [&](int32_t y) { return y >= here.s.end || (y < here.s.lo && y >= a.sinks); };
+        if (edge) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (hidden(x + i * 8 + c + j)) s[i][j] = s[i][2 + j] = -INFINITY;
         }
         float top[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            top[j] = fmaxf(fmaxf(s[0][2 * j], s[0][2 * j + 1]), fmaxf(s[1][2 * j], s[1][2 * j + 1])) * scale;
-            top[j] = fmaxf(top[j], __shfl_xor_sync(~0u, top[j], 1));
-            top[j] = fmaxf(top[j], __shfl_xor_sync(~0u, top[j], 2));
+            float most = fmaxf(s[0][2 * j], s[0][2 * j + 1]);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) most = fmaxf(most, fmaxf(s[i][2 * j], s[i][2 * j + 1]));
+            most *= scale;
+            most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
+            top[j] = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
         }
         if (__any_sync(~0u, top[0] > m[0] || top[1] > m[1])) {
             float fix[2];
@@ -323,163 +316,234 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             }
         }
         const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
-        float p[2][4];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                p[i][j] = ex2(fmaf(s[i][j], scale, -ref[j >> 1]));
-                l[j >> 1] += p[i][j];
-            }
         // weights are rounded to the cache's type for the product, as the tensor instruction takes them;
         // the sum l is of the unrounded ones
-        const uint32_t w[4] = {Half<T>::pack(p[0][0], p[0][1]), Half<T>::pack(p[0][2], p[0][3]),
-                               Half<T>::pack(p[1][0], p[1][1]), Half<T>::pack(p[1][2], p[1][3])};
-        {
-            const int r = (lane & 7) + ((lane >> 3) & 1) * 8, up = lane >> 4;
-            const uint32_t at = base + S::kSideBytes + r * 128, turn = (up ^ (r & 7)) << 4;
+        uint32_t w[2][4];
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                uint32_t b[4];
-                ldsm4t(b, at + (k / 4) * S::kHalfBytes + (turn ^ ((k % 4) << 5)));
-                Half<T>::mma(o[2 * k], w, b[0], b[1]);
-                Half<T>::mma(o[2 * k + 1], w, b[2], b[3]);
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float u = ex2(fmaf(s[i][2 * j], scale, -ref[j])), v = ex2(fmaf(s[i][2 * j + 1], scale, -ref[j]));
+                l[j] += u + v;
+                w[i / 2][(i & 1) * 2 + j] = Half<T>::pack(u, v);
             }
+        const uint32_t values = next_stage();
+        if (edge) {
+            // a weight of 0 does not silence an infinite or undefined value: what is not seen becomes 0
+            for (int i = lane; i < kSlice * S::kHalves * 8; i += 32)
+                if (hidden(x + (i / 8) % kSlice))
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(values + i * 16), "r"(0) : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before the next copy to this stage
+            __syncwarp();
+        }
+        {
+            const int row = (lane & 7) + ((lane >> 3) & 1) * 8, up = lane >> 4;
+            const uint32_t at = values + row * 128, turn = (up ^ (row & 7)) << 4;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t b[4];
+                    ldsm4t(b, at + h * 2048 + (k / 4) * S::kHalfBytes + (turn ^ ((k % 4) << 5)));
+                    Half<T>::mma(o[2 * k], w[h], b[0], b[1]);
+                    Half<T>::mma(o[2 * k + 1], w[h], b[2], b[3]);
+                }
         }
     };
 
-    // ---- the end of an item, or of this block's piece of it
-    auto end_item = [&]() {
-        const int t = here.t, kv = here.h / parts, first = kv * g.group + (here.h - kv * parts) * 16;
-        const int live = min(16, (kv + 1) * g.group - first);
-        const int64_t i0 = (int64_t)before[t] * H + (int64_t)here.h * here.s.tiles, i1 = i0 + here.s.tiles;
-        const int64_t c0 = ((i0 + 1) * C - 1) / W, c1 = (i1 * C - 1) / W;         // its first and last block
-        const bool whole = c0 == c1;
+    // ---- results, and pieces of cut items
+    auto inverse = [](float total) { return total > 0.f || total != total ? 1.f / total : 0.f; };
+    auto log_of = [](float top, float total) { return total > 0.f || total != total ? (top + log2f(total)) * kLn2 : -INFINITY; };
+    auto slot_of = [&](int64_t worker, bool tail) { return (worker * 2 + (tail ? 1 : 0)) * 16; };
+    auto sum_rows = [&]() {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             l[j] += __shfl_xor_sync(~0u, l[j], 1);
             l[j] += __shfl_xor_sync(~0u, l[j], 2);
-            if ((lane & 3) == 0) stats[warp * 16 + (lane >> 2) + 8 * j] = make_float2(m[j], l[j]);
-        }
-        __syncthreads();
-        float mine[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int r = (lane >> 2) + 8 * j;
-            if (8 * j >= live) break;
-            float top = -INFINITY, sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stats[w * 16 + r].x);
-            const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) sum += stats[w * 16 + r].y * ex2(stats[w * 16 + r].x - ref);
-            mine[j] = ex2(m[j] - ref);
-            if (warp == 0 && (lane & 3) == 0) row_stat[r] = make_float2(top, sum);
-        }
-        const int64_t mypart = (me * 2 + (me == c0 ? 1 : 0)) * 16;
-        T *out = static_cast<T *>(a.out) + t * a.out_stride[0] + first * a.out_stride[1];
-        const int rr = lane >> 2, cc = (lane & 3) * 2;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {                 // rows 8 j .. 8 j + 7
-            if (8 * j >= live) break;
-            float *to = join + (warp & 1) * 8 * S::kJoinRow + rr * S::kJoinRow + cc;
-            if (j) __syncthreads();                   // the first rows have been read
-            if (warp >= 2) {
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i)
-                    *reinterpret_cast<float2 *>(to + i * 8) = make_float2(o[i][2 * j] * mine[j], o[i][2 * j + 1] * mine[j]);
-            }
-            __syncthreads();
-            if (warp < 2) {
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
-                    float2 *at = reinterpret_cast<float2 *>(to + i * 8);
-                    const float2 u = *at;
-                    *at = make_float2(fmaf(o[i][2 * j], mine[j], u.x), fmaf(o[i][2 * j + 1], mine[j], u.y));
-                }
-            }
-            __syncthreads();
-            for (int i = threadIdx.x; i < min(8, live - 8 * j) * (D / 4); i += kThreads) {
-                const int r = i / (D / 4), d = (i % (D / 4)) * 4;
-                const float4 u = *reinterpret_cast<const float4 *>(join + r * S::kJoinRow + d);
-                const float4 v = *reinterpret_cast<const float4 *>(join + (8 + r) * S::kJoinRow + d);
-                const float4 sum = make_float4(u.x + v.x, u.y + v.y, u.z + v.z, u.w + v.w);
-                if (whole) {
-                    const float total = row_stat[8 * j + r].y, inv = total > 0.f || total != total ? 1.f / total : 0.f;
-                    *reinterpret_cast<uint2 *>(out + (8 * j + r) * a.out_stride[1] + d) =
-                        make_uint2(Half<T>::pack(sum.x * inv, sum.y * inv), Half<T>::pack(sum.z * inv, sum.w * inv));
-                } else {
-                    *reinterpret_cast<float4 *>(g.part_o + (mypart + 8 * j + r) * D + d) = sum;
-                }
-            }
-        }
-        if (threadIdx.x < live) {
-            const float2 s = row_stat[threadIdx.x];
-            if (whole) {
-                if (a.lse) a.lse[(int64_t)t * hq + first + threadIdx.x] = s.y > 0.f || s.y != s.y ? (s.x + log2f(s.y)) * 0.6931471805599453f : -INFINITY;
-            } else {
-                g.part_ml[mypart + threadIdx.x] = s;
-            }
-        }
-        if (whole) { __syncthreads(); return; }
-        // the last of the item's blocks to arrive joins the pieces, in the order of the blocks
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            // c0's count is that of the one item that begins in c0 and ends beyond it
-            const uint32_t all = (uint32_t)(c1 - c0);
-            const uint32_t seen = atomicAdd(g.arrived + c0, 1u);
-            last_one = seen == all;
-            if (seen == all) g.arrived[c0] = 0u;
-        }
-        __syncthreads();
-        if (!last_one) return;
-        __threadfence();
-        const int pieces = (int)(c1 - c0) + 1;
-        auto piece = [&](int k) { return ((c0 + k) * 2 + (k == 0 ? 1 : 0)) * 16; };
-        for (int i = threadIdx.x; i < live * (D / 4); i += kThreads) {
-            const int r = i / (D / 4), d = (i % (D / 4)) * 4;
-            float top = -INFINITY;
-            for (int k = 0; k < pieces; ++k) top = fmaxf(top, __ldcg(&g.part_ml[piece(k) + r]).x);
-            const float ref = top == -INFINITY ? 0.f : top;
-            float total = 0.f;
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            auto add = [&](float2 ml, float4 v) {
-                const float w = ex2(ml.x - ref);
-                total += ml.y * w;
-                sum.x += v.x * w;
-                sum.y += v.y * w;
-                sum.z += v.z * w;
-                sum.w += v.w * w;
-            };
-#pragma unroll 4
-            for (int k = 0; k < pieces; ++k)
-                add(__ldcg(&g.part_ml[piece(k) + r]), __ldcg(reinterpret_cast<const float4 *>(g.part_o + (piece(k) + r) * D + d)));
-            const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
-            *reinterpret_cast<uint2 *>(out + r * a.out_stride[1] + d) =
-                make_uint2(Half<T>::pack(sum.x * inv, sum.y * inv), Half<T>::pack(sum.z * inv, sum.w * inv));
-            if (d == 0 && a.lse)
-                a.lse[(int64_t)t * hq + first + r] = total > 0.f || total != total ? (top + log2f(total)) * 0.6931471805599453f : -INFINITY;
         }
     };
+    // an item's pieces: of each block the joined ones of the warps whose runs it fills to the end, and that of the
+    // last warp, in whose run it ends
+    struct Pieces {
+        int64_t first, last;       // warps
+        __device__ int count() const { return (int)((last - 1) / kWarps - first / kWarps) + 2; }
+        __device__ int64_t at(int k) const {            // place of piece k
+            const int64_t w = max(first, (first / kWarps + k) * kWarps);
+            return k + 1 == count() ? last * 2 * 16 : (w * 2 + 1) * 16;
+        }
+    };
+    auto pieces_of = [&](int64_t i0, int64_t slices) { return Pieces{((i0 + 1) * C - 1) / W, ((i0 + slices) * C - 1) / W}; };
+    // join the pieces of item (t, query heads from `from`, `rows` of them): by `count` threads, this one number `id`
+    auto join_pieces = [&](const Pieces &ps, int t, int from, int rows, int id, int count) {
+        T *out = static_cast<T *>(a.out) + t * a.out_stride[0] + from * a.out_stride[1];
+        const int pieces = ps.count();
+        for (int x = id; x < rows * (D / 4); x += count) {
+            const int row = x / (D / 4), d = (x % (D / 4)) * 4;
+            float top = -INFINITY, total = 0.f;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k0 = 0; k0 < pieces; k0 += 4) {      // four at a time: their loads are under way together
+                float2 ml[4];
+                float4 v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int64_t at = ps.at(min(k0 + k, pieces - 1)) + row;
+                    ml[k] = __ldcg(&g.part_ml[at]);
+                    v[k] = __ldcg(reinterpret_cast<const float4 *>(g.part_o + at * D + d));
+                }
+                float next = top;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) next = fmaxf(next, ml[k].x);
+                const float ref = next == -INFINITY ? 0.f : next, fix = ex2(top - ref);
+                top = next;
+                total *= fix;
+                sum.x *= fix;
+                sum.y *= fix;
+                sum.z *= fix;
+                sum.w *= fix;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k0 + k >= pieces) break;
+                    const float w = ex2(ml[k].x - ref);
+                    total += ml[k].y * w;
+                    sum.x += v[k].x * w;
+                    sum.y += v[k].y * w;
+                    sum.z += v[k].z * w;
+                    sum.w += v[k].w * w;
+                }
+            }
+            const float inv = inverse(total);
+            *reinterpret_cast<uint2 *>(out + row * a.out_stride[1] + d) =
+                make_uint2(Half<T>::pack(sum.x * inv, sum.y * inv), Half<T>::pack(sum.z * inv, sum.w * inv));
+            if (d == 0 && a.lse) a.lse[(int64_t)t * hq + from + row] = log_of(top, total);
+        }
+    };
+    auto arrive = [&](const Pieces &ps) {               // true: all pieces are there
+        const uint32_t others = (uint32_t)ps.count() - 1;
+        const bool all = atomicAdd(g.arrived + ps.first, 1u) == others;
+        if (all) g.arrived[ps.first] = 0u;
+        return all;
+    };
 
-    int stage = 0;
-    uint32_t phase = 0;
-    bool stuck = false;
-    begin_item();
+    // the end of an item in this warp's run
+    auto end_item = [&]() {
+        const int64_t i0 = (int64_t)before[here.t] * H + (int64_t)here.h * here.s.slices;
+        sum_rows();
+        if (i0 >= f0) {                                 // all of it was this warp's
+            T *out = static_cast<T *>(a.out) + here.t * a.out_stride[0] + first * a.out_stride[1];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int row = r + 8 * j;
+                if (row >= live) break;
+                const float inv = inverse(l[j]);
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i)
+                    *reinterpret_cast<uint32_t *>(out + row * a.out_stride[1] + 8 * i + c) = Half<T>::pack(o[i][2 * j] * inv, o[i][2 * j + 1] * inv);
+                if ((lane & 3) == 0 && a.lse) a.lse[(int64_t)here.t * hq + first + row] = log_of(m[j], l[j]);
+            }
+            return;
+        }
+        const Pieces ps = pieces_of(i0, here.s.slices);
+        const int64_t at = slot_of(me, false);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int row = r + 8 * j;
+            if (row >= live) break;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+                *reinterpret_cast<float2 *>(g.part_o + (at + row) * D + 8 * i + c) = make_float2(o[i][2 * j], o[i][2 * j + 1]);
+            if ((lane & 3) == 0) g.part_ml[at + row] = make_float2(m[j], l[j]);
+        }
+        __threadfence();
+        __syncwarp();
+        bool all = false;
+        if (lane == 0) all = arrive(ps);
+        all = __any_sync(~0u, all);
+        if (!all) return;
+        __threadfence();
+        join_pieces(ps, here.t, first, live, lane, 32);
+    };
+
+    if (f0 < f1) begin_item();
     for (int64_t f = f0; f < f1; ++f) {
-        __syncwarp();                                   // all have read the stage that is fed now
-        feed(stage == 0 ? S::kStages - 1 : stage - 1);
-        if (!stuck && !bar_wait(bar0 + 8 * stage, phase)) stuck = true;
-        compute(stage);
-        if (++stage == S::kStages) { stage = 0; phase ^= 1; }
-        if (here.tile + 1 == here.s.tiles || f + 1 == f1) end_item();
+        slice();
+        if (here.i + 1 == here.s.slices) end_item();
         if (f + 1 < f1) {
             advance(here);
-            if (here.tile == 0) begin_item();
+            if (here.i == 0) begin_item();
         }
     }
     if (stuck) atomicOr(g.status, 2);
+
+    // ---- what the runs' ends cut: `here` is each warp's last slice
+    const bool tail = f0 < f1 && here.i + 1 < here.s.slices;
+    if (tail) sum_rows();
+    if (lane == 0) cut[warp] = tail ? (int64_t)before[here.t] * H + (int64_t)here.h * here.s.slices : -1;
+    if (tail && (lane & 3) == 0) {
+        stats[warp * 16 + r] = make_float2(m[0], l[0]);
+        stats[warp * 16 + r + 8] = make_float2(m[1], l[1]);
+    }
+    __syncthreads();
+    float *join = reinterpret_cast<float *>(smem);                                   // [kWarps][16][kJoinRow]
+    int lead = warp, last = warp;                       // the neighbours that cut the same item
+    if (tail) {
+        while (lead > 0 && cut[lead - 1] == cut[warp]) --lead;
+        while (last + 1 < kWarps && cut[last + 1] == cut[warp]) ++last;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int row = r + 8 * j;
+            if (row >= live) break;
+            float top = -INFINITY;
+            for (int w = lead; w <= last; ++w) top = fmaxf(top, stats[w * 16 + row].x);
+            const float fix = ex2(m[j] - (top == -INFINITY ? 0.f : top));
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+                *reinterpret_cast<float2 *>(join + (warp * 16 + row) * S::kJoinRow + 8 * i + c) = make_float2(o[i][2 * j] * fix, o[i][2 * j + 1] * fix);
+        }
+    }
+    __syncthreads();
+    // the first of each group of neighbours writes the group's piece
+    bool all = false;
+    if (tail && lead == warp) {
+        const int64_t at = slot_of(me, true);
+        for (int x = lane; x < live * (D / 4); x += 32) {
+            const int row = x / (D / 4), d = (x % (D / 4)) * 4;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int w = warp; w <= last; ++w) {
+                const float4 v = *reinterpret_cast<const float4 *>(join + (w * 16 + row) * S::kJoinRow + d);
+                sum.x += v.x;
+                sum.y += v.y;
+                sum.z += v.z;
+                sum.w += v.w;
+            }
+            *reinterpret_cast<float4 *>(g.part_o + (at + row) * D + d) = sum;
+        }
+        if (lane < live) {
+            float top = -INFINITY, total = 0.f;
+            for (int w = warp; w <= last; ++w) top = fmaxf(top, stats[w * 16 + lane].x);
+            for (int w = warp; w <= last; ++w) total += stats[w * 16 + lane].y * ex2(stats[w * 16 + lane].x - (top == -INFINITY ? 0.f : top));
+            g.part_ml[at + lane] = make_float2(top, total);
+        }
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) all = arrive(pieces_of(cut[warp], here.s.slices));
+    }
+    if (lane == 0) complete[warp] = all;
+    __syncthreads();
+    for (int w = 0; w < kWarps; ++w) {
+        if (!complete[w]) continue;
+        __threadfence();
+        // the item, found again by all threads
+        const int64_t i0 = cut[w];
+        int lo = 0, hi = n;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((int64_t)before[mid] * H <= i0) lo = mid; else hi = mid;
+        }
+        const int32_t slices = before[lo + 1] - before[lo];
+        const int h = (int)((i0 - (int64_t)before[lo] * H) / slices), kv = h / parts;
+        const int from = kv * g.group + (h - kv * parts) * 16;
+        join_pieces(pieces_of(i0, slices), lo, from, min(16, (kv + 1) * g.group - from), threadIdx.x, kThreads);
+    }
 }
 
 template <int D, typename T>
@@ -504,9 +568,8 @@ cudaError_t grid_of(int max_rows, int sms, int *grid) {
 }  // namespace
 
 size_t attend_smem(int head_dim, int n) {
-    const size_t fixed = head_dim == 64 ? Shape<64>::kRing + Shape<64>::kJoin
-                       : head_dim == 128 ? Shape<128>::kRing + Shape<128>::kJoin : Shape<256>::kRing + Shape<256>::kJoin;
-    return fixed + (kWarps + 1) * 16 * sizeof(float2) + (size_t)(n + 1) * sizeof(int32_t);
+    const size_t ring = head_dim == 64 ? Shape<64>::kRing : head_dim == 128 ? Shape<128>::kRing : Shape<256>::kRing;
+    return ring + kWarps * 16 * sizeof(float2) + (size_t)(n + 1) * sizeof(int32_t);
 }
 
 cudaError_t attend_grid(int head_dim, int type, int max_rows, int sms, int *grid) {
@@ -519,7 +582,7 @@ cudaError_t attend_grid(int head_dim, int type, int max_rows, int sms, int *grid
 
 cudaError_t launch_attend(const AttendArgs &g, void *encoder, int head_dim, int type, int grid, cudaStream_t st) {
     CUtensorMap k, v;
-    const int rows = g.shift == 3 ? 8 : kSlice;
+    const int rows = min(1 << g.shift, kSlice);
     if (!encode_cache(encoder, &k, g.cache.k, g.cache.k_stride, rows, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||
         !encode_cache(encoder, &v, g.cache.v, g.cache.v_stride, rows, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type))
         return cudaErrorInvalidValue;

@@ -110,6 +110,7 @@ PrefixLine prefix_line(int n, int group, int n_kv_heads, int tokens, int sms);
 cudaError_t launch_prefix(const PrefixArgs &g, const isjl_kv_cache &cache, void *encoder, int head_dim, int type, cudaStream_t st);
 
 // ---- attend (kv_attend.cu)
+constexpr int kAttendWarps = 4;   // of a block
 struct AttendArgs {
     isjl_kv_attend_args a;
     isjl_kv_cache cache;
@@ -117,9 +118,9 @@ struct AttendArgs {
     PrefixLine line;              // blocks > 0: the prefix's tokens are done by kv_prefix.cu and merged here
     const float *prefix_o;
     const float2 *prefix_ml;
-    float *part_o;                // [grid][2][16][head_dim] pieces of (query, key head) items
-    float2 *part_ml;              // [grid][2][16]
-    uint32_t *arrived;            // [grid], zero between calls
+    float *part_o;                // [kAttendWarps * grid][2][16][head_dim] pieces of (query, key head) items
+    float2 *part_ml;              // [kAttendWarps * grid][2][16]
+    uint32_t *arrived;            // [kAttendWarps * grid], zero between calls
     int32_t *status;
 };
 size_t attend_smem(int head_dim, int n);
