@@ -13,7 +13,7 @@ struct isjl_kv {
     unsigned char *d_work = nullptr;
     int32_t *d_status = nullptr;
     int32_t *d_first_take = nullptr, *d_first_back = nullptr;
-    uint32_t *d_arrived = nullptr;
+    int32_t *d_before = nullptr;
     float2 *d_part_ml = nullptr;
     float *d_part_o = nullptr;
     float2 *d_prefix_ml = nullptr;       // null: this shape has no prefix kernel
@@ -61,16 +61,16 @@ void *tensor_map_encoder() {
     return fn;
 }
 
-bool encode_cache(void *encoder, CUtensorMap *map, void *p, const int64_t *stride, int rows, int n_blocks, int shift, int n_kv_heads,
-                  int head_dim, int type) {
+bool encode_cache(void *encoder, CUtensorMap *map, void *p, const int64_t *stride, int rows, int halves, int n_blocks, int shift,
+                  int n_kv_heads, int head_dim, int type) {
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    const cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)1 << shift, (cuuint64_t)n_kv_heads, (cuuint64_t)n_blocks};
-    const cuuint64_t strides[3] = {2 * (cuuint64_t)stride[1], 2 * (cuuint64_t)stride[2], 2 * (cuuint64_t)stride[0]};
-    const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, steps[4] = {1, 1, 1, 1};
+    const cuuint64_t dims[5] = {64, (cuuint64_t)1 << shift, (cuuint64_t)head_dim / 64, (cuuint64_t)n_kv_heads, (cuuint64_t)n_blocks};
+    const cuuint64_t strides[4] = {2 * (cuuint64_t)stride[1], 128, 2 * (cuuint64_t)stride[2], 2 * (cuuint64_t)stride[0]};
+    const cuuint32_t box[5] = {64, (cuuint32_t)rows, (cuuint32_t)halves, 1, 1}, steps[5] = {1, 1, 1, 1, 1};
     return reinterpret_cast<Encode>(encoder)(
-               map, type == ISJL_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, p, dims, strides, box,
+               map, type == ISJL_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, p, dims, strides, box,
                steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -103,18 +103,16 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
     }
     const size_t rows = rounded(sizeof(int32_t) * ((size_t)cfg->max_rows + 1));
     const size_t warps = (size_t)kv->grid * isjl::kAttendWarps;
-    const size_t arrived = rounded(sizeof(uint32_t) * warps);
     const size_t ml = rounded(sizeof(float2) * 32 * warps), o = sizeof(float) * 32 * cfg->head_dim * warps;
-    const size_t zeroed = kAlign + arrived;
-    // pieces of the prefix part: an item of 256 rows lies in at most sms / items + 2 blocks
+    // pieces of the prefix part: an item of 256 rows lies in at most sms / items + 2 blocks; and the own tokens' part
     const bool shares = cfg->head_dim <= 128 && cfg->n_q_heads / cfg->n_kv_heads <= 128;
-    const size_t pieces = shares ? (size_t)kv->sms * 256 + 2 * (size_t)queries * cfg->n_q_heads : 0;
+    const size_t pieces = shares ? (size_t)kv->sms * 256 + 3 * (size_t)queries * cfg->n_q_heads : 0;
     const size_t prefix_ml = rounded(sizeof(float2) * pieces), prefix_o = sizeof(float) * cfg->head_dim * pieces;
     if (!(kv->encoder = isjl::tensor_map_encoder())) {
         delete kv;
         return ISJL_ERR_CUDA;
     }
-    const size_t total = zeroed + 2 * rows + ml + rounded(o) + prefix_ml + prefix_o;
+    const size_t total = kAlign + 3 * rows + ml + rounded(o) + prefix_ml + prefix_o;
     if (cudaMalloc(reinterpret_cast<void **>(&kv->d_work), total) != cudaSuccess) {
         cudaGetLastError();
         delete kv;
@@ -123,8 +121,8 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
     unsigned char *p = kv->d_work;
     kv->d_status = reinterpret_cast<int32_t *>(p);
     p += kAlign;
-    kv->d_arrived = reinterpret_cast<uint32_t *>(p);
-    p += arrived;
+    kv->d_before = reinterpret_cast<int32_t *>(p);
+    p += rows;
     kv->d_first_take = reinterpret_cast<int32_t *>(p);
     p += rows;
     kv->d_first_back = reinterpret_cast<int32_t *>(p);
@@ -137,8 +135,8 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
         kv->d_prefix_ml = reinterpret_cast<float2 *>(p);
         kv->d_prefix_o = reinterpret_cast<float *>(p + prefix_ml);
     }
-    // calls may come on any stream: the zeros have to be there before create returns
-    if (cudaMemset(kv->d_work, 0, zeroed) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+    // calls may come on any stream: the status word has to be there before create returns
+    if (cudaMemset(kv->d_work, 0, kAlign) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
         cudaGetLastError();
         cudaFree(kv->d_work);
         delete kv;
@@ -222,7 +220,7 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
     g.group = kv->cfg.n_q_heads / kv->cfg.n_kv_heads;
     g.part_o = kv->d_part_o;
     g.part_ml = kv->d_part_ml;
-    g.arrived = kv->d_arrived;
+    g.before = kv->d_before;
     g.status = kv->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (kv->d_prefix_o && a->n_prefix_blocks > 0 && a->window == 0) {

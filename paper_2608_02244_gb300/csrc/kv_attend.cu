@@ -7,8 +7,9 @@
 // slices come by TMA through a ring of its own and no warp waits for another: the running maximum and sum of
 // the softmax, the sums and an item's result are the warp's own, and while one is between items the others
 // keep the memory busy.  The query heads of a key head are the 16 rows of a tensor instruction.  An item cut
-// by the runs' ends leaves pieces, which the last of their owners to arrive joins in their order, so that the
-// result does not depend on the order of arrival; pieces of neighbouring warps are joined in shared memory first.
+// by the runs' ends leaves pieces (those of neighbouring warps joined in shared memory first), which a second
+// kernel joins in their order.  Joining them here, by the last of an item's warps to arrive, took a fence and an
+// atomic under full memory load: 10 to 20 us of stall against 3 us of a small kernel that starts as this one ends.
 #include "kv_tma.cuh"
 
 namespace isjl {
@@ -67,6 +68,12 @@ __device__ __forceinline__ int32_t slice_start(const Sight &s, int i) {
     return (i < s.head ? i : s.lo / kSlice + i - s.head) * kSlice;
 }
 
+__device__ __forceinline__ float inverse(float total) { return total > 0.f || total != total ? 1.f / total : 0.f; }
+// the logarithm of a sum of exp2, in the natural base
+__device__ __forceinline__ float log_of(float top, float total) {
+    return total > 0.f || total != total ? (top + log2f(total)) * kLn2 : -INFINITY;
+}
+
 // place on the line of slices
 struct Place {
     int t, h, i;
@@ -82,7 +89,6 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     int32_t *before = reinterpret_cast<int32_t *>(stats + kWarps * 16);              // [n + 1] slices before a query
     __shared__ int32_t warp_sum[kWarps];
     __shared__ int64_t cut[kWarps];           // where on the line the item begins that a warp's run leaves cut, or -1
-    __shared__ int32_t complete[kWarps];
     __shared__ __align__(8) uint64_t bars[kWarps * S::kStages];
 
     const isjl_kv_attend_args &a = g.a;
@@ -91,7 +97,10 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     const float scale = a.scale * kLog2e;
 
     const uint32_t bar0 = smem_addr(bars) + warp * S::kStages * 8;
+    start_next();
     if (lane == 0) {
+        tma_prefetch(&kmap);
+        tma_prefetch(&vmap);
         for (int i = 0; i < S::kStages; ++i) bar_init(bar0 + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -122,11 +131,12 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         }
         if (threadIdx.x == kThreads - 1) before[n] = base;
         __syncthreads();
+        if (blockIdx.x == 0)
+            for (int t = threadIdx.x; t <= n; t += kThreads) g.before[t] = before[t];
     }
     const int64_t W = (int64_t)before[n] * H;
     const int64_t C = min((int64_t)gridDim.x * kWarps, W);               // warps with work
     const int64_t me = (int64_t)blockIdx.x * kWarps + warp;
-    if ((int64_t)blockIdx.x * kWarps >= C) return;
     const int64_t f0 = me < C ? W * me / C : W, f1 = me < C ? W * (me + 1) / C : W;
 
     auto advance = [&](Place &p) {
@@ -138,12 +148,15 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     };
 
     // ---- the ring: keys and values of a slice, one stage each.  A lane has one copy of a stage: the rows of one
-    // of the slice's blocks (or of the slice, in a larger block) and 64 of their values.
+    // of the slice's blocks, or all of them where the block is larger.
     const uint32_t ring = smem_addr(smem) + warp * S::kStages * S::kStageBytes;
     const int32_t prefix_blocks = g.line.blocks ? 0 : a.n_prefix_blocks;
-    const int rows_shift = min(g.shift, 5), half = lane % S::kHalves, piece = lane / S::kHalves;
+    const int rows_shift = min(g.shift, 5), piece = lane;
     const bool copies = piece < (kSlice >> rows_shift);
-    const uint32_t copy_at = ring + half * S::kHalfBytes + ((piece << rows_shift) << 7);
+    const uint32_t half_bytes = 128u << rows_shift;                    // a copy's rows of 64 values
+    const uint32_t copy_at = ring + piece * S::kHalves * half_bytes;
+    // where a row lies in a stage
+    auto row_at = [&](int row) { return (row >> rows_shift) * S::kHalves * half_bytes + (row & ((1 << rows_shift) - 1)) * 128; };
     // the number of this lane's block, asked for one slice ahead of the copies that use it and looked at only there
     constexpr int32_t kNone = INT32_MIN;
     auto block_of = [&](const Place &p) {
@@ -181,8 +194,8 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         }
         if (lane == 0) bar_expect(bar, S::kStageBytes);
         if (copies)
-            tma_load(copy_at + stage * S::kStageBytes, ahead_values ? &vmap : &kmap, bar, half * 64,
-                     slice_start(ahead.s, ahead.i) & ((1 << g.shift) - 1) & ~((1 << rows_shift) - 1), ahead.h / parts, block);
+            tma_load(copy_at + stage * S::kStageBytes, ahead_values ? &vmap : &kmap, bar,
+                     slice_start(ahead.s, ahead.i) & ((1 << g.shift) - 1) & ~((1 << rows_shift) - 1), 0, ahead.h / parts, block);
         ahead_values = !ahead_values;
         if (ahead_values) return;
         if (--ahead_left == 0) return;
@@ -213,31 +226,6 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
         m[0] = m[1] = -INFINITY;
         l[0] = l[1] = 0.f;
-        if (g.line.blocks && here.i == 0 && here.s.end > 0) {
-            // the prefix's pieces are where the item starts from
-            const int item = kv * g.line.pairs + here.t / g.line.tokens_of_tile / 2;
-            const int pieces = g.line.last_block(item) - g.line.first_block(item) + 1;
-            const int64_t step = (int64_t)n * hq;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (r + 8 * j >= live) continue;
-                const int64_t at = (int64_t)here.t * hq + first + r + 8 * j;
-                for (int k = 0; k < pieces; ++k) {
-                    const float2 ml = g.prefix_ml[at + k * step];
-                    const float next = fmaxf(m[j], ml.x), ref = next == -INFINITY ? 0.f : next;
-                    const float fix = ex2(m[j] - ref), w = ex2(ml.x - ref);
-                    m[j] = next;
-                    l[j] = l[j] * fix + ((lane & 3) == 0 ? ml.y * w : 0.f);
-                    const float *from = g.prefix_o + (at + k * step) * D + c;
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        const float2 v = *reinterpret_cast<const float2 *>(from + i * 8);
-                        o[i][2 * j] = o[i][2 * j] * fix + v.x * w;
-                        o[i][2 * j + 1] = o[i][2 * j + 1] * fix + v.y * w;
-                    }
-                }
-            }
-        }
         const T *qt = static_cast<const T *>(a.q) + here.t * a.q_stride[0] + first * a.q_stride[1];
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
@@ -261,20 +249,25 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         return at;
     };
 
+    uint32_t key_row[2], value_row[2];                 // of this lane's rows in tensor operands
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        key_row[h] = row_at((lane & 7) + (lane >> 4) * 8 + 16 * h);
+        value_row[h] = row_at((lane & 7) + ((lane >> 3) & 1) * 8 + 16 * h);
+    }
     auto slice = [&]() {
         const int32_t x = slice_start(here.s, here.i);
         const uint32_t keys = next_stage();
         float s[4][4] = {};
         {
             // lanes 0-7: tokens 0-7 low half of 16 values, 8-15: high half, 16-23: tokens 8-15 low, 24-31: high
-            const int row = (lane & 7) + (lane >> 4) * 8, up = (lane >> 3) & 1;
-            const uint32_t at = keys + row * 128, turn = (up ^ (row & 7)) << 4;
+            const uint32_t turn = (((lane >> 3) & 1) ^ (lane & 7)) << 4;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t b[4];
-                    ldsm4(b, at + h * 2048 + (k / 4) * S::kHalfBytes + (turn ^ ((k % 4) << 5)));
+                    ldsm4(b, keys + key_row[h] + (k / 4) * half_bytes + (turn ^ ((k % 4) << 5)));
                     Half<T>::mma(s[2 * h], q[k], b[0], b[1]);
                     Half<T>::mma(s[2 * h + 1], q[k], b[2], b[3]);
                 }
@@ -330,31 +323,30 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         const uint32_t values = next_stage();
         if (edge) {
             // a weight of 0 does not silence an infinite or undefined value: what is not seen becomes 0
-            for (int i = lane; i < kSlice * S::kHalves * 8; i += 32)
-                if (hidden(x + (i / 8) % kSlice))
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(values + i * 16), "r"(0) : "memory");
+            for (int i = lane; i < kSlice * S::kHalves * 8; i += 32) {
+                const int row = (i / 8) % kSlice;
+                if (hidden(x + row))
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"
+                                 ::"r"(values + row_at(row) + i / (8 * kSlice) * half_bytes + i % 8 * 16), "r"(0) : "memory");
+            }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before the next copy to this stage
             __syncwarp();
         }
         {
-            const int row = (lane & 7) + ((lane >> 3) & 1) * 8, up = lane >> 4;
-            const uint32_t at = values + row * 128, turn = (up ^ (row & 7)) << 4;
+            const uint32_t turn = ((lane >> 4) ^ (lane & 7)) << 4;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t b[4];
-                    ldsm4t(b, at + h * 2048 + (k / 4) * S::kHalfBytes + (turn ^ ((k % 4) << 5)));
+                    ldsm4t(b, values + value_row[h] + (k / 4) * half_bytes + (turn ^ ((k % 4) << 5)));
                     Half<T>::mma(o[2 * k], w[h], b[0], b[1]);
                     Half<T>::mma(o[2 * k + 1], w[h], b[2], b[3]);
                 }
         }
     };
 
-    // ---- results, and pieces of cut items
-    auto inverse = [](float total) { return total > 0.f || total != total ? 1.f / total : 0.f; };
-    auto log_of = [](float top, float total) { return total > 0.f || total != total ? (top + log2f(total)) * kLn2 : -INFINITY; };
-    auto slot_of = [&](int64_t worker, bool tail) { return (worker * 2 + (tail ? 1 : 0)) * 16; };
+    // ---- results, and pieces of items
     auto sum_rows = [&]() {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -362,73 +354,11 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             l[j] += __shfl_xor_sync(~0u, l[j], 2);
         }
     };
-    // an item's pieces: of each block the joined ones of the warps whose runs it fills to the end, and that of the
-    // last warp, in whose run it ends
-    struct Pieces {
-        int64_t first, last;       // warps
-        __device__ int count() const { return (int)((last - 1) / kWarps - first / kWarps) + 2; }
-        __device__ int64_t at(int k) const {            // place of piece k
-            const int64_t w = max(first, (first / kWarps + k) * kWarps);
-            return k + 1 == count() ? last * 2 * 16 : (w * 2 + 1) * 16;
-        }
-    };
-    auto pieces_of = [&](int64_t i0, int64_t slices) { return Pieces{((i0 + 1) * C - 1) / W, ((i0 + slices) * C - 1) / W}; };
-    // join the pieces of item (t, query heads from `from`, `rows` of them): by `count` threads, this one number `id`
-    auto join_pieces = [&](const Pieces &ps, int t, int from, int rows, int id, int count) {
-        T *out = static_cast<T *>(a.out) + t * a.out_stride[0] + from * a.out_stride[1];
-        const int pieces = ps.count();
-        for (int x = id; x < rows * (D / 4); x += count) {
-            const int row = x / (D / 4), d = (x % (D / 4)) * 4;
-            float top = -INFINITY, total = 0.f;
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int k0 = 0; k0 < pieces; k0 += 4) {      // four at a time: their loads are under way together
-                float2 ml[4];
-                float4 v[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int64_t at = ps.at(min(k0 + k, pieces - 1)) + row;
-                    ml[k] = __ldcg(&g.part_ml[at]);
-                    v[k] = __ldcg(reinterpret_cast<const float4 *>(g.part_o + at * D + d));
-                }
-                float next = top;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) next = fmaxf(next, ml[k].x);
-                const float ref = next == -INFINITY ? 0.f : next, fix = ex2(top - ref);
-                top = next;
-                total *= fix;
-                sum.x *= fix;
-                sum.y *= fix;
-                sum.z *= fix;
-                sum.w *= fix;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (k0 + k >= pieces) break;
-                    const float w = ex2(ml[k].x - ref);
-                    total += ml[k].y * w;
-                    sum.x += v[k].x * w;
-                    sum.y += v[k].y * w;
-                    sum.z += v[k].z * w;
-                    sum.w += v[k].w * w;
-                }
-            }
-            const float inv = inverse(total);
-            *reinterpret_cast<uint2 *>(out + row * a.out_stride[1] + d) =
-                make_uint2(Half<T>::pack(sum.x * inv, sum.y * inv), Half<T>::pack(sum.z * inv, sum.w * inv));
-            if (d == 0 && a.lse) a.lse[(int64_t)t * hq + from + row] = log_of(top, total);
-        }
-    };
-    auto arrive = [&](const Pieces &ps) {               // true: all pieces are there
-        const uint32_t others = (uint32_t)ps.count() - 1;
-        const bool all = atomicAdd(g.arrived + ps.first, 1u) == others;
-        if (all) g.arrived[ps.first] = 0u;
-        return all;
-    };
-
     // the end of an item in this warp's run
     auto end_item = [&]() {
-        const int64_t i0 = (int64_t)before[here.t] * H + (int64_t)here.h * here.s.slices;
+        const bool whole = (int64_t)before[here.t] * H + (int64_t)here.h * here.s.slices >= f0;
         sum_rows();
-        if (i0 >= f0) {                                 // all of it was this warp's
+        if (whole && !g.line.blocks) {
             T *out = static_cast<T *>(a.out) + here.t * a.out_stride[0] + first * a.out_stride[1];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -442,25 +372,19 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             }
             return;
         }
-        const Pieces ps = pieces_of(i0, here.s.slices);
-        const int64_t at = slot_of(me, false);
+        // a piece: beside the prefix's, or the last one of an item that earlier warps began
+        const int64_t at = whole ? ((int64_t)g.line.pieces * n + here.t) * hq + first : me * 2 * 16;
+        float *po = whole ? g.prefix_o : g.part_o;
+        float2 *pml = whole ? g.prefix_ml : g.part_ml;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int row = r + 8 * j;
             if (row >= live) break;
 #pragma unroll
             for (int i = 0; i < D / 8; ++i)
-                *reinterpret_cast<float2 *>(g.part_o + (at + row) * D + 8 * i + c) = make_float2(o[i][2 * j], o[i][2 * j + 1]);
-            if ((lane & 3) == 0) g.part_ml[at + row] = make_float2(m[j], l[j]);
+                *reinterpret_cast<float2 *>(po + (at + row) * D + 8 * i + c) = make_float2(o[i][2 * j], o[i][2 * j + 1]);
+            if ((lane & 3) == 0) pml[at + row] = make_float2(m[j], l[j]);
         }
-        __threadfence();
-        __syncwarp();
-        bool all = false;
-        if (lane == 0) all = arrive(ps);
-        all = __any_sync(~0u, all);
-        if (!all) return;
-        __threadfence();
-        join_pieces(ps, here.t, first, live, lane, 32);
     };
 
     if (f0 < f1) begin_item();
@@ -502,9 +426,8 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     }
     __syncthreads();
     // the first of each group of neighbours writes the group's piece
-    bool all = false;
     if (tail && lead == warp) {
-        const int64_t at = slot_of(me, true);
+        const int64_t at = (me * 2 + 1) * 16;
         for (int x = lane; x < live * (D / 4); x += 32) {
             const int row = x / (D / 4), d = (x % (D / 4)) * 4;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -523,33 +446,103 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             for (int w = warp; w <= last; ++w) total += stats[w * 16 + lane].y * ex2(stats[w * 16 + lane].x - (top == -INFINITY ? 0.f : top));
             g.part_ml[at + lane] = make_float2(top, total);
         }
-        __threadfence();
-        __syncwarp();
-        if (lane == 0) all = arrive(pieces_of(cut[warp], here.s.slices));
     }
-    if (lane == 0) complete[warp] = all;
-    __syncthreads();
-    for (int w = 0; w < kWarps; ++w) {
-        if (!complete[w]) continue;
-        __threadfence();
-        // the item, found again by all threads
-        const int64_t i0 = cut[w];
+    wait_for_previous();          // the prefix's kernel, if there is one: the kernel after this one reads its pieces
+}
+
+// Joins pieces: of the items that runs' ends cut, a block for the warp in whose run one begins; where a prefix was
+// done apart, of all items, a block for each, with the prefix's pieces.
+constexpr int kJoinThreads = 256;
+
+template <int D, typename T>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendArgs g) {
+    const isjl_kv_attend_args &a = g.a;
+    const int n = a.n, parts = (g.group + 15) / 16, H = g.n_kv_heads * parts, hq = g.n_kv_heads * g.group;
+    wait_for_previous();
+    const int64_t W = (int64_t)g.before[n] * H, C = min((int64_t)g.grid * kWarps, W);
+    int t, h;
+    int64_t i0;
+    int32_t slices;
+    if (g.line.blocks) {
+        t = blockIdx.x / H;
+        h = blockIdx.x % H;
+        slices = g.before[t + 1] - g.before[t];
+        i0 = (int64_t)g.before[t] * H + (int64_t)h * slices;
+    } else {
+        const int64_t f0 = W * blockIdx.x / C, f1 = W * (blockIdx.x + 1) / C;
+        if ((int64_t)blockIdx.x >= C) return;
         int lo = 0, hi = n;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if ((int64_t)before[mid] * H <= i0) lo = mid; else hi = mid;
+            if ((int64_t)g.before[mid] * H <= f1 - 1) lo = mid; else hi = mid;
         }
-        const int32_t slices = before[lo + 1] - before[lo];
-        const int h = (int)((i0 - (int64_t)before[lo] * H) / slices), kv = h / parts;
-        const int from = kv * g.group + (h - kv * parts) * 16;
-        join_pieces(pieces_of(i0, slices), lo, from, min(16, (kv + 1) * g.group - from), threadIdx.x, kThreads);
+        t = lo;
+        slices = g.before[t + 1] - g.before[t];
+        h = (int)((f1 - 1 - (int64_t)g.before[t] * H) / slices);
+        i0 = (int64_t)g.before[t] * H + (int64_t)h * slices;
+        if (i0 < f0 || i0 + slices <= f1) return;        // begun earlier, or not cut
+    }
+    const int kv = h / parts, from = kv * g.group + (h - kv * parts) * 16, rows = min(16, (kv + 1) * g.group - from);
+    // An item's pieces: of each block the joined ones of the warps whose runs it fills to the end, and that of the
+    // last warp, in whose run it ends; or the one of an item that is a warp's own.
+    const int64_t first = ((i0 + 1) * C - 1) / W, last = ((i0 + slices) * C - 1) / W;
+    const int cut = first == last ? 0 : (int)((last - 1) / kWarps - first / kWarps) + 2;
+    const int prefix_item = g.line.blocks ? kv * g.line.pairs + t / g.line.tokens_of_tile / 2 : 0;
+    const int shared = g.line.blocks && sight(g, t).end > 0 ? g.line.last_block(prefix_item) - g.line.first_block(prefix_item) + 1 : 0;
+    const int own = cut ? cut : 1, pieces = own + shared;
+    T *out = static_cast<T *>(a.out) + t * a.out_stride[0] + from * a.out_stride[1];
+    for (int x = threadIdx.x; x < rows * (D / 4); x += kJoinThreads) {
+        const int row = x / (D / 4), d = (x % (D / 4)) * 4;
+        float top = -INFINITY, total = 0.f;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k0 = 0; k0 < pieces; k0 += 8) {          // eight at a time: their loads are under way together
+            float2 ml[8];
+            float4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int p = min(k0 + k, pieces - 1);
+                const bool from_cut = cut && p < own;
+                const int64_t w = max(first, (first / kWarps + p) * kWarps);
+                const int64_t at = from_cut ? (p + 1 == own ? last * 2 * 16 : (w * 2 + 1) * 16) + row
+                                            : ((int64_t)(p < own ? g.line.pieces : p - own) * n + t) * hq + from + row;
+                ml[k] = (from_cut ? g.part_ml : g.prefix_ml)[at];
+                v[k] = *reinterpret_cast<const float4 *>((from_cut ? g.part_o : g.prefix_o) + at * D + d);
+            }
+            float next = top;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) next = fmaxf(next, ml[k].x);
+            const float ref = next == -INFINITY ? 0.f : next, fix = ex2(top - ref);
+            top = next;
+            total *= fix;
+            sum.x *= fix;
+            sum.y *= fix;
+            sum.z *= fix;
+            sum.w *= fix;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (k0 + k >= pieces) break;
+                const float w = ex2(ml[k].x - ref);
+                total += ml[k].y * w;
+                sum.x += v[k].x * w;
+                sum.y += v[k].y * w;
+                sum.z += v[k].z * w;
+                sum.w += v[k].w * w;
+            }
+        }
+        const float inv = inverse(total);
+        *reinterpret_cast<uint2 *>(out + row * a.out_stride[1] + d) =
+            make_uint2(Half<T>::pack(sum.x * inv, sum.y * inv), Half<T>::pack(sum.z * inv, sum.w * inv));
+        if (d == 0 && a.lse) a.lse[(int64_t)t * hq + from + row] = log_of(top, total);
     }
 }
 
 template <int D, typename T>
 cudaError_t launch_of(const AttendArgs &g, const CUtensorMap &k, const CUtensorMap &v, int grid, cudaStream_t st) {
-    attend_kernel<D, T><<<grid, kThreads, attend_smem(D, g.a.n), st>>>(g, k, v);
-    return cudaGetLastError();
+    const bool apart = g.line.blocks > 0;
+    const cudaError_t e = launch_kernel(attend_kernel<D, T>, grid, kThreads, attend_smem(D, g.a.n), st, apart, g, k, v);
+    if (e != cudaSuccess) return e;
+    const int items = g.a.n * g.n_kv_heads * ((g.group + 15) / 16);
+    return launch_kernel(join_kernel<D, T>, apart ? items : grid * kWarps, kJoinThreads, 0, st, true, g);
 }
 
 template <int D, typename T>
@@ -580,11 +573,13 @@ cudaError_t attend_grid(int head_dim, int type, int max_rows, int sms, int *grid
          : head_dim == 128 ? grid_of<128, __half>(max_rows, sms, grid) : grid_of<256, __half>(max_rows, sms, grid);
 }
 
-cudaError_t launch_attend(const AttendArgs &g, void *encoder, int head_dim, int type, int grid, cudaStream_t st) {
+cudaError_t launch_attend(const AttendArgs &args, void *encoder, int head_dim, int type, int grid, cudaStream_t st) {
+    AttendArgs g = args;
+    g.grid = grid;
     CUtensorMap k, v;
     const int rows = min(1 << g.shift, kSlice);
-    if (!encode_cache(encoder, &k, g.cache.k, g.cache.k_stride, rows, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||
-        !encode_cache(encoder, &v, g.cache.v, g.cache.v_stride, rows, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type))
+    if (!encode_cache(encoder, &k, g.cache.k, g.cache.k_stride, rows, head_dim / 64, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||
+        !encode_cache(encoder, &v, g.cache.v, g.cache.v_stride, rows, head_dim / 64, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type))
         return cudaErrorInvalidValue;
     if (type == ISJL_KV_BF16)
         return head_dim == 64 ? launch_of<64, __nv_bfloat16>(g, k, v, grid, st)

@@ -99,7 +99,7 @@ struct PrefixArgs {
     const void *q;
     int64_t q_stride[2];
     const int32_t *prefix;
-    float *part_o;                // [pieces][n][n_q_heads][head_dim], sums of exp2(s - m) v
+    float *part_o;                // [pieces][n][n_q_heads][head_dim], sums of exp2(s - m) v; one more [n] for own tokens
     float2 *part_ml;              // [pieces][n][n_q_heads], m and the sum of exp2(s - m)
     int32_t *status;
     float scale;
@@ -116,11 +116,12 @@ struct AttendArgs {
     isjl_kv_cache cache;
     int32_t n_blocks, shift, n_kv_heads, group;
     PrefixLine line;              // blocks > 0: the prefix's tokens are done by kv_prefix.cu and merged here
-    const float *prefix_o;
-    const float2 *prefix_ml;
+    float *prefix_o;
+    float2 *prefix_ml;
     float *part_o;                // [kAttendWarps * grid][2][16][head_dim] pieces of (query, key head) items
     float2 *part_ml;              // [kAttendWarps * grid][2][16]
-    uint32_t *arrived;            // [kAttendWarps * grid], zero between calls
+    int32_t *before;              // [n + 1] slices before each query, for the kernel that joins the pieces
+    int32_t grid;
     int32_t *status;
 };
 size_t attend_smem(int head_dim, int n);

@@ -103,7 +103,10 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
     const uint32_t bar0 = smem_addr(bars);
     auto bar = [&](int i) { return bar0 + 8 * i; };
 
+    start_next();
     if (threadIdx.x == 0) {
+        tma_prefetch(&kmap);
+        tma_prefetch(&vmap);
         failed_word = 0;
         for (int i = 0; i < S::kStages; ++i) { bar_init(bar(kFull + i), 1); bar_init(bar(kEmpty + i), 1); }
         for (int i = 0; i < 2; ++i) {
@@ -286,7 +289,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                         __syncwarp();
                         for (int half = lane / pieces; half < S::kHalves; half += 32 / pieces)
                             tma_load(ring + stage * S::kTileBytes + half * S::kHalfBytes + piece * piece_bytes, side ? &vmap : &kmap,
-                                     bar(kFull + stage), half * 64, slot, head, block);
+                                     bar(kFull + stage), slot, half, head, block);
                         ++load;
                         if (++stage == S::kStages) { stage = 0; turn ^= 1; }
                     }
@@ -384,8 +387,7 @@ template <int D, typename T>
 cudaError_t launch_of(const PrefixArgs &g, const CUtensorMap &k, const CUtensorMap &v, cudaStream_t st) {
     cudaError_t e = cudaFuncSetAttribute(prefix_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem);
     if (e != cudaSuccess) return e;
-    prefix_kernel<D, T><<<(unsigned)g.line.blocks, kThreads, Shape<D>::kSmem, st>>>(g, k, v);
-    return cudaGetLastError();
+    return launch_kernel(prefix_kernel<D, T>, g.line.blocks, kThreads, Shape<D>::kSmem, st, false, g, k, v);
 }
 
 }  // namespace
@@ -406,8 +408,8 @@ PrefixLine prefix_line(int n, int group, int n_kv_heads, int tokens, int sms) {
 cudaError_t launch_prefix(const PrefixArgs &g, const isjl_kv_cache &cache, void *encoder, int head_dim, int type, cudaStream_t st) {
     CUtensorMap k, v;
     const int rows = g.shift < 7 ? 1 << g.shift : kKeys;
-    if (!encode_cache(encoder, &k, cache.k, cache.k_stride, rows, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||
-        !encode_cache(encoder, &v, cache.v, cache.v_stride, rows, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type))
+    if (!encode_cache(encoder, &k, cache.k, cache.k_stride, rows, 1, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||
+        !encode_cache(encoder, &v, cache.v, cache.v_stride, rows, 1, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type))
         return cudaErrorInvalidValue;
     if (type == ISJL_KV_BF16)
         return head_dim == 64 ? launch_of<64, __nv_bfloat16>(g, k, v, st) : launch_of<128, __nv_bfloat16>(g, k, v, st);

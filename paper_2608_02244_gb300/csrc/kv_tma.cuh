@@ -46,14 +46,36 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t phase, volatile 
     return true;
 }
 
-__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap *map, uint32_t bar, int x, int slot, int head, int block) {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-                 ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(slot), "r"(head), "r"(block) : "memory");
+__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap *map, uint32_t bar, int slot, int half, int head, int block) {
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+                 ::"r"(to), "l"(map), "r"(bar), "r"(0), "r"(slot), "r"(half), "r"(head), "r"(block) : "memory");
 }
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
-// A map of a cache side for copies of `rows` slots of one block and head, 64 values wide (128 bytes, swizzled by
-// 128); coordinates: value (0, 64, ...), slot, head, block.  A block number beyond the cache reads as zeros.
-bool encode_cache(void *encoder, CUtensorMap *map, void *p, const int64_t *stride, int rows, int n_blocks, int shift, int n_kv_heads,
-                  int head_dim, int type);
+// Kernels of one call start while the one before them ends; what waits sees all of its predecessor's writes.
+__device__ __forceinline__ void start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// A map of a cache side for copies of `rows` slots of one block and head and of `halves` times 64 values: in shared
+// memory rows of 128 bytes, swizzled by 128, one 64 values' rows after the other's.  Coordinates: value in the 64
+// (always 0), slot, which 64, head, block.  A block number beyond the cache reads as zeros.
+bool encode_cache(void *encoder, CUtensorMap *map, void *p, const int64_t *stride, int rows, int halves, int n_blocks, int shift,
+                  int n_kv_heads, int head_dim, int type);
+
+// launch, started while the kernel before it in the stream ends (`early`) or after that
+template <typename... Args>
+cudaError_t launch_kernel(void (*kernel)(Args...), int grid, int threads, size_t smem, cudaStream_t st, bool early, const Args &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = early ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 }  // namespace isjl
