@@ -12,7 +12,7 @@ struct isjl_kv {
     // one allocation: the status word, then the workspaces of assign and attend
     unsigned char *d_work = nullptr;
     int32_t *d_status = nullptr;
-    int32_t *d_first_take = nullptr, *d_first_back = nullptr;
+    int32_t *d_sums = nullptr;
     int32_t *d_before = nullptr;
     float2 *d_part_ml = nullptr;
     float *d_part_o = nullptr;
@@ -101,18 +101,20 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
         delete kv;
         return ISJL_ERR_CUDA;
     }
-    const size_t rows = rounded(sizeof(int32_t) * ((size_t)cfg->max_rows + 1));
+    const size_t rows = rounded(sizeof(int32_t) * ((size_t)queries + 1)), sums = rounded(sizeof(int32_t) * (8 + 4 * (size_t)cfg->max_rows));
     const size_t warps = (size_t)kv->grid * isjl::kAttendWarps;
     const size_t ml = rounded(sizeof(float2) * 32 * warps), o = sizeof(float) * 32 * cfg->head_dim * warps;
     // pieces of the prefix part: an item of 256 rows lies in at most sms / items + 2 blocks; and the own tokens' part
     const bool shares = cfg->head_dim <= 128 && cfg->n_q_heads / cfg->n_kv_heads <= 128;
     const size_t pieces = shares ? (size_t)kv->sms * 256 + 3 * (size_t)queries * cfg->n_q_heads : 0;
     const size_t prefix_ml = rounded(sizeof(float2) * pieces), prefix_o = sizeof(float) * cfg->head_dim * pieces;
-    if (!(kv->encoder = isjl::tensor_map_encoder())) {
+    if (!(kv->encoder = isjl::tensor_map_encoder()) ||
+        (shares && isjl::prepare_prefix(cfg->head_dim, cfg->type) != cudaSuccess)) {
+        cudaGetLastError();
         delete kv;
         return ISJL_ERR_CUDA;
     }
-    const size_t total = kAlign + 3 * rows + ml + rounded(o) + prefix_ml + prefix_o;
+    const size_t total = kAlign + rows + sums + ml + rounded(o) + prefix_ml + prefix_o;
     if (cudaMalloc(reinterpret_cast<void **>(&kv->d_work), total) != cudaSuccess) {
         cudaGetLastError();
         delete kv;
@@ -123,10 +125,8 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
     p += kAlign;
     kv->d_before = reinterpret_cast<int32_t *>(p);
     p += rows;
-    kv->d_first_take = reinterpret_cast<int32_t *>(p);
-    p += rows;
-    kv->d_first_back = reinterpret_cast<int32_t *>(p);
-    p += rows;
+    kv->d_sums = reinterpret_cast<int32_t *>(p);
+    p += sums;
     kv->d_part_ml = reinterpret_cast<float2 *>(p);
     p += ml;
     kv->d_part_o = reinterpret_cast<float *>(p);
@@ -165,8 +165,7 @@ isjl_status isjl_kv_assign(isjl_kv *kv, const isjl_kv_assign_args *a, void *stre
     g.a = *a;
     g.n_blocks = kv->cfg.n_blocks;
     g.shift = kv->shift;
-    g.first_take = kv->d_first_take;
-    g.first_back = kv->d_first_back;
+    g.work = kv->d_sums;
     g.status = kv->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return launched(kv, isjl::launch_assign(g, kv->sms, st), st);

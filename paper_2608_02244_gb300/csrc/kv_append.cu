@@ -9,11 +9,10 @@
 namespace isjl {
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kThreads = 128, kAhead = 3;
 
 template <typename T>
-__device__ __forceinline__ void load8(const void *p, float (&x)[8]) {
-    const uint4 w = *reinterpret_cast<const uint4 *>(p);
+__device__ __forceinline__ void unpack8(const uint4 &w, float (&x)[8]) {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -29,90 +28,103 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
     const isjl_kv_append_args &a = g.a;
     const int t = blockIdx.x, c = threadIdx.x % kLanes, part = threadIdx.x / kLanes;
     const int hq = g.n_q_heads, hkv = g.n_kv_heads, heads = hq + 2 * hkv, half = a.rot / 2;
-    int64_t slot = a.slots[t];
-    int position = 0;
-    if (slot >= 0) {
-        position = a.rot ? a.positions[t] : 0;
-        if (slot >= g.n_slots || position < 0 || (a.rot && position >= a.n_positions)) {
-            if (threadIdx.x == 0) report(g.status);
-            slot = -1;
+    const T *x_in = static_cast<const T *>(a.qkv) + t * a.qkv_stride + 8 * c;
+    // values are asked for kAhead heads at a time, the first ones before anything that they do not need
+    uint4 raw[kAhead];
+    auto fetch = [&](int h0) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int h = h0 + u * kHeads + part;
+            raw[u] = h < heads ? *reinterpret_cast<const uint4 *>(x_in + (int64_t)h * D) : make_uint4(0, 0, 0, 0);
         }
+    };
+    fetch(0);
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    const uint4 qw = a.q_weight ? *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q_weight) + 8 * c) : none;
+    const uint4 kw = a.k_weight ? *reinterpret_cast<const uint4 *>(static_cast<const T *>(a.k_weight) + 8 * c) : none;
+    int64_t slot = a.slots[t];
+    int position = a.rot ? a.positions[t] : 0;
+    if (slot >= 0 && (slot >= g.n_slots || position < 0 || (a.rot && position >= a.n_positions))) {
+        if (threadIdx.x == 0) report(g.status);
+        slot = -1;
     }
     T *q_out = static_cast<T *>(a.q_out) + t * a.q_out_stride;
     if (slot < 0) {
-        for (int i = threadIdx.x; i < hq * kLanes; i += kThreads)
-            reinterpret_cast<uint4 *>(q_out)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = threadIdx.x; i < hq * kLanes; i += kThreads) reinterpret_cast<uint4 *>(q_out)[i] = none;
         return;
     }
-    const T *x_in = static_cast<const T *>(a.qkv) + t * a.qkv_stride;
     const int64_t block = slot >> g.shift, place = slot & ((1 << g.shift) - 1);
     T *k_out = static_cast<T *>(g.cache.k) + block * g.cache.k_stride[0] + place * g.cache.k_stride[1];
     T *v_out = static_cast<T *>(g.cache.v) + block * g.cache.v_stride[0] + place * g.cache.v_stride[1];
 
     // values 8 c .. 8 c + 7 of a head: their angles, and where their pairs are
     const bool turns = 8 * c < a.rot;
-    float cosv[8], sinv[8];
     const bool second = !a.interleaved && 8 * c >= half;
+    float cosv[8], sinv[8];                  // sines with the sign that the pair's other value has
 #pragma unroll
     for (int i = 0; i < 8; ++i) { cosv[i] = 1.f; sinv[i] = 0.f; }
     if (turns) {
         const float *angle = a.rope + (int64_t)position * a.rot;
+        const int j = a.interleaved ? 4 * c : 8 * c - (second ? half : 0), count = a.interleaved ? 1 : 2;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int j = a.interleaved ? 4 * c + i / 2 : 8 * c + i - (second ? half : 0);
-            cosv[i] = angle[j];
-            sinv[i] = angle[half + j];
+        for (int k = 0; k < 2; ++k) {
+            if (k >= count) break;
+            const float4 x = *reinterpret_cast<const float4 *>(angle + j + 4 * k), y = *reinterpret_cast<const float4 *>(angle + half + j + 4 * k);
+            const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (a.interleaved) {
+                    cosv[2 * i] = cosv[2 * i + 1] = xs[i];
+                    sinv[2 * i] = -ys[i];
+                    sinv[2 * i + 1] = ys[i];
+                } else {
+                    cosv[4 * k + i] = xs[i];
+                    sinv[4 * k + i] = second ? ys[i] : -ys[i];
+                }
+            }
         }
     }
     const int partner = turns && !a.interleaved ? (second ? c - half / 8 : c + half / 8) : c;
     const int lane = threadIdx.x & 31, from = lane - (lane % kLanes) + partner;
 
     // the same number of turns for every thread, so that whole warps take part in the shuffles
-    for (int h0 = 0; h0 < heads; h0 += kHeads) {
-        const int h = h0 + part;
-        const bool live = h < heads;
-        float x[8];
-        if (live) load8<T>(x_in + h * D + 8 * c, x);
-        else
+    for (int h0 = 0; h0 < heads; h0 += kAhead * kHeads) {
+        if (h0) fetch(h0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.f;
-        const bool is_v = h >= hq + hkv, is_k = !is_v && h >= hq;
-        const void *weight = is_v ? nullptr : is_k ? a.k_weight : a.q_weight;
-        float sum = 0.f;
+        for (int u = 0; u < kAhead; ++u) {
+            if (h0 + u * kHeads >= heads) break;
+            const int h = h0 + u * kHeads + part;
+            const bool is_v = h >= hq + hkv, is_k = !is_v && h >= hq;
+            float x[8];
+            unpack8<T>(raw[u], x);
+            uint4 w = raw[u];
+            if (h0 + u * kHeads < hq + hkv) {        // some of the warps' heads are q or k heads
+                const bool normed = is_k ? a.k_weight != nullptr : a.q_weight != nullptr;
+                if (a.q_weight || a.k_weight) {
+                    float sum = 0.f, scale[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
+                    for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
 #pragma unroll
-        for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
-        if (weight) {
-            float w[8];
-            load8<T>(static_cast<const T *>(weight) + 8 * c, w);
-            const float r = rsqrtf(sum * (1.f / D) + a.eps);
+                    for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
+                    unpack8<T>(is_k ? kw : qw, scale);
+                    const float r = rsqrtf(sum * (1.f / D) + a.eps);
+                    if (normed)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= r * w[i];
-        }
-        float y[8];
-        if (a.interleaved) {
+                        for (int i = 0; i < 8; ++i) x[i] *= r * scale[i];
+                }
+                float y[8];
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                y[i] = x[i] * cosv[i] - x[i + 1] * sinv[i];
-                y[i + 1] = x[i + 1] * cosv[i] + x[i] * sinv[i];
+                for (int i = 0; i < 8; ++i) {
+                    const float other = __shfl_sync(~0u, x[i], from);
+                    y[i] = turns ? x[i] * cosv[i] + (a.interleaved ? x[i ^ 1] : other) * sinv[i] : x[i];
+                }
+                if (!is_v) w = make_uint4(Half<T>::pack(y[0], y[1]), Half<T>::pack(y[2], y[3]), Half<T>::pack(y[4], y[5]), Half<T>::pack(y[6], y[7]));
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float other = __shfl_sync(~0u, x[i], from);
-                y[i] = x[i] * cosv[i] + (second ? other : -other) * sinv[i];
-            }
+            if (h >= heads) continue;
+            T *to = is_v ? v_out + (h - hq - hkv) * g.cache.v_stride[2]
+                         : is_k ? k_out + (h - hq) * g.cache.k_stride[2] : q_out + (int64_t)h * D;
+            *reinterpret_cast<uint4 *>(to + 8 * c) = w;
         }
-        if (!live) continue;
-        uint4 w;
-        if (is_v || !turns) w = make_uint4(Half<T>::pack(x[0], x[1]), Half<T>::pack(x[2], x[3]),
-                                           Half<T>::pack(x[4], x[5]), Half<T>::pack(x[6], x[7]));
-        else w = make_uint4(Half<T>::pack(y[0], y[1]), Half<T>::pack(y[2], y[3]), Half<T>::pack(y[4], y[5]),
-                            Half<T>::pack(y[6], y[7]));
-        T *to = is_v ? v_out + (h - hq - hkv) * g.cache.v_stride[2]
-                     : is_k ? k_out + (h - hq) * g.cache.k_stride[2] : q_out + (int64_t)h * D;
-        *reinterpret_cast<uint4 *>(to + 8 * c) = w;
     }
 }
 

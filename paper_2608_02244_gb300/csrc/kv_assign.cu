@@ -5,44 +5,43 @@
 // block of threads takes the sums and everything else is independent: entry t of the maps finds its row by a
 // search in `starts`, the k-th new block is the k-th from the top of the free list (or, where that was
 // pushed in this very call, an entry of an ended row's table row, found by a search in `first_back`).
-// Bound by latency for a step's few hundred tokens, by the 20 bytes a map entry for prompts.
-#include "kv_internal.cuh"
+// Bound by latency for a step's few hundred tokens: one kernel does it all from shared memory.  Prompts are
+// bound by the 20 bytes a map entry: the block of the sums is followed by a grid that fills the maps.
+#include "kv_tma.cuh"
 
 namespace isjl {
 namespace {
 
 constexpr int kScan = 1024;   // threads of the block that takes the sums
-constexpr int kFill = 256;    // threads of the blocks that fill the maps
+constexpr int kFill = 256;    // threads of the blocks that fill the maps, 4 entries each
 
-// exclusive sums of two numbers over the block's threads, and their totals
-__device__ __forceinline__ void scan2(int64_t &x, int64_t &y, int64_t &tx, int64_t &ty, int64_t (*sums)[2]) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t ix = x, iy = y;
+// inclusive sums of N numbers over the block's threads, and their totals
+template <int N>
+__device__ __forceinline__ void scan(int64_t (&x)[N], int64_t (&total)[N], int64_t (*sums)[3]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int64_t px = __shfl_up_sync(~0u, ix, d), py = __shfl_up_sync(~0u, iy, d);
-        if (lane >= d) { ix += px; iy += py; }
-    }
-    __syncthreads();
-    if (lane == 31) { sums[warp][0] = ix; sums[warp][1] = iy; }
-    __syncthreads();
-    if (warp == 0) {
-        const int64_t vx = sums[lane][0], vy = sums[lane][1];
-        int64_t sx = vx, sy = vy;
+    for (int d = 1; d < 32; d <<= 1)
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int64_t px = __shfl_up_sync(~0u, sx, d), py = __shfl_up_sync(~0u, sy, d);
-            if (lane >= d) { sx += px; sy += py; }
+        for (int k = 0; k < N; ++k) {
+            const int64_t p = __shfl_up_sync(~0u, x[k], d);
+            if (lane >= d) x[k] += p;
         }
-        sums[lane][0] = sx - vx;
-        sums[lane][1] = sy - vy;
-        if (lane == 31) { sums[32][0] = sx; sums[32][1] = sy; }
-    }
     __syncthreads();
-    x = sums[warp][0] + ix - x;
-    y = sums[warp][1] + iy - y;
-    tx = sums[32][0];
-    ty = sums[32][1];
+    if (lane == 31)
+#pragma unroll
+        for (int k = 0; k < N; ++k) sums[warp][k] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {       // each warp sums those before it
+        int64_t v = lane < warps ? sums[lane][k] : 0, before = lane < warp ? v : 0;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            v += __shfl_xor_sync(~0u, v, d);
+            before += __shfl_xor_sync(~0u, before, d);
+        }
+        x[k] += before;
+        total[k] = v;
+    }
 }
 
 struct Row {
@@ -65,9 +64,8 @@ __device__ __forceinline__ Row load_row(const AssignArgs &g, int i) {
     return r;
 }
 
-// last i in 0..n-1 with first[i] <= x, for first[0] = 0
-__device__ __forceinline__ int find(const int32_t *first, int n, int32_t x) {
-    int lo = 0, hi = n;
+// last i in lo..hi-1 with first[i] <= x, for first[lo] <= x
+__device__ __forceinline__ int find(const int32_t *first, int lo, int hi, int32_t x) {
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (first[mid] <= x) lo = mid; else hi = mid;
@@ -75,12 +73,18 @@ __device__ __forceinline__ int find(const int32_t *first, int n, int32_t x) {
     return lo;
 }
 
+// the sums, in the block's shared memory or where they were written for a grid
+struct Sums {
+    const int32_t *starts, *take, *back, *old;      // tokens, blocks taken, blocks given back before each row; its length
+    int32_t n_free, avail, tokens, takes, backs;
+};
+
 // entry `index` of the free list after the pushes of this call
-__device__ __forceinline__ int32_t free_block(const AssignArgs &g, int32_t n_free, int32_t index) {
-    if (index < n_free) return g.a.free_list[index];
-    const int32_t k = index - n_free;
-    const int i = find(g.first_back, g.a.n_rows, k);
-    return g.a.table[(int64_t)i * g.a.table_width + (k - g.first_back[i])];
+__device__ __forceinline__ int32_t free_block(const AssignArgs &g, const Sums &h, int32_t index) {
+    if (index < h.n_free) return g.a.free_list[index];
+    const int32_t k = index - h.n_free;
+    const int i = find(h.back, 0, g.a.n_rows, k);
+    return g.a.table[(int64_t)i * g.a.table_width + (k - h.back[i])];
 }
 
 __device__ __forceinline__ int32_t free_count(const AssignArgs &g) {
@@ -89,113 +93,192 @@ __device__ __forceinline__ int32_t free_count(const AssignArgs &g) {
     return min(max(n, 0), g.n_blocks);
 }
 
-// n_free and n_free_out may be the same word: what the fill needs of it was put here
-struct Head {
-    int32_t n_free, avail;
+struct Entry {
+    int64_t slot;
+    int32_t position, row, visible;
 };
 
-// the maps, the new table entries and the pushes, by `count` threads of which this is number `me`
-__device__ __forceinline__ void fill(const AssignArgs &g, Head h, int me, int count) {
+// entry t of the maps, whose row lies in lo..hi-1
+__device__ __forceinline__ Entry entry_of(const AssignArgs &g, const Sums &h, int32_t t, int lo, int hi) {
+    if (t >= h.tokens) return {-1, 0, -1, 0};
+    const int mask = (1 << g.shift) - 1;
+    const int row = find(h.starts, lo, hi, t);
+    const int32_t old = h.old[row], at = old + t - h.starts[row];
+    const int32_t j = at >> g.shift, held = (int32_t)(((int64_t)old + mask) >> g.shift);
+    const int32_t block = j < held ? g.a.table[(int64_t)row * g.a.table_width + j]
+                                   : free_block(g, h, h.avail - 1 - (h.take[row] + j - held));
+    return {((int64_t)block << g.shift) + (at & mask), g.a.prefix_len + at, row, at + 1};
+}
+
+// the new table entries and the pushes, by `count` threads of which this is number `me`
+__device__ __forceinline__ void move_blocks(const AssignArgs &g, const Sums &h, int me, int count) {
     const isjl_kv_assign_args &a = g.a;
-    const int n = a.n_rows, mask = (1 << g.shift) - 1;
-    const int32_t total = n ? a.starts[n] : 0;
-    for (int64_t t = me; t < a.max_tokens; t += count) {
-        int64_t slot = -1;
-        int32_t position = 0, row = -1, visible = 0;
-        if (t < total) {
-            row = find(a.starts, n, (int32_t)t);
-            const int32_t old = a.lens_out[row] - a.granted[row];
-            const int32_t at = old + (int32_t)t - a.starts[row];
-            const int32_t j = at >> g.shift, held = (old + mask) >> g.shift;
-            const int32_t block = j < held ? a.table[(int64_t)row * a.table_width + j]
-                                           : free_block(g, h.n_free, h.avail - 1 - (g.first_take[row] + j - held));
-            slot = ((int64_t)block << g.shift) + (at & mask);
-            position = a.prefix_len + at;
-            visible = at + 1;
-        }
-        a.slots[t] = slot;
-        a.positions[t] = position;
-        a.rows[t] = row;
-        a.visible[t] = visible;
+    const int mask = (1 << g.shift) - 1;
+    for (int32_t k = me; k < h.takes; k += count) {
+        const int i = find(h.take, 0, a.n_rows, k);
+        const int32_t j = (int32_t)(((int64_t)h.old[i] + mask) >> g.shift) + k - h.take[i];
+        a.table[(int64_t)i * a.table_width + j] = free_block(g, h, h.avail - 1 - k);
     }
-    const int32_t takes = n ? g.first_take[n] : 0, backs = n ? g.first_back[n] : 0;
-    for (int32_t k = me; k < takes; k += count) {
-        const int i = find(g.first_take, n, k);
-        const int32_t old = a.lens_out[i] - a.granted[i];
-        const int32_t j = ((old + mask) >> g.shift) + k - g.first_take[i];
-        a.table[(int64_t)i * a.table_width + j] = free_block(g, h.n_free, h.avail - 1 - k);
-    }
-    for (int32_t k = me; k < backs; k += count) {
+    for (int32_t k = me; k < h.backs; k += count) {
         if (h.n_free + k >= g.n_blocks) { report(g.status); break; }
-        const int i = find(g.first_back, n, k);
-        a.free_list[h.n_free + k] = a.table[(int64_t)i * a.table_width + (k - g.first_back[i])];
+        const int i = find(h.back, 0, a.n_rows, k);
+        a.free_list[h.n_free + k] = a.table[(int64_t)i * a.table_width + (k - h.back[i])];
     }
 }
 
-// The sums over the rows.  Each thread takes a run of neighbouring rows, so that one scan over the block is
-// enough for any number of them; asked and granted sums take a scan each, since grants depend on the former.
-__device__ __forceinline__ Head sums(const AssignArgs &g, int64_t (*smem)[2]) {
+// The sums over the rows, into the given arrays [n_rows + 1] (old: [n_rows]).  Each thread takes a run of
+// neighbouring rows, so that one scan over the block is enough for any number of them; a second one is needed
+// only where something is refused.
+__device__ __forceinline__ Sums sums(const AssignArgs &g, int32_t *starts, int32_t *take, int32_t *back, int32_t *old, int64_t (*smem)[3]) {
     const isjl_kv_assign_args &a = g.a;
-    const int n = a.n_rows, per = (n + kScan - 1) / kScan;
+    const int n = a.n_rows, per = (n + blockDim.x - 1) / blockDim.x;
     const int begin = min(n, (int)threadIdx.x * per), end = min(n, begin + per);
     const int32_t n_free = free_count(g);
-    int64_t need = 0, ask = 0, back = 0, unused = 0, all_need, all_ask, backs, none;
+    int64_t x[3] = {0, 0, 0}, total[3], own[3];
+    Row r = {};
     for (int i = begin; i < end; ++i) {
-        const Row r = load_row(g, i);
+        r = load_row(g, i);
+        x[0] += r.need;
+        x[1] += r.ask;
+        x[2] += r.back;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) own[k] = x[k];
+    scan(x, total, smem);
+    const int32_t avail = (int32_t)min((int64_t)n_free + total[2], (int64_t)g.n_blocks);
+    int64_t need = x[0] - own[0], ask = x[1] - own[1], given = x[2] - own[2];          // before this thread's rows
+    int64_t y[2] = {need, ask}, got[2] = {total[0], total[1]};
+    const bool all = total[0] <= avail && total[1] <= a.max_tokens;
+    if (!all) {
+        int64_t need_to = need, ask_to = ask;
+        y[0] = y[1] = 0;
+        for (int i = begin; i < end; ++i) {
+            if (per > 1) r = load_row(g, i);
+            need_to += r.need;
+            ask_to += r.ask;
+            const bool ok = (r.need == 0 || need_to <= avail) && ask_to <= a.max_tokens;
+            y[0] += ok ? r.need : 0;
+            y[1] += ok ? r.ask : 0;
+        }
+        const int64_t mine[2] = {y[0], y[1]};
+        scan(y, got, smem);
+        y[0] -= mine[0];
+        y[1] -= mine[1];
+    }
+    for (int i = begin; i < end; ++i) {
+        if (per > 1) r = load_row(g, i);
         need += r.need;
         ask += r.ask;
-        back += r.back;
-    }
-    scan2(need, ask, all_need, all_ask, smem);
-    scan2(back, unused, backs, none, smem);
-    const int32_t avail = (int32_t)min((int64_t)n_free + backs, (int64_t)g.n_blocks);
-    int64_t takes = 0, tokens = 0, total_takes, total_tokens, need_before = need, ask_before = ask;
-    for (int i = begin; i < end; ++i) {
-        const Row r = load_row(g, i);
-        need_before += r.need;
-        ask_before += r.ask;
-        const bool ok = (r.need == 0 || need_before <= avail) && ask_before <= a.max_tokens;
-        takes += ok ? r.need : 0;
-        tokens += ok ? r.ask : 0;
-    }
-    scan2(takes, tokens, total_takes, total_tokens, smem);
-    for (int i = begin; i < end; ++i) {
-        const Row r = load_row(g, i);
-        need += r.need;
-        ask += r.ask;
-        const bool ok = (r.need == 0 || need <= avail) && ask <= a.max_tokens;
-        g.first_back[i] = (int32_t)back;
-        g.first_take[i] = (int32_t)takes;
-        a.starts[i] = (int32_t)tokens;
-        const bool ends = a.new_tokens[i] < 0;
+        const bool ok = all || ((r.need == 0 || need <= avail) && ask <= a.max_tokens);
+        take[i] = (int32_t)y[0];
+        starts[i] = (int32_t)y[1];
+        back[i] = (int32_t)given;
+        old[i] = r.len;
         a.granted[i] = ok ? r.ask : 0;
-        back += r.back;
-        if (ok) { takes += r.need; tokens += r.ask; }
+        a.starts[i] = (int32_t)y[1];
+        const bool ends = a.new_tokens[i] < 0;
         a.lens_out[i] = ends ? 0 : r.len + (ok ? r.ask : 0);
+        given += r.back;
+        if (ok) { y[0] += r.need; y[1] += r.ask; }
     }
-    if (threadIdx.x == 0) {
-        g.first_back[n] = (int32_t)backs;
-        g.first_take[n] = (int32_t)total_takes;
-        a.starts[n] = (int32_t)total_tokens;
-    }
-    __syncthreads();              // all have read n_free
-    if (threadIdx.x == 0) *a.n_free_out = avail - (int32_t)total_takes;
-    return {n_free, avail};
+    if (threadIdx.x == 0) a.starts[n] = (int32_t)got[1];
+    __syncthreads();              // all have read n_free, all sums are written
+    if (threadIdx.x == 0) *a.n_free_out = avail - (int32_t)got[0];
+    return {starts, take, back, old, n_free, avail, (int32_t)got[1], (int32_t)got[0], (int32_t)total[2]};
 }
 
+// a whole step of at most kScan rows
 __global__ void __launch_bounds__(kScan) assign_kernel(const __grid_constant__ AssignArgs g) {
-    __shared__ int64_t smem[33][2];
-    const Head h = sums(g, smem);
-    __syncthreads();
-    fill(g, h, threadIdx.x, kScan);
+    __shared__ int64_t smem[32][3];
+    __shared__ int32_t rows[4][kScan];
+    const Sums h = sums(g, rows[0], rows[1], rows[2], rows[3], smem);
+    const isjl_kv_assign_args &a = g.a;
+    for (int64_t t = threadIdx.x; t < a.max_tokens; t += blockDim.x) {
+        const Entry e = entry_of(g, h, (int32_t)t, 0, a.n_rows);
+        a.slots[t] = e.slot;
+        a.positions[t] = e.position;
+        a.rows[t] = e.row;
+        a.visible[t] = e.visible;
+    }
+    move_blocks(g, h, threadIdx.x, blockDim.x);
+}
+
+__global__ void __launch_bounds__(kScan) sums_kernel(const __grid_constant__ AssignArgs g) {
+    __shared__ int64_t smem[32][3];
+    start_next();
+    int32_t *w = g.work;
+    const int n = g.a.n_rows;
+    const Sums h = sums(g, w + 8, w + 8 + n, w + 8 + 2 * n, w + 8 + 3 * n, smem);
+    if (threadIdx.x == 0) {
+        w[0] = h.n_free;
+        w[1] = h.avail;
+        w[2] = h.tokens;
+        w[3] = h.takes;
+        w[4] = h.backs;
+    }
+}
+
+__global__ void __launch_bounds__(kFill) fill_kernel(const __grid_constant__ AssignArgs g) {
+    wait_for_previous();
+    const isjl_kv_assign_args &a = g.a;
+    const int n = a.n_rows;
+    const int32_t *w = g.work;
+    const Sums h = {w + 8, w + 8 + n, w + 8 + 2 * n, w + 8 + 3 * n, w[0], w[1], w[2], w[3], w[4]};
+    // 4 neighbouring entries a thread, of 4 kFill a block: their rows are between those of the block's ends
+    for (int64_t t0 = (int64_t)blockIdx.x * 4 * kFill; t0 < a.max_tokens; t0 += (int64_t)gridDim.x * 4 * kFill) {
+        int lo = 0, hi = n;
+        if (t0 < h.tokens) {
+            lo = find(h.starts, 0, n, (int32_t)t0);
+            hi = find(h.starts, lo, n, (int32_t)min(t0 + 4 * kFill - 1, (int64_t)h.tokens - 1)) + 1;
+        }
+        const int64_t t = t0 + 4 * threadIdx.x;
+        if (t >= a.max_tokens) continue;
+        Entry e[4];
+        e[0] = entry_of(g, h, (int32_t)t, lo, hi);
+        const int mask = (1 << g.shift) - 1;
+        const bool one_block = t + 3 < h.tokens && (e[0].slot & mask) + 3 <= mask && (e[0].row + 1 == n || t + 3 < h.starts[e[0].row + 1]);
+#pragma unroll
+        for (int k = 1; k < 4; ++k) {
+            if (one_block) e[k] = {e[0].slot + k, e[0].position + k, e[0].row, e[0].visible + k};
+            else e[k] = entry_of(g, h, (int32_t)min(t + k, (int64_t)INT32_MAX), lo, hi);
+        }
+        if (t + 3 < a.max_tokens && g.aligned) {
+            reinterpret_cast<longlong2 *>(a.slots + t)[0] = make_longlong2(e[0].slot, e[1].slot);
+            reinterpret_cast<longlong2 *>(a.slots + t)[1] = make_longlong2(e[2].slot, e[3].slot);
+            *reinterpret_cast<int4 *>(a.positions + t) = make_int4(e[0].position, e[1].position, e[2].position, e[3].position);
+            *reinterpret_cast<int4 *>(a.rows + t) = make_int4(e[0].row, e[1].row, e[2].row, e[3].row);
+            *reinterpret_cast<int4 *>(a.visible + t) = make_int4(e[0].visible, e[1].visible, e[2].visible, e[3].visible);
+        } else {
+            for (int k = 0; k < 4 && t + k < a.max_tokens; ++k) {
+                a.slots[t + k] = e[k].slot;
+                a.positions[t + k] = e[k].position;
+                a.rows[t + k] = e[k].row;
+                a.visible[t + k] = e[k].visible;
+            }
+        }
+    }
+    move_blocks(g, h, blockIdx.x * kFill + threadIdx.x, gridDim.x * kFill);
 }
 
 }  // namespace
 
-cudaError_t launch_assign(const AssignArgs &g, int sms, cudaStream_t st) {
-    (void)sms;
-    assign_kernel<<<1, kScan, 0, st>>>(g);
-    return cudaGetLastError();
+// One kernel fills 1,024 entries in about 0.5 us and its block alone moves the blocks; the grid's sums pass
+// through memory and a second kernel's start.  Measured at 256 rows: see kOneKernel.
+constexpr int kOneKernel = 4096;
+
+cudaError_t launch_assign(const AssignArgs &args, int sms, cudaStream_t st) {
+    AssignArgs g = args;
+    if (g.a.n_rows <= kScan && g.a.max_tokens <= kOneKernel) {
+        const int most = g.a.n_rows > g.a.max_tokens ? g.a.n_rows : g.a.max_tokens;
+        const int threads = most >= kScan ? kScan : most <= 128 ? 128 : (most + 31) / 32 * 32;
+        return launch_kernel(assign_kernel, 1, threads, 0, st, false, g);
+    }
+    g.aligned = ((reinterpret_cast<uintptr_t>(g.a.slots) | reinterpret_cast<uintptr_t>(g.a.positions) |
+                  reinterpret_cast<uintptr_t>(g.a.rows) | reinterpret_cast<uintptr_t>(g.a.visible)) & 15u) == 0;
+    const cudaError_t e = launch_kernel(sums_kernel, 1, kScan, 0, st, false, g);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = ((int64_t)g.a.max_tokens + 4 * kFill - 1) / (4 * kFill);
+    return launch_kernel(fill_kernel, (int)(blocks < 8 * sms ? blocks : 8 * sms), kFill, 0, st, true, g);
 }
 
 }  // namespace isjl

@@ -66,8 +66,8 @@ __device__ __forceinline__ void report(int32_t *status) { atomicOr(status, 1); }
 struct AssignArgs {
     isjl_kv_assign_args a;
     int32_t n_blocks, shift;      // block_size = 1 << shift
-    int32_t *first_take;          // [n_rows + 1] new blocks taken before each row, and in all
-    int32_t *first_back;          // [n_rows + 1] blocks given back before each row, and in all
+    int32_t *work;                // [8 + 4 n_rows], the sums for the kernel that fills
+    int32_t aligned;              // the maps to 16 bytes
     int32_t *status;
 };
 cudaError_t launch_assign(const AssignArgs &a, int sms, cudaStream_t st);
@@ -106,6 +106,7 @@ struct PrefixArgs {
     int32_t n, tokens, n_blocks, shift, n_kv_heads, group;
 };
 void *tensor_map_encoder();       // null if the driver has none
+cudaError_t prepare_prefix(int head_dim, int type);   // once for a shape, before its first launch
 PrefixLine prefix_line(int n, int group, int n_kv_heads, int tokens, int sms);
 cudaError_t launch_prefix(const PrefixArgs &g, const isjl_kv_cache &cache, void *encoder, int head_dim, int type, cudaStream_t st);
 

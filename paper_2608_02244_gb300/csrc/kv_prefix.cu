@@ -385,12 +385,20 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
 
 template <int D, typename T>
 cudaError_t launch_of(const PrefixArgs &g, const CUtensorMap &k, const CUtensorMap &v, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(prefix_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem);
-    if (e != cudaSuccess) return e;
     return launch_kernel(prefix_kernel<D, T>, g.line.blocks, kThreads, Shape<D>::kSmem, st, false, g, k, v);
 }
 
+template <int D, typename T>
+cudaError_t prepare_of() {
+    return cudaFuncSetAttribute(prefix_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem);
+}
+
 }  // namespace
+
+cudaError_t prepare_prefix(int head_dim, int type) {
+    if (type == ISJL_KV_BF16) return head_dim == 64 ? prepare_of<64, __nv_bfloat16>() : prepare_of<128, __nv_bfloat16>();
+    return head_dim == 64 ? prepare_of<64, __half>() : prepare_of<128, __half>();
+}
 
 PrefixLine prefix_line(int n, int group, int n_kv_heads, int tokens, int sms) {
     PrefixLine ln;

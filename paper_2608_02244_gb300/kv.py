@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import collections
 import ctypes
+import struct
 
 from . import sim
 from .sim import ISJL_ERR_INVALID_ARG, ISJL_OK, IsjlError
@@ -51,6 +52,12 @@ class isjl_kv_attend_args(ctypes.Structure):
         ("lens", _vp), ("rows", _vp), ("table", _vp), ("prefix", _vp)]
 
 
+# The same layouts as bytes: filling a structure field by field costs a call 3 us of host time, packing 0.3
+_CACHE = struct.Struct("=2Q6q")
+_ASSIGN = struct.Struct("=4i13Q")
+_APPEND = struct.Struct("=4if4xQqQq5Q")
+_ATTEND = struct.Struct("=6if4xQ2qQ2q5Q")
+
 _lib = None
 
 
@@ -62,9 +69,9 @@ def lib():
         L.isjl_kv_create.argtypes = [ctypes.POINTER(isjl_kv_config), ctypes.POINTER(_vp)]
         L.isjl_kv_destroy.argtypes = [_vp]
         L.isjl_kv_destroy.restype = None
-        L.isjl_kv_assign.argtypes = [_vp, ctypes.POINTER(isjl_kv_assign_args), _vp]
-        L.isjl_kv_append.argtypes = [_vp, ctypes.POINTER(isjl_kv_append_args), ctypes.POINTER(isjl_kv_cache), _vp]
-        L.isjl_kv_attend.argtypes = [_vp, ctypes.POINTER(isjl_kv_attend_args), ctypes.POINTER(isjl_kv_cache), _vp]
+        L.isjl_kv_assign.argtypes = [_vp, _vp, _vp]            # structures by address, or their bytes
+        L.isjl_kv_append.argtypes = [_vp, _vp, _vp, _vp]
+        L.isjl_kv_attend.argtypes = [_vp, _vp, _vp, _vp]
         L.isjl_kv_status.argtypes = [_vp]
         for f in ("create", "assign", "append", "attend", "status"):
             getattr(L, "isjl_kv_" + f).restype = ctypes.c_int
@@ -116,7 +123,10 @@ class Decoder:
         self.handle = isjl_kv_create(n_blocks, block_size, n_q_heads, n_kv_heads, head_dim,
                                      BF16 if self.dtype == torch.bfloat16 else FP16, max_rows)
         self._lib = lib()
+        self._index = self.device.index
+        self._raw_stream = torch._C._cuda_getCurrentRawStream      # 0.1 us; torch.cuda.current_stream 1.9
         self._cache_shape = (self.n_blocks, self.block_size, self.n_kv_heads, self.head_dim)
+        self._qkv = (self.n_q_heads + 2 * self.n_kv_heads) * self.head_dim
 
     def close(self):
         if self.handle:
@@ -134,31 +144,30 @@ class Decoder:
         raise IsjlError(ISJL_ERR_INVALID_ARG, f"Decoder: {what}")
 
     def _ints(self, name, t, shape, dtype):
-        if t.dtype != dtype or t.device != self.device or t.shape != shape or not t.is_contiguous():
+        if t.dtype is not dtype or t.get_device() != self._index or t.shape != shape or not t.is_contiguous():
             self._bad(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}")
         return t.data_ptr()
 
     def _cache(self, k, v):
-        for name, t in (("k", k), ("v", v)):
-            if t.shape != self._cache_shape or t.dtype != self.dtype or t.device != self.device or t.stride(3) != 1:
-                self._bad(f"{name} cache must be {self.dtype} of shape {self._cache_shape} on {self.device} with stride 1 last")
+        shape, dtype, index = self._cache_shape, self.dtype, self._index
         ks, vs = k.stride(), v.stride()
-        return isjl_kv_cache(k.data_ptr(), v.data_ptr(), (_i64 * 3)(*self._steps(ks, k.shape)), (_i64 * 3)(*self._steps(vs, v.shape)))
-
-    @staticmethod
-    def _steps(strides, shape):
-        # the stride of an axis of one element says nothing: any valid one
-        return [s if n > 1 else 8 for s, n in zip(strides[:3], shape)]
+        if k.shape != shape or v.shape != shape or k.dtype is not dtype or v.dtype is not dtype or \
+                k.get_device() != index or v.get_device() != index or ks[3] != 1 or vs[3] != 1:
+            self._bad(f"caches must be {dtype} of shape {shape} on {self.device} with stride 1 last")
+        if shape[0] == 1 or shape[2] == 1:
+            # the stride of an axis of one element says nothing: any valid one
+            ks, vs = ([x if n > 1 else 8 for x, n in zip(y, shape)] for y in (ks, vs))
+        return _CACHE.pack(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2])
 
     def _stream(self, stream, tensors):
         """The stream's number; memory of a call on another stream than the current one stays
         until that stream is done with it."""
-        current = self.torch.cuda.current_stream(self.device)
-        if stream is None or stream == current:
-            return current.cuda_stream
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+        if stream is None:
+            return self._raw_stream(self._index)
+        if stream != self.torch.cuda.current_stream(self.device):
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
         return stream.cuda_stream
 
     # ---- the step's parts --------------------------------------------------
@@ -168,27 +177,31 @@ class Decoder:
         torch = self.torch
         i32 = torch.int32
         n, m = lens.shape[0], int(max_tokens)
-        if m < 1 or n > self.max_rows or table.dim() != 2 or table.shape[0] != n:
+        if not 1 <= m < 2**31 or n > self.max_rows or table.dim() != 2 or table.shape[0] != n:
             self._bad("assign needs max_tokens >= 1, at most max_rows lengths and a table row for each")
-        a = isjl_kv_assign_args(n, table.shape[1], m, int(prefix_len))
-        a.lens = self._ints("lens", lens, (n,), i32)
-        a.new_tokens = self._ints("new_tokens", new_tokens, (n,), i32)
-        a.table = self._ints("table", table, table.shape, i32)
-        a.free_list = self._ints("free", free, (self.n_blocks,), i32)
-        a.n_free = self._ints("n_free", n_free, (1,), i32)
-        # one allocation for the 32-bit results
-        sizes = [m, m, m, n + 1, n] + ([] if in_place else [n, 1])
+        prefix_len = int(prefix_len)
+        if not 0 <= prefix_len < 2**31:
+            self._bad("prefix_len out of range")
+        ptrs = (self._ints("lens", lens, (n,), i32), self._ints("new_tokens", new_tokens, (n,), i32),
+                self._ints("table", table, table.shape, i32), self._ints("free", free, (self.n_blocks,), i32),
+                self._ints("n_free", n_free, (1,), i32))
+        # one allocation for the 32-bit results, whose maps begin at multiples of 16 bytes
+        w = (m + 3) & ~3
+        sizes = [w, w, w, n + 1, n] if in_place else [w, w, w, n + 1, n, n, 1]
         slots = torch.empty(m, dtype=torch.int64, device=self.device)
-        block = torch.empty(sum(sizes), dtype=i32, device=self.device)
-        parts = block.split(sizes)
+        block = torch.empty(3 * w + (2 * n + 1 if in_place else 3 * n + 2), dtype=i32, device=self.device)
+        parts = block.split_with_sizes(sizes)
         positions, rows, visible, starts, granted = parts[:5]
+        if w != m:
+            positions, rows, visible = positions[:m], rows[:m], visible[:m]
         lens_out, n_free_out = (lens, n_free) if in_place else parts[5:]
-        a.slots, base = slots.data_ptr(), block.data_ptr()
-        a.positions, a.rows, a.visible, a.starts = base, base + 4 * m, base + 8 * m, base + 12 * m
-        a.granted = a.starts + 4 * (n + 1)
-        a.lens_out, a.n_free_out = (a.lens, a.n_free) if in_place else (a.granted + 4 * n, a.granted + 8 * n)
+        base = block.data_ptr()
+        at = base + 12 * w + 4 * (n + 1)
+        out = (ptrs[0], ptrs[4]) if in_place else (at + 4 * n, at + 8 * n)
+        args = _ASSIGN.pack(n, table.shape[1], m, prefix_len, *ptrs, *out, at, base + 12 * w, slots.data_ptr(), base,
+                            base + 4 * w, base + 8 * w)
         st = self._stream(stream, (lens, new_tokens, table, free, n_free, slots, block))
-        _check(self._lib.isjl_kv_assign(self.handle, ctypes.byref(a), st), "isjl_kv_assign")
+        _check(self._lib.isjl_kv_assign(self.handle, args, st), "isjl_kv_assign")
         return Plan(slots, positions, rows, visible, starts, granted, lens_out, n_free_out)
 
     def append(self, qkv, positions, slots, k, v, rope=None, q_weight=None, k_weight=None, eps=1e-6, pairs=False,
@@ -197,32 +210,30 @@ class Decoder:
         [tokens, (n_q_heads + 2 n_kv_heads) * head_dim]; returns the queries,
         [tokens, n_q_heads, head_dim].  rope None: no rotation; `pairs`: neighbours."""
         torch = self.torch
-        n, hq, d = qkv.shape[0], self.n_q_heads, self.head_dim
-        if qkv.dim() != 2 or qkv.shape[1] != (hq + 2 * self.n_kv_heads) * d or qkv.dtype != self.dtype or \
-                qkv.device != self.device or (n > 0 and qkv.stride(1) != 1):
-            self._bad(f"qkv must be {self.dtype} [tokens, {(hq + 2 * self.n_kv_heads) * d}] with stride 1 last")
+        hq, d, dtype, index = self.n_q_heads, self.head_dim, self.dtype, self._index
+        n = qkv.shape[0]
+        if qkv.shape != (n, self._qkv) or qkv.dtype is not dtype or qkv.get_device() != index or (n > 0 and qkv.stride(1) != 1):
+            self._bad(f"qkv must be {dtype} [tokens, {self._qkv}] with stride 1 last")
         cache = self._cache(k, v)
         if out is None:
-            out = torch.empty(n, hq, d, dtype=self.dtype, device=self.device)
-        elif out.shape != (n, hq, d) or out.dtype != self.dtype or out.device != self.device or \
+            out = torch.empty((n, hq, d), dtype=dtype, device=self.device)
+        elif out.shape != (n, hq, d) or out.dtype is not dtype or out.get_device() != index or \
                 out.stride(2) != 1 or (hq > 1 and out.stride(1) != d):
             self._bad("out must be [tokens, n_q_heads, head_dim] of the cache's type, heads side by side")
-        a = isjl_kv_append_args(n, 0, 0, bool(pairs), float(eps), qkv.data_ptr(), qkv.stride(0) if n > 1 else qkv.shape[1],
-                                out.data_ptr(), out.stride(0) if n > 1 else hq * d)
-        if n == 1 and a.q_out == a.qkv:
-            a.q_out_stride = a.qkv_stride
+        angles = places = n_positions = rot = 0
         if rope is not None:
-            if rope.dim() != 2 or rope.dtype != torch.float32 or rope.device != self.device or not rope.is_contiguous():
+            if rope.dim() != 2 or rope.dtype is not torch.float32 or rope.get_device() != index or not rope.is_contiguous():
                 self._bad("rope must be contiguous float32 [positions, rot]")
-            a.n_positions, a.rot = rope.shape
-            a.rope = rope.data_ptr()
-            a.positions = self._ints("positions", positions, (n,), torch.int32)
-        a.slots = self._ints("slots", slots, (n,), torch.int64)
-        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if w is not None:
-                setattr(a, name, self._ints(name, w, (d,), self.dtype))
+            n_positions, rot = rope.shape
+            angles, places = rope.data_ptr(), self._ints("positions", positions, (n,), torch.int32)
+        weights = [0 if w is None else self._ints(name, w, (d,), dtype) for name, w in (("q_weight", q_weight), ("k_weight", k_weight))]
+        x, y = qkv.data_ptr(), out.data_ptr()
+        # the stride of a single row says nothing
+        step, out_step = (qkv.stride(0), out.stride(0)) if n > 1 else (self._qkv, self._qkv if x == y else hq * d)
+        args = _APPEND.pack(n, n_positions, rot, bool(pairs), eps, x, step, y, out_step, *weights, angles, places,
+                            self._ints("slots", slots, (n,), torch.int64))
         st = self._stream(stream, (qkv, out, k, v, rope, positions, slots, q_weight, k_weight))
-        _check(self._lib.isjl_kv_append(self.handle, ctypes.byref(a), ctypes.byref(cache), st), "isjl_kv_append")
+        _check(self._lib.isjl_kv_append(self.handle, args, cache, st), "isjl_kv_append")
         return out
 
     def attend(self, q, k, v, table, lens, rows=None, prefix=None, window=0, sinks=0, scale=None, out=None, lse=False,
@@ -231,35 +242,35 @@ class Decoder:
         tokens: see isjl_kv_attend.  scale defaults to head_dim ** -0.5.  With `lse`
         returns (out, lse)."""
         torch = self.torch
-        n, hq, d = q.shape[0], self.n_q_heads, self.head_dim
+        hq, d, dtype, index = self.n_q_heads, self.head_dim, self.dtype, self._index
+        n = q.shape[0]
         shape = (n, hq, d)
-        if q.shape != shape or q.dtype != self.dtype or q.device != self.device or q.stride(2) != 1 or n > self.max_rows:
-            self._bad(f"q must be {self.dtype} [at most {self.max_rows}, {hq}, {d}] with stride 1 last")
+        if q.shape != shape or q.dtype is not dtype or q.get_device() != index or q.stride(2) != 1 or n > self.max_rows:
+            self._bad(f"q must be {dtype} [at most {self.max_rows}, {hq}, {d}] with stride 1 last")
         cache = self._cache(k, v)
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
-        elif out.shape != shape or out.dtype != self.dtype or out.device != self.device or out.stride(2) != 1:
+            out = torch.empty(shape, dtype=dtype, device=self.device)
+        elif out.shape != shape or out.dtype is not dtype or out.get_device() != index or out.stride(2) != 1:
             self._bad("out must have q's shape and type with stride 1 last")
         if table.dim() != 2:
             self._bad("table must be [rows, width]")
-        a = isjl_kv_attend_args(n, table.shape[0], table.shape[1], 0, int(window), int(sinks),
-                                d ** -0.5 if scale is None else float(scale), q.data_ptr())
-        a.q_stride[0], a.q_stride[1] = q.stride(0) if n > 1 else 8, q.stride(1) if hq > 1 else 8
-        a.out_stride[0], a.out_stride[1] = out.stride(0) if n > 1 else 8, out.stride(1) if hq > 1 else 8
-        a.out = out.data_ptr()
-        weights = None
-        if lse:
-            weights = torch.empty((n, hq), dtype=torch.float32, device=self.device)
-            a.lse = weights.data_ptr()
-        a.table = self._ints("table", table, table.shape, torch.int32)
-        a.lens = self._ints("lens", lens, (n,), torch.int32)
-        if rows is not None:
-            a.rows = self._ints("rows", rows, (n,), torch.int32)
-        if prefix is not None:
-            a.n_prefix_blocks = prefix.numel()
-            a.prefix = self._ints("prefix", prefix, (prefix.numel(),), torch.int32)
+        window, sinks = int(window), int(sinks)
+        if not (0 <= window < 2**31 and 0 <= sinks < 2**31):
+            self._bad("window and sinks must be in 0..2^31 - 1")
+        weights = torch.empty((n, hq), dtype=torch.float32, device=self.device) if lse else None
+        # the stride of an axis of one element says nothing: any valid one
+        qs, os = q.stride(), out.stride()
+        if n <= 1 or hq == 1:
+            qs, os = ([x if m > 1 else 8 for x, m in zip(y, shape)] for y in (qs, os))
+        i32 = torch.int32
+        args = _ATTEND.pack(n, table.shape[0], table.shape[1], 0 if prefix is None else prefix.numel(), window, sinks,
+                            d ** -0.5 if scale is None else scale, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1],
+                            weights.data_ptr() if lse else 0, self._ints("lens", lens, (n,), i32),
+                            0 if rows is None else self._ints("rows", rows, (n,), i32),
+                            self._ints("table", table, table.shape, i32),
+                            0 if prefix is None else self._ints("prefix", prefix, (prefix.numel(),), i32))
         st = self._stream(stream, (q, k, v, table, lens, rows, prefix, out, weights))
-        _check(self._lib.isjl_kv_attend(self.handle, ctypes.byref(a), ctypes.byref(cache), st), "isjl_kv_attend")
+        _check(self._lib.isjl_kv_attend(self.handle, args, cache, st), "isjl_kv_attend")
         return (out, weights) if lse else out
 
     def status(self):

@@ -47,6 +47,20 @@ def test_layout(kv):
             assert int(out["%s.%s" % (s, f[0])]) == getattr(cls, f[0]).offset, (s, f[0])
 
 
+@pytest.mark.parametrize("name,packed", [("isjl_kv_cache", "_CACHE"), ("isjl_kv_assign_args", "_ASSIGN"),
+                                         ("isjl_kv_append_args", "_APPEND"), ("isjl_kv_attend_args", "_ATTEND")])
+def test_packed_layout(kv, name, packed):
+    """The bytes that Decoder packs are the structure's: each value at its field."""
+    cls, s = getattr(kv, name), getattr(kv, packed)
+    assert s.size == ctypes.sizeof(cls)
+    flat = []
+    for f, t in cls._fields_:
+        flat += [(f, i) for i in range(t._length_)] if hasattr(t, "_length_") else [(f, None)]
+    a = cls.from_buffer_copy(s.pack(*range(1, len(flat) + 1)))
+    for k, (f, i) in enumerate(flat):
+        assert (getattr(a, f) if i is None else getattr(a, f)[i]) == k + 1, f
+
+
 @pytest.mark.parametrize("change", [dict(n_blocks=0), dict(block_size=4), dict(block_size=24), dict(block_size=512),
                                     dict(n_kv_heads=0), dict(n_q_heads=12), dict(n_q_heads=2048), dict(n_q_heads=4),
                                     dict(head_dim=96), dict(head_dim=512), dict(type=2), dict(max_rows=0)])
