@@ -13,7 +13,7 @@ struct isjl_kv {
     unsigned char *d_work = nullptr;
     int32_t *d_status = nullptr;
     int32_t *d_sums = nullptr;
-    int32_t *d_before = nullptr;
+    isjl::CutItem *d_cut = nullptr;
     float2 *d_part_ml = nullptr;
     float *d_part_o = nullptr;
     float2 *d_prefix_ml = nullptr;       // null: this shape has no prefix kernel
@@ -26,6 +26,7 @@ struct isjl_kv {
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr int kFiner = 4;     // blocks of the own tokens' kernel for each that fits, beside a prefix's kernel
 size_t rounded(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -44,6 +45,28 @@ isjl_status launched(isjl_kv *kv, cudaError_t e, cudaStream_t st) {
     kv->last_stream = st;
     kv->ran = true;
     return ISJL_OK;
+}
+
+// Own tokens are bound by memory, the prefix by the tensor cores, and a block of either fills its SM: some SMs are
+// left to the former, which start at once.  Measured: 1.45 us for a step of the prefix's line (256 rows and 128
+// tokens; 0.9 for a single row tile) after 5 us; own tokens at 65 GB/s an SM beside it, 5.5 TB/s on all.  How long
+// requests are only the device knows: they are taken as a quarter of the table's width.
+isjl::PrefixLine share_sms(const isjl_kv *kv, const isjl_kv_attend_args *a, int group, int n_kv_heads, int tokens, int *grid) {
+    const double own = 0.25 * a->n * ((double)a->table_width * kv->cfg.block_size) * 4.0 * kv->cfg.head_dim * n_kv_heads;
+    isjl::PrefixLine best{};
+    double least = 0;
+    int left_best = 0;
+    for (int left = 0; left <= kv->sms * 5 / 8; left += 8) {
+        const isjl::PrefixLine ln = isjl::prefix_line(a->n, group, n_kv_heads, tokens, kv->sms - left);
+        const double steps = (double)((ln.work() + ln.blocks - 1) / ln.blocks);
+        const double alone = 5e-6 + steps * (a->n > ln.tokens_of_tile ? 1.45e-6 : 0.9e-6);
+        const double rest = own - alone * (kv->sms - ln.blocks) * 65e9;
+        const double all = alone + (rest > 0 ? rest / 5.5e12 : 0);
+        if (left == 0 || all < least) { least = all; best = ln; left_best = left; }
+    }
+    // many runs end one after another beside a long prefix
+    if (left_best > 0 && least > 100e-6) *grid *= kFiner;
+    return best;
 }
 
 }  // namespace
@@ -101,11 +124,14 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
         delete kv;
         return ISJL_ERR_CUDA;
     }
-    const size_t rows = rounded(sizeof(int32_t) * ((size_t)queries + 1)), sums = rounded(sizeof(int32_t) * (8 + 4 * (size_t)cfg->max_rows));
-    const size_t warps = (size_t)kv->grid * isjl::kAttendWarps;
+    const bool shares = cfg->head_dim <= 128 && cfg->n_q_heads / cfg->n_kv_heads <= 128;
+    const size_t sums = rounded(sizeof(int32_t) * (8 + 4 * (size_t)cfg->max_rows));
+    const size_t warps = (size_t)kv->grid * isjl::kAttendWarps * (shares ? kFiner : 1);
+    const int group = cfg->n_q_heads / cfg->n_kv_heads;
+    const size_t items = (size_t)queries * cfg->n_kv_heads * ((group + 15) / 16);
+    const size_t cuts = rounded(sizeof(isjl::CutItem) * (items > warps ? items : warps));
     const size_t ml = rounded(sizeof(float2) * 32 * warps), o = sizeof(float) * 32 * cfg->head_dim * warps;
     // pieces of the prefix part: an item of 256 rows lies in at most sms / items + 2 blocks; and the own tokens' part
-    const bool shares = cfg->head_dim <= 128 && cfg->n_q_heads / cfg->n_kv_heads <= 128;
     const size_t pieces = shares ? (size_t)kv->sms * 256 + 3 * (size_t)queries * cfg->n_q_heads : 0;
     const size_t prefix_ml = rounded(sizeof(float2) * pieces), prefix_o = sizeof(float) * cfg->head_dim * pieces;
     if (!(kv->encoder = isjl::tensor_map_encoder()) ||
@@ -114,7 +140,7 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
         delete kv;
         return ISJL_ERR_CUDA;
     }
-    const size_t total = kAlign + rows + sums + ml + rounded(o) + prefix_ml + prefix_o;
+    const size_t total = kAlign + cuts + sums + ml + rounded(o) + prefix_ml + prefix_o;
     if (cudaMalloc(reinterpret_cast<void **>(&kv->d_work), total) != cudaSuccess) {
         cudaGetLastError();
         delete kv;
@@ -123,8 +149,8 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
     unsigned char *p = kv->d_work;
     kv->d_status = reinterpret_cast<int32_t *>(p);
     p += kAlign;
-    kv->d_before = reinterpret_cast<int32_t *>(p);
-    p += rows;
+    kv->d_cut = reinterpret_cast<isjl::CutItem *>(p);
+    p += cuts;
     kv->d_sums = reinterpret_cast<int32_t *>(p);
     p += sums;
     kv->d_part_ml = reinterpret_cast<float2 *>(p);
@@ -219,14 +245,15 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
     g.group = kv->cfg.n_q_heads / kv->cfg.n_kv_heads;
     g.part_o = kv->d_part_o;
     g.part_ml = kv->d_part_ml;
-    g.before = kv->d_before;
+    g.cut = kv->d_cut;
     g.status = kv->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int grid = kv->grid;
     if (kv->d_prefix_o && a->n_prefix_blocks > 0 && a->window == 0) {
         isjl::PrefixArgs p;
         std::memset(&p, 0, sizeof(p));
         p.tokens = a->n_prefix_blocks << kv->shift;
-        p.line = isjl::prefix_line(a->n, g.group, g.n_kv_heads, p.tokens, kv->sms);
+        p.line = share_sms(kv, a, g.group, g.n_kv_heads, p.tokens, &grid);
         p.q = a->q;
         p.q_stride[0] = a->q_stride[0];
         p.q_stride[1] = a->q_stride[1];
@@ -245,7 +272,7 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
         g.prefix_ml = kv->d_prefix_ml;
         if (isjl::launch_prefix(p, *cache, kv->encoder, kv->cfg.head_dim, kv->cfg.type, st) != cudaSuccess) return ISJL_ERR_CUDA;
     }
-    return launched(kv, isjl::launch_attend(g, kv->encoder, kv->cfg.head_dim, kv->cfg.type, kv->grid, st), st);
+    return launched(kv, isjl::launch_attend(g, kv->encoder, kv->cfg.head_dim, kv->cfg.type, grid, st), st);
 }
 
 isjl_status isjl_kv_status(isjl_kv *kv) {

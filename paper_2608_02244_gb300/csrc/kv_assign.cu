@@ -13,6 +13,7 @@ namespace isjl {
 namespace {
 
 constexpr int kScan = 1024;   // threads of the block that takes the sums
+constexpr int kKeep = 4;      // rows of its threads that stay in registers
 constexpr int kFill = 256;    // threads of the blocks that fill the maps, 4 entries each
 
 // inclusive sums of N numbers over the block's threads, and their totals
@@ -46,6 +47,7 @@ __device__ __forceinline__ void scan(int64_t (&x)[N], int64_t (&total)[N], int64
 
 struct Row {
     int32_t len, held, back, ask, need;
+    bool ends;
 };
 
 __device__ __forceinline__ Row load_row(const AssignArgs &g, int i) {
@@ -57,6 +59,7 @@ __device__ __forceinline__ Row load_row(const AssignArgs &g, int i) {
     const bool bad = r.len < 0 || r.len > room;
     if (bad) report(g.status);
     r.held = bad ? 0 : (int32_t)(((int64_t)r.len + bs1) >> g.shift);
+    r.ends = fresh < 0;
     r.back = fresh < 0 ? r.held : 0;
     r.ask = bad || fresh < 0 || (int64_t)r.len + fresh > room ? 0 : fresh;
     r.need = (int32_t)(((int64_t)r.len + r.ask + bs1) >> g.shift) - r.held;
@@ -69,6 +72,18 @@ __device__ __forceinline__ int find(const int32_t *first, int lo, int hi, int32_
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (first[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// the same by a whole warp: 32 places looked at together, three loads in a row where the search above takes twelve
+__device__ __forceinline__ int find_by_warp(const int32_t *first, int lo, int hi, int32_t x) {
+    const int lane = threadIdx.x & 31;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+        const uint32_t below = __ballot_sync(~0u, at < hi && first[min(at, hi - 1)] <= x);
+        lo += (31 - __clz(below)) * step;          // lane 0's place is one of them
+        hi = min(hi, lo + step);
     }
     return lo;
 }
@@ -135,9 +150,27 @@ __device__ __forceinline__ Sums sums(const AssignArgs &g, int32_t *starts, int32
     const int begin = min(n, (int)threadIdx.x * per), end = min(n, begin + per);
     const int32_t n_free = free_count(g);
     int64_t x[3] = {0, 0, 0}, total[3], own[3];
-    Row r = {};
+    // up to kKeep rows of a thread stay in registers: their loads are under way together
+    Row kept[kKeep] = {}, r = {};
+    const bool keeps = per <= kKeep;
+    if (keeps) {
+#pragma unroll
+        for (int k = 0; k < kKeep; ++k)
+            if (begin + k < end) kept[k] = load_row(g, begin + k);
+    }
+    auto row_of = [&](int i) {
+        Row v = {};
+        if (keeps) {
+#pragma unroll
+            for (int k = 0; k < kKeep; ++k)
+                if (i == begin + k) v = kept[k];
+        } else {
+            v = load_row(g, i);
+        }
+        return v;
+    };
     for (int i = begin; i < end; ++i) {
-        r = load_row(g, i);
+        r = row_of(i);
         x[0] += r.need;
         x[1] += r.ask;
         x[2] += r.back;
@@ -153,7 +186,7 @@ __device__ __forceinline__ Sums sums(const AssignArgs &g, int32_t *starts, int32
         int64_t need_to = need, ask_to = ask;
         y[0] = y[1] = 0;
         for (int i = begin; i < end; ++i) {
-            if (per > 1) r = load_row(g, i);
+            r = row_of(i);
             need_to += r.need;
             ask_to += r.ask;
             const bool ok = (r.need == 0 || need_to <= avail) && ask_to <= a.max_tokens;
@@ -166,7 +199,7 @@ __device__ __forceinline__ Sums sums(const AssignArgs &g, int32_t *starts, int32
         y[1] -= mine[1];
     }
     for (int i = begin; i < end; ++i) {
-        if (per > 1) r = load_row(g, i);
+        r = row_of(i);
         need += r.need;
         ask += r.ask;
         const bool ok = all || ((r.need == 0 || need <= avail) && ask <= a.max_tokens);
@@ -176,8 +209,7 @@ __device__ __forceinline__ Sums sums(const AssignArgs &g, int32_t *starts, int32
         old[i] = r.len;
         a.granted[i] = ok ? r.ask : 0;
         a.starts[i] = (int32_t)y[1];
-        const bool ends = a.new_tokens[i] < 0;
-        a.lens_out[i] = ends ? 0 : r.len + (ok ? r.ask : 0);
+        a.lens_out[i] = r.ends ? 0 : r.len + (ok ? r.ask : 0);
         given += r.back;
         if (ok) { y[0] += r.need; y[1] += r.ask; }
     }
@@ -224,14 +256,15 @@ __global__ void __launch_bounds__(kFill) fill_kernel(const __grid_constant__ Ass
     const int n = a.n_rows;
     const int32_t *w = g.work;
     const Sums h = {w + 8, w + 8 + n, w + 8 + 2 * n, w + 8 + 3 * n, w[0], w[1], w[2], w[3], w[4]};
-    // 4 neighbouring entries a thread, of 4 kFill a block: their rows are between those of the block's ends
-    for (int64_t t0 = (int64_t)blockIdx.x * 4 * kFill; t0 < a.max_tokens; t0 += (int64_t)gridDim.x * 4 * kFill) {
+    // 4 neighbouring entries a thread, 128 a warp: their rows are between those of the warp's ends
+    const int lane = threadIdx.x & 31, warps = gridDim.x * (kFill / 32);
+    for (int64_t t0 = 128 * (int64_t)(blockIdx.x * (kFill / 32) + threadIdx.x / 32); t0 < a.max_tokens; t0 += 128 * (int64_t)warps) {
         int lo = 0, hi = n;
         if (t0 < h.tokens) {
-            lo = find(h.starts, 0, n, (int32_t)t0);
-            hi = find(h.starts, lo, n, (int32_t)min(t0 + 4 * kFill - 1, (int64_t)h.tokens - 1)) + 1;
+            lo = find_by_warp(h.starts, 0, n, (int32_t)t0);
+            hi = find_by_warp(h.starts, lo, n, (int32_t)min(t0 + 127, (int64_t)h.tokens - 1)) + 1;
         }
-        const int64_t t = t0 + 4 * threadIdx.x;
+        const int64_t t = t0 + 4 * lane;
         if (t >= a.max_tokens) continue;
         Entry e[4];
         e[0] = entry_of(g, h, (int32_t)t, lo, hi);

@@ -131,8 +131,6 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         }
         if (threadIdx.x == kThreads - 1) before[n] = base;
         __syncthreads();
-        if (blockIdx.x == 0)
-            for (int t = threadIdx.x; t <= n; t += kThreads) g.before[t] = before[t];
     }
     const int64_t W = (int64_t)before[n] * H;
     const int64_t C = min((int64_t)gridDim.x * kWarps, W);               // warps with work
@@ -373,6 +371,7 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             return;
         }
         // a piece: beside the prefix's, or the last one of an item that earlier warps began
+        if (whole && lane == 0) g.cut[here.t * H + here.h] = {here.t, here.h, (int)me, (int)me};
         const int64_t at = whole ? ((int64_t)g.line.pieces * n + here.t) * hq + first : me * 2 * 16;
         float *po = whole ? g.prefix_o : g.part_o;
         float2 *pml = whole ? g.prefix_ml : g.part_ml;
@@ -401,6 +400,14 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     // ---- what the runs' ends cut: `here` is each warp's last slice
     const bool tail = f0 < f1 && here.i + 1 < here.s.slices;
     if (tail) sum_rows();
+    if (lane == 0) {                                    // an item that begins here and is cut, for the kernel that joins it
+        const int64_t i0 = (int64_t)before[here.t] * H + (int64_t)here.h * here.s.slices;
+        const bool begins = tail && i0 >= f0;
+        CutItem item = {-1, 0, 0, 0};
+        if (begins) item = {here.t, here.h, (int)(((i0 + 1) * C - 1) / W), (int)(((i0 + here.s.slices) * C - 1) / W)};
+        if (!g.line.blocks) g.cut[me] = item;
+        else if (begins) g.cut[here.t * H + here.h] = item;
+    }
     if (lane == 0) cut[warp] = tail ? (int64_t)before[here.t] * H + (int64_t)here.h * here.s.slices : -1;
     if (tail && (lane & 3) == 0) {
         stats[warp * 16 + r] = make_float2(m[0], l[0]);
@@ -447,46 +454,27 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             g.part_ml[at + lane] = make_float2(top, total);
         }
     }
-    wait_for_previous();          // the prefix's kernel, if there is one: the kernel after this one reads its pieces
+    // The kernel after this one also reads the prefix's pieces: this one ends after the prefix's kernel.  One block
+    // sees to that, the others leave their SM to those that have not started.
+    if (blockIdx.x + 1 == gridDim.x) wait_for_previous();
 }
 
 // Joins pieces: of the items that runs' ends cut, a block for the warp in whose run one begins; where a prefix was
 // done apart, of all items, a block for each, with the prefix's pieces.
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 128;
 
-template <int D, typename T>
+template <int D, typename T, int kBatch>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendArgs g) {
     const isjl_kv_attend_args &a = g.a;
-    const int n = a.n, parts = (g.group + 15) / 16, H = g.n_kv_heads * parts, hq = g.n_kv_heads * g.group;
+    const int n = a.n, parts = (g.group + 15) / 16, hq = g.n_kv_heads * g.group;
     wait_for_previous();
-    const int64_t W = (int64_t)g.before[n] * H, C = min((int64_t)g.grid * kWarps, W);
-    int t, h;
-    int64_t i0;
-    int32_t slices;
-    if (g.line.blocks) {
-        t = blockIdx.x / H;
-        h = blockIdx.x % H;
-        slices = g.before[t + 1] - g.before[t];
-        i0 = (int64_t)g.before[t] * H + (int64_t)h * slices;
-    } else {
-        const int64_t f0 = W * blockIdx.x / C, f1 = W * (blockIdx.x + 1) / C;
-        if ((int64_t)blockIdx.x >= C) return;
-        int lo = 0, hi = n;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if ((int64_t)g.before[mid] * H <= f1 - 1) lo = mid; else hi = mid;
-        }
-        t = lo;
-        slices = g.before[t + 1] - g.before[t];
-        h = (int)((f1 - 1 - (int64_t)g.before[t] * H) / slices);
-        i0 = (int64_t)g.before[t] * H + (int64_t)h * slices;
-        if (i0 < f0 || i0 + slices <= f1) return;        // begun earlier, or not cut
-    }
-    const int kv = h / parts, from = kv * g.group + (h - kv * parts) * 16, rows = min(16, (kv + 1) * g.group - from);
+    const CutItem item = g.cut[blockIdx.x];
+    if (item.t < 0) return;
+    const int t = item.t, h = item.h, first = item.first, last = item.last;
     // An item's pieces: of each block the joined ones of the warps whose runs it fills to the end, and that of the
     // last warp, in whose run it ends; or the one of an item that is a warp's own.
-    const int64_t first = ((i0 + 1) * C - 1) / W, last = ((i0 + slices) * C - 1) / W;
-    const int cut = first == last ? 0 : (int)((last - 1) / kWarps - first / kWarps) + 2;
+    const int kv = h / parts, from = kv * g.group + (h - kv * parts) * 16, rows = min(16, (kv + 1) * g.group - from);
+    const int cut = first == last ? 0 : (last - 1) / kWarps - first / kWarps + 2;
     const int prefix_item = g.line.blocks ? kv * g.line.pairs + t / g.line.tokens_of_tile / 2 : 0;
     const int shared = g.line.blocks && sight(g, t).end > 0 ? g.line.last_block(prefix_item) - g.line.first_block(prefix_item) + 1 : 0;
     const int own = cut ? cut : 1, pieces = own + shared;
@@ -495,22 +483,22 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         const int row = x / (D / 4), d = (x % (D / 4)) * 4;
         float top = -INFINITY, total = 0.f;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k0 = 0; k0 < pieces; k0 += 8) {          // eight at a time: their loads are under way together
-            float2 ml[8];
-            float4 v[8];
+        for (int k0 = 0; k0 < pieces; k0 += kBatch) {     // some at a time: their loads are under way together
+            float2 ml[kBatch];
+            float4 v[kBatch];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < kBatch; ++k) {
                 const int p = min(k0 + k, pieces - 1);
                 const bool from_cut = cut && p < own;
-                const int64_t w = max(first, (first / kWarps + p) * kWarps);
-                const int64_t at = from_cut ? (p + 1 == own ? last * 2 * 16 : (w * 2 + 1) * 16) + row
+                const int w = max(first, (first / kWarps + p) * kWarps);
+                const int64_t at = from_cut ? (p + 1 == own ? last * 2 : w * 2 + 1) * 16 + row
                                             : ((int64_t)(p < own ? g.line.pieces : p - own) * n + t) * hq + from + row;
                 ml[k] = (from_cut ? g.part_ml : g.prefix_ml)[at];
                 v[k] = *reinterpret_cast<const float4 *>((from_cut ? g.part_o : g.prefix_o) + at * D + d);
             }
             float next = top;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) next = fmaxf(next, ml[k].x);
+            for (int k = 0; k < kBatch; ++k) next = fmaxf(next, ml[k].x);
             const float ref = next == -INFINITY ? 0.f : next, fix = ex2(top - ref);
             top = next;
             total *= fix;
@@ -519,7 +507,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
             sum.z *= fix;
             sum.w *= fix;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < kBatch; ++k) {
                 if (k0 + k >= pieces) break;
                 const float w = ex2(ml[k].x - ref);
                 total += ml[k].y * w;
@@ -541,8 +529,11 @@ cudaError_t launch_of(const AttendArgs &g, const CUtensorMap &k, const CUtensorM
     const bool apart = g.line.blocks > 0;
     const cudaError_t e = launch_kernel(attend_kernel<D, T>, grid, kThreads, attend_smem(D, g.a.n), st, apart, g, k, v);
     if (e != cudaSuccess) return e;
-    const int items = g.a.n * g.n_kv_heads * ((g.group + 15) / 16);
-    return launch_kernel(join_kernel<D, T>, apart ? items : grid * kWarps, kJoinThreads, 0, st, true, g);
+    const int items = apart ? g.a.n * g.n_kv_heads * ((g.group + 15) / 16) : grid * kWarps;
+    // Few pieces of many items: few registers, many blocks at once.  Many pieces of few items: their loads together.
+    const bool few = apart ? g.line.pieces < 4 : items < 4 * g.a.n * g.n_kv_heads;
+    if (few) return launch_kernel(join_kernel<D, T, 3>, items, kJoinThreads, 0, st, true, g);
+    return launch_kernel(join_kernel<D, T, 12>, items, kJoinThreads, 0, st, true, g);
 }
 
 template <int D, typename T>

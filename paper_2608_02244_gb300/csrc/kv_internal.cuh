@@ -112,6 +112,12 @@ cudaError_t launch_prefix(const PrefixArgs &g, const isjl_kv_cache &cache, void 
 
 // ---- attend (kv_attend.cu)
 constexpr int kAttendWarps = 4;   // of a block
+// an item (query t, key head or part of one h) in pieces: the warps in whose runs it begins and ends
+struct alignas(16) CutItem {
+    int32_t t, h;                 // t < 0: none
+    int32_t first, last;
+};
+
 struct AttendArgs {
     isjl_kv_attend_args a;
     isjl_kv_cache cache;
@@ -121,7 +127,8 @@ struct AttendArgs {
     float2 *prefix_ml;
     float *part_o;                // [kAttendWarps * grid][2][16][head_dim] pieces of (query, key head) items
     float2 *part_ml;              // [kAttendWarps * grid][2][16]
-    int32_t *before;              // [n + 1] slices before each query, for the kernel that joins the pieces
+    CutItem *cut;                 // for the kernel that joins: the cut items at the warps in whose runs they begin
+                                  // [kAttendWarps * grid], or with a prefix all items [n * key heads (parts of them)]
     int32_t grid;
     int32_t *status;
 };
