@@ -48,7 +48,7 @@ isjl_status launched(isjl_kv *kv, cudaError_t e, cudaStream_t st) {
 }
 
 // Own tokens are bound by memory, the prefix by the tensor cores, and a block of either fills its SM: some SMs are
-// left to the former, which start at once.  Measured: 1.45 us for a step of the prefix's line (256 rows and 128
+// left to the former, which start at once.  Measured: 1.4 us for a step of the prefix's line (256 rows and 128
 // tokens; 0.9 for a single row tile) after 5 us; own tokens at 65 GB/s an SM beside it, 5.5 TB/s on all.  How long
 // requests are only the device knows: they are taken as a quarter of the table's width.
 isjl::PrefixLine share_sms(const isjl_kv *kv, const isjl_kv_attend_args *a, int group, int n_kv_heads, int tokens, int *grid) {
@@ -59,7 +59,7 @@ isjl::PrefixLine share_sms(const isjl_kv *kv, const isjl_kv_attend_args *a, int 
     for (int left = 0; left <= kv->sms * 5 / 8; left += 8) {
         const isjl::PrefixLine ln = isjl::prefix_line(a->n, group, n_kv_heads, tokens, kv->sms - left);
         const double steps = (double)((ln.work() + ln.blocks - 1) / ln.blocks);
-        const double alone = 5e-6 + steps * (a->n > ln.tokens_of_tile ? 1.45e-6 : 0.9e-6);
+        const double alone = 5e-6 + steps * (a->n > ln.tokens_of_tile ? 1.4e-6 : 0.9e-6);
         const double rest = own - alone * (kv->sms - ln.blocks) * 65e9;
         const double all = alone + (rest > 0 ? rest / 5.5e12 : 0);
         if (left == 0 || all < least) { least = all; best = ln; left_best = left; }

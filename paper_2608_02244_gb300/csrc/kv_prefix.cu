@@ -63,6 +63,18 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 #define R8(v, i) "=r"((v)[(i)]), "=r"((v)[(i) + 1]), "=r"((v)[(i) + 2]), "=r"((v)[(i) + 3]), "=r"((v)[(i) + 4]), "=r"((v)[(i) + 5]), "=r"((v)[(i) + 6]), "=r"((v)[(i) + 7])
 #define W8(v, i) "r"((v)[(i)]), "r"((v)[(i) + 1]), "r"((v)[(i) + 2]), "r"((v)[(i) + 3]), "r"((v)[(i) + 4]), "r"((v)[(i) + 5]), "r"((v)[(i) + 6]), "r"((v)[(i) + 7])
 
+// two 32-bit operations in one instruction: 378 -> 361 us for the exponents' arguments and sums of 512 queries of 8 x 8 heads over 32,768 tokens
+__device__ __forceinline__ float2 fma2(float x, float y, float scale, float offset) {
+    float2 z;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %4};\nmov.b64 c, {%5, %5};\nfma.rn.f32x2 d, a, b, c;\n"
+        "mov.b64 {%0, %1}, d;\n}" : "=f"(z.x), "=f"(z.y) : "f"(x), "f"(y), "f"(scale), "f"(offset));
+    return z;
+}
+__device__ __forceinline__ void add2(float2 &sum, float x, float y) {
+    asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nadd.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+        : "+f"(sum.x), "+f"(sum.y) : "f"(x), "f"(y));
+}
+
 // 32 columns of this thread's TMEM lane
 __device__ __forceinline__ void tmem_load(uint32_t (&v)[32], uint32_t at) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -219,16 +231,16 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                     }
                 }
                 const float ref = top == -INFINITY ? 0.f : top;
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
+                float2 part[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t p[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         const int c = 2 * h + i / 16, e = 2 * (i % 16);
-                        const float x = ex2(fmaf(__uint_as_float(s[c][e]), scale, -ref));
-                        const float y = ex2(fmaf(__uint_as_float(s[c][e + 1]), scale, -ref));
-                        part[2 * h + (i & 1)] += x + y;
+                        const float2 z = fma2(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1]), scale, -ref);
+                        const float x = ex2(z.x), y = ex2(z.y);
+                        add2(part[i & 1], x, y);
                         p[i] = Half<T>::pack(x, y);
                     }
                     tmem_store(s_at + 32 * h, p);
@@ -236,7 +248,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                     fence_before();
                     bar_arrive(bar((h ? kRest : kWeights) + group));      // the product starts with the first half
                 }
-                total += (part[0] + part[1]) + (part[2] + part[3]);
+                total += (part[0].x + part[0].y) + (part[1].x + part[1].y);
             }
             ok = ok && __all_sync(~0u, bar_wait(bar(kSums + group), item_no & 1, failed));
             if (!ok) break;
