@@ -170,10 +170,11 @@ isjl_status isjl_kv_assign(isjl_kv *kv, const isjl_kv_assign_args *args, void *s
 isjl_status isjl_kv_append(isjl_kv *kv, const isjl_kv_append_args *args, const isjl_kv_cache *cache, void *stream);
 isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *args, const isjl_kv_cache *cache, void *stream);
 
-/* Wait for the last call on its stream; INVALID_ARG if any call since the last
- * report met an invalid value on the device (see above), INTERNAL if a kernel gave
- * up a wait (a library bug: the call's outputs are not valid), else OK.  Resets the
- * report.  CUDA on a failed sync.  Not inside a capture. */
+/* Wait for the device's work (calls may have been replayed from graphs on any
+ * stream); INVALID_ARG if any call since the last report met an invalid value on
+ * the device (see above), INTERNAL if a kernel gave up a wait (a library bug: the
+ * call's outputs are not valid), else OK.  Resets the report.  CUDA on a failed
+ * sync.  Not inside a capture. */
 isjl_status isjl_kv_status(isjl_kv *kv);
 
 #ifdef __cplusplus

@@ -8,4 +8,4 @@ binding and ``workloads`` draws seeded synthetic instances.
 """
 from . import workloads  # noqa: F401
 
-__all__ = ["workloads", "sim", "kv", "build"]
+__all__ = ["workloads", "sim", "kv", "replay", "build"]

@@ -19,8 +19,6 @@ struct isjl_kv {
     float2 *d_prefix_ml = nullptr;       // null: this shape has no prefix kernel
     float *d_prefix_o = nullptr;
     void *encoder = nullptr;
-    cudaStream_t last_stream = nullptr;
-    bool ran = false;
 };
 
 namespace {
@@ -40,12 +38,7 @@ bool cache_ok(const isjl_kv_cache *c) {
     return true;
 }
 
-isjl_status launched(isjl_kv *kv, cudaError_t e, cudaStream_t st) {
-    if (e != cudaSuccess) return ISJL_ERR_CUDA;
-    kv->last_stream = st;
-    kv->ran = true;
-    return ISJL_OK;
-}
+isjl_status launched(cudaError_t e) { return e == cudaSuccess ? ISJL_OK : ISJL_ERR_CUDA; }
 
 // Own tokens are bound by memory, the prefix by the tensor cores, and a block of either fills its SM: some SMs are
 // left to the former, which start at once.  Measured: 1.4 us for a step of the prefix's line (256 rows and 128
@@ -194,7 +187,7 @@ isjl_status isjl_kv_assign(isjl_kv *kv, const isjl_kv_assign_args *a, void *stre
     g.work = kv->d_sums;
     g.status = kv->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return launched(kv, isjl::launch_assign(g, kv->sms, st), st);
+    return launched(isjl::launch_assign(g, kv->sms, st));
 }
 
 isjl_status isjl_kv_append(isjl_kv *kv, const isjl_kv_append_args *a, const isjl_kv_cache *cache, void *stream) {
@@ -219,7 +212,7 @@ isjl_status isjl_kv_append(isjl_kv *kv, const isjl_kv_append_args *a, const isjl
     g.n_slots = (int64_t)kv->cfg.n_blocks << kv->shift;
     g.status = kv->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return launched(kv, isjl::launch_append(g, kv->cfg.head_dim, kv->cfg.type, kv->sms, st), st);
+    return launched(isjl::launch_append(g, kv->cfg.head_dim, kv->cfg.type, kv->sms, st));
 }
 
 isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl_kv_cache *cache, void *stream) {
@@ -272,16 +265,16 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
         g.prefix_ml = kv->d_prefix_ml;
         if (isjl::launch_prefix(p, *cache, kv->encoder, kv->cfg.head_dim, kv->cfg.type, st) != cudaSuccess) return ISJL_ERR_CUDA;
     }
-    return launched(kv, isjl::launch_attend(g, kv->encoder, kv->cfg.head_dim, kv->cfg.type, grid, st), st);
+    return launched(isjl::launch_attend(g, kv->encoder, kv->cfg.head_dim, kv->cfg.type, grid, st));
 }
 
 isjl_status isjl_kv_status(isjl_kv *kv) {
     if (!kv) return ISJL_ERR_INVALID_ARG;
-    if (!kv->ran) return ISJL_OK;
+    // calls may have been replayed from graphs on any stream: all of the device's work is waited for
     int32_t word = 0;
-    if (cudaMemcpyAsync(&word, kv->d_status, sizeof(word), cudaMemcpyDeviceToHost, kv->last_stream) != cudaSuccess ||
-        cudaMemsetAsync(kv->d_status, 0, sizeof(word), kv->last_stream) != cudaSuccess ||
-        cudaStreamSynchronize(kv->last_stream) != cudaSuccess)
+    if (cudaDeviceSynchronize() != cudaSuccess ||
+        cudaMemcpy(&word, kv->d_status, sizeof(word), cudaMemcpyDeviceToHost) != cudaSuccess ||
+        cudaMemset(kv->d_status, 0, sizeof(word)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
         return ISJL_ERR_CUDA;
     return word & 2 ? ISJL_ERR_INTERNAL : word ? ISJL_ERR_INVALID_ARG : ISJL_OK;
 }

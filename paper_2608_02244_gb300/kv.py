@@ -274,5 +274,5 @@ class Decoder:
         return (out, weights) if lse else out
 
     def status(self):
-        """Wait for the last call; the status code of everything since the last report."""
+        """Wait for the device; the status code of all calls since the last report."""
         return self._lib.isjl_kv_status(self.handle)
