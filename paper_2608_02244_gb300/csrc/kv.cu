@@ -8,7 +8,8 @@
 
 struct isjl_kv {
     isjl_kv_config cfg;
-    int sms = 0, shift = 0, grid = 0;
+    int sms = 0, shift = 0;
+    int per_sm = 0, full = 0;            // the attention's blocks of an SM, with at most `full` queries
     // one allocation: the status word, then the workspaces of assign and attend
     unsigned char *d_work = nullptr;
     int32_t *d_status = nullptr;
@@ -112,14 +113,14 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
     const int queries = cfg->max_rows < ISJL_KV_MAX_ROWS ? cfg->max_rows : ISJL_KV_MAX_ROWS;
     if (cudaGetDevice(&device) != cudaSuccess ||
         cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
-        isjl::attend_grid(cfg->head_dim, cfg->type, queries, kv->sms, &kv->grid) != cudaSuccess || kv->grid < 1) {
+        isjl::prepare_attend(cfg->head_dim, cfg->type, &kv->per_sm, &kv->full) != cudaSuccess || kv->per_sm < 1) {
         cudaGetLastError();
         delete kv;
         return ISJL_ERR_CUDA;
     }
     const bool shares = cfg->head_dim <= 128 && cfg->n_q_heads / cfg->n_kv_heads <= 128;
     const size_t sums = rounded(sizeof(int32_t) * (8 + 4 * (size_t)cfg->max_rows));
-    const size_t warps = (size_t)kv->grid * isjl::kAttendWarps * (shares ? kFiner : 1);
+    const size_t warps = (size_t)kv->per_sm * kv->sms * isjl::kAttendWarps * (shares ? kFiner : 1);
     const int group = cfg->n_q_heads / cfg->n_kv_heads;
     const size_t items = (size_t)queries * cfg->n_kv_heads * ((group + 15) / 16);
     const size_t cuts = rounded(sizeof(isjl::CutItem) * (items > warps ? items : warps));
@@ -241,7 +242,7 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
     g.cut = kv->d_cut;
     g.status = kv->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    int grid = kv->grid;
+    int grid = kv->sms * (a->n <= kv->full || kv->per_sm == 1 ? kv->per_sm : kv->per_sm - 1);
     if (kv->d_prefix_o && a->n_prefix_blocks > 0 && a->window == 0) {
         isjl::PrefixArgs p;
         std::memset(&p, 0, sizeof(p));

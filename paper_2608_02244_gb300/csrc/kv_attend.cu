@@ -537,15 +537,18 @@ cudaError_t launch_of(const AttendArgs &g, const CUtensorMap &k, const CUtensorM
 }
 
 template <int D, typename T>
-cudaError_t grid_of(int max_rows, int sms, int *grid) {
-    const int bytes = (int)attend_smem(D, max_rows);
+cudaError_t prepare_of(int *blocks, int *queries) {
     // the limit belongs to the function, not to a handle: always the largest
     cudaError_t e = cudaFuncSetAttribute(attend_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          (int)attend_smem(D, ISJL_KV_MAX_ROWS));
-    if (e != cudaSuccess) return e;
-    int per = 0;
-    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, attend_kernel<D, T>, kThreads, bytes);
-    *grid = per * sms;
+    int lo = 1, hi = ISJL_KV_MAX_ROWS + 1, per = 0;
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(blocks, attend_kernel<D, T>, kThreads, attend_smem(D, 1));
+    while (e == cudaSuccess && hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, attend_kernel<D, T>, kThreads, attend_smem(D, mid));
+        if (per == *blocks) lo = mid; else hi = mid;
+    }
+    *queries = lo;
     return e;
 }
 
@@ -556,12 +559,12 @@ size_t attend_smem(int head_dim, int n) {
     return ring + kWarps * 16 * sizeof(float2) + (size_t)(n + 1) * sizeof(int32_t);
 }
 
-cudaError_t attend_grid(int head_dim, int type, int max_rows, int sms, int *grid) {
+cudaError_t prepare_attend(int head_dim, int type, int *blocks, int *queries) {
     if (type == ISJL_KV_BF16)
-        return head_dim == 64 ? grid_of<64, __nv_bfloat16>(max_rows, sms, grid)
-             : head_dim == 128 ? grid_of<128, __nv_bfloat16>(max_rows, sms, grid) : grid_of<256, __nv_bfloat16>(max_rows, sms, grid);
-    return head_dim == 64 ? grid_of<64, __half>(max_rows, sms, grid)
-         : head_dim == 128 ? grid_of<128, __half>(max_rows, sms, grid) : grid_of<256, __half>(max_rows, sms, grid);
+        return head_dim == 64 ? prepare_of<64, __nv_bfloat16>(blocks, queries)
+             : head_dim == 128 ? prepare_of<128, __nv_bfloat16>(blocks, queries) : prepare_of<256, __nv_bfloat16>(blocks, queries);
+    return head_dim == 64 ? prepare_of<64, __half>(blocks, queries)
+         : head_dim == 128 ? prepare_of<128, __half>(blocks, queries) : prepare_of<256, __half>(blocks, queries);
 }
 
 cudaError_t launch_attend(const AttendArgs &args, void *encoder, int head_dim, int type, int grid, cudaStream_t st) {

@@ -133,8 +133,9 @@ struct AttendArgs {
     int32_t *status;
 };
 size_t attend_smem(int head_dim, int n);
-// blocks of one full wave for calls of up to max_rows queries
-cudaError_t attend_grid(int head_dim, int type, int max_rows, int sms, int *grid);
+// once for a shape, before its first launch: blocks that fit an SM, and the most queries of a call with which they do
+// (with more, one block less fits: each holds 4 bytes a query)
+cudaError_t prepare_attend(int head_dim, int type, int *blocks, int *queries);
 cudaError_t launch_attend(const AttendArgs &a, void *encoder, int head_dim, int type, int grid, cudaStream_t st);
 
 }  // namespace isjl
