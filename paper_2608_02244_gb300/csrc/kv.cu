@@ -41,26 +41,35 @@ bool cache_ok(const isjl_kv_cache *c) {
 
 isjl_status launched(cudaError_t e) { return e == cudaSuccess ? ISJL_OK : ISJL_ERR_CUDA; }
 
-// Own tokens are bound by memory, the prefix by the tensor cores, and a block of either fills its SM: some SMs are
-// left to the former, which start at once.  Measured: 1.4 us for a step of the prefix's line (256 rows and 128
-// tokens; 0.9 for a single row tile) after 5 us; own tokens at 65 GB/s an SM beside it, 5.5 TB/s on all.  How long
-// requests are only the device knows: they are taken as a quarter of the table's width.
+// Own tokens are bound by memory, the prefix by the tensor cores, and a block of either fills its SM.
+//
+// A short prefix gets about 64 SMs and own tokens the other 88, which reach nearly the card's bandwidth: both run from
+// the start.  Of 0 to 136 SMs for own tokens this was within 7% of the best for eight shapes (4 to 512 requests of 64
+// to 8,192 tokens, prefixes of 512 to 8,192), 4 to 28% before one after the other (17 requests over 2,048 tokens 19.2
+// and 26.3 us, 128 over 8,192 105 and 140).  The blocks and the prefix's items divide one another where they can,
+// since a change of items costs a block about 3 us (64 blocks 43 us where 88 took 52).
+//
+// Beside a long prefix own tokens get a few SMs, in small runs, and all of them once it is done: 512 requests over
+// 32,768 tokens 465 us with 40 SMs, 551 one after the other.  Steps of the prefix's line (256 rows by 128 tokens)
+// take 1.4 us, own tokens run at 60 GB/s an SM.  How long requests are only the device knows: they are taken as a
+// quarter of the table's width.
 isjl::PrefixLine share_sms(const isjl_kv *kv, const isjl_kv_attend_args *a, int group, int n_kv_heads, int tokens, int *grid) {
+    const int sms = kv->sms, per_sm = *grid / sms;
+    const isjl::PrefixLine ln = isjl::prefix_line(a->n, group, n_kv_heads, tokens, sms);
     const double own = 0.25 * a->n * ((double)a->table_width * kv->cfg.block_size) * 4.0 * kv->cfg.head_dim * n_kv_heads;
-    isjl::PrefixLine best{};
-    double least = 0;
-    int left_best = 0;
-    for (int left = 0; left <= kv->sms * 5 / 8; left += 8) {
-        const isjl::PrefixLine ln = isjl::prefix_line(a->n, group, n_kv_heads, tokens, kv->sms - left);
-        const double steps = (double)((ln.work() + ln.blocks - 1) / ln.blocks);
-        const double alone = 5e-6 + steps * (a->n > ln.tokens_of_tile ? 1.4e-6 : 0.9e-6);
-        const double rest = own - alone * (kv->sms - ln.blocks) * 65e9;
-        const double all = alone + (rest > 0 ? rest / 5.5e12 : 0);
-        if (left == 0 || all < least) { least = all; best = ln; left_best = left; }
+    int blocks = sms * 64 / 152;
+    const int even = sms * 72 / 152 / ln.items * ln.items;
+    if (even > 0) blocks = even;
+    const double prefix = 6e-6 + 1.4e-6 * (double)((ln.work() + blocks - 1) / blocks);
+    if (prefix <= 40e-6 || prefix <= own / 5.5e12) {
+        const isjl::PrefixLine some = isjl::prefix_line(a->n, group, n_kv_heads, tokens, blocks);
+        *grid = per_sm * (sms - some.blocks);
+        return some;
     }
-    // many runs end one after another beside a long prefix
-    if (left_best > 0 && least > 100e-6) *grid *= kFiner;
-    return best;
+    const double all = 6e-6 + 1.4e-6 * (double)((ln.work() + sms - 1) / sms), share = own / (60e9 * all);
+    const int most = sms * 40 / 152, left = (share < most ? (int)share : most) / 8 * 8;
+    if (left > 0) *grid *= kFiner;
+    return isjl::prefix_line(a->n, group, n_kv_heads, tokens, sms - left);
 }
 
 }  // namespace

@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kRows = 128, kKeys = 128;        // of a row tile, of a token tile
 constexpr int kThreads = 384;                  // two groups of four warps; the loading and the issuing warp's group
-constexpr int kLoadWarp = 8, kIssueWarp = 9;
+constexpr int kLoadWarp = 8, kIssueWarp = 10;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGrow = 8.f;                   // log2 of the growth of a maximum that is let pass
 
@@ -30,8 +30,8 @@ struct Shape {
     static constexpr int kHalves = D / 64;                       // rows of 128 bytes hold 64 values
     static constexpr int kHalfBytes = 128 * 128;                 // 128 rows of them
     static constexpr int kTileBytes = kHalves * kHalfBytes;
-    static constexpr int kStages = D == 128 ? 5 : 8;
-    static constexpr int kSmem = 2 * kTileBytes + kStages * kTileBytes + 1024;
+    static constexpr int kKeyStages = D == 128 ? 3 : 4, kValueStages = D == 128 ? 2 : 4;
+    static constexpr int kSmem = (2 + kKeyStages + kValueStages) * kTileBytes + 1024;
 };
 
 // shared-memory operand with rows of 128 bytes, swizzled by 128 bytes
@@ -92,7 +92,7 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
 // barriers, in 8-byte words after the tiles
-enum { kFull = 0, kEmpty = 8, kScores = 16, kWeights = 18, kSums = 20, kQueries = 22, kRest = 24, kBars = 26 };
+enum { kKeyFull = 0, kValueFull = 8, kFree = 4 /* after a stage's full one */, kScores = 16, kWeights = 18, kSums = 20, kQueries = 22, kRest = 24, kBars = 26 };
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -120,7 +120,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
         tma_prefetch(&kmap);
         tma_prefetch(&vmap);
         failed_word = 0;
-        for (int i = 0; i < S::kStages; ++i) { bar_init(bar(kFull + i), 1); bar_init(bar(kEmpty + i), 1); }
+        for (int i = 0; i < 16; ++i) bar_init(bar(i), 1);
         for (int i = 0; i < 2; ++i) {
             bar_init(bar(kScores + i), 1);
             bar_init(bar(kWeights + i), 128);
@@ -155,7 +155,8 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
         const float scale = g.scale * kLog2e;
         uint32_t step = 0;
         int item_no = 0;
-        int stage = 0;                             // of the tile's keys; its values are in the next one
+        int key_stage = 0, value_stage = 0;        // of the keys and values that are freed next
+        auto next = [](int &at, int by, int stages) { at = (at + by) % stages; };
         bool ok = true;
         for (int64_t f = f0; f < f1 && ok;) {
             const int item = (int)(f / ln.tiles), j0 = (int)(f - (int64_t)item * ln.tiles);
@@ -163,7 +164,8 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
             f += count;
             const bool two = two_of(pair);
             if (group == 1 && !two) {
-                stage = (stage + 2 * count) % S::kStages;
+                next(key_stage, count, S::kKeyStages);
+                next(value_stage, count, S::kValueStages);
                 continue;
             }
             // The last group to use a tile frees its stages: when it sees its scores, the products of the keys are
@@ -191,11 +193,11 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                 if (!ok) break;
                 fence_after();
                 if (frees) {
-                    bar_arrive(bar(kEmpty + stage));
-                    if (j > 0) bar_arrive(bar(kEmpty + (stage == 0 ? S::kStages - 1 : stage - 1)));
+                    bar_arrive(bar(kKeyFull + kFree + key_stage));
+                    if (j > 0) bar_arrive(bar(kValueFull + kFree + value_stage));
                 }
-                stage += 2;
-                if (stage >= S::kStages) stage -= S::kStages;
+                next(key_stage, 1, S::kKeyStages);
+                if (j > 0) next(value_stage, 1, S::kValueStages);
                 uint32_t s[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_load(s[c], s_at + 32 * c);
@@ -254,7 +256,8 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
             if (!ok) break;
             fence_after();
             ++item_no;
-            if (frees) bar_arrive(bar(kEmpty + (stage == 0 ? S::kStages - 1 : stage - 1)));
+            if (frees) bar_arrive(bar(kValueFull + kFree + value_stage));
+            next(value_stage, 1, S::kValueStages);
             const int64_t at = ((int64_t)(blockIdx.x - ln.first_block(item)) * g.n + token) * (g.n_kv_heads * g.group) + q_head;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -271,8 +274,8 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        if (warp == kLoadWarp) {
-            // ---- keys and values: one copy for each cache block (or part of one) of a tile and 64 of its values
+        if (warp == kLoadWarp || warp == kLoadWarp + 1) {
+            // ---- keys by one warp, values by the other: one copy for each cache block (or part of one) of a tile and 64 of its values
             const int rows = min(1 << g.shift, kKeys), pieces = kKeys / rows;      // pieces: 1 .. 16
             const uint32_t piece_bytes = rows * 128;
             // this lane's part of a tile: piece lane % pieces, and every 32 / pieces-th half
@@ -281,6 +284,11 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                 const int token = j * kKeys + piece * rows;
                 return token < g.tokens ? g.prefix[token >> g.shift] : g.n_blocks;       // beyond the prefix: zeros
             };
+            // A ring for each: a stage's turns are one warp's, which cannot be two turns ahead of itself.
+            const bool values = warp != kLoadWarp;
+            const int stages = values ? S::kValueStages : S::kKeyStages, full = values ? kValueFull : kKeyFull;
+            const uint32_t to = ring + (values ? S::kKeyStages * S::kTileBytes : 0);
+            const CUtensorMap *map = values ? &vmap : &kmap;
             int load = 0, stage = 0;
             uint32_t turn = 0;
             bool ok = true;
@@ -294,21 +302,19 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                     const int slot = (j * kKeys + piece * rows) & ((1 << g.shift) - 1);
                     if (j + 1 < j0 + count) coming = block_of(j + 1);
                     if ((uint32_t)block > (uint32_t)g.n_blocks) { report(g.status); block = g.n_blocks; }
-                    for (int side = 0; side < 2; ++side) {
-                        ok = __all_sync(~0u, load < S::kStages || bar_wait(bar(kEmpty + stage), turn ^ 1, failed));
-                        if (!ok) break;
-                        if (lane == 0) bar_expect(bar(kFull + stage), S::kTileBytes);
-                        __syncwarp();
-                        for (int half = lane / pieces; half < S::kHalves; half += 32 / pieces)
-                            tma_load(ring + stage * S::kTileBytes + half * S::kHalfBytes + piece * piece_bytes, side ? &vmap : &kmap,
-                                     bar(kFull + stage), slot, half, head, block);
-                        ++load;
-                        if (++stage == S::kStages) { stage = 0; turn ^= 1; }
-                    }
+                    ok = __all_sync(~0u, load < stages || bar_wait(bar(full + kFree + stage), turn ^ 1, failed));
+                    if (!ok) break;
+                    if (lane == 0) bar_expect(bar(full + stage), S::kTileBytes);
+                    __syncwarp();
+                    for (int half = lane / pieces; half < S::kHalves; half += 32 / pieces)
+                        tma_load(to + stage * S::kTileBytes + half * S::kHalfBytes + piece * piece_bytes, map, bar(full + stage), slot, half,
+                                 head, block);
+                    ++load;
+                    if (++stage == stages) { stage = 0; turn ^= 1; }
                 }
             }
             // nothing is left in flight, also after a failure
-            for (int i = max(0, load - S::kStages); i < load; ++i) bar_wait(bar(kFull + i % S::kStages), (i / S::kStages) & 1, nullptr);
+            for (int i = max(0, load - stages); i < load; ++i) bar_wait(bar(full + i % stages), (i / stages) & 1, nullptr);
         } else if (warp == kIssueWarp) {
             // The whole warp runs this loop, so that addresses stay uniform, and one thread of it issues: with the
             // products of 64 cycles each, their issue has to take less.
@@ -317,7 +323,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
             bool ok = tmem_base == 0;                            // all columns are ours: they begin at 0
             // operands differ in their address field alone: low word plus 16-byte steps
             const uint32_t q_lo = (uint32_t)operand(q_at, 16, 1024), k_lo = (uint32_t)operand(ring, 16, 1024);
-            const uint32_t v_lo = (uint32_t)operand(ring, S::kHalfBytes, 1024);
+            const uint32_t v_lo = (uint32_t)operand(ring + S::kKeyStages * S::kTileBytes, S::kHalfBytes, 1024);
             constexpr uint32_t high = (1024 >> 4) | (1u << 14) | (2u << 29);
             auto scores = [&](int i, int stage) {
                 const uint32_t a = q_lo + i * (S::kTileBytes >> 4), b = k_lo + stage * (S::kTileBytes >> 4);
@@ -340,16 +346,15 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                 }
             };
             auto wait = [&](int b, uint32_t phase) { ok = ok && __all_sync(~0u, bar_wait(bar(b), phase, failed)); };
-            int k_at = 0, v_at = 1;                              // stages of the tile's keys and values, and their turns
+            int k_at = 0, v_at = 0;                              // stages of the tile's keys and values, and their turns
             uint32_t k_turn = 0, v_turn = 0;
-            auto next = [&](int &at, uint32_t &turn) {
-                at += 2;
-                if (at >= S::kStages) { at -= S::kStages; turn ^= 1; }
+            auto next = [](int &at, uint32_t &turn, int stages) {
+                if (++at == stages) { at = 0; turn ^= 1; }
             };
             for (int64_t f = f0; f < f1 && ok;) {
                 const int item = (int)(f / ln.tiles), j0 = (int)(f - (int64_t)item * ln.tiles);
                 const int count = (int)min((int64_t)ln.tiles - j0, f1 - f), groups = two_of(item % ln.pairs) ? 2 : 1;
-                wait(kFull + k_at, k_turn);
+                wait(kKeyFull + k_at, k_turn);
                 for (int i = 0; i < groups && ok; ++i) {
                     wait(kQueries + i, begun[i]++ & 1);
                     if (!ok) break;
@@ -357,31 +362,28 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                     scores(i, k_at);
                 }
                 if (!ok) break;
-                next(k_at, k_turn);
+                next(k_at, k_turn, S::kKeyStages);
                 for (int j = 0; j < count && ok; ++j) {
                     const bool more = j + 1 < count;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         if (i >= groups) break;
-                        
                         // one wait for weights and (before the first row tile's) copies: a lane for each barrier
                         const bool copies = lane == 1 && i == 0;
-                        wait(copies ? kFull + v_at : kWeights + i, copies ? v_turn : step[i] & 1);
+                        wait(copies ? kValueFull + v_at : kWeights + i, copies ? v_turn : step[i] & 1);
                         if (!ok) break;
                         fence_after();
-                        
                         sums(i, v_at, 0, j > 0);
-                        wait(copies && more ? kFull + k_at : kRest + i, copies && more ? k_turn : step[i] & 1);
+                        wait(copies && more ? kKeyFull + k_at : kRest + i, copies && more ? k_turn : step[i] & 1);
                         ++step[i];
                         if (!ok) break;
                         fence_after();
                         sums(i, v_at, 1, true);
                         if (more) scores(i, k_at);
                         else if (one) commit(bar(kSums + i));
-                        
                     }
-                    next(v_at, v_turn);
-                    if (more) next(k_at, k_turn);
+                    next(v_at, v_turn, S::kValueStages);
+                    if (more) next(k_at, k_turn, S::kKeyStages);
                 }
                 f += count;
             }
