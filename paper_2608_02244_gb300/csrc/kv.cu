@@ -41,6 +41,15 @@ bool cache_ok(const isjl_kv_cache *c) {
 
 isjl_status launched(cudaError_t e) { return e == cudaSuccess ? ISJL_OK : ISJL_ERR_CUDA; }
 
+// Whether a prefix is done apart, by its own kernel, or read by each query's warps with its own tokens.  The former
+// saves n - 1 of n readings of the prefix and costs a launch and the joining of its pieces.  Measured, read against
+// apart (32 + 8 heads of 128 values, 256 own tokens): 8 queries over 512 tokens 13.4 and 12.1 us, 16 over 512 15.4 and
+// 15.2, 64 over 128 23 and 28, 8 over 2,048 17.2 and 15.0, 64 over 2,048 62 and 30; 4 over 8,192 24.2 and 24.7, 2 over
+// 32,768 39 and 38, 4 over 32,768 62 and 39; 64 over 32,768 689 and 73.
+bool worth_apart(int n, int tokens) {
+    return (int64_t)(n - 1) * tokens >= (n >= 8 ? 12288 : 32768);
+}
+
 // Own tokens are bound by memory, the prefix by the tensor cores, and a block of either fills its SM.
 //
 // A short prefix gets about 64 SMs and own tokens the other 88, which reach nearly the card's bandwidth: both run from
@@ -252,7 +261,7 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
     g.status = kv->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int grid = kv->sms * (a->n <= kv->full || kv->per_sm == 1 ? kv->per_sm : kv->per_sm - 1);
-    if (kv->d_prefix_o && a->n_prefix_blocks > 0 && a->window == 0) {
+    if (kv->d_prefix_o && a->window == 0 && worth_apart(a->n, a->n_prefix_blocks << kv->shift)) {
         isjl::PrefixArgs p;
         std::memset(&p, 0, sizeof(p));
         p.tokens = a->n_prefix_blocks << kv->shift;

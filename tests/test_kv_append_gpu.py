@@ -86,6 +86,31 @@ def test_many_tokens():
     check(inputs(20011, 8, 2, 128, 128, torch.bfloat16, True, 16, 1), 8, 2, 128)
 
 
+@pytest.mark.parametrize("n", [3647, 3648, 4999])
+@pytest.mark.parametrize("dim,hq,hkv", [(64, 3, 1), (128, 6, 2), (256, 2, 1)])
+def test_around_many_tokens(n, dim, hq, hkv):
+    """Both sides of the token count from which a token is one warp's."""
+    import torch
+    s = inputs(n, hq, hkv, dim, dim // 2, torch.bfloat16, True, 32, n)
+    s["slots"][5::97] = -1
+    check(s, hq, hkv, dim, pairs=n % 2 == 0)
+
+
+def test_infinite_values_stay_in_their_place():
+    """A value outside the rotated part, or a v value, is copied whatever it is; a rotated pair shows it."""
+    import math
+
+    import torch
+    from paper_2608_02244_gb300 import kv
+    s = inputs(3, 2, 1, 64, 16, torch.bfloat16, False, 8, 11)
+    s["qkv"][0, 40], s["qkv"][1, 3 * 64 + 5] = math.inf, math.nan          # q head 0 beyond rot; v
+    q = kv.Decoder(s["k"].shape[0], 8, 2, 1, 64, max_rows=1).append(**s)
+    bad = ~torch.isfinite(q)
+    assert bad.sum() == 1 and q[0, 0, 40] == math.inf
+    at = s["slots"][1]
+    assert torch.isnan(s["v"][at // 8, at % 8]).sum() == 1
+
+
 def test_padding_one_weight_and_large_values():
     import torch
     s = inputs(50, 4, 2, 64, 32, torch.float16, True, 8, 5)

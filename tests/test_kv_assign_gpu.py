@@ -61,9 +61,16 @@ def check(case, block, **kw):
         assert got[f] == want[f], f
 
 
-@pytest.mark.parametrize("n", [1, 2, 31, 33, 256, 1000, 1023, 1024, 1025, 2999, 5000])
+@pytest.mark.parametrize("n", [1, 2, 31, 33, 256, 1000, 1023, 1024, 1025, 2999, 4096, 4097, 5000])
 def test_rows(n):
     check(step(n, 16, 9, 6 * n + 3, 60 * n + 5, n), 16)
+
+
+@pytest.mark.parametrize("room", [1, 5, 4095, 4096, 4097, 4100])
+@pytest.mark.parametrize("n", [40, 1024, 1025])
+def test_around_one_kernel(n, room):
+    """Both sides of the sizes up to which one kernel does it all; maps of odd lengths."""
+    check(step(n, 8, 30, 20 * n, room, n + room), 8, prefix=16)
 
 
 @pytest.mark.parametrize("block", [8, 16, 32, 64, 128, 256])

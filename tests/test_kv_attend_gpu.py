@@ -96,8 +96,56 @@ def test_prefix_of_many(n, hq, hkv, shared, block, dim, dtype):
     check(inputs(lens, hq, hkv, dim, block, dtype, shared=shared, seed=n))
 
 
+@pytest.mark.parametrize("n,shared", [(7, 1023), (7, 1024), (8, 219), (8, 220), (9, 191), (9, 192)])
+def test_around_prefix_apart(n, shared):
+    """Both sides of the sizes from which a prefix has its own kernel."""
+    check(inputs([20 + 7 * i for i in range(n)], 8, 2, 64, 8, shared=shared, seed=n))
+
+
+@pytest.mark.parametrize("n,hq,hkv,dim,shared,block", [(40, 2, 2, 64, 500, 8), (500, 3, 1, 128, 60, 32), (70, 20, 10, 64, 300, 16),
+                                                       (150, 128, 1, 64, 20, 128), (16, 130, 1, 128, 40, 64), (9, 8, 8, 128, 200, 64)])
+def test_prefix_items_and_blocks(n, hq, hkv, dim, shared, block):
+    """Row tiles with rows left over, one or two to an item, items cut by blocks and blocks of several items; more
+    query heads on a key head than rows in a tile (not apart)."""
+    check(inputs([1 + i % 9 for i in range(n)], hq, hkv, dim, block, shared=shared, seed=n))
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, "float16"), (128, "bfloat16")])
+@pytest.mark.parametrize("shape", ["rising", "falling", "steps"])
+def test_prefix_maxima_that_move(dim, dtype, shape):
+    """Scores that grow along the prefix: the running maximum moves often, by little and by much."""
+    import torch
+    s = inputs([30, 0, 1, 5] * 8, 4, 1, dim, 16, dtype, shared=80, seed=1)
+    x = torch.linspace(0, 1, 80 * 16, device="cuda")
+    size = {"rising": 6 * x, "falling": 6 * (1 - x), "steps": 8 * (x * 5).floor() / 5}[shape].view(80, 16, 1, 1)
+    s["k"][s["prefix"].long()] = (s["k"][s["prefix"].long()] * size).to(s["k"].dtype)
+    check(s)
+
+
+def test_prefix_extreme_keys():
+    """Keys of -infinite score in whole tiles, and an undefined one, which every query sees."""
+    import torch
+    s = inputs([30, 2, 90, 1] * 16, 2, 1, 128, 64, shared=40, seed=2)
+    s["q"] = s["q"].abs()
+    b = s["prefix"].long()
+    s["k"][b[:10]] = -math.inf
+    s["k"][b[30]] = -math.inf
+    out, lse = decoder(s).attend(**s, lse=True)
+    want, want_lse, size = kv_plain.attend(**s)
+    kv_plain.check_attend(out, lse, want, want_lse, size)
+    s["k"][b[20], 3, 0, 5] = math.nan
+    out, lse = decoder(s).attend(**s, lse=True)
+    assert out.isnan().all() and lse.isnan().all()
+
+
+@pytest.mark.parametrize("n", [1700, 1900, 2600])
+def test_many_queries_of_128(n):
+    """Both sides of the query count from which one block less fits an SM."""
+    check(inputs(np.arange(n) % 50, 2, 1, 128, 16, seed=n))
+
+
 @pytest.mark.parametrize("order", ["token", "head", "apart"])
-@pytest.mark.parametrize("shared", [0, 20])
+@pytest.mark.parametrize("shared", [0, 20, 200])
 def test_cache_orders(order, shared):
     check(inputs([100] * 40 + [0, 3], 8, 2, 128, 16, order=order, shared=shared))
 
