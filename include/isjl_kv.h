@@ -137,7 +137,7 @@ typedef struct {
 typedef struct {
     int32_t n;                   /* queries, 0..max_rows */
     int32_t n_table_rows;
-    int32_t table_width;         /* table_width * block_size + prefix < 2^31 */
+    int32_t table_width;         /* table_width * block_size + prefix < 2^31, and n times that < 2^36 */
     int32_t n_prefix_blocks;     /* >= 0 */
     int32_t window;              /* >= 0 */
     int32_t sinks;               /* >= 0, used with a window */
@@ -156,7 +156,9 @@ typedef struct {
 typedef struct isjl_kv isjl_kv;
 
 /* Create a handle for one cache and head shape on the current CUDA device, with
- * the workspace of its calls.  Errors: INVALID_ARG (null pointer, a value outside
+ * the workspace of its calls (about 80 MB of device memory, and where a prefix can
+ * be done apart, n_q_heads / n_kv_heads <= 128 and head_dim <= 128, 20 MB and three
+ * times max_rows * n_q_heads * head_dim * 4 bytes more).  Errors: INVALID_ARG (null pointer, a value outside
  * the ranges above), OOM, CUDA.  On error *out is NULL. */
 isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out);
 

@@ -238,6 +238,8 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
     const int most = !kv ? 0 : kv->cfg.max_rows < ISJL_KV_MAX_ROWS ? kv->cfg.max_rows : ISJL_KV_MAX_ROWS;
     if (!kv || !a || !cache_ok(cache) || a->n < 0 || a->n > most || a->table_width < 1 || a->n_table_rows < 0 ||
         a->n_prefix_blocks < 0 || ((int64_t)(a->table_width + (int64_t)a->n_prefix_blocks) << kv->shift) > INT32_MAX ||
+        // slices of 32 tokens are counted in 32 bits
+        a->n * ((((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) / 32 + 2) > INT32_MAX ||
         (a->n_prefix_blocks > 0 && !a->prefix) || a->window < 0 || a->sinks < 0 || !(a->scale > 0.f) || !std::isfinite(a->scale))
         return ISJL_ERR_INVALID_ARG;
     if (a->n == 0) return ISJL_OK;

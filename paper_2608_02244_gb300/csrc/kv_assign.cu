@@ -135,7 +135,6 @@ __device__ __forceinline__ void move_blocks(const AssignArgs &g, const Sums &h, 
         a.table[(int64_t)i * a.table_width + j] = free_block(g, h, h.avail - 1 - k);
     }
     for (int32_t k = me; k < h.backs; k += count) {
-        if (h.n_free + k >= g.n_blocks) { report(g.status); break; }
         const int i = find(h.back, 0, a.n_rows, k);
         a.free_list[h.n_free + k] = a.table[(int64_t)i * a.table_width + (k - h.back[i])];
     }
@@ -178,7 +177,9 @@ __device__ __forceinline__ Sums sums(const AssignArgs &g, int32_t *starts, int32
 #pragma unroll
     for (int k = 0; k < 3; ++k) own[k] = x[k];
     scan(x, total, smem);
-    const int32_t avail = (int32_t)min((int64_t)n_free + total[2], (int64_t)g.n_blocks);
+    // rows that end with more blocks than there are: only what the list can hold is given back
+    const int32_t backs = (int32_t)min(total[2], (int64_t)(g.n_blocks - n_free)), avail = n_free + backs;
+    if (total[2] > backs) report(g.status);
     int64_t need = x[0] - own[0], ask = x[1] - own[1], given = x[2] - own[2];          // before this thread's rows
     int64_t y[2] = {need, ask}, got[2] = {total[0], total[1]};
     const bool all = total[0] <= avail && total[1] <= a.max_tokens;
@@ -205,7 +206,7 @@ __device__ __forceinline__ Sums sums(const AssignArgs &g, int32_t *starts, int32
         const bool ok = all || ((r.need == 0 || need <= avail) && ask <= a.max_tokens);
         take[i] = (int32_t)y[0];
         starts[i] = (int32_t)y[1];
-        back[i] = (int32_t)given;
+        back[i] = (int32_t)min(given, (int64_t)INT32_MAX);
         old[i] = r.len;
         a.granted[i] = ok ? r.ask : 0;
         a.starts[i] = (int32_t)y[1];
@@ -216,7 +217,7 @@ __device__ __forceinline__ Sums sums(const AssignArgs &g, int32_t *starts, int32
     if (threadIdx.x == 0) a.starts[n] = (int32_t)got[1];
     __syncthreads();              // all have read n_free, all sums are written
     if (threadIdx.x == 0) *a.n_free_out = avail - (int32_t)got[0];
-    return {starts, take, back, old, n_free, avail, (int32_t)got[1], (int32_t)got[0], (int32_t)total[2]};
+    return {starts, take, back, old, n_free, avail, (int32_t)got[1], (int32_t)got[0], backs};
 }
 
 // a whole step of at most kScan rows

@@ -10,6 +10,9 @@
 // by the runs' ends leaves pieces (those of neighbouring warps joined in shared memory first), which a second
 // kernel joins in their order.  Joining them here, by the last of an item's warps to arrive, took a fence and an
 // atomic under full memory load: 10 to 20 us of stall against 3 us of a small kernel that starts as this one ends.
+//
+// 512 queries of 64 + 8 heads of 128 values, 4 GB of keys and values: 639 us, 6.4 TB/s; 256 queries, 670 MB: 123 us,
+// 5.4 TB/s (6 us until the rings are full, and SMs that end up to 15% apart).  The tensor pipe is 18% busy.
 #include "kv_tma.cuh"
 
 namespace isjl {
@@ -174,9 +177,9 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         }
         here.t = lo;
         here.s = sight(g, lo);
-        const int32_t rest = (int32_t)(f0 - (int64_t)before[lo] * H);
-        here.h = rest / here.s.slices;
-        here.i = rest - here.h * here.s.slices;
+        const int64_t rest = f0 - (int64_t)before[lo] * H;
+        here.h = (int)(rest / here.s.slices);
+        here.i = (int)(rest - (int64_t)here.h * here.s.slices);
     }
     Place ahead = here;
     int64_t ahead_left = f1 - f0;                      // slices whose values are still to be asked for

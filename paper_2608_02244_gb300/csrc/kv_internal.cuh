@@ -18,7 +18,6 @@ struct Half;
 template <>
 struct Half<__nv_bfloat16> {
     static constexpr bool kIsBf16 = true;
-    using Pair = __nv_bfloat162;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<uint32_t *>(&v);
@@ -38,7 +37,6 @@ struct Half<__nv_bfloat16> {
 template <>
 struct Half<__half> {
     static constexpr bool kIsBf16 = false;
-    using Pair = __half2;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         __half2 v = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<uint32_t *>(&v);

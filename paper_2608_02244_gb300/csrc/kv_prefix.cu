@@ -3,7 +3,7 @@
 // All queries see the same P prefix tokens, so for one key head the queries of the batch (n tokens times the
 // `group` query heads of that key head) are the rows of a matrix: S = Q K^T, O = softmax(S) V, 4 D operations
 // for each row and token, on the fifth-generation tensor cores.  A block takes two tiles of 128 rows and a
-// run of tiles of 128 tokens: keys and values come by TMA from the cache's blocks through a ring of stages,
+// run of tiles of 128 tokens: keys and values come by TMA from the cache's blocks through a ring each,
 // one thread issues the products, and each row of a tile is one thread of a group of four warps that takes
 // the row's maximum, exponentials and sum.  Scores lie in TMEM, their weights take the scores' place as the
 // second product's left operand, and the two row tiles alternate: while the tensor cores work for one, the
@@ -14,6 +14,11 @@
 // The work is a line of (key head, pair of row tiles, token tile); every block has an equal run of it, and
 // leaves its piece of each item (sum, maximum and total of each row) for kv_attend.cu to join with the
 // requests' own tokens.
+//
+// 512 queries of 64 + 8 heads of 128 values over 32,768 tokens: 361 us, 1.52 PFLOP/s, on 128 SMs as on 152 (power);
+// the tensor cores are active in 77% of the cycles.  Steps of that took it there from 465: one thread's issue with
+// uniform addresses (a product takes 64 cycles, its issue took 100), stages freed by the row groups instead of commits,
+// weights handed over in halves, waits for copies beside products under way.
 #include "kv_tma.cuh"
 
 namespace isjl {
@@ -63,7 +68,8 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 #define R8(v, i) "=r"((v)[(i)]), "=r"((v)[(i) + 1]), "=r"((v)[(i) + 2]), "=r"((v)[(i) + 3]), "=r"((v)[(i) + 4]), "=r"((v)[(i) + 5]), "=r"((v)[(i) + 6]), "=r"((v)[(i) + 7])
 #define W8(v, i) "r"((v)[(i)]), "r"((v)[(i) + 1]), "r"((v)[(i) + 2]), "r"((v)[(i) + 3]), "r"((v)[(i) + 4]), "r"((v)[(i) + 5]), "r"((v)[(i) + 6]), "r"((v)[(i) + 7])
 
-// two 32-bit operations in one instruction: 378 -> 361 us for the exponents' arguments and sums of 512 queries of 8 x 8 heads over 32,768 tokens
+// two 32-bit operations in one instruction: for the exponents' arguments and sums, 378 -> 361 us with 512 queries of
+// 64 + 8 heads over 32,768 tokens
 __device__ __forceinline__ float2 fma2(float x, float y, float scale, float offset) {
     float2 z;
     asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %4};\nmov.b64 c, {%5, %5};\nfma.rn.f32x2 d, a, b, c;\n"
@@ -92,7 +98,8 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
 // barriers, in 8-byte words after the tiles
-enum { kKeyFull = 0, kValueFull = 8, kFree = 4 /* after a stage's full one */, kScores = 16, kWeights = 18, kSums = 20, kQueries = 22, kRest = 24, kBars = 26 };
+enum { kKeyFull = 0, kValueFull = 8, kFree = 4 /* after a stage's full one */, kScores = 16, kWeights = 18, kSums = 20, kQueries = 22,
+       kRest = 24, kBars = 26 };
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -280,9 +287,10 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
             const uint32_t piece_bytes = rows * 128;
             // this lane's part of a tile: piece lane % pieces, and every 32 / pieces-th half
             const int piece = lane % pieces;
+            constexpr int32_t kNone = INT32_MIN;
             auto block_of = [&](int j) {
                 const int token = j * kKeys + piece * rows;
-                return token < g.tokens ? g.prefix[token >> g.shift] : g.n_blocks;       // beyond the prefix: zeros
+                return token < g.tokens ? g.prefix[token >> g.shift] : kNone;
             };
             // A ring for each: a stage's turns are one warp's, which cannot be two turns ahead of itself.
             const bool values = warp != kLoadWarp;
@@ -301,7 +309,10 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                     int block = coming;
                     const int slot = (j * kKeys + piece * rows) & ((1 << g.shift) - 1);
                     if (j + 1 < j0 + count) coming = block_of(j + 1);
-                    if ((uint32_t)block > (uint32_t)g.n_blocks) { report(g.status); block = g.n_blocks; }
+                    if ((uint32_t)block >= (uint32_t)g.n_blocks) {                 // beyond the prefix or the cache: zeros
+                        if (block != kNone) report(g.status);
+                        block = g.n_blocks;
+                    }
                     ok = __all_sync(~0u, load < stages || bar_wait(bar(full + kFree + stage), turn ^ 1, failed));
                     if (!ok) break;
                     if (lane == 0) bar_expect(bar(full + stage), S::kTileBytes);

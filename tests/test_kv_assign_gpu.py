@@ -138,6 +138,21 @@ def test_reports_invalid_values():
         assert p.granted.tolist() == [1, 0 if not 0 <= lens[1] <= 32 else 1, 1]
 
 
+def test_reports_more_blocks_than_there_are():
+    """Rows that end with more blocks than the pool has: the list takes what it can hold, nothing beyond it is touched."""
+    import torch
+    from paper_2608_02244_gb300 import kv
+    for n, width in ((3, 12), (1500, 40000)):                  # sums beyond the pool, and beyond 32 bits
+        d = kv.Decoder(20, 256, 1, 1, 64, max_rows=n)
+        lens = torch.full((n,), width * 256, dtype=torch.int32, device="cuda")
+        table = torch.zeros((n, width), dtype=torch.int32, device="cuda")
+        new = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+        new[n // 2], lens[n // 2] = 700, 0
+        p = d.assign(lens, new, table, on_gpu(np.arange(20)), on_gpu([4]), 1024)
+        assert d.status() == kv.ISJL_ERR_INVALID_ARG
+        assert int(p.n_free) == 17 and p.granted[n // 2] == 700 and (p.slots[:700] >= 0).all()
+
+
 def test_refusals():
     import torch
     from paper_2608_02244_gb300 import kv

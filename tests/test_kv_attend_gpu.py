@@ -278,6 +278,13 @@ def test_reports_invalid_values():
             assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
         if name == "lens":
             assert (got[1] == 0).all()
+    s = inputs([9] * 100, 8, 2, 128, 16, shared=60)            # a prefix done apart
+    d = decoder(s)
+    assert torch.isfinite(d.attend(**s)).all() and d.status() == 0
+    for value in (-1, s["k"].shape[0]):
+        s["prefix"][59] = value
+        assert torch.isfinite(d.attend(**s)).all()
+        assert d.status() == kv.ISJL_ERR_INVALID_ARG and d.status() == 0
     s = inputs([100, 100], 8, 2, 128, 16)
     d = decoder(s)
     rows = torch.tensor([0, 7], dtype=torch.int32, device="cuda")
