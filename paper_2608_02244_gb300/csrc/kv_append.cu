@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (h0 + u * kHeads >= heads) break;
+            __syncwarp();
             const int h = h0 + u * kHeads + part;
             const bool is_v = h >= hq + hkv, is_k = !is_v && h >= hq;
             float x[8];

@@ -20,6 +20,7 @@ constexpr int kFill = 256;    // threads of the blocks that fill the maps, 4 ent
 template <int N>
 __device__ __forceinline__ void scan(int64_t (&x)[N], int64_t (&total)[N], int64_t (*sums)[3]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    __syncwarp();                    // the threads come from loops of different lengths
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1)
 #pragma unroll
@@ -260,6 +261,7 @@ __global__ void __launch_bounds__(kFill) fill_kernel(const __grid_constant__ Ass
     // 4 neighbouring entries a thread, 128 a warp: their rows are between those of the warp's ends
     const int lane = threadIdx.x & 31, warps = gridDim.x * (kFill / 32);
     for (int64_t t0 = 128 * (int64_t)(blockIdx.x * (kFill / 32) + threadIdx.x / 32); t0 < a.max_tokens; t0 += 128 * (int64_t)warps) {
+        __syncwarp();                // the searches below are the whole warp's
         int lo = 0, hi = n;
         if (t0 < h.tokens) {
             lo = find_by_warp(h.starts, 0, n, (int32_t)t0);

@@ -117,6 +117,7 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             before[t] = k;
             sum += k;
         }
+        __syncwarp();                // the threads come from loops of different lengths
         int32_t inc = sum;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
