@@ -251,7 +251,9 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
     isjl::AttendArgs g;
     std::memset(&g, 0, sizeof(g));
     g.a = *a;
-    if (a->window == 0) g.a.sinks = 0;
+    // a window as long as any request can be hides nothing
+    if ((int64_t)g.a.window >= ((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) g.a.window = 0;
+    if (g.a.window == 0) g.a.sinks = 0;
     g.cache = *cache;
     g.n_blocks = kv->cfg.n_blocks;
     g.shift = kv->shift;
@@ -263,7 +265,7 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
     g.status = kv->d_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int grid = kv->sms * (a->n <= kv->full || kv->per_sm == 1 ? kv->per_sm : kv->per_sm - 1);
-    if (kv->d_prefix_o && a->window == 0 && worth_apart(a->n, a->n_prefix_blocks << kv->shift)) {
+    if (kv->d_prefix_o && g.a.window == 0 && worth_apart(a->n, a->n_prefix_blocks << kv->shift)) {
         isjl::PrefixArgs p;
         std::memset(&p, 0, sizeof(p));
         p.tokens = a->n_prefix_blocks << kv->shift;

@@ -87,6 +87,17 @@ def test_prefix_with_window(window, sinks):
     check(inputs(LENS, 4, 1, 128, 16, shared=9, seed=window), window=window, sinks=sinks)
 
 
+def test_window_that_hides_nothing():
+    """A window of at least the table's and the prefix's tokens is none; one token less is one."""
+    import torch
+    s = inputs([128, 100, 1] * 10, 4, 1, 64, 16, shared=60)
+    whole = 16 * (60 + s["table"].shape[1])
+    want = check(s)[0]
+    assert torch.equal(decoder(s).attend(**s, window=whole, sinks=3), want)
+    assert torch.equal(decoder(s).attend(**s, window=2**31 - 1), want)
+    check(s, window=whole - 1)
+
+
 @pytest.mark.parametrize("n,hq,hkv,shared,block", [(100, 8, 1, 40, 16), (33, 28, 4, 130, 8), (300, 4, 4, 9, 64), (129, 16, 2, 33, 32),
                                                    (17, 64, 8, 7, 256), (260, 7, 1, 65, 8)])
 @pytest.mark.parametrize("dim,dtype", [(64, "bfloat16"), (128, "float16"), (256, "bfloat16")])
