@@ -190,7 +190,7 @@ class Decoder:
         sizes = [w, w, w, n + 1, n] if in_place else [w, w, w, n + 1, n, n, 1]
         slots = torch.empty(m, dtype=torch.int64, device=self.device)
         block = torch.empty(3 * w + (2 * n + 1 if in_place else 3 * n + 2), dtype=i32, device=self.device)
-        parts = block.split_with_sizes(sizes)
+        parts = block.unsafe_split_with_sizes(sizes)       # integers: no view to keep track of, 2 us less
         positions, rows, visible, starts, granted = parts[:5]
         if w != m:
             positions, rows, visible = positions[:m], rows[:m], visible[:m]
