@@ -11,7 +11,7 @@
 // kernel joins in their order.  Joining them here, by the last of an item's warps to arrive, took a fence and an
 // atomic under full memory load: 10 to 20 us of stall against 3 us of a small kernel that starts as this one ends.
 //
-// 512 queries of 64 + 8 heads of 128 values, 4 GB of keys and values: 639 us, 6.4 TB/s; 256 queries, 670 MB: 123 us,
+// 512 queries of 64 + 8 heads of 128 values, 4 GB of keys and values: 647 us, 6.3 TB/s; 256 queries, 670 MB: 123 us,
 // 5.4 TB/s (6 us until the rings are full, and SMs that end up to 15% apart).  The tensor pipe is 18% busy.
 #include "kv_tma.cuh"
 
