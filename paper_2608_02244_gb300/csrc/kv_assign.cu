@@ -4,7 +4,7 @@
 // rows before it say which blocks of the free list are its own and where its tokens lie in the maps, so one
 // block of threads takes the sums and everything else is independent: entry t of the maps finds its row by a
 // search in `starts`, the k-th new block is the k-th from the top of the free list (or, where that was
-// pushed in this very call, an entry of an ended row's table row, found by a search in `first_back`).
+// pushed in this very call, an entry of an ended row's table row, found by a search in `back`).
 // Bound by latency for a step's few hundred tokens: one kernel does it all from shared memory.  Prompts are
 // bound by the 20 bytes a map entry: the block of the sums is followed by a grid that fills the maps.
 #include "kv_tma.cuh"
