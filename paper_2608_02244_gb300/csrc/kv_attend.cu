@@ -241,11 +241,13 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     int stage = 0;
     uint32_t phase = 0;
     bool stuck = false;
-    // the next stage of the ring, when it has come; the one before it, which all have read by now, is fed
+    // The next stage of the ring, when it has come; the one before it, which all have read by now, is fed.  Lanes leave
+    // the prefetches and the wait at different times, and the products that follow are the whole warp's.
     auto next_stage = [&]() {
         __syncwarp();
         feed(stage == 0 ? S::kStages - 1 : stage - 1);
-        if (!stuck && !bar_wait(bar0 + 8 * stage, phase)) stuck = true;
+        if (!stuck) stuck = !__all_sync(~0u, bar_wait(bar0 + 8 * stage, phase));
+        __syncwarp();
         const uint32_t at = ring + stage * S::kStageBytes;
         if (++stage == S::kStages) { stage = 0; phase ^= 1; }
         return at;
@@ -399,7 +401,7 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             if (here.i == 0) begin_item();
         }
     }
-    if (stuck) atomicOr(g.status, 2);
+    if (stuck && lane == 0) atomicOr(g.status, 2);
 
     // ---- what the runs' ends cut: `here` is each warp's last slice
     const bool tail = f0 < f1 && here.i + 1 < here.s.slices;

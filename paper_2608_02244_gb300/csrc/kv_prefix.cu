@@ -205,6 +205,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                 }
                 next(key_stage, 1, S::kKeyStages);
                 if (j > 0) next(value_stage, 1, S::kValueStages);
+                __syncwarp();                     // lanes come from the wait one by one, loads from TMEM are the warp's
                 uint32_t s[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_load(s[c], s_at + 32 * c);
@@ -269,6 +270,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t o[32];
+                __syncwarp();
                 tmem_load(o, o_at + 32 * c);
                 tmem_load_wait();
                 if (live)
