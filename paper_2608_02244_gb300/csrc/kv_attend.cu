@@ -13,6 +13,7 @@
 //
 // 512 queries of 64 + 8 heads of 128 values, 4 GB of keys and values: 647 us, 6.3 TB/s; 256 queries, 670 MB: 123 us,
 // 5.4 TB/s (6 us until the rings are full, and SMs that end up to 15% apart).  The tensor pipe is 18% busy.
+#include "kv_ring.cuh"
 #include "kv_tma.cuh"
 
 namespace isjl {
@@ -238,18 +239,26 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             }
     };
 
-    int stage = 0;
-    uint32_t phase = 0;
+    RingPlace<S::kStages> place;
+    int64_t f = f0;                                    // the slice at hand, on the line
     bool stuck = false;
-    // The next stage of the ring, when it has come; the one before it, which all have read by now, is fed.  Lanes leave
-    // the prefetches and the wait at different times, and the products that follow are the whole warp's.
-    auto next_stage = [&]() {
+    // The next stage of the ring (a slice's keys, 0, or values, 1), when it has come; the one before it, which all have
+    // read by now, is fed.  Lanes leave the prefetches and the wait at different times, and the products that follow
+    // are the whole warp's.  So is giving up: nothing is asked for after it, and what is under way is waited for, since
+    // the ring's memory is used again and then becomes another block's.
+    auto next_stage = [&](int values) {
         __syncwarp();
-        feed(stage == 0 ? S::kStages - 1 : stage - 1);
-        if (!stuck) stuck = !__all_sync(~0u, bar_wait(bar0 + 8 * stage, phase));
+        feed(place.before());
+        const uint32_t at = ring + place.stage * S::kStageBytes;
+        if (!stuck) {
+            stuck = !__all_sync(~0u, bar_wait(bar0 + 8 * place.stage, place.phase));
+            if (stuck) {
+                ahead_left = 0;
+                for (int k = place.under_way(2 * (f1 - f) - values); k > 0; --k, place.take()) bar_wait(bar0 + 8 * place.stage, place.phase);
+            }
+            place.take();
+        }
         __syncwarp();
-        const uint32_t at = ring + stage * S::kStageBytes;
-        if (++stage == S::kStages) { stage = 0; phase ^= 1; }
         return at;
     };
 
@@ -261,7 +270,7 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     }
     auto slice = [&]() {
         const int32_t x = slice_start(here.s, here.i);
-        const uint32_t keys = next_stage();
+        const uint32_t keys = next_stage(0);
         float s[4][4] = {};
         {
             // lanes 0-7: tokens 0-7 low half of 16 values, 8-15: high half, 16-23: tokens 8-15 low, 24-31: high
@@ -324,7 +333,7 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
                 l[j] += u + v;
                 w[i / 2][(i & 1) * 2 + j] = Half<T>::pack(u, v);
             }
-        const uint32_t values = next_stage();
+        const uint32_t values = next_stage(1);
         if (edge) {
             // a weight of 0 does not silence an infinite or undefined value: what is not seen becomes 0
             for (int i = lane; i < kSlice * S::kHalves * 8; i += 32) {
@@ -393,8 +402,8 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     };
 
     if (f0 < f1) begin_item();
-    for (int64_t f = f0; f < f1; ++f) {
-        slice();
+    for (; f < f1; ++f) {
+        if (!stuck) slice();                            // the records of items stay whole
         if (here.i + 1 == here.s.slices) end_item();
         if (f + 1 < f1) {
             advance(here);
