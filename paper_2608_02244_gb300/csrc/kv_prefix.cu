@@ -99,7 +99,7 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 
 // barriers, in 8-byte words after the tiles
 enum { kKeyFull = 0, kValueFull = 8, kFree = 4 /* after a stage's full one */, kScores = 16, kWeights = 18, kSums = 20, kQueries = 22,
-       kRest = 24, kBars = 26 };
+       kRest = 24, kDrain = 26, kBars = 27 };
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -135,6 +135,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
             bar_init(bar(kSums + i), 1);
             bar_init(bar(kQueries + i), 128);
         }
+        bar_init(bar(kDrain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kIssueWarp) {
@@ -400,7 +401,13 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                 }
                 f += count;
             }
-            if (!ok) *failed = 1;
+            if (!ok) {
+                // products under way still read shared memory and write TMEM
+                *failed = 1;
+                if (one) commit(bar(kDrain));
+                __syncwarp();
+                bar_wait(bar(kDrain), 0);
+            }
             __syncwarp();
         }
     }

@@ -25,8 +25,8 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t phase) {
     return done != 0;
 }
 
-// Waits end: after kLimit nanoseconds without the barrier's turn whoever waits gives up, waits for the copies
-// that are under way, reports it and returns.
+// Waits end: after kLimit nanoseconds without the barrier's turn whoever waits gives up, waits for the copies (and
+// products) that are under way, reports it and returns.
 constexpr uint64_t kLimit = 2000000000ull;
 __device__ __forceinline__ uint64_t now() {
     uint64_t t;
