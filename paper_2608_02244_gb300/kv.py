@@ -106,8 +106,10 @@ Plan = collections.namedtuple("Plan", "slots positions rows visible starts grant
 class Decoder:
     """Owns a library handle for one cache and head shape.  Caches, tables and
     lengths are the caller's.  Calls go to `stream` (default: the current one) and
-    must not overlap on the GPU.  Caches are [n_blocks, block_size, n_kv_heads,
-    head_dim] with any order of the first three axes in memory."""
+    must not overlap on the GPU.  A call's inputs have to be ready for its stream, and
+    its results are ready when that stream is done with it.  Caches are
+    [n_blocks, block_size, n_kv_heads, head_dim] with any order of the first three axes
+    in memory."""
 
     def __init__(self, n_blocks, block_size, n_q_heads, n_kv_heads, head_dim, dtype=None, max_rows=512):
         import torch
@@ -159,9 +161,22 @@ class Decoder:
             ks, vs = ([x if n > 1 else 8 for x, n in zip(y, shape)] for y in (ks, vs))
         return _CACHE.pack(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2])
 
+    def _empty(self, stream, shape, dtype):
+        """Memory for a result.  The allocator hands out what is free in the order of one stream's
+        work, so it is asked on the stream that the call goes to; the current stream may use the
+        result until it is dropped."""
+        torch = self.torch
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        current = torch.cuda.current_stream(self.device)
+        with torch.cuda.stream(stream):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(current)
+        return t
+
     def _stream(self, stream, tensors):
-        """The stream's number; memory of a call on another stream than the current one stays
-        until that stream is done with it."""
+        """The stream's number; the caller's memory in a call on another stream than the current one
+        stays until that stream is done with it."""
         if stream is None:
             return self._raw_stream(self._index)
         if stream != self.torch.cuda.current_stream(self.device):
@@ -188,8 +203,8 @@ class Decoder:
         # one allocation for the 32-bit results, whose maps begin at multiples of 16 bytes
         w = (m + 3) & ~3
         sizes = [w, w, w, n + 1, n] if in_place else [w, w, w, n + 1, n, n, 1]
-        slots = torch.empty(m, dtype=torch.int64, device=self.device)
-        block = torch.empty(3 * w + (2 * n + 1 if in_place else 3 * n + 2), dtype=i32, device=self.device)
+        slots = self._empty(stream, m, torch.int64)
+        block = self._empty(stream, 3 * w + (2 * n + 1 if in_place else 3 * n + 2), i32)
         parts = block.unsafe_split_with_sizes(sizes)       # integers: no view to keep track of, 2 us less
         positions, rows, visible, starts, granted = parts[:5]
         if w != m:
@@ -200,7 +215,7 @@ class Decoder:
         out = (ptrs[0], ptrs[4]) if in_place else (at + 4 * n, at + 8 * n)
         args = _ASSIGN.pack(n, table.shape[1], m, prefix_len, *ptrs, *out, at, base + 12 * w, slots.data_ptr(), base,
                             base + 4 * w, base + 8 * w)
-        st = self._stream(stream, (lens, new_tokens, table, free, n_free, slots, block))
+        st = self._stream(stream, (lens, new_tokens, table, free, n_free))
         _check(self._lib.isjl_kv_assign(self.handle, args, st), "isjl_kv_assign")
         return Plan(slots, positions, rows, visible, starts, granted, lens_out, n_free_out)
 
@@ -216,7 +231,7 @@ class Decoder:
             self._bad(f"qkv must be {dtype} [tokens, {self._qkv}] with stride 1 last")
         cache = self._cache(k, v)
         if out is None:
-            out = torch.empty((n, hq, d), dtype=dtype, device=self.device)
+            out = self._empty(stream, (n, hq, d), dtype)
         elif out.shape != (n, hq, d) or out.dtype is not dtype or out.get_device() != index or \
                 out.stride(2) != 1 or (hq > 1 and out.stride(1) != d):
             self._bad("out must be [tokens, n_q_heads, head_dim] of the cache's type, heads side by side")
@@ -249,7 +264,7 @@ class Decoder:
             self._bad(f"q must be {dtype} [at most {self.max_rows}, {hq}, {d}] with stride 1 last")
         cache = self._cache(k, v)
         if out is None:
-            out = torch.empty(shape, dtype=dtype, device=self.device)
+            out = self._empty(stream, shape, dtype)
         elif out.shape != shape or out.dtype is not dtype or out.get_device() != index or out.stride(2) != 1:
             self._bad("out must have q's shape and type with stride 1 last")
         if table.dim() != 2:
@@ -257,7 +272,7 @@ class Decoder:
         window, sinks = int(window), int(sinks)
         if not (0 <= window < 2**31 and 0 <= sinks < 2**31):
             self._bad("window and sinks must be in 0..2^31 - 1")
-        weights = torch.empty((n, hq), dtype=torch.float32, device=self.device) if lse else None
+        weights = self._empty(stream, (n, hq), torch.float32) if lse else None
         # the stride of an axis of one element says nothing: any valid one
         qs, os = q.stride(), out.stride()
         if n <= 1 or hq == 1:

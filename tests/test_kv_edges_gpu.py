@@ -25,3 +25,68 @@ def test_lanes_that_part_ways(hq, hkv, dim, shared):
     for _ in range(20):
         out, again = d.attend(**s, lse=True)
         assert torch.equal(out, want) and torch.equal(again, lse)
+
+
+def _results_of(call, want, side):
+    """The call's results on another stream, asked for while the current one still has work to do on memory of
+    their sizes that it has given back."""
+    import torch
+    torch.cuda.synchronize()
+    left = [torch.empty_like(t) for t in want]
+    at = [t.data_ptr() for t in left]
+    torch.cuda._sleep(200_000_000)                   # a tenth of a second
+    for t in left:
+        t.view(torch.uint8).fill_(255)
+    del t
+    left.clear()
+    again = [torch.empty_like(t) for t in want]
+    assert {t.data_ptr() for t in again} & set(at)   # the current stream would get that memory
+    again.clear()
+    got = call(side)
+    side.synchronize()
+    early = [t.cpu() for t in got]                   # copies on the current stream: after its work
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b.cpu()) for a, b in zip(early, want))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    return got
+
+
+def test_results_on_another_stream():
+    """Their memory is not what the current stream still uses, and stays theirs while the current stream uses them."""
+    import torch
+    from paper_2608_02244_gb300 import kv
+    side = torch.cuda.Stream()
+    s = inputs([40] * 300 + [0], 32, 4, 128, 16)
+    d = decoder(s)
+    want = d.attend(**s, lse=True)
+    _results_of(lambda stream: d.attend(**s, lse=True, stream=stream), want, side)
+
+    n = 1000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    qkv = torch.randn(n, 40 * 128, generator=g, device="cuda").bfloat16()
+    slots = torch.randperm(s["k"].shape[0] * 16, generator=g, device="cuda")[:n]
+    k, v = torch.zeros_like(s["k"]), torch.zeros_like(s["v"])
+    want = [d.append(qkv, None, slots, k, v)]
+    _results_of(lambda stream: [d.append(qkv, None, slots, k, v, stream=stream)], want, side)
+
+    rows, m = 200, 300_000
+    i32 = dict(dtype=torch.int32, device="cuda")
+    lens, new, table = torch.arange(rows, **i32) % 50, torch.full((rows,), 3, **i32), torch.arange(rows * 8, **i32).view(rows, 8)
+    d = kv.Decoder(rows * 8 + 1000, 16, 1, 1, 64, max_rows=rows)
+    free, n_free = torch.zeros(rows * 8 + 1000, **i32), torch.tensor([1000], **i32)
+    free[:1000] = torch.arange(rows * 8, rows * 8 + 1000, **i32)
+    want = d.assign(lens, new, table, free, n_free, m)
+    got = _results_of(lambda stream: d.assign(lens, new, table, free, n_free, m, stream=stream), want, side)
+    # dropped after use on the current stream: the other stream does not get the memory before that use is over
+    out = got.slots
+    at, before = out.data_ptr(), out.clone()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    kept = out + 0
+    del out, got
+    with torch.cuda.stream(side):
+        other = torch.empty_like(before)
+        other.fill_(7)
+    assert other.data_ptr() != at
+    torch.cuda.synchronize()
+    assert torch.equal(kept, before)
