@@ -28,7 +28,8 @@
  * reported by isjl_kv_status and skipped: tokens in a block whose number is outside
  * the cache read as 0, a request whose length is beyond its table's width is
  * inactive, a token with a slot or position out of range is padding.  A handle holds the workspace of its calls: they must not
- * overlap on the GPU, and a handle is not thread safe.
+ * overlap on the GPU, and a handle is not thread safe.  It belongs to the device that was current when it was created:
+ * with another one current its calls are refused (INVALID_ARG), the report too; it can be destroyed.
  */
 #ifndef ISJL_KV_H
 #define ISJL_KV_H

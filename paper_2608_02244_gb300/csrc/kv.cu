@@ -8,6 +8,7 @@
 
 struct isjl_kv {
     isjl_kv_config cfg;
+    int device = 0;                      // whose memory and kernels these are: calls with another one current are refused
     int sms = 0, shift = 0;
     int per_sm = 0, full = 0;            // the attention's blocks of an SM, with at most `full` queries
     // one allocation: the status word, then the workspaces of assign and attend
@@ -37,6 +38,12 @@ bool cache_ok(const isjl_kv_cache *c) {
     for (int i = 0; i < 3; ++i)
         if (!stride_ok(c->k_stride[i]) || !stride_ok(c->v_stride[i])) return false;
     return true;
+}
+
+// Streams and pointers do not say whose they are: stream 0 is that of the current device.
+bool device_ok(const isjl_kv *kv) {
+    int current = -1;
+    return cudaGetDevice(&current) == cudaSuccess && current == kv->device;
 }
 
 isjl_status launched(cudaError_t e) { return e == cudaSuccess ? ISJL_OK : ISJL_ERR_CUDA; }
@@ -127,10 +134,9 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
     if (!kv) return ISJL_ERR_OOM;
     kv->cfg = *cfg;
     while ((1 << kv->shift) < cfg->block_size) ++kv->shift;
-    int device = 0;
     const int queries = cfg->max_rows < ISJL_KV_MAX_ROWS ? cfg->max_rows : ISJL_KV_MAX_ROWS;
-    if (cudaGetDevice(&device) != cudaSuccess ||
-        cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
+    if (cudaGetDevice(&kv->device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, kv->device) != cudaSuccess ||
         isjl::prepare_attend(cfg->head_dim, cfg->type, &kv->per_sm, &kv->full) != cudaSuccess || kv->per_sm < 1) {
         cudaGetLastError();
         delete kv;
@@ -186,13 +192,17 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
 
 void isjl_kv_destroy(isjl_kv *kv) {
     if (!kv) return;
+    int current = kv->device;
+    cudaGetDevice(&current);
+    if (current != kv->device) cudaSetDevice(kv->device);
     cudaDeviceSynchronize();
     cudaFree(kv->d_work);
+    if (current != kv->device) cudaSetDevice(current);
     delete kv;
 }
 
 isjl_status isjl_kv_assign(isjl_kv *kv, const isjl_kv_assign_args *a, void *stream) {
-    if (!kv || !a || a->n_rows < 0 || a->n_rows > kv->cfg.max_rows || a->table_width < 1 ||
+    if (!kv || !device_ok(kv) || !a || a->n_rows < 0 || a->n_rows > kv->cfg.max_rows || a->table_width < 1 ||
         ((int64_t)a->table_width << kv->shift) > INT32_MAX || a->max_tokens < 1 || a->prefix_len < 0 ||
         (int64_t)a->prefix_len + ((int64_t)a->table_width << kv->shift) > INT32_MAX ||
         !a->free_list || !a->n_free || !a->n_free_out || !a->starts || !a->slots || !a->positions || !a->rows || !a->visible ||
@@ -210,7 +220,7 @@ isjl_status isjl_kv_assign(isjl_kv *kv, const isjl_kv_assign_args *a, void *stre
 }
 
 isjl_status isjl_kv_append(isjl_kv *kv, const isjl_kv_append_args *a, const isjl_kv_cache *cache, void *stream) {
-    if (!kv || !a || !cache_ok(cache) || a->n_tokens < 0 || a->rot < 0 || a->rot > kv->cfg.head_dim || a->rot % 16 != 0 ||
+    if (!kv || !device_ok(kv) || !a || !cache_ok(cache) || a->n_tokens < 0 || a->rot < 0 || a->rot > kv->cfg.head_dim || a->rot % 16 != 0 ||
         (a->interleaved != 0 && a->interleaved != 1) || !(a->eps >= 0.f) || !std::isfinite(a->eps))
         return ISJL_ERR_INVALID_ARG;
     if (a->n_tokens == 0) return ISJL_OK;
@@ -236,7 +246,7 @@ isjl_status isjl_kv_append(isjl_kv *kv, const isjl_kv_append_args *a, const isjl
 
 isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl_kv_cache *cache, void *stream) {
     const int most = !kv ? 0 : kv->cfg.max_rows < ISJL_KV_MAX_ROWS ? kv->cfg.max_rows : ISJL_KV_MAX_ROWS;
-    if (!kv || !a || !cache_ok(cache) || a->n < 0 || a->n > most || a->table_width < 1 || a->n_table_rows < 0 ||
+    if (!kv || !device_ok(kv) || !a || !cache_ok(cache) || a->n < 0 || a->n > most || a->table_width < 1 || a->n_table_rows < 0 ||
         a->n_prefix_blocks < 0 || ((int64_t)(a->table_width + (int64_t)a->n_prefix_blocks) << kv->shift) > INT32_MAX ||
         // slices of 32 tokens are counted in 32 bits
         a->n * ((((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) / 32 + 2) > INT32_MAX ||
@@ -292,7 +302,7 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
 }
 
 isjl_status isjl_kv_status(isjl_kv *kv) {
-    if (!kv) return ISJL_ERR_INVALID_ARG;
+    if (!kv || !device_ok(kv)) return ISJL_ERR_INVALID_ARG;
     // calls may have been replayed from graphs on any stream: all of the device's work is waited for
     int32_t word = 0;
     if (cudaDeviceSynchronize() != cudaSuccess ||

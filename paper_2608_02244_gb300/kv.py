@@ -106,7 +106,8 @@ Plan = collections.namedtuple("Plan", "slots positions rows visible starts grant
 class Decoder:
     """Owns a library handle for one cache and head shape.  Caches, tables and
     lengths are the caller's.  Calls go to `stream` (default: the current one) and
-    must not overlap on the GPU.  A call's inputs have to be ready for its stream, and
+    must not overlap on the GPU; the device that was current when the decoder was made
+    has to be current (else IsjlError).  A call's inputs have to be ready for its stream, and
     its results are ready when that stream is done with it.  Caches are
     [n_blocks, block_size, n_kv_heads, head_dim] with any order of the first three axes
     in memory."""

@@ -90,3 +90,37 @@ def test_results_on_another_stream():
     assert other.data_ptr() != at
     torch.cuda.synchronize()
     assert torch.equal(kept, before)
+
+
+def test_handle_of_another_device():
+    """With another device current than the handle's, calls are refused on the host and nothing is launched.  One GPU is
+    enough for that: the number of the device that the handle keeps, after its configuration, is changed."""
+    import ctypes
+
+    import torch
+    from paper_2608_02244_gb300 import kv
+    s = inputs([30, 1], 4, 2, 64, 16)
+    d = decoder(s)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    qkv = torch.randn(2, 8 * 64, device="cuda").bfloat16()
+    slots = torch.tensor([-1, -1], device="cuda")
+    free = torch.zeros(d.n_blocks, **i32)
+    n_free, new = torch.zeros(1, **i32), torch.zeros(2, **i32)
+    out = torch.full_like(s["q"], math.nan)
+    calls = [lambda: d.assign(s["lens"], new, s["table"], free, n_free, 4), lambda: d.append(qkv, None, slots, s["k"], s["v"]),
+             lambda: d.attend(**s, out=out)]
+    kept = ctypes.c_int32.from_address(d.handle.value + ctypes.sizeof(kv.isjl_kv_config))
+    assert kept.value == torch.cuda.current_device()
+    kept.value += 1
+    try:
+        for call in calls:
+            with pytest.raises(kv.IsjlError) as e:
+                call()
+            assert e.value.status == kv.ISJL_ERR_INVALID_ARG
+        assert d.status() == kv.ISJL_ERR_INVALID_ARG
+    finally:
+        kept.value -= 1
+    assert out.isnan().all()
+    for call in calls:
+        call()
+    assert d.status() == 0 and torch.isfinite(out).all()
