@@ -138,7 +138,7 @@ typedef struct {
 typedef struct {
     int32_t n;                   /* queries, 0..max_rows */
     int32_t n_table_rows;
-    int32_t table_width;         /* table_width * block_size + prefix < 2^31, and n times that < 2^36 */
+    int32_t table_width;         /* table_width * block_size + prefix <= 2^31 - 256, and n times that < 2^36 */
     int32_t n_prefix_blocks;     /* >= 0 */
     int32_t window;              /* >= 0 */
     int32_t sinks;               /* >= 0, used with a window */

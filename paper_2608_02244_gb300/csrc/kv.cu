@@ -26,6 +26,7 @@ struct isjl_kv {
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr int64_t kMostTokens = INT32_MAX - 255;     // of a request with its prefix: 32-bit places, rounded up to tiles
 constexpr int kFiner = 4;     // blocks of the own tokens' kernel for each that fits, beside a prefix's kernel
 size_t rounded(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 
@@ -247,7 +248,7 @@ isjl_status isjl_kv_append(isjl_kv *kv, const isjl_kv_append_args *a, const isjl
 isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl_kv_cache *cache, void *stream) {
     const int most = !kv ? 0 : kv->cfg.max_rows < ISJL_KV_MAX_ROWS ? kv->cfg.max_rows : ISJL_KV_MAX_ROWS;
     if (!kv || !device_ok(kv) || !a || !cache_ok(cache) || a->n < 0 || a->n > most || a->table_width < 1 || a->n_table_rows < 0 ||
-        a->n_prefix_blocks < 0 || ((int64_t)(a->table_width + (int64_t)a->n_prefix_blocks) << kv->shift) > INT32_MAX ||
+        a->n_prefix_blocks < 0 || (((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) > kMostTokens ||
         // slices of 32 tokens are counted in 32 bits
         a->n * ((((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) / 32 + 2) > INT32_MAX ||
         (a->n_prefix_blocks > 0 && !a->prefix) || a->window < 0 || a->sinks < 0 || !(a->scale > 0.f) || !std::isfinite(a->scale))

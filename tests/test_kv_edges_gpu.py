@@ -124,3 +124,30 @@ def test_handle_of_another_device():
     for call in calls:
         call()
     assert d.status() == 0 and torch.isfinite(out).all()
+
+
+def test_most_tokens():
+    """Tables and prefixes of up to 2^31 - 256 tokens: places are rounded up to whole tiles in 32 bits.  The tables
+    repeat one block; what a call does not see is not read."""
+    import torch
+    from paper_2608_02244_gb300 import kv
+    for block in (8, 256):
+        most = (2**31 - 256) // block
+        s = inputs([300], 2, 1, 64, block, seed=block)
+        want = check(s)
+        wide = torch.full((1, most + 1), -1, dtype=torch.int32, device="cuda")
+        wide[0, :s["table"].shape[1]] = s["table"][0]
+        d = decoder(s)
+        for more in (dict(table=wide), dict(table=wide[:, :most - 4].contiguous(), prefix=wide[0, :5])):
+            with pytest.raises(kv.IsjlError) as e:
+                d.attend(**dict(s, **more))
+            assert e.value.status == kv.ISJL_ERR_INVALID_ARG
+        out, lse = d.attend(**dict(s, table=wide[:, :most].contiguous()), lse=True)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        # the longest request there can be, in a window at its end
+        table = s["table"][:, :1].expand(1, most).contiguous()
+        lens = torch.full((1,), most * block, dtype=torch.int32, device="cuda")
+        out, lse = d.attend(**dict(s, table=table, lens=lens), window=block, lse=True)
+        assert d.status() == 0
+        one = dict(s, table=s["table"][:, :1].contiguous(), lens=torch.full((1,), block, dtype=torch.int32, device="cuda"))
+        kv_plain.check_attend(out, lse, *kv_plain.attend(**one))
