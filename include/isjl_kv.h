@@ -21,7 +21,8 @@
  * prefix lie in blocks of their own, named once for the whole batch, and come
  * before every request's own tokens.
  *
- * Conventions are those of isjl_sim.h: device pointers unless said otherwise,
+ * Conventions are those of isjl_sim.h: device pointers unless said otherwise
+ * (numbers at multiples of their size, what holds heads at multiples of 16 bytes),
  * stream is a cudaStream_t passed as void*, calls are asynchronous on it and
  * allocate nothing (they can be captured into a graph), no entry point throws,
  * traps or aborts, errors are isjl_status codes.  What only the device can see is

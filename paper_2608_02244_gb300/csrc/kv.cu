@@ -31,6 +31,9 @@ constexpr int kFiner = 4;     // blocks of the own tokens' kernel for each that 
 size_t rounded(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// arrays of numbers lie at multiples of their size
+template <typename... T>
+bool natural(const T *...p) { return (... && (reinterpret_cast<uintptr_t>(p) % sizeof(T) == 0)); }
 // what a copy's map can hold: less than 2^40 bytes
 bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0 && s < ((int64_t)1 << 39); }
 
@@ -207,7 +210,9 @@ isjl_status isjl_kv_assign(isjl_kv *kv, const isjl_kv_assign_args *a, void *stre
         ((int64_t)a->table_width << kv->shift) > INT32_MAX || a->max_tokens < 1 || a->prefix_len < 0 ||
         (int64_t)a->prefix_len + ((int64_t)a->table_width << kv->shift) > INT32_MAX ||
         !a->free_list || !a->n_free || !a->n_free_out || !a->starts || !a->slots || !a->positions || !a->rows || !a->visible ||
-        (a->n_rows > 0 && (!a->lens || !a->new_tokens || !a->table || !a->lens_out || !a->granted)))
+        (a->n_rows > 0 && (!a->lens || !a->new_tokens || !a->table || !a->lens_out || !a->granted)) ||
+        !natural(a->lens, a->new_tokens, a->table, a->free_list, a->n_free, a->lens_out, a->n_free_out, a->granted, a->starts,
+                 a->slots, a->positions, a->rows, a->visible))
         return ISJL_ERR_INVALID_ARG;
     isjl::AssignArgs g;
     std::memset(&g, 0, sizeof(g));
@@ -230,7 +235,7 @@ isjl_status isjl_kv_append(isjl_kv *kv, const isjl_kv_append_args *a, const isjl
     if (!a->qkv || !a->q_out || !a->slots || !aligned16(a->qkv) || !aligned16(a->q_out) || !aligned16(a->q_weight) ||
         !aligned16(a->k_weight) || a->qkv_stride < row || a->qkv_stride % 8 != 0 || a->q_out_stride < q_row ||
         a->q_out_stride % 8 != 0 || (a->rot > 0 && (!a->rope || !a->positions || a->n_positions < 1 || !aligned16(a->rope))) ||
-        (a->q_out == a->qkv && a->q_out_stride != a->qkv_stride))
+        (a->q_out == a->qkv && a->q_out_stride != a->qkv_stride) || !natural(a->positions, a->slots))
         return ISJL_ERR_INVALID_ARG;
     isjl::AppendArgs g;
     std::memset(&g, 0, sizeof(g));
@@ -255,7 +260,7 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
         return ISJL_ERR_INVALID_ARG;
     if (a->n == 0) return ISJL_OK;
     if (!a->q || !a->out || !a->lens || !a->table || !aligned16(a->q) || !aligned16(a->out) ||
-        (!a->rows && a->n > a->n_table_rows))
+        (!a->rows && a->n > a->n_table_rows) || !natural(a->lse, a->lens, a->rows, a->table, a->prefix))
         return ISJL_ERR_INVALID_ARG;
     for (int i = 0; i < 2; ++i)
         if (!stride_ok(a->q_stride[i]) || !stride_ok(a->out_stride[i])) return ISJL_ERR_INVALID_ARG;

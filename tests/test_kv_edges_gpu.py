@@ -151,3 +151,42 @@ def test_most_tokens():
         assert d.status() == 0
         one = dict(s, table=s["table"][:, :1].contiguous(), lens=torch.full((1,), block, dtype=torch.int32, device="cuda"))
         kv_plain.check_attend(out, lse, *kv_plain.attend(**one))
+
+
+def test_misaligned_pointers_are_refused():
+    """Each array of numbers of the three calls, a byte beside its place: INVALID_ARG on the host, nothing launched."""
+    import ctypes
+
+    import torch
+    from paper_2608_02244_gb300 import kv
+    L, d = kv.lib(), kv.Decoder(20, 8, 2, 1, 64, max_rows=3)
+    memory = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    base = memory.data_ptr()
+    cache = kv.isjl_kv_cache(base, base, (ctypes.c_int64 * 3)(512, 64, 8), (ctypes.c_int64 * 3)(512, 64, 8))
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def args(cls, numbers, pointers, other):
+        a = cls(**numbers, **other)
+        for i, f in enumerate(pointers):
+            setattr(a, f, base + 4096 + 1024 * i)
+        return a
+
+    ints = ("lens", "new_tokens", "table", "free_list", "n_free", "lens_out", "n_free_out", "granted", "starts", "slots", "positions",
+            "rows", "visible")
+    assign = args(kv.isjl_kv_assign_args, dict(n_rows=3, table_width=4, max_tokens=4), ints, {})
+    append = args(kv.isjl_kv_append_args, dict(n_tokens=2, n_positions=2, rot=16), ("positions", "slots"),
+                  dict(qkv=base, qkv_stride=256, q_out=base + 32768, q_out_stride=128, rope=base))
+    attend = args(kv.isjl_kv_attend_args, dict(n=2, n_table_rows=2, table_width=2, n_prefix_blocks=1, scale=1.0),
+                  ("lse", "lens", "rows", "table", "prefix"),
+                  dict(q=base, q_stride=(128, 64), out=base + 32768, out_stride=(128, 64)))
+    for a, fields, call in ((assign, ints, lambda a: L.isjl_kv_assign(d.handle, ctypes.byref(a), stream)),
+                            (append, ("positions", "slots"), lambda a: L.isjl_kv_append(d.handle, ctypes.byref(a), ctypes.byref(cache), stream)),
+                            (attend, ("lse", "lens", "rows", "table", "prefix"),
+                             lambda a: L.isjl_kv_attend(d.handle, ctypes.byref(a), ctypes.byref(cache), stream))):
+        assert call(a) == kv.ISJL_OK
+        for f in fields:
+            for by in (1, 2, 4) if f == "slots" else (1, 2):
+                setattr(a, f, getattr(a, f) + by)
+                assert call(a) == kv.ISJL_ERR_INVALID_ARG, f
+                setattr(a, f, getattr(a, f) - by)
+    torch.cuda.synchronize()
