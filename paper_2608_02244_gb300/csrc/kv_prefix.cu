@@ -228,7 +228,8 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                 if (j == 0) {
                     top = high;
                 } else if (__any_sync(~0u, high > top + kGrow)) {
-                    const float next = high > top + kGrow ? high : top, fix = ex2(top - next);
+                    const float next = high > top + kGrow ? high : top;
+                    const float fix = top == next ? 1.f : ex2(top - next);      // of -infinity too: another row's maximum grew
                     top = next;
                     total *= fix;
 #pragma unroll 1

@@ -190,3 +190,24 @@ def test_misaligned_pointers_are_refused():
                 assert call(a) == kv.ISJL_ERR_INVALID_ARG, f
                 setattr(a, f, getattr(a, f) - by)
     torch.cuda.synchronize()
+
+
+def long_runs(dim, dtype="bfloat16", seed=0):
+    """Enough queries that a block of the prefix's kernel has runs of ten token tiles of an item: 32 items of 20 tiles on
+    64 blocks."""
+    return inputs([30, 2, 90, 1] * 128, 16, 8, dim, 64, dtype, shared=40, seed=seed)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_prefix_row_of_minus_infinity_beside_growing_ones(dim):
+    """A row whose scores are -infinity in the first tiles, in a warp where other rows' maxima grow: its later tiles
+    give it a result all the same."""
+    s = long_runs(dim, seed=3)
+    first = s["prefix"].long()
+    s["k"][first[:2]] *= 0.1
+    s["k"][first[2:6]] *= 8
+    s["k"][..., 0] = 0
+    s["k"][first[:6], :, :, 0] = -1e20
+    s["q"][..., 0] = 0
+    s["q"][1::2, :, 0] = 1e20                        # times -1e20: beyond 32 bits
+    check(s)
