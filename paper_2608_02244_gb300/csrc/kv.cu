@@ -47,10 +47,16 @@ bool cache_ok(const isjl_kv_cache *c) {
 // Streams and pointers do not say whose they are: stream 0 is that of the current device.
 bool device_ok(const isjl_kv *kv) {
     int current = -1;
-    return cudaGetDevice(&current) == cudaSuccess && current == kv->device;
+    if (cudaGetDevice(&current) != cudaSuccess) cudaGetLastError();
+    return current == kv->device;
 }
 
-isjl_status launched(cudaError_t e) { return e == cudaSuccess ? ISJL_OK : ISJL_ERR_CUDA; }
+// The runtime keeps a failed call's error until it is asked for: the next check of a launch would take it for its own.
+isjl_status launched(cudaError_t e) {
+    if (e == cudaSuccess) return ISJL_OK;
+    cudaGetLastError();
+    return ISJL_ERR_CUDA;
+}
 
 // Whether a prefix is done apart, by its own kernel, or read by each query's warps with its own tokens.  The former
 // saves n - 1 of n readings of the prefix and costs a launch and the joining of its pieces.  Measured, read against
@@ -202,6 +208,7 @@ void isjl_kv_destroy(isjl_kv *kv) {
     cudaDeviceSynchronize();
     cudaFree(kv->d_work);
     if (current != kv->device) cudaSetDevice(current);
+    cudaGetLastError();
     delete kv;
 }
 
@@ -302,7 +309,8 @@ isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl
         g.line = p.line;
         g.prefix_o = kv->d_prefix_o;
         g.prefix_ml = kv->d_prefix_ml;
-        if (isjl::launch_prefix(p, *cache, kv->encoder, kv->cfg.head_dim, kv->cfg.type, st) != cudaSuccess) return ISJL_ERR_CUDA;
+        const cudaError_t e = isjl::launch_prefix(p, *cache, kv->encoder, kv->cfg.head_dim, kv->cfg.type, st);
+        if (e != cudaSuccess) return launched(e);
     }
     return launched(isjl::launch_attend(g, kv->encoder, kv->cfg.head_dim, kv->cfg.type, grid, st));
 }
@@ -311,10 +319,11 @@ isjl_status isjl_kv_status(isjl_kv *kv) {
     if (!kv || !device_ok(kv)) return ISJL_ERR_INVALID_ARG;
     // calls may have been replayed from graphs on any stream: all of the device's work is waited for
     int32_t word = 0;
-    if (cudaDeviceSynchronize() != cudaSuccess ||
-        cudaMemcpy(&word, kv->d_status, sizeof(word), cudaMemcpyDeviceToHost) != cudaSuccess ||
-        cudaMemset(kv->d_status, 0, sizeof(word)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
-        return ISJL_ERR_CUDA;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpy(&word, kv->d_status, sizeof(word), cudaMemcpyDeviceToHost);
+    if (e == cudaSuccess) e = cudaMemset(kv->d_status, 0, sizeof(word));
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) return launched(e);
     return word & 2 ? ISJL_ERR_INTERNAL : word ? ISJL_ERR_INVALID_ARG : ISJL_OK;
 }
 

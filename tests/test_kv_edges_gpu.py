@@ -211,3 +211,33 @@ def test_prefix_row_of_minus_infinity_beside_growing_ones(dim):
     s["q"][..., 0] = 0
     s["q"][1::2, :, 0] = 1e20                        # times -1e20: beyond 32 bits
     check(s)
+
+
+def test_errors_do_not_outlive_their_call():
+    """A call that fails in the CUDA runtime (a report asked for during a capture, a launch into a capture that this
+    broke) leaves nothing behind that a later call reports as its own."""
+    import ctypes
+
+    import torch
+    from paper_2608_02244_gb300 import kv, sim
+    rt = ctypes.CDLL("libcudart.so.%s" % torch.version.cuda.split(".")[0])
+    s = inputs([30, 1], 4, 2, 64, 16)
+    d = decoder(s)
+    qkv = torch.randn(2, 8 * 64, device="cuda").bfloat16()
+    slots = torch.tensor([-1, -1], device="cuda")
+    q, out = torch.empty_like(s["q"]), torch.empty_like(s["q"])
+    side = torch.cuda.Stream()
+    for fails in (False, True):
+        d.append(qkv, None, slots, s["k"], s["v"], out=q)
+        torch.cuda.synchronize()
+        graph = ctypes.c_void_p()
+        assert rt.cudaStreamBeginCapture(ctypes.c_void_p(side.cuda_stream), 1) == 0
+        assert d.status() == sim.ISJL_ERR_CUDA
+        if fails:
+            with pytest.raises(kv.IsjlError) as e:
+                d.attend(**s, out=out, stream=side)
+            assert e.value.status == sim.ISJL_ERR_CUDA
+        assert rt.cudaStreamEndCapture(ctypes.c_void_p(side.cuda_stream), ctypes.byref(graph)) != 0
+        rt.cudaGetLastError()
+        d.append(qkv, None, slots, s["k"], s["v"], out=q)
+        assert d.status() == 0 and (q == 0).all()
