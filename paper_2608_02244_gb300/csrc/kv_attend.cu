@@ -302,7 +302,7 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             for (int i = 1; i < 4; ++i) most = fmaxf(most, fmaxf(s[i][2 * j], s[i][2 * j + 1]));
             most *= scale;
             most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-            top[j] = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
+            top[j] = fmaxf(most, __shfl_xor_sync(~0u, most, 2)) - Half<T>::kTop;     // what weights are relative to
         }
         if (__any_sync(~0u, top[0] > m[0] || top[1] > m[1])) {
             float fix[2];
@@ -322,17 +322,20 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             }
         }
         const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
-        // weights are rounded to the cache's type for the product, as the tensor instruction takes them;
-        // the sum l is of the unrounded ones
+        // Weights are rounded to the cache's type for the product, as the tensor instruction takes them; the sum l is
+        // of the unrounded ones, a slice's among themselves first: beside a large l small ones would be lost one by one.
+        float part[2] = {0.f, 0.f};
         uint32_t w[2][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const float u = ex2(fmaf(s[i][2 * j], scale, -ref[j])), v = ex2(fmaf(s[i][2 * j + 1], scale, -ref[j]));
-                l[j] += u + v;
+                part[j] += u + v;
                 w[i / 2][(i & 1) * 2 + j] = Half<T>::pack(u, v);
             }
+        l[0] += part[0];
+        l[1] += part[1];
         const uint32_t values = next_stage(1);
         if (edge) {
             // a weight of 0 does not silence an infinite or undefined value: what is not seen becomes 0

@@ -18,6 +18,7 @@ struct Half;
 template <>
 struct Half<__nv_bfloat16> {
     static constexpr bool kIsBf16 = true;
+    static constexpr int kTop = 0;             // its range is that of 32 bits
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<uint32_t *>(&v);
@@ -37,6 +38,9 @@ struct Half<__nv_bfloat16> {
 template <>
 struct Half<__half> {
     static constexpr bool kIsBf16 = false;
+    // log2 of the largest softmax weight.  Weights below 2^-14 lose bits and below 2^-25 all of them, and tens of
+    // thousands of those can count: with the largest at 2^15 that begins 2^29 and 2^40 below it.
+    static constexpr int kTop = 15;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         __half2 v = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<uint32_t *>(&v);

@@ -8,8 +8,8 @@
 // the row's maximum, exponentials and sum.  Scores lie in TMEM, their weights take the scores' place as the
 // second product's left operand, and the two row tiles alternate: while the tensor cores work for one, the
 // other's group is at its exponentials.  The sums O stay in TMEM for the whole run; they are rescaled only
-// when a row's maximum has grown by more than 2^8 since the last time, so that weights stay below 2^8 and
-// rounding them to 16 bits is as exact as with the true maximum.
+// when a row's maximum has grown by more than 2^8 since the last time (fp16: 2^4, from 2^11, so that weights stay
+// within 2^15 and small ones keep their bits); rounding weights to 16 bits is as exact as with the true maximum.
 //
 // The work is a line of (key head, pair of row tiles, token tile); every block has an equal run of it, and
 // leaves its piece of each item (sum, maximum and total of each row) for kv_attend.cu to join with the
@@ -28,7 +28,11 @@ constexpr int kRows = 128, kKeys = 128;        // of a row tile, of a token tile
 constexpr int kThreads = 384;                  // two groups of four warps; the loading and the issuing warp's group
 constexpr int kLoadWarp = 8, kIssueWarp = 10;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kGrow = 8.f;                   // log2 of the growth of a maximum that is let pass
+// log2 of the growth of a maximum that is let pass, and of the largest weight of the tile that set it
+template <typename T>
+struct Grow {
+    static constexpr float kPass = Half<T>::kIsBf16 ? 8.f : 4.f, kTop = Half<T>::kTop > 0 ? Half<T>::kTop - kPass : 0.f;
+};
 
 template <int D>
 struct Shape {
@@ -224,11 +228,11 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                 for (int i = 0; i < 32; ++i)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) most[c] = fmaxf(most[c], __uint_as_float(s[c][i]));
-                const float high = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * scale;
+                const float high = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * scale - Grow<T>::kTop;
                 if (j == 0) {
                     top = high;
-                } else if (__any_sync(~0u, high > top + kGrow)) {
-                    const float next = high > top + kGrow ? high : top;
+                } else if (__any_sync(~0u, high > top + Grow<T>::kPass)) {
+                    const float next = high > top + Grow<T>::kPass ? high : top;
                     const float fix = top == next ? 1.f : ex2(top - next);      // of -infinity too: another row's maximum grew
                     top = next;
                     total *= fix;

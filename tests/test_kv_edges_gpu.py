@@ -241,3 +241,49 @@ def test_errors_do_not_outlive_their_call():
         rt.cudaGetLastError()
         d.append(qkv, None, slots, s["k"], s["v"], out=q)
         assert d.status() == 0 and (q == 0).all()
+
+
+def tail(got, lse, s, **kw):
+    """All queries are the same: each is compared with the first one's 64 bits."""
+    want, want_lse, size = kv_plain.attend(**dict(s, q=s["q"][:1], lens=s["lens"][:1]), **kw)
+    kv_plain.check_attend(got, lse, want.expand(got.shape), want_lse.expand(lse.shape), size.expand(got.shape))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_small_weights_of_fp16(dim):
+    """Tens of thousands of weights 2^-24 or less of the largest, which together count, since the largest's value is 0:
+    no weight is lost to the range of 16 bits.  Enough queries that one warp has the whole of a request."""
+    import torch
+    n = 1300
+    s = inputs([49152], 1, 1, dim, 64, "float16", rows=range(n), seed=4)
+    s["q"][:] = 0
+    s["q"][..., 0] = dim ** 0.5
+    own = s["table"][0].long()
+    s["k"][..., 0] = 0.4
+    s["v"][:] = 1
+    s["k"][own[0], 7, 0, 0] = 18                     # 25.4 powers of two above the others
+    s["v"][own[0], 7] = 0
+    s["lens"] = s["lens"].expand(n).contiguous()
+    rows = torch.zeros_like(s["lens"])
+    d = decoder(s)
+    got, lse = d.attend(**s, rows=rows, lse=True)
+    assert d.status() == 0
+    tail(got, lse, s, rows=rows)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_small_weights_of_fp16_in_a_prefix(dim):
+    s = inputs([1] * 512, 16, 8, dim, 64, "float16", shared=512, seed=5)
+    s["q"][:] = 0
+    s["q"][..., 0] = dim ** 0.5
+    s["k"][..., 0] = 0.4
+    s["v"][:] = 1
+    first = s["prefix"].long()
+    s["k"][first[0], 7, :, 0] = 17                   # 23.9 powers of two above the others
+    s["v"][first[0], 7] = 0
+    s["k"][first[100], 9, :, 0] = 17.9               # and one that comes later, 25.2
+    s["v"][first[100], 9] = 0
+    d = decoder(s)
+    got, lse = d.attend(**s, lse=True)
+    assert d.status() == 0
+    tail(got, lse, s)
