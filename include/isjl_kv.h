@@ -28,7 +28,8 @@
  * traps or aborts, errors are isjl_status codes.  What only the device can see is
  * reported by isjl_kv_status and skipped: tokens in a block whose number is outside
  * the cache read as 0, a request whose length is beyond its table's width is
- * inactive, a token with a slot or position out of range is padding.  A handle holds the workspace of its calls: they must not
+ * inactive, a token with a slot or position out of range is padding, a token that
+ * assign finds a block number outside the cache for gets slot -1.  A handle holds the workspace of its calls: they must not
  * overlap on the GPU, and a handle is not thread safe.  It belongs to the device that was current when it was created:
  * with another one current its calls are refused (INVALID_ARG), the report too; it can be destroyed.
  */

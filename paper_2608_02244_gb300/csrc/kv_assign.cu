@@ -109,6 +109,12 @@ __device__ __forceinline__ int32_t free_count(const AssignArgs &g) {
     return min(max(n, 0), g.n_blocks);
 }
 
+// a number that a table or the free list holds for a block, reported if there is no such block
+__device__ __forceinline__ int32_t seen(const AssignArgs &g, int32_t block) {
+    if ((uint32_t)block >= (uint32_t)g.n_blocks) report(g.status);
+    return block;
+}
+
 struct Entry {
     int64_t slot;
     int32_t position, row, visible;
@@ -121,9 +127,10 @@ __device__ __forceinline__ Entry entry_of(const AssignArgs &g, const Sums &h, in
     const int row = find(h.starts, lo, hi, t);
     const int32_t old = h.old[row], at = old + t - h.starts[row];
     const int32_t j = at >> g.shift, held = (int32_t)(((int64_t)old + mask) >> g.shift);
-    const int32_t block = j < held ? g.a.table[(int64_t)row * g.a.table_width + j]
-                                   : free_block(g, h, h.avail - 1 - (h.take[row] + j - held));
-    return {((int64_t)block << g.shift) + (at & mask), g.a.prefix_len + at, row, at + 1};
+    const int32_t block = seen(g, j < held ? g.a.table[(int64_t)row * g.a.table_width + j]
+                                           : free_block(g, h, h.avail - 1 - (h.take[row] + j - held)));
+    const int64_t slot = (uint32_t)block < (uint32_t)g.n_blocks ? ((int64_t)block << g.shift) + (at & mask) : -1;
+    return {slot, g.a.prefix_len + at, row, at + 1};
 }
 
 // the new table entries and the pushes, by `count` threads of which this is number `me`
@@ -133,11 +140,11 @@ __device__ __forceinline__ void move_blocks(const AssignArgs &g, const Sums &h, 
     for (int32_t k = me; k < h.takes; k += count) {
         const int i = find(h.take, 0, a.n_rows, k);
         const int32_t j = (int32_t)(((int64_t)h.old[i] + mask) >> g.shift) + k - h.take[i];
-        a.table[(int64_t)i * a.table_width + j] = free_block(g, h, h.avail - 1 - k);
+        a.table[(int64_t)i * a.table_width + j] = seen(g, free_block(g, h, h.avail - 1 - k));
     }
     for (int32_t k = me; k < h.backs; k += count) {
         const int i = find(h.back, 0, a.n_rows, k);
-        a.free_list[h.n_free + k] = a.table[(int64_t)i * a.table_width + (k - h.back[i])];
+        a.free_list[h.n_free + k] = seen(g, a.table[(int64_t)i * a.table_width + (k - h.back[i])]);
     }
 }
 
@@ -272,7 +279,7 @@ __global__ void __launch_bounds__(kFill) fill_kernel(const __grid_constant__ Ass
         Entry e[4];
         e[0] = entry_of(g, h, (int32_t)t, lo, hi);
         const int mask = (1 << g.shift) - 1;
-        const bool one_block = t + 3 < h.tokens && (e[0].slot & mask) + 3 <= mask && (e[0].row + 1 == n || t + 3 < h.starts[e[0].row + 1]);
+        const bool one_block = t + 3 < h.tokens && e[0].slot >= 0 && (e[0].slot & mask) + 3 <= mask && (e[0].row + 1 == n || t + 3 < h.starts[e[0].row + 1]);
 #pragma unroll
         for (int k = 1; k < 4; ++k) {
             if (one_block) e[k] = {e[0].slot + k, e[0].position + k, e[0].row, e[0].visible + k};

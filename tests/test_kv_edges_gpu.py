@@ -287,3 +287,31 @@ def test_many_small_weights_of_fp16_in_a_prefix(dim):
     got, lse = d.attend(**s, lse=True)
     assert d.status() == 0
     tail(got, lse, s)
+
+
+@pytest.mark.parametrize("rows,room", [(3, 16), (3, 5000), (1200, 1300)])
+@pytest.mark.parametrize("number", [-3, 40])
+@pytest.mark.parametrize("where", ["held", "free", "ends"])
+def test_blocks_outside_the_cache(rows, room, number, where):
+    """A block number outside the cache, in the place where a row's next token goes, on the free list or among those
+    given back, is reported; no token gets a slot in it."""
+    import torch
+    from paper_2608_02244_gb300 import kv
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    d = kv.Decoder(40, 8, 1, 1, 64, max_rows=rows)
+    lens, new = [0] * rows, [0] * rows
+    table = np.full((rows, 2), -1)
+    lens[0], lens[1], lens[2], new[0], new[1], new[2] = 3, 8, 5, 2, 1, -1 if where == "ends" else 1
+    table[0, 0], table[1, 0], table[2, 0] = 10, 11, 12
+    free = np.arange(40)
+    if where == "held":
+        table[0, 0] = number
+    elif where == "free":
+        free[6] = number
+    else:
+        table[2, 0], new[1] = number, 0
+    p = d.assign(i32(lens), i32(new), i32(table), i32(free), i32([7]), room)
+    assert d.status() == kv.ISJL_ERR_INVALID_ARG and d.status() == 0
+    want = {"held": [-1, -1, 6 * 8, 12 * 8 + 5], "free": [10 * 8 + 3, 10 * 8 + 4, -1, 12 * 8 + 5], "ends": [10 * 8 + 3, 10 * 8 + 4]}[where]
+    assert p.slots.tolist() == want + [-1] * (room - len(want))
+    assert p.granted.tolist()[:3] == [2, 0 if where == "ends" else 1, 0 if where == "ends" else 1]
