@@ -585,9 +585,7 @@ cudaError_t prepare_attend(int head_dim, int type, int *blocks, int *queries) {
          : head_dim == 128 ? prepare_of<128, __half>(blocks, queries) : prepare_of<256, __half>(blocks, queries);
 }
 
-cudaError_t launch_attend(const AttendArgs &args, void *encoder, int head_dim, int type, int grid, cudaStream_t st) {
-    AttendArgs g = args;
-    g.grid = grid;
+cudaError_t launch_attend(const AttendArgs &g, void *encoder, int head_dim, int type, int grid, cudaStream_t st) {
     CUtensorMap k, v;
     const int rows = min(1 << g.shift, kSlice);
     if (!encode_cache(encoder, &k, g.cache.k, g.cache.k_stride, rows, head_dim / 64, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||

@@ -131,13 +131,12 @@ struct AttendArgs {
     float2 *part_ml;              // [kAttendWarps * grid][2][16]
     CutItem *cut;                 // for the kernel that joins: the cut items at the warps in whose runs they begin
                                   // [kAttendWarps * grid], or with a prefix all items [n * key heads (parts of them)]
-    int32_t grid;
     int32_t *status;
 };
 size_t attend_smem(int head_dim, int n);
 // once for a shape, before its first launch: blocks that fit an SM, and the most queries of a call with which they do
 // (with more, one block less fits: each holds 4 bytes a query)
 cudaError_t prepare_attend(int head_dim, int type, int *blocks, int *queries);
-cudaError_t launch_attend(const AttendArgs &a, void *encoder, int head_dim, int type, int grid, cudaStream_t st);
+cudaError_t launch_attend(const AttendArgs &g, void *encoder, int head_dim, int type, int grid, cudaStream_t st);
 
 }  // namespace isjl

@@ -1,8 +1,9 @@
 """Python binding of the decode step over a paged KV cache (argument marshalling only).
 
-The functions with C names forward to the entry points of ``include/isjl_kv.h``;
-``Decoder`` checks tensors, allocates outputs and calls them.  All work runs in
-the library's CUDA kernels: there is no CPU fallback.
+``Decoder`` checks tensors, allocates outputs and calls the entry points of
+``include/isjl_kv.h``, whose structures it packs as bytes (the ctypes ones have the
+same layout, for callers of the library itself).  All work runs in the library's
+CUDA kernels: there is no CPU fallback.
 
     d = kv.Decoder(n_blocks, block_size, n_q_heads, n_kv_heads, head_dim, max_rows=B)
     plan = d.assign(lens, new_tokens, table, free, n_free, max_tokens)
@@ -110,7 +111,9 @@ class Decoder:
     has to be current (else IsjlError).  A call's inputs have to be ready for its stream, and
     its results are ready when that stream is done with it.  Caches are
     [n_blocks, block_size, n_kv_heads, head_dim] with any order of the first three axes
-    in memory."""
+    in memory.  Serving only: results carry no gradient, whatever the inputs require,
+    and torch's version counters do not see what is written to caches, tables and
+    lengths."""
 
     def __init__(self, n_blocks, block_size, n_q_heads, n_kv_heads, head_dim, dtype=None, max_rows=512):
         import torch
