@@ -62,7 +62,8 @@ isjl_status launched(cudaError_t e) {
 // saves n - 1 of n readings of the prefix and costs a launch and the joining of its pieces.  Measured, read against
 // apart (32 + 8 heads of 128 values, 256 own tokens): 8 queries over 512 tokens 13.4 and 12.1 us, 16 over 512 15.4 and
 // 15.2, 64 over 128 23 and 28, 8 over 2,048 17.2 and 15.0, 64 over 2,048 62 and 30; 4 over 8,192 24.2 and 24.7, 2 over
-// 32,768 39 and 38, 4 over 32,768 62 and 39; 64 over 32,768 689 and 73.
+// 32,768 39 and 38, 4 over 32,768 62 and 39; 64 over 32,768 689 and 73.  The rule goes by queries and tokens alone: of
+// these it loses 1.3 and 0.2 us with 8 and 16 over 512, and other head shapes, which save other bytes, were not measured.
 bool worth_apart(int n, int tokens) {
     return (int64_t)(n - 1) * tokens >= (n >= 8 ? 12288 : 32768);
 }
@@ -77,8 +78,10 @@ bool worth_apart(int n, int tokens) {
 //
 // Beside a long prefix own tokens get a few SMs, in small runs, and all of them once it is done: 512 requests over
 // 32,768 tokens 465 us with 40 SMs, 551 one after the other.  Steps of the prefix's line (256 rows by 128 tokens)
-// take 1.4 us, own tokens run at 60 GB/s an SM.  How long requests are only the device knows: they are taken as a
-// quarter of the table's width.
+// take 1.4 us with 128 values (taken for 64 too), own tokens run at 60 GB/s an SM.  How long requests are only the device
+// knows: they are taken as a quarter of the table's width.  With 512 requests of 256 tokens in the middle and 2,048 at most
+// over 32,768 that is right for a table of 2,048 tokens (490 us from a cold L2), and too much for one of 8,192 (822): the
+// prefix is taken for the shorter part.
 isjl::PrefixLine share_sms(const isjl_kv *kv, const isjl_kv_attend_args *a, int group, int n_kv_heads, int tokens, int *grid) {
     const int sms = kv->sms, per_sm = *grid / sms;
     const isjl::PrefixLine ln = isjl::prefix_line(a->n, group, n_kv_heads, tokens, sms);

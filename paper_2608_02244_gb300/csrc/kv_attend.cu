@@ -11,8 +11,10 @@
 // kernel joins in their order.  Joining them here, by the last of an item's warps to arrive, took a fence and an
 // atomic under full memory load: 10 to 20 us of stall against 3 us of a small kernel that starts as this one ends.
 //
-// 512 queries of 64 + 8 heads of 128 values, 4 GB of keys and values: 647 us, 6.3 TB/s; 256 queries, 670 MB: 123 us,
-// 5.4 TB/s (6 us until the rings are full, and SMs that end up to 15% apart).  The tensor pipe is 18% busy.
+// 512 queries of 64 + 8 heads of 128 values, 4 GB of keys and values: 627 us, 6.5 TB/s; 256 queries, 670 MB: 121 us,
+// 5.5 TB/s (6 us until the rings are full, and SMs that end up to 15% apart).  The tensor pipe is 18% busy.  64 queries
+// of 8 + 8 heads of 256 values, 2.1 GB: 354 us, 6.1 TB/s.  More than 16 query heads on a key head read it again for
+// each 16: 256 queries of 16 + 1 heads over 8,192 tokens 214 us, of 64 + 1 heads 706.
 #include "kv_ring.cuh"
 #include "kv_tma.cuh"
 
@@ -549,6 +551,10 @@ cudaError_t launch_of(const AttendArgs &g, const CUtensorMap &k, const CUtensorM
     if (e != cudaSuccess) return e;
     const int items = apart ? g.a.n * g.n_kv_heads * ((g.group + 15) / 16) : grid * kWarps;
     // Few pieces of many items: few registers, many blocks at once.  Many pieces of few items: their loads together.
+    // Whole calls from a cold L2 with 3 and with 12 at a time: window of 1,024 with 256 queries 140 and 143 us, 512 queries
+    // over a prefix of 32,768 482 and 496, 900 over 2,560 46 and 50; 1 query over 3,000 tokens 21.6 and 17.5, 17 over a
+    // prefix of 2,048 29.8 and 27.8, 40 over 16,384 54.4 and 52.4; equal with 32 over 8,192.  128 queries over 4,096
+    // (5 pieces) are 50 and 53: there the rule takes the slower one.
     const bool few = apart ? g.line.pieces < 4 : items < 4 * g.a.n * g.n_kv_heads;
     if (few) return launch_kernel(join_kernel<D, T, 3>, items, kJoinThreads, 0, st, true, g);
     return launch_kernel(join_kernel<D, T, 12>, items, kJoinThreads, 0, st, true, g);

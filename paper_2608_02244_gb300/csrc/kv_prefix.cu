@@ -15,10 +15,15 @@
 // leaves its piece of each item (sum, maximum and total of each row) for kv_attend.cu to join with the
 // requests' own tokens.
 //
-// 512 queries of 64 + 8 heads of 128 values over 32,768 tokens: 361 us, 1.52 PFLOP/s, on 128 SMs as on 152 (power);
-// the tensor cores are active in 77% of the cycles.  Steps of that took it there from 465: one thread's issue with
+// 512 queries of 64 + 8 heads of 128 values over 32,768 tokens: 361 us, 1.52 PFLOP/s, on 128 SMs and 421 on 112, 1.4 us
+// a step (two tiles of 128 rows by 128 tokens): at 1.93 GHz 2,700 cycles for 2,048 of products, with the tensor cores
+// active in 77% of the cycles.  There the step itself is the bound, a row group's way from scores to weights.  On all 152
+// SMs the whole call takes 389 us for the first 20 calls and 423 when called for seconds, at 1.64 GHz under the power
+// cap (1.36 kW).  Steps of that took it there from 465: one thread's issue with
 // uniform addresses (a product takes 64 cycles, its issue took 100), stages freed by the row groups instead of commits,
 // weights handed over in halves, waits for copies beside products under way.
+//
+// Heads of 256 values have no such kernel: two row tiles' scores and sums fill TMEM at 128.
 #include "kv_tma.cuh"
 
 namespace isjl {
