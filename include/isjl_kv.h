@@ -1,5 +1,5 @@
 /*
- * isjl_kv.h -- C ABI of a decode step over a paged KV cache.
+ * isjl_kv.h -- C ABI of a decode step over a paged KV cache, of its prompts, and of a cache in 4 bits.
  *
  * The simulator (isjl_sim.h) decides which requests run in a step, and charges
  * the step c + tau * |S| * max r.  This part of the library is that step on the
@@ -13,6 +13,17 @@
  *   isjl_kv_attend   attention of each query over its request's tokens: all of
  *                    them, or a sliding window and a few first tokens; with or
  *                    without a prefix that all requests share
+ *
+ * Prompts bring many tokens of a request at once:
+ *
+ *   isjl_kv_prompt   causal attention of the tokens that a step has just written,
+ *                    all rows' packed one after another
+ *
+ * A cache in 4 bits holds 3.2 times the tokens in the same memory:
+ *
+ *   isjl_kv_append4  as append, keys and values rounded to codes of 4 bits
+ *   isjl_kv_attend4  as attend, over what the codes stand for
+ *   isjl_kv_read4    16-bit values of given slots, for a cache that isjl_kv_prompt reads
  *
  * The cache.  Key and value caches hold n_blocks blocks of block_size tokens;
  * element [b][s][h][d] lies at b * stride[0] + s * stride[1] + h * stride[2] + d
@@ -156,6 +167,78 @@ typedef struct {
     const int32_t *prefix;       /* [n_prefix_blocks], NULL if there are none */
 } isjl_kv_attend_args;
 
+/* Queries of the rows' newest tokens.  Row i has lens[i] own tokens, after the
+ * n_prefix_blocks * block_size tokens of the prefix; its queries are q's tokens
+ * starts[i] .. starts[i + 1] - 1, of its last starts[i + 1] - starts[i] own tokens in
+ * order.  A query sees the tokens up to its own: the last `window` of those (all if
+ * window is 0) and the first `sinks`.  out and lse are isjl_kv_attend's formulas.
+ * starts, lens and table are as isjl_kv_assign leaves them (starts, lens_out), so
+ * that a step is assign, append and prompt.  What q, out and lse hold beyond
+ * starts[n_rows] is neither read nor written.
+ *
+ * Reported by isjl_kv_status: a row whose starts do not ascend in 0..n_tokens is
+ * skipped, its outputs are left as they were; a row with fewer own tokens than
+ * queries, or more than its table holds, sees nothing (out 0, lse -infinity); tokens
+ * of a block outside the cache read as 0. */
+typedef struct {
+    int32_t n_rows;              /* 0..max_rows, at most ISJL_KV_MAX_ROWS */
+    int32_t n_tokens;            /* most queries: tokens of q, out and lse; times n_q_heads < 2^31 */
+    int32_t table_width;         /* table_width * block_size + prefix <= 2^31 - 256 */
+    int32_t n_prefix_blocks;     /* >= 0 */
+    int32_t window;              /* >= 0 */
+    int32_t sinks;               /* >= 0, used with a window */
+    float scale;                 /* > 0, finite */
+    const void *q;               /* [n_tokens][n_q_heads][head_dim], 16-byte aligned */
+    int64_t q_stride[2];         /* elements between queries and between heads, multiples of 8 */
+    void *out;
+    int64_t out_stride[2];
+    float *lse;                  /* [n_tokens][n_q_heads] or NULL */
+    const int32_t *starts;       /* [n_rows + 1] */
+    const int32_t *lens;         /* [n_rows] */
+    const int32_t *table;        /* [n_rows][table_width] */
+    const int32_t *prefix;       /* [n_prefix_blocks], NULL if there are none */
+} isjl_kv_prompt_args;
+
+/* A cache in 4 bits.  A head's values are in groups of 32 neighbours.  A group has
+ * a scale S and an offset B, numbers of the handle's type T, and a value's code c
+ * (0..15) stands for T(B + (1 + c / 16) S), rounded once.  Codes: value j of a head
+ * lies in byte j / 2, in its low bits if j is even; element [b][s][h] of them
+ * (head_dim / 2 bytes) at b * stride[0] + s * stride[1] + h * stride[2] bytes, each a
+ * positive multiple of 16.  Scales: S and B of a head's groups one after another
+ * (head_dim / 16 numbers), the same with strides in numbers, multiples of
+ * min(8, head_dim / 16).  All four 16-byte aligned.
+ *
+ * A value x is written so: with lo and hi the least and largest of its group,
+ * S = T((hi - lo) * 16 / 15), B = T(lo - S) and c = 16 (x - B) / S - 16, rounded to the
+ * nearest (ties to even) and clamped to 0..15, or 0 where S is 0; x and the
+ * arithmetic have 32 bits.  What it stands for is within
+ *     S / 32 + u (2 |lo| + 4 S)
+ * of x (and T's smallest positive number), where u is T's unit roundoff (2^-8 for bf16,
+ * 2^-11 for fp16).  A group with an infinite or
+ * undefined value has S = B = NaN and stands for NaN; so does, in fp16, one whose S or
+ * B is beyond the type (never with values within +-20,000). */
+typedef struct {
+    void *k;
+    void *v;
+    void *k_scale;
+    void *v_scale;
+    int64_t k_stride[3];
+    int64_t v_stride[3];
+    int64_t k_scale_stride[3];
+    int64_t v_scale_stride[3];
+} isjl_kv_cache4;
+
+/* Values of slots: k_out and v_out of token i are what slot slots[i] holds, 0 for a
+ * negative one, and for one outside the cache (reported by isjl_kv_status). */
+typedef struct {
+    int32_t n_tokens;            /* >= 0 */
+    const int64_t *slots;        /* [n_tokens] */
+    void *k_out;                 /* [n_tokens][n_kv_heads][head_dim], 16-byte aligned */
+    int64_t k_stride[2];         /* elements between tokens and between heads, multiples of 8 */
+    void *v_out;
+    int64_t v_stride[2];
+} isjl_kv_read4_args;
+
 typedef struct isjl_kv isjl_kv;
 
 /* Create a handle for one cache and head shape on the current CUDA device, with
@@ -174,6 +257,13 @@ void isjl_kv_destroy(isjl_kv *kv);
 isjl_status isjl_kv_assign(isjl_kv *kv, const isjl_kv_assign_args *args, void *stream);
 isjl_status isjl_kv_append(isjl_kv *kv, const isjl_kv_append_args *args, const isjl_kv_cache *cache, void *stream);
 isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *args, const isjl_kv_cache *cache, void *stream);
+
+/* Attention of the rows' newest tokens, and a cache in 4 bits: the same errors.
+ * isjl_kv_append4 and isjl_kv_attend4 take append's and attend's arguments. */
+isjl_status isjl_kv_prompt(isjl_kv *kv, const isjl_kv_prompt_args *args, const isjl_kv_cache *cache, void *stream);
+isjl_status isjl_kv_append4(isjl_kv *kv, const isjl_kv_append_args *args, const isjl_kv_cache4 *cache, void *stream);
+isjl_status isjl_kv_attend4(isjl_kv *kv, const isjl_kv_attend_args *args, const isjl_kv_cache4 *cache, void *stream);
+isjl_status isjl_kv_read4(isjl_kv *kv, const isjl_kv_read4_args *args, const isjl_kv_cache4 *cache, void *stream);
 
 /* Wait for the device's work (calls may have been replayed from graphs on any
  * stream); INVALID_ARG if any call since the last report met an invalid value on

@@ -1,4 +1,4 @@
-// kv.cu -- the C ABI of the decode step (include/isjl_kv.h): handle, checks, launches.
+// kv.cu -- the C ABI of the decode step, prompts and the cache in 4 bits (include/isjl_kv.h): handle, checks, launches.
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -44,6 +44,20 @@ bool cache_ok(const isjl_kv_cache *c) {
     return true;
 }
 
+bool cache4_ok(const isjl_kv *kv, const isjl_kv_cache4 *c) {
+    if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_scale) ||
+        !aligned16(c->v_scale))
+        return false;
+    const int64_t numbers = kv->cfg.head_dim / 16 < 8 ? kv->cfg.head_dim / 16 : 8;
+    for (int i = 0; i < 3; ++i) {
+        for (const int64_t s : {c->k_stride[i], c->v_stride[i]})
+            if (s <= 0 || s % 16 != 0 || s >= (int64_t)1 << 40) return false;
+        for (const int64_t s : {c->k_scale_stride[i], c->v_scale_stride[i]})
+            if (s <= 0 || s % numbers != 0 || s >= (int64_t)1 << 39) return false;
+    }
+    return true;
+}
+
 // Streams and pointers do not say whose they are: stream 0 is that of the current device.
 bool device_ok(const isjl_kv *kv) {
     int current = -1;
@@ -56,6 +70,59 @@ isjl_status launched(cudaError_t e) {
     if (e == cudaSuccess) return ISJL_OK;
     cudaGetLastError();
     return ISJL_ERR_CUDA;
+}
+
+// what attend and attend4 ask of their arguments, but for the cache
+bool attend_ok(const isjl_kv *kv, const isjl_kv_attend_args *a) {
+    const int most = !kv ? 0 : kv->cfg.max_rows < ISJL_KV_MAX_ROWS ? kv->cfg.max_rows : ISJL_KV_MAX_ROWS;
+    if (!kv || !device_ok(kv) || !a || a->n < 0 || a->n > most || a->table_width < 1 || a->n_table_rows < 0 ||
+        a->n_prefix_blocks < 0 || (((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) > kMostTokens ||
+        // slices of 32 tokens are counted in 32 bits
+        a->n * ((((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) / 32 + 2) > INT32_MAX ||
+        (a->n_prefix_blocks > 0 && !a->prefix) || a->window < 0 || a->sinks < 0 || !(a->scale > 0.f) || !std::isfinite(a->scale))
+        return false;
+    if (a->n == 0) return true;
+    if (!a->q || !a->out || !a->lens || !a->table || !aligned16(a->q) || !aligned16(a->out) ||
+        (!a->rows && a->n > a->n_table_rows) || !natural(a->lse, a->lens, a->rows, a->table, a->prefix))
+        return false;
+    for (int i = 0; i < 2; ++i)
+        if (!stride_ok(a->q_stride[i]) || !stride_ok(a->out_stride[i])) return false;
+    return true;
+}
+
+// a window as long as any request can be hides nothing
+template <typename Args>
+void plain_window(const isjl_kv *kv, Args *a) {
+    if ((int64_t)a->window >= ((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) a->window = 0;
+    if (a->window == 0) a->sinks = 0;
+}
+
+// append and append4: one of the caches is null
+isjl_status append_to(isjl_kv *kv, const isjl_kv_append_args *a, const isjl_kv_cache *cache, const isjl_kv_cache4 *cache4,
+                      void *stream) {
+    if (!kv || !device_ok(kv) || !a || !(cache4 ? cache4_ok(kv, cache4) : cache_ok(cache)) || a->n_tokens < 0 || a->rot < 0 || a->rot > kv->cfg.head_dim || a->rot % 16 != 0 ||
+        (a->interleaved != 0 && a->interleaved != 1) || !(a->eps >= 0.f) || !std::isfinite(a->eps))
+        return ISJL_ERR_INVALID_ARG;
+    if (a->n_tokens == 0) return ISJL_OK;
+    const int64_t q_row = (int64_t)kv->cfg.n_q_heads * kv->cfg.head_dim;
+    const int64_t row = q_row + 2 * (int64_t)kv->cfg.n_kv_heads * kv->cfg.head_dim;
+    if (!a->qkv || !a->q_out || !a->slots || !aligned16(a->qkv) || !aligned16(a->q_out) || !aligned16(a->q_weight) ||
+        !aligned16(a->k_weight) || a->qkv_stride < row || a->qkv_stride % 8 != 0 || a->q_out_stride < q_row ||
+        a->q_out_stride % 8 != 0 || (a->rot > 0 && (!a->rope || !a->positions || a->n_positions < 1 || !aligned16(a->rope))) ||
+        (a->q_out == a->qkv && a->q_out_stride != a->qkv_stride) || !natural(a->positions, a->slots))
+        return ISJL_ERR_INVALID_ARG;
+    isjl::AppendArgs g;
+    std::memset(&g, 0, sizeof(g));
+    g.a = *a;
+    if (cache4) g.cache4 = *cache4;
+    else g.cache = *cache;
+    g.n_q_heads = kv->cfg.n_q_heads;
+    g.n_kv_heads = kv->cfg.n_kv_heads;
+    g.shift = kv->shift;
+    g.n_slots = (int64_t)kv->cfg.n_blocks << kv->shift;
+    g.status = kv->d_status;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return launched((cache4 ? isjl::launch_append4 : isjl::launch_append)(g, kv->cfg.head_dim, kv->cfg.type, kv->sms, st));
 }
 
 // Whether a prefix is done apart, by its own kernel, or read by each query's warps with its own tokens.  The former
@@ -236,50 +303,81 @@ isjl_status isjl_kv_assign(isjl_kv *kv, const isjl_kv_assign_args *a, void *stre
 }
 
 isjl_status isjl_kv_append(isjl_kv *kv, const isjl_kv_append_args *a, const isjl_kv_cache *cache, void *stream) {
-    if (!kv || !device_ok(kv) || !a || !cache_ok(cache) || a->n_tokens < 0 || a->rot < 0 || a->rot > kv->cfg.head_dim || a->rot % 16 != 0 ||
-        (a->interleaved != 0 && a->interleaved != 1) || !(a->eps >= 0.f) || !std::isfinite(a->eps))
-        return ISJL_ERR_INVALID_ARG;
+    return append_to(kv, a, cache, nullptr, stream);
+}
+
+isjl_status isjl_kv_append4(isjl_kv *kv, const isjl_kv_append_args *a, const isjl_kv_cache4 *cache, void *stream) {
+    if (!cache) return ISJL_ERR_INVALID_ARG;
+    return append_to(kv, a, nullptr, cache, stream);
+}
+
+isjl_status isjl_kv_read4(isjl_kv *kv, const isjl_kv_read4_args *a, const isjl_kv_cache4 *cache, void *stream) {
+    if (!kv || !device_ok(kv) || !a || !cache4_ok(kv, cache) || a->n_tokens < 0) return ISJL_ERR_INVALID_ARG;
     if (a->n_tokens == 0) return ISJL_OK;
-    const int64_t q_row = (int64_t)kv->cfg.n_q_heads * kv->cfg.head_dim;
-    const int64_t row = q_row + 2 * (int64_t)kv->cfg.n_kv_heads * kv->cfg.head_dim;
-    if (!a->qkv || !a->q_out || !a->slots || !aligned16(a->qkv) || !aligned16(a->q_out) || !aligned16(a->q_weight) ||
-        !aligned16(a->k_weight) || a->qkv_stride < row || a->qkv_stride % 8 != 0 || a->q_out_stride < q_row ||
-        a->q_out_stride % 8 != 0 || (a->rot > 0 && (!a->rope || !a->positions || a->n_positions < 1 || !aligned16(a->rope))) ||
-        (a->q_out == a->qkv && a->q_out_stride != a->qkv_stride) || !natural(a->positions, a->slots))
+    if (!a->slots || !a->k_out || !a->v_out || !aligned16(a->k_out) || !aligned16(a->v_out) || !natural(a->slots))
         return ISJL_ERR_INVALID_ARG;
-    isjl::AppendArgs g;
+    for (int i = 0; i < 2; ++i)
+        if (!stride_ok(a->k_stride[i]) || !stride_ok(a->v_stride[i])) return ISJL_ERR_INVALID_ARG;
+    isjl::Read4Args g;
     std::memset(&g, 0, sizeof(g));
     g.a = *a;
     g.cache = *cache;
-    g.n_q_heads = kv->cfg.n_q_heads;
     g.n_kv_heads = kv->cfg.n_kv_heads;
     g.shift = kv->shift;
     g.n_slots = (int64_t)kv->cfg.n_blocks << kv->shift;
     g.status = kv->d_status;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return launched(isjl::launch_append(g, kv->cfg.head_dim, kv->cfg.type, kv->sms, st));
+    return launched(isjl::launch_read4(g, kv->cfg.head_dim, kv->cfg.type, kv->sms, static_cast<cudaStream_t>(stream)));
 }
 
-isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl_kv_cache *cache, void *stream) {
-    const int most = !kv ? 0 : kv->cfg.max_rows < ISJL_KV_MAX_ROWS ? kv->cfg.max_rows : ISJL_KV_MAX_ROWS;
-    if (!kv || !device_ok(kv) || !a || !cache_ok(cache) || a->n < 0 || a->n > most || a->table_width < 1 || a->n_table_rows < 0 ||
-        a->n_prefix_blocks < 0 || (((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) > kMostTokens ||
-        // slices of 32 tokens are counted in 32 bits
-        a->n * ((((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) / 32 + 2) > INT32_MAX ||
-        (a->n_prefix_blocks > 0 && !a->prefix) || a->window < 0 || a->sinks < 0 || !(a->scale > 0.f) || !std::isfinite(a->scale))
-        return ISJL_ERR_INVALID_ARG;
+isjl_status isjl_kv_attend4(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl_kv_cache4 *cache, void *stream) {
+    if (!attend_ok(kv, a) || !cache4_ok(kv, cache)) return ISJL_ERR_INVALID_ARG;
     if (a->n == 0) return ISJL_OK;
-    if (!a->q || !a->out || !a->lens || !a->table || !aligned16(a->q) || !aligned16(a->out) ||
-        (!a->rows && a->n > a->n_table_rows) || !natural(a->lse, a->lens, a->rows, a->table, a->prefix))
+    isjl::Attend4Args g;
+    std::memset(&g, 0, sizeof(g));
+    g.a = *a;
+    plain_window(kv, &g.a);
+    g.cache = *cache;
+    g.n_blocks = kv->cfg.n_blocks;
+    g.shift = kv->shift;
+    g.n_kv_heads = kv->cfg.n_kv_heads;
+    g.group = kv->cfg.n_q_heads / kv->cfg.n_kv_heads;
+    g.status = kv->d_status;
+    return launched(isjl::launch_attend4(g, kv->cfg.head_dim, kv->cfg.type, static_cast<cudaStream_t>(stream)));
+}
+
+isjl_status isjl_kv_prompt(isjl_kv *kv, const isjl_kv_prompt_args *a, const isjl_kv_cache *cache, void *stream) {
+    const int most = !kv ? 0 : kv->cfg.max_rows < ISJL_KV_MAX_ROWS ? kv->cfg.max_rows : ISJL_KV_MAX_ROWS;
+    if (!kv || !device_ok(kv) || !a || !cache_ok(cache) || a->n_rows < 0 || a->n_rows > most || a->n_tokens < 0 ||
+        (int64_t)a->n_tokens * kv->cfg.n_q_heads > INT32_MAX || a->table_width < 1 || a->n_prefix_blocks < 0 ||
+        (((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) > kMostTokens || (a->n_prefix_blocks > 0 && !a->prefix) ||
+        a->window < 0 || a->sinks < 0 || !(a->scale > 0.f) || !std::isfinite(a->scale))
+        return ISJL_ERR_INVALID_ARG;
+    if (a->n_rows == 0 || a->n_tokens == 0) return ISJL_OK;
+    if (!a->q || !a->out || !a->starts || !a->lens || !a->table || !aligned16(a->q) || !aligned16(a->out) ||
+        !natural(a->lse, a->starts, a->lens, a->table, a->prefix))
         return ISJL_ERR_INVALID_ARG;
     for (int i = 0; i < 2; ++i)
         if (!stride_ok(a->q_stride[i]) || !stride_ok(a->out_stride[i])) return ISJL_ERR_INVALID_ARG;
+    isjl::PromptArgs g;
+    std::memset(&g, 0, sizeof(g));
+    g.a = *a;
+    plain_window(kv, &g.a);
+    g.cache = *cache;
+    g.n_blocks = kv->cfg.n_blocks;
+    g.shift = kv->shift;
+    g.n_kv_heads = kv->cfg.n_kv_heads;
+    g.group = kv->cfg.n_q_heads / kv->cfg.n_kv_heads;
+    g.status = kv->d_status;
+    return launched(isjl::launch_prompt(g, kv->cfg.head_dim, kv->cfg.type, static_cast<cudaStream_t>(stream)));
+}
+
+isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl_kv_cache *cache, void *stream) {
+    if (!attend_ok(kv, a) || !cache_ok(cache)) return ISJL_ERR_INVALID_ARG;
+    if (a->n == 0) return ISJL_OK;
     isjl::AttendArgs g;
     std::memset(&g, 0, sizeof(g));
     g.a = *a;
-    // a window as long as any request can be hides nothing
-    if ((int64_t)g.a.window >= ((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) g.a.window = 0;
-    if (g.a.window == 0) g.a.sinks = 0;
+    plain_window(kv, &g.a);
     g.cache = *cache;
     g.n_blocks = kv->cfg.n_blocks;
     g.shift = kv->shift;

@@ -1,10 +1,13 @@
-// kv_append.cu -- norms, position rotation and cache write of new tokens (isjl_kv_append).
+// kv_append.cu -- norms, position rotation and cache write of new tokens (isjl_kv_append, isjl_kv_append4).
 //
 // A head of D values is D / 8 threads of 8 values (16 bytes) each.  A thread keeps its place in the head and
 // goes over the token's heads, so that the angles and weights of that place are loaded once per token; the
 // sum of squares and the other half of a rotated pair come from the head's other threads by shuffles.  All
 // arithmetic is in 32 bits with one rounding at the end.  Bound by memory: 4 bytes a value (49,152 tokens of
 // 32 + 2 x 8 heads of 128 values 202 us, 6.1 TB/s).
+//
+// A cache in 4 bits: a group of 32 values is four neighbouring threads, whose least and largest value come by two
+// shuffles; each thread makes a word of its eight codes, the first of the four writes scale and offset.
 #include "kv_internal.cuh"
 
 namespace isjl {
@@ -23,7 +26,39 @@ __device__ __forceinline__ void unpack8(const uint4 &w, float (&x)[8]) {
     }
 }
 
-template <int D, typename T, int kThreads>
+// The codes of this thread's 8 values of a group, and the group's scale and offset, in T.  The divisions are exact, as
+// their definition has them: 16-bit values lie on borders between codes often.
+template <typename T>
+__device__ __forceinline__ uint32_t codes4(const float (&x)[8], uint32_t *scales) {
+    float lo = x[0], hi = x[0];
+    bool fine = true;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        lo = fminf(lo, x[i]);
+        hi = fmaxf(hi, x[i]);
+        fine = fine && fabsf(x[i]) < INFINITY;
+    }
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) {
+        lo = fminf(lo, __shfl_xor_sync(~0u, lo, d));
+        hi = fmaxf(hi, __shfl_xor_sync(~0u, hi, d));
+        fine = __shfl_xor_sync(~0u, (int)fine, d) && fine;
+    }
+    const float s = Half<T>::unpack(Half<T>::pack((hi - lo) * (16.f / 15.f), 0.f)).x;
+    const float b = Half<T>::unpack(Half<T>::pack(lo - s, 0.f)).x;
+    fine = fine && s < INFINITY && b > -INFINITY;
+    *scales = fine ? Half<T>::pack(s, b) : Half<T>::pack(NAN, NAN);
+    uint32_t word = 0;
+    if (fine && s > 0.f)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float c = rintf(__fdiv_rn(x[i] - b, s) * 16.f - 16.f);
+            word |= (uint32_t)fminf(fmaxf(c, 0.f), 15.f) << (4 * i);
+        }
+    return word;
+}
+
+template <int D, typename T, int kThreads, bool kFour>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendArgs g) {
     constexpr int kLanes = D / 8, kHeads = kThreads / kLanes;   // threads of a head, heads at a time
     const isjl_kv_append_args &a = g.a;
@@ -55,6 +90,16 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
         return;
     }
     const int64_t block = slot >> g.shift, place = slot & ((1 << g.shift) - 1);
+    // the token's part of each array: [2] keys and values
+    unsigned char *codes[2];
+    T *scales[2];
+    if (kFour)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t *cs = i ? g.cache4.v_stride : g.cache4.k_stride, *ss = i ? g.cache4.v_scale_stride : g.cache4.k_scale_stride;
+            codes[i] = static_cast<unsigned char *>(i ? g.cache4.v : g.cache4.k) + block * cs[0] + place * cs[1] + 4 * c;
+            scales[i] = static_cast<T *>(i ? g.cache4.v_scale : g.cache4.k_scale) + block * ss[0] + place * ss[1] + c / 4 * 2;
+        }
     T *k_out = static_cast<T *>(g.cache.k) + block * g.cache.k_stride[0] + place * g.cache.k_stride[1];
     T *v_out = static_cast<T *>(g.cache.v) + block * g.cache.v_stride[0] + place * g.cache.v_stride[1];
 
@@ -120,7 +165,23 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
                     const float other = __shfl_sync(~0u, x[i], from);
                     y[i] = turns ? x[i] * cosv[i] + (a.interleaved ? x[i ^ 1] : other) * sinv[i] : x[i];
                 }
+                if (kFour && is_v) unpack8<T>(raw[u], x);
+                else if (kFour)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = y[i];
                 if (!is_v) w = make_uint4(Half<T>::pack(y[0], y[1]), Half<T>::pack(y[2], y[3]), Half<T>::pack(y[4], y[5]), Half<T>::pack(y[6], y[7]));
+            }
+            if (kFour && h0 + (u + 1) * kHeads > hq) {      // some of the warps' heads are k or v heads
+                uint32_t pair;
+                __syncwarp();
+                const uint32_t word = codes4<T>(x, &pair);
+                if (h >= hq && h < heads) {
+                    const int head = is_v ? h - hq - hkv : h - hq;
+                    *reinterpret_cast<uint32_t *>(codes[is_v] + head * (is_v ? g.cache4.v_stride : g.cache4.k_stride)[2]) = word;
+                    if (c % 4 == 0)
+                        *reinterpret_cast<uint32_t *>(scales[is_v] + head * (is_v ? g.cache4.v_scale_stride : g.cache4.k_scale_stride)[2]) = pair;
+                }
+                if (h >= hq) continue;
             }
             if (h >= heads) continue;
             T *to = is_v ? v_out + (h - hq - hkv) * g.cache.v_stride[2]
@@ -137,23 +198,32 @@ int many_tokens(int sms) { return 24 * sms; }
 
 // A token is a block.  Few tokens: four warps each, which halve its latency.  Many: a warp each, for more of them under
 // way on an SM without waiting for one another's longest.
-template <int D, typename T>
+template <int D, typename T, bool kFour>
 cudaError_t launch_of(const AppendArgs &g, int sms, cudaStream_t st) {
-    if (g.a.n_tokens >= many_tokens(sms)) append_kernel<D, T, 32><<<g.a.n_tokens, 32, 0, st>>>(g);
-    else append_kernel<D, T, 128><<<g.a.n_tokens, 128, 0, st>>>(g);
+    if (g.a.n_tokens >= many_tokens(sms)) append_kernel<D, T, 32, kFour><<<g.a.n_tokens, 32, 0, st>>>(g);
+    else append_kernel<D, T, 128, kFour><<<g.a.n_tokens, 128, 0, st>>>(g);
     return cudaGetLastError();
 }
 
-template <int D>
+template <int D, bool kFour>
 cudaError_t launch_dim(const AppendArgs &g, int type, int sms, cudaStream_t st) {
-    return type == ISJL_KV_BF16 ? launch_of<D, __nv_bfloat16>(g, sms, st) : launch_of<D, __half>(g, sms, st);
+    return type == ISJL_KV_BF16 ? launch_of<D, __nv_bfloat16, kFour>(g, sms, st) : launch_of<D, __half, kFour>(g, sms, st);
+}
+
+template <bool kFour>
+cudaError_t launch_any(const AppendArgs &g, int head_dim, int type, int sms, cudaStream_t st) {
+    return head_dim == 64 ? launch_dim<64, kFour>(g, type, sms, st)
+         : head_dim == 128 ? launch_dim<128, kFour>(g, type, sms, st) : launch_dim<256, kFour>(g, type, sms, st);
 }
 
 }  // namespace
 
 cudaError_t launch_append(const AppendArgs &g, int head_dim, int type, int sms, cudaStream_t st) {
-    return head_dim == 64 ? launch_dim<64>(g, type, sms, st)
-         : head_dim == 128 ? launch_dim<128>(g, type, sms, st) : launch_dim<256>(g, type, sms, st);
+    return launch_any<false>(g, head_dim, type, sms, st);
+}
+
+cudaError_t launch_append4(const AppendArgs &g, int head_dim, int type, int sms, cudaStream_t st) {
+    return launch_any<true>(g, head_dim, type, sms, st);
 }
 
 }  // namespace isjl

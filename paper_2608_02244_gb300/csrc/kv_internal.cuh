@@ -78,11 +78,24 @@ cudaError_t launch_assign(const AssignArgs &a, int sms, cudaStream_t st);
 struct AppendArgs {
     isjl_kv_append_args a;
     isjl_kv_cache cache;
+    isjl_kv_cache4 cache4;        // launch_append4: the cache
     int32_t n_q_heads, n_kv_heads, shift;
     int64_t n_slots;
     int32_t *status;
 };
 cudaError_t launch_append(const AppendArgs &a, int head_dim, int type, int sms, cudaStream_t st);
+cudaError_t launch_append4(const AppendArgs &a, int head_dim, int type, int sms, cudaStream_t st);
+
+// ---- read4 (kv_read4.cu)
+constexpr int kGroup4 = 32;       // values of a group of a cache in 4 bits
+struct Read4Args {
+    isjl_kv_read4_args a;
+    isjl_kv_cache4 cache;
+    int32_t n_kv_heads, shift;
+    int64_t n_slots;
+    int32_t *status;
+};
+cudaError_t launch_read4(const Read4Args &a, int head_dim, int type, int sms, cudaStream_t st);
 
 // ---- a shared prefix computed once for the batch (kv_prefix.cu)
 
@@ -133,6 +146,22 @@ struct AttendArgs {
                                   // [kAttendWarps * grid], or with a prefix all items [n * key heads (parts of them)]
     int32_t *status;
 };
+// ---- prompt and attend4, one warp's dot products (kv_simple.cu)
+struct PromptArgs {
+    isjl_kv_prompt_args a;
+    isjl_kv_cache cache;
+    int32_t n_blocks, shift, n_kv_heads, group;
+    int32_t *status;
+};
+struct Attend4Args {
+    isjl_kv_attend_args a;
+    isjl_kv_cache4 cache;
+    int32_t n_blocks, shift, n_kv_heads, group;
+    int32_t *status;
+};
+cudaError_t launch_prompt(const PromptArgs &g, int head_dim, int type, cudaStream_t st);
+cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, cudaStream_t st);
+
 size_t attend_smem(int head_dim, int n);
 // once for a shape, before its first launch: blocks that fit an SM, and the most queries of a call with which they do
 // (with more, one block less fits: each holds 4 bytes a query)

@@ -1,4 +1,5 @@
-"""Python binding of the decode step over a paged KV cache (argument marshalling only).
+"""Python binding of the decode step over a paged KV cache, of prompts and of a cache in 4 bits (argument
+marshalling only).
 
 ``Decoder`` checks tensors, allocates outputs and calls the entry points of
 ``include/isjl_kv.h``, whose structures it packs as bytes (the ctypes ones have the
@@ -9,6 +10,16 @@ CUDA kernels: there is no CPU fallback.
     plan = d.assign(lens, new_tokens, table, free, n_free, max_tokens)
     q = d.append(qkv, plan.positions, plan.slots, k_cache, v_cache, rope, q_weight, k_weight)
     out = d.attend(q, k_cache, v_cache, table, plan.visible, rows=plan.rows, window=4096, sinks=4)
+
+Prompts, whose tokens `assign` and `append` take all at once:
+
+    out = d.prompt(q, k_cache, v_cache, table, plan.starts, plan.lens)
+
+A cache in 4 bits, in append's and attend's place:
+
+    cache = d.cache4()
+    q = d.append4(qkv, plan.positions, plan.slots, cache, rope, q_weight, k_weight)
+    out = d.attend4(q, cache, table, plan.visible, rows=plan.rows)
 """
 from __future__ import annotations
 
@@ -22,7 +33,8 @@ from .sim import ISJL_ERR_INVALID_ARG, ISJL_OK, IsjlError
 BF16, FP16 = 0, 1
 MAX_ROWS = 4096
 EXPORTS = ["isjl_kv_create", "isjl_kv_destroy", "isjl_kv_assign", "isjl_kv_append", "isjl_kv_attend",
-           "isjl_kv_status"]
+           "isjl_kv_status", "isjl_kv_prompt", "isjl_kv_append4", "isjl_kv_attend4", "isjl_kv_read4"]
+GROUP4 = 32      # values of a group of a cache in 4 bits
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
@@ -53,11 +65,30 @@ class isjl_kv_attend_args(ctypes.Structure):
         ("lens", _vp), ("rows", _vp), ("table", _vp), ("prefix", _vp)]
 
 
+class isjl_kv_prompt_args(ctypes.Structure):
+    _fields_ = [(f, _i32) for f in ("n_rows", "n_tokens", "table_width", "n_prefix_blocks", "window", "sinks")] + [
+        ("scale", _f32), ("q", _vp), ("q_stride", _i64 * 2), ("out", _vp), ("out_stride", _i64 * 2), ("lse", _vp),
+        ("starts", _vp), ("lens", _vp), ("table", _vp), ("prefix", _vp)]
+
+
+class isjl_kv_cache4(ctypes.Structure):
+    _fields_ = [(f, _vp) for f in ("k", "v", "k_scale", "v_scale")] + [
+        (f, _i64 * 3) for f in ("k_stride", "v_stride", "k_scale_stride", "v_scale_stride")]
+
+
+class isjl_kv_read4_args(ctypes.Structure):
+    _fields_ = [("n_tokens", _i32), ("slots", _vp), ("k_out", _vp), ("k_stride", _i64 * 2), ("v_out", _vp),
+                ("v_stride", _i64 * 2)]
+
+
 # The same layouts as bytes: filling a structure field by field costs a call 3 us of host time, packing 0.3
 _CACHE = struct.Struct("=2Q6q")
 _ASSIGN = struct.Struct("=4i13Q")
 _APPEND = struct.Struct("=4if4xQqQq5Q")
 _ATTEND = struct.Struct("=6if4xQ2qQ2q5Q")
+_PROMPT = struct.Struct("=6if4xQ2qQ2q5Q")
+_CACHE4 = struct.Struct("=4Q12q")
+_READ4 = struct.Struct("=i4x2Q2qQ2q")
 
 _lib = None
 
@@ -73,8 +104,12 @@ def lib():
         L.isjl_kv_assign.argtypes = [_vp, _vp, _vp]            # structures by address, or their bytes
         L.isjl_kv_append.argtypes = [_vp, _vp, _vp, _vp]
         L.isjl_kv_attend.argtypes = [_vp, _vp, _vp, _vp]
+        L.isjl_kv_prompt.argtypes = [_vp, _vp, _vp, _vp]
+        L.isjl_kv_append4.argtypes = [_vp, _vp, _vp, _vp]
+        L.isjl_kv_attend4.argtypes = [_vp, _vp, _vp, _vp]
+        L.isjl_kv_read4.argtypes = [_vp, _vp, _vp, _vp]
         L.isjl_kv_status.argtypes = [_vp]
-        for f in ("create", "assign", "append", "attend", "status"):
+        for f in ("create", "assign", "append", "attend", "prompt", "append4", "attend4", "read4", "status"):
             getattr(L, "isjl_kv_" + f).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -102,6 +137,10 @@ def isjl_kv_destroy(handle):
 # entry of each row in them and their total (starts), tokens granted to each row,
 # lengths and free blocks after the step.
 Plan = collections.namedtuple("Plan", "slots positions rows visible starts granted lens n_free")
+
+# A cache in 4 bits: codes of keys and values, uint8 [n_blocks, block_size, n_kv_heads, head_dim / 2], and the scales and
+# offsets of their groups, [n_blocks, block_size, n_kv_heads, head_dim / 32, 2] of the decoder's type.
+Cache4 = collections.namedtuple("Cache4", "k v k_scale v_scale")
 
 
 class Decoder:
@@ -133,6 +172,8 @@ class Decoder:
         self._raw_stream = torch._C._cuda_getCurrentRawStream      # 0.1 us; torch.cuda.current_stream 1.9
         self._cache_shape = (self.n_blocks, self.block_size, self.n_kv_heads, self.head_dim)
         self._qkv = (self.n_q_heads + 2 * self.n_kv_heads) * self.head_dim
+        self._codes_shape = self._cache_shape[:3] + (self.head_dim // 2,)
+        self._scales_shape = self._cache_shape[:3] + (self.head_dim // GROUP4, 2)
 
     def close(self):
         if self.handle:
@@ -164,6 +205,23 @@ class Decoder:
             # the stride of an axis of one element says nothing: any valid one
             ks, vs = ([x if n > 1 else 8 for x, n in zip(y, shape)] for y in (ks, vs))
         return _CACHE.pack(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2])
+
+    def _cache4(self, cache):
+        if len(cache) != 4:
+            self._bad("a cache in 4 bits is codes of keys and of values, scales of keys and of values")
+        codes, scales, index, steps = self._codes_shape, self._scales_shape, self._index, []
+        for t, shape, dtype, inner in ((cache[0], codes, self.torch.uint8, (1,)), (cache[1], codes, self.torch.uint8, (1,)),
+                                       (cache[2], scales, self.dtype, (2, 1)), (cache[3], scales, self.dtype, (2, 1))):
+            st = t.stride()
+            # the stride of an axis of one element says nothing
+            if t.shape != shape or t.dtype is not dtype or t.get_device() != index or st[-1] != 1 or \
+                    (len(inner) == 2 and st[3] != 2 and shape[3] > 1):
+                self._bad(f"a cache in 4 bits has codes of torch.uint8 {codes} and scales of {self.dtype} {scales} on "
+                          f"{self.device}, a head's next to one another")
+            if shape[0] == 1 or shape[2] == 1:
+                st = [x if n > 1 else 16 for x, n in zip(st, shape)]
+            steps += st[:3]
+        return _CACHE4.pack(*(t.data_ptr() for t in cache), *steps)
 
     def _empty(self, stream, shape, dtype):
         """Memory for a result.  The allocator hands out what is free in the order of one stream's
@@ -228,12 +286,21 @@ class Decoder:
         """Norms, rotation and cache write of new tokens: see isjl_kv_append.  qkv is
         [tokens, (n_q_heads + 2 n_kv_heads) * head_dim]; returns the queries,
         [tokens, n_q_heads, head_dim].  rope None: no rotation; `pairs`: neighbours."""
+        return self._append(self._lib.isjl_kv_append, "isjl_kv_append", (k, v), self._cache(k, v), qkv, positions, slots, rope,
+                            q_weight, k_weight, eps, pairs, out, stream)
+
+    def append4(self, qkv, positions, slots, cache, rope=None, q_weight=None, k_weight=None, eps=1e-6, pairs=False,
+                out=None, stream=None):
+        """append with a cache in 4 bits (`cache4`): see isjl_kv_append4."""
+        return self._append(self._lib.isjl_kv_append4, "isjl_kv_append4", cache, self._cache4(cache), qkv, positions, slots,
+                            rope, q_weight, k_weight, eps, pairs, out, stream)
+
+    def _append(self, call, name, tensors, cache, qkv, positions, slots, rope, q_weight, k_weight, eps, pairs, out, stream):
         torch = self.torch
         hq, d, dtype, index = self.n_q_heads, self.head_dim, self.dtype, self._index
         n = qkv.shape[0]
         if qkv.shape != (n, self._qkv) or qkv.dtype is not dtype or qkv.get_device() != index or (n > 0 and qkv.stride(1) != 1):
             self._bad(f"qkv must be {dtype} [tokens, {self._qkv}] with stride 1 last")
-        cache = self._cache(k, v)
         if out is None:
             out = self._empty(stream, (n, hq, d), dtype)
         elif out.shape != (n, hq, d) or out.dtype is not dtype or out.get_device() != index or \
@@ -251,8 +318,8 @@ class Decoder:
         step, out_step = (qkv.stride(0), out.stride(0)) if n > 1 else (self._qkv, self._qkv if x == y else hq * d)
         args = _APPEND.pack(n, n_positions, rot, bool(pairs), eps, x, step, y, out_step, *weights, angles, places,
                             self._ints("slots", slots, (n,), torch.int64))
-        st = self._stream(stream, (qkv, out, k, v, rope, positions, slots, q_weight, k_weight))
-        _check(self._lib.isjl_kv_append(self.handle, args, cache, st), "isjl_kv_append")
+        st = self._stream(stream, (qkv, out, *tensors, rope, positions, slots, q_weight, k_weight))
+        _check(call(self.handle, args, cache, st), name)
         return out
 
     def attend(self, q, k, v, table, lens, rows=None, prefix=None, window=0, sinks=0, scale=None, out=None, lse=False,
@@ -260,37 +327,104 @@ class Decoder:
         """Attention of single queries [n, n_q_heads, head_dim] over their requests'
         tokens: see isjl_kv_attend.  scale defaults to head_dim ** -0.5.  With `lse`
         returns (out, lse)."""
-        torch = self.torch
+        return self._attend(self._lib.isjl_kv_attend, "isjl_kv_attend", (k, v), self._cache(k, v), q, table, lens, rows, prefix,
+                            window, sinks, scale, out, lse, stream)
+
+    def attend4(self, q, cache, table, lens, rows=None, prefix=None, window=0, sinks=0, scale=None, out=None, lse=False,
+                stream=None):
+        """attend over a cache in 4 bits (`cache4`): see isjl_kv_attend4."""
+        return self._attend(self._lib.isjl_kv_attend4, "isjl_kv_attend4", cache, self._cache4(cache), q, table, lens, rows,
+                            prefix, window, sinks, scale, out, lse, stream)
+
+    def _queries(self, q, out, stream, most):
+        """Checks of queries and results; the results and both's strides, any valid one for an axis of one element
+        (it says nothing)."""
         hq, d, dtype, index = self.n_q_heads, self.head_dim, self.dtype, self._index
         n = q.shape[0]
         shape = (n, hq, d)
-        if q.shape != shape or q.dtype is not dtype or q.get_device() != index or q.stride(2) != 1 or n > self.max_rows:
-            self._bad(f"q must be {dtype} [at most {self.max_rows}, {hq}, {d}] with stride 1 last")
-        cache = self._cache(k, v)
+        if q.shape != shape or q.dtype is not dtype or q.get_device() != index or q.stride(2) != 1 or n > most:
+            self._bad(f"q must be {dtype} [at most {most}, {hq}, {d}] with stride 1 last")
         if out is None:
             out = self._empty(stream, shape, dtype)
         elif out.shape != shape or out.dtype is not dtype or out.get_device() != index or out.stride(2) != 1:
             self._bad("out must have q's shape and type with stride 1 last")
+        qs, os = q.stride(), out.stride()
+        if n <= 1 or hq == 1:
+            qs, os = ([x if m > 1 else 8 for x, m in zip(y, shape)] for y in (qs, os))
+        return out, qs, os
+
+    def _sight(self, table, window, sinks):
         if table.dim() != 2:
             self._bad("table must be [rows, width]")
         window, sinks = int(window), int(sinks)
         if not (0 <= window < 2**31 and 0 <= sinks < 2**31):
             self._bad("window and sinks must be in 0..2^31 - 1")
-        weights = self._empty(stream, (n, hq), torch.float32) if lse else None
-        # the stride of an axis of one element says nothing: any valid one
-        qs, os = q.stride(), out.stride()
-        if n <= 1 or hq == 1:
-            qs, os = ([x if m > 1 else 8 for x, m in zip(y, shape)] for y in (qs, os))
-        i32 = torch.int32
+        return window, sinks
+
+    def _attend(self, call, name, tensors, cache, q, table, lens, rows, prefix, window, sinks, scale, out, lse, stream):
+        n, i32 = q.shape[0], self.torch.int32
+        out, qs, os = self._queries(q, out, stream, self.max_rows)
+        window, sinks = self._sight(table, window, sinks)
+        weights = self._empty(stream, (n, self.n_q_heads), self.torch.float32) if lse else None
         args = _ATTEND.pack(n, table.shape[0], table.shape[1], 0 if prefix is None else prefix.numel(), window, sinks,
-                            d ** -0.5 if scale is None else scale, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1],
-                            weights.data_ptr() if lse else 0, self._ints("lens", lens, (n,), i32),
+                            self.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), qs[0], qs[1], out.data_ptr(),
+                            os[0], os[1], weights.data_ptr() if lse else 0, self._ints("lens", lens, (n,), i32),
                             0 if rows is None else self._ints("rows", rows, (n,), i32),
                             self._ints("table", table, table.shape, i32),
                             0 if prefix is None else self._ints("prefix", prefix, (prefix.numel(),), i32))
-        st = self._stream(stream, (q, k, v, table, lens, rows, prefix, out, weights))
-        _check(self._lib.isjl_kv_attend(self.handle, args, cache, st), "isjl_kv_attend")
+        st = self._stream(stream, (q, *tensors, table, lens, rows, prefix, out, weights))
+        _check(call(self.handle, args, cache, st), name)
         return (out, weights) if lse else out
+
+    def prompt(self, q, k, v, table, starts, lens, prefix=None, window=0, sinks=0, scale=None, out=None, lse=False,
+               stream=None):
+        """Causal attention of the rows' newest tokens, packed: see isjl_kv_prompt.  q is [tokens, n_q_heads,
+        head_dim], row i's queries at starts[i]..starts[i + 1] - 1, the last of its lens[i] own tokens.  scale
+        defaults to head_dim ** -0.5.  With `lse` returns (out, lse).  Of tokens beyond starts[-1] a given `out`
+        keeps what it holds; in new results they are not defined."""
+        torch, i32, n = self.torch, self.torch.int32, lens.shape[0]
+        cache = self._cache(k, v)
+        out, qs, os = self._queries(q, out, stream, (2**31 - 1) // self.n_q_heads)
+        window, sinks = self._sight(table, window, sinks)
+        if n > self.max_rows or table.shape[0] != n:
+            self._bad("prompt needs at most max_rows lengths and a table row for each")
+        weights = self._empty(stream, (q.shape[0], self.n_q_heads), torch.float32) if lse else None
+        args = _PROMPT.pack(n, q.shape[0], table.shape[1], 0 if prefix is None else prefix.numel(), window, sinks,
+                            self.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), qs[0], qs[1], out.data_ptr(),
+                            os[0], os[1], weights.data_ptr() if lse else 0, self._ints("starts", starts, (n + 1,), i32),
+                            self._ints("lens", lens, (n,), i32), self._ints("table", table, table.shape, i32),
+                            0 if prefix is None else self._ints("prefix", prefix, (prefix.numel(),), i32))
+        st = self._stream(stream, (q, k, v, table, starts, lens, prefix, out, weights))
+        _check(self._lib.isjl_kv_prompt(self.handle, args, cache, st), "isjl_kv_prompt")
+        return (out, weights) if lse else out
+
+    # ---- a cache in 4 bits ---------------------------------------------------
+    def cache4(self):
+        """A new cache in 4 bits whose tokens stand for zeros, each block's heads outermost in memory: a head's
+        codes and scales of a block then lie next to one another, which is the fastest order to read."""
+        n, bs, heads, _ = self._cache_shape
+
+        def zeros(dtype, *inner):
+            return self.torch.zeros((n, heads, bs) + inner, dtype=dtype, device=self.device).transpose(1, 2)
+
+        codes, scales = (self.torch.uint8, self.head_dim // 2), (self.dtype, self.head_dim // GROUP4, 2)
+        return Cache4(zeros(*codes), zeros(*codes), zeros(*scales), zeros(*scales))
+
+    def read4(self, slots, cache, k=None, v=None, stream=None):
+        """Keys and values of slots in 16 bits, [tokens, n_kv_heads, head_dim] each: see isjl_kv_read4.  `k` and `v`
+        take them if given: any strides but 1 last, such as a cache's own slots."""
+        n = slots.shape[0]
+        shape, args = (n, self.n_kv_heads, self.head_dim), [n, self._ints("slots", slots, (n,), self.torch.int64)]
+        packed, given = self._cache4(cache), (k, v)
+        k, v = (self._empty(stream, shape, self.dtype) if t is None else t for t in given)
+        for t in (k, v):
+            if t.shape != shape or t.dtype is not self.dtype or t.get_device() != self._index or t.stride(2) != 1:
+                self._bad(f"k and v must be {self.dtype} {shape} on {self.device} with stride 1 last")
+            # the stride of an axis of one element says nothing: any valid one
+            args += [t.data_ptr()] + [x if m > 1 else 8 for x, m in zip(t.stride()[:2], shape)]
+        st = self._stream(stream, (slots, *cache, k, v))
+        _check(self._lib.isjl_kv_read4(self.handle, _READ4.pack(*args), packed, st), "isjl_kv_read4")
+        return k, v
 
     def status(self):
         """Wait for the device; the status code of all calls since the last report."""
