@@ -1,4 +1,5 @@
 // kv.cu -- the C ABI of the decode step, prompts and the cache in 4 bits (include/isjl_kv.h): handle, checks, launches.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -228,12 +229,15 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
     const int group = cfg->n_q_heads / cfg->n_kv_heads;
     const size_t items = (size_t)queries * cfg->n_kv_heads * ((group + 15) / 16);
     const size_t cuts = rounded(sizeof(isjl::CutItem) * (items > warps ? items : warps));
-    const size_t ml = rounded(sizeof(float2) * 32 * warps), o = sizeof(float) * 32 * cfg->head_dim * warps;
+    // pieces of attend's cut items, 32 rows a warp, or of prompt's, two items a block
+    const size_t cut_rows = std::max((size_t)32 * warps, (size_t)2 * isjl::kPromptRows * kv->sms);
+    const size_t ml = rounded(sizeof(float2) * cut_rows), o = sizeof(float) * cfg->head_dim * cut_rows;
     // pieces of the prefix part: an item of 256 rows lies in at most sms / items + 2 blocks; and the own tokens' part
     const size_t pieces = shares ? (size_t)kv->sms * 256 + 3 * (size_t)queries * cfg->n_q_heads : 0;
     const size_t prefix_ml = rounded(sizeof(float2) * pieces), prefix_o = sizeof(float) * cfg->head_dim * pieces;
     if (!(kv->encoder = isjl::tensor_map_encoder()) ||
-        (shares && isjl::prepare_prefix(cfg->head_dim, cfg->type) != cudaSuccess)) {
+        (shares && isjl::prepare_prefix(cfg->head_dim, cfg->type) != cudaSuccess) ||
+        isjl::prepare_prompt(cfg->head_dim, cfg->type) != cudaSuccess) {
         cudaGetLastError();
         delete kv;
         return ISJL_ERR_CUDA;
@@ -367,8 +371,11 @@ isjl_status isjl_kv_prompt(isjl_kv *kv, const isjl_kv_prompt_args *a, const isjl
     g.shift = kv->shift;
     g.n_kv_heads = kv->cfg.n_kv_heads;
     g.group = kv->cfg.n_q_heads / kv->cfg.n_kv_heads;
+    g.part_o = kv->d_part_o;
+    g.part_ml = kv->d_part_ml;
+    g.cut = reinterpret_cast<isjl::PromptCut *>(kv->d_cut);
     g.status = kv->d_status;
-    return launched(isjl::launch_prompt(g, kv->cfg.head_dim, kv->cfg.type, static_cast<cudaStream_t>(stream)));
+    return launched(isjl::launch_prompt(g, kv->encoder, kv->cfg.head_dim, kv->cfg.type, kv->sms, static_cast<cudaStream_t>(stream)));
 }
 
 isjl_status isjl_kv_attend(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl_kv_cache *cache, void *stream) {

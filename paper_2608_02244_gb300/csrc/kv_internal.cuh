@@ -146,20 +146,13 @@ struct AttendArgs {
                                   // [kAttendWarps * grid], or with a prefix all items [n * key heads (parts of them)]
     int32_t *status;
 };
-// ---- prompt and attend4, one warp's dot products (kv_simple.cu)
-struct PromptArgs {
-    isjl_kv_prompt_args a;
-    isjl_kv_cache cache;
-    int32_t n_blocks, shift, n_kv_heads, group;
-    int32_t *status;
-};
+// ---- attend4, one warp's dot products (kv_simple.cu)
 struct Attend4Args {
     isjl_kv_attend_args a;
     isjl_kv_cache4 cache;
     int32_t n_blocks, shift, n_kv_heads, group;
     int32_t *status;
 };
-cudaError_t launch_prompt(const PromptArgs &g, int head_dim, int type, cudaStream_t st);
 cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, cudaStream_t st);
 
 size_t attend_smem(int head_dim, int n);
@@ -167,5 +160,28 @@ size_t attend_smem(int head_dim, int n);
 // (with more, one block less fits: each holds 4 bytes a query)
 cudaError_t prepare_attend(int head_dim, int type, int *blocks, int *queries);
 cudaError_t launch_attend(const AttendArgs &g, void *encoder, int head_dim, int type, int grid, cudaStream_t st);
+
+
+// ---- prompt (kv_prompt.cu)
+// an item that the end of its block's run cuts; the blocks up to `last` have a piece of it
+struct alignas(16) PromptCut {
+    int32_t row, head, item;      // row < 0: none
+    int32_t last;
+};
+
+struct PromptArgs {
+    isjl_kv_prompt_args a;
+    isjl_kv_cache cache;
+    int32_t n_blocks, shift, n_kv_heads, group;
+    // by launch_prompt: rows of a tile for each token, tokens of a tile, and how many such parts a key head's queries make
+    int32_t rows_of_token, tokens_of_tile, parts;
+    float *part_o;                // [blocks][2][rows of an item][head_dim]
+    float2 *part_ml;              // [blocks][2][rows of an item], as the prefix's
+    PromptCut *cut;               // [blocks]
+    int32_t *status;
+};
+constexpr int kPromptRows = 256;  // of an item, at most
+cudaError_t prepare_prompt(int head_dim, int type);   // once for a shape, before its first launch
+cudaError_t launch_prompt(PromptArgs &g, void *encoder, int head_dim, int type, int sms, cudaStream_t st);
 
 }  // namespace isjl

@@ -1,4 +1,4 @@
-// kv_simple.cu -- attention of prompts (isjl_kv_prompt) and over a cache in 4 bits (isjl_kv_attend4), a block for each
+// kv_simple.cu -- attention of single queries over a cache in 4 bits (isjl_kv_attend4), a block for each
 // query and query head: each warp takes every fourth visible token, a lane D / 32 of the values, with the running
 // maximum and sum of a softmax; the warps' results are joined at the end.
 #include "kv_four.cuh"
@@ -98,61 +98,12 @@ __global__ void __launch_bounds__(32 * kWarps) attend4_kernel(const __grid_const
 }
 
 template <int D, typename T>
-__global__ void __launch_bounds__(32 * kWarps) prompt_kernel(const __grid_constant__ PromptArgs g) {
-    const isjl_kv_prompt_args &a = g.a;
-    const int t = blockIdx.x, h = blockIdx.y, kv = h / g.group, lane = threadIdx.x & 31;
-    __shared__ int row_word;
-    if (threadIdx.x == 0) row_word = -1;
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.n_rows; i += blockDim.x) {
-        const int32_t s0 = a.starts[i], s1 = a.starts[i + 1];
-        if (s0 < 0 || s1 < s0 || s1 > a.n_tokens) {
-            if (t == 0 && h == 0) report(g.status);
-        } else if (s0 <= t && t < s1) {
-            row_word = i;
-        }
-    }
-    __syncthreads();
-    const int row = row_word;
-    if (row < 0) return;
-    const int32_t s0 = a.starts[row], s1 = a.starts[row + 1], len = a.lens[row];
-    const bool bad = len < s1 - s0 || ((len - 1) >> g.shift) >= a.table_width;
-    if (bad && threadIdx.x == 0) report(g.status);
-    const int32_t end = bad ? 0 : (a.n_prefix_blocks << g.shift) + len - (s1 - s0) + (t - s0) + 1;
-    const int32_t lo = a.window && end > a.window ? end - a.window : 0;
-    attend_one<D, T>(static_cast<const T *>(a.q) + t * a.q_stride[0] + h * a.q_stride[1],
-                     static_cast<T *>(a.out) + t * a.out_stride[0] + h * a.out_stride[1],
-                     a.lse ? a.lse + (int64_t)t * gridDim.y + h : nullptr, end, lo, a.sinks, a.scale, [&](float (&v)[D / 32], int32_t y, bool value) {
-        const int32_t j = y >> g.shift, place = y & ((1 << g.shift) - 1);
-        const int32_t block = j < a.n_prefix_blocks ? a.prefix[j] : a.table[(int64_t)row * a.table_width + j - a.n_prefix_blocks];
-        if ((uint32_t)block >= (uint32_t)g.n_blocks) {
-            report(g.status);
-            for (float &e : v) e = 0.f;
-            return;
-        }
-        const int64_t *s = value ? g.cache.v_stride : g.cache.k_stride;
-        load_values<D, T>(v, static_cast<const T *>(value ? g.cache.v : g.cache.k) + block * s[0] + place * s[1] + kv * s[2], lane);
-    });
-}
-
-template <int D, typename T>
-cudaError_t prompt_of(const PromptArgs &g, cudaStream_t st) {
-    prompt_kernel<D, T><<<dim3(g.a.n_tokens, g.n_kv_heads * g.group), 32 * kWarps, 0, st>>>(g);
-    return cudaGetLastError();
-}
-template <int D, typename T>
 cudaError_t attend4_of(const Attend4Args &g, cudaStream_t st) {
     attend4_kernel<D, T><<<dim3(g.a.n, g.n_kv_heads * g.group), 32 * kWarps, 0, st>>>(g);
     return cudaGetLastError();
 }
 
 }  // namespace
-
-cudaError_t launch_prompt(const PromptArgs &g, int head_dim, int type, cudaStream_t st) {
-    if (type == ISJL_KV_BF16)
-        return head_dim == 64 ? prompt_of<64, __nv_bfloat16>(g, st) : head_dim == 128 ? prompt_of<128, __nv_bfloat16>(g, st) : prompt_of<256, __nv_bfloat16>(g, st);
-    return head_dim == 64 ? prompt_of<64, __half>(g, st) : head_dim == 128 ? prompt_of<128, __half>(g, st) : prompt_of<256, __half>(g, st);
-}
 
 cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, cudaStream_t st) {
     if (type == ISJL_KV_BF16)

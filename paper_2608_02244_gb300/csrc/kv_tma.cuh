@@ -65,9 +65,9 @@ bool encode_cache(void *encoder, CUtensorMap *map, void *p, const int64_t *strid
 
 // launch, started while the kernel before it in the stream ends (`early`) or after that
 template <typename... Args>
-cudaError_t launch_kernel(void (*kernel)(Args...), int grid, int threads, size_t smem, cudaStream_t st, bool early, const Args &...args) {
+cudaError_t launch_kernel(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t st, bool early, const Args &...args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
