@@ -229,8 +229,8 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
     const int group = cfg->n_q_heads / cfg->n_kv_heads;
     const size_t items = (size_t)queries * cfg->n_kv_heads * ((group + 15) / 16);
     const size_t cuts = rounded(sizeof(isjl::CutItem) * (items > warps ? items : warps));
-    // pieces of attend's cut items, 32 rows a warp, or of prompt's, two items a block
-    const size_t cut_rows = std::max((size_t)32 * warps, (size_t)2 * isjl::kPromptRows * kv->sms);
+    // pieces of attend's cut items, 32 rows a warp, or of prompt's
+    const size_t cut_rows = std::max((size_t)32 * warps, (size_t)isjl::kPromptRows * kv->sms);
     const size_t ml = rounded(sizeof(float2) * cut_rows), o = sizeof(float) * cfg->head_dim * cut_rows;
     // pieces of the prefix part: an item of 256 rows lies in at most sms / items + 2 blocks; and the own tokens' part
     const size_t pieces = shares ? (size_t)kv->sms * 256 + 3 * (size_t)queries * cfg->n_q_heads : 0;

@@ -36,16 +36,6 @@ struct Shape {
     static_assert(kWarps * 16 * kJoinRow * 4 <= kRing, "the joined pieces take the ring's place");
 };
 
-__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-
-__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t at) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-
 // what a query sees: tokens end - window .. end - 1 and 0 .. sinks - 1, counted from the first token that
 // this kernel reads (the prefix's, or the own ones' where the prefix is done elsewhere)
 struct Sight {

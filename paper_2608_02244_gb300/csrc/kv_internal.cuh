@@ -62,6 +62,16 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+
 __device__ __forceinline__ void report(int32_t *status) { atomicOr(status, 1); }
 
 // ---- assign (kv_assign.cu)
@@ -162,7 +172,7 @@ cudaError_t prepare_attend(int head_dim, int type, int *blocks, int *queries);
 cudaError_t launch_attend(const AttendArgs &g, void *encoder, int head_dim, int type, int grid, cudaStream_t st);
 
 
-// ---- prompt (kv_prompt.cu)
+// ---- prompt (kv_prompt.cu; heads of 256 values: kv_prompt_wide.cu)
 // an item that the end of its block's run cuts; the blocks up to `last` have a piece of it
 struct alignas(16) PromptCut {
     int32_t row, head, item;      // row < 0: none
@@ -175,13 +185,15 @@ struct PromptArgs {
     int32_t n_blocks, shift, n_kv_heads, group;
     // by launch_prompt: rows of a tile for each token, tokens of a tile, and how many such parts a key head's queries make
     int32_t rows_of_token, tokens_of_tile, parts;
-    float *part_o;                // [blocks][2][rows of an item][head_dim]
+    float *part_o;                // [blocks][2][rows of an item][head_dim]: kPromptRows rows an SM
     float2 *part_ml;              // [blocks][2][rows of an item], as the prefix's
     PromptCut *cut;               // [blocks]
     int32_t *status;
 };
-constexpr int kPromptRows = 256;  // of an item, at most
+constexpr int kPromptRows = 512;  // of the pieces of an SM's blocks
 cudaError_t prepare_prompt(int head_dim, int type);   // once for a shape, before its first launch
 cudaError_t launch_prompt(PromptArgs &g, void *encoder, int head_dim, int type, int sms, cudaStream_t st);
+cudaError_t prepare_prompt_wide(int type);
+cudaError_t launch_prompt_wide(PromptArgs &g, int type, int sms, cudaStream_t st);
 
 }  // namespace isjl

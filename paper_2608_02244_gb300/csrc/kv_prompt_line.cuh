@@ -6,7 +6,7 @@
 #include <cstdint>
 
 #ifdef __CUDACC__
-#define ISJL_LINE __host__ __device__ inline
+#define ISJL_LINE __host__ __device__ __forceinline__
 #else
 #define ISJL_LINE inline
 #endif
@@ -15,14 +15,14 @@ namespace isjl {
 
 // The sum of floor((a i + b) / m) over i < n.  What a and b have of whole m's comes out at once; the rest counts the
 // points under a line, column by column, which is as many as row by row: y rows, of which row j has the columns from
-// ceil((m (j + 1) - b) / a) on.  The roles of a and m change as in Euclid's algorithm.  a (n - 1) + b < 2^32.
+// ceil((m (j + 1) - b) / a) on.  The roles of a and m change as in Euclid's algorithm.  a (n - 1) + b + m < 2^32.
 ISJL_LINE int64_t line_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
     int64_t sum = 0, sign = 1;
     while (n > 0) {
         sum += sign * ((int64_t)n * (n - 1) / 2 * (a / m) + (int64_t)n * (b / m));
         a %= m;
         b %= m;
-        const uint32_t y = (uint32_t)(((uint64_t)a * (n - 1) + b) / m);
+        const uint32_t y = (a * (n - 1) + b) / m;
         if (y == 0) break;
         sum += sign * (int64_t)n * y;
         sign = -sign;
@@ -46,7 +46,7 @@ struct PromptShape {
 // A row's `count` queries lie at places first, first + 1, ...; a query sees the tokens up to its own place.
 struct PromptRow {
     int32_t count, first;
-    ISJL_LINE int32_t items(const PromptShape &s) const { return (int32_t)(((int64_t)count + s.step - 1) / s.step); }
+    ISJL_LINE int32_t items(const PromptShape &s) const { return (int32_t)(((uint32_t)count + (uint32_t)s.step - 1) / (uint32_t)s.step); }
     // one more than the last place that item p's queries see
     ISJL_LINE int32_t end(const PromptShape &s, int32_t p) const {
         const int64_t last = ((int64_t)p + 1) * s.step;
@@ -67,15 +67,16 @@ struct PromptRow {
     static ISJL_LINE int32_t tile(const PromptShape &s, int32_t skipped, int32_t j) { return j < s.sink_tiles() ? j : j + skipped; }
     // tiles of the items before p, p <= items
     ISJL_LINE int64_t before(const PromptShape &s, int32_t p) const {
-        if (p > 0 && p == items(s)) return before(s, p - 1) + tiles(s, p - 1);
-        int64_t sum = line_sum((uint32_t)p, (uint32_t)s.keys, (uint32_t)s.step, (uint32_t)first + (uint32_t)s.step + (uint32_t)s.keys - 1);
+        const bool all = p > 0 && p == items(s);           // the last item may be a shorter one
+        const int32_t n = all ? p - 1 : p;
+        int64_t sum = line_sum((uint32_t)n, (uint32_t)s.keys, (uint32_t)s.step, (uint32_t)first + (uint32_t)s.step + (uint32_t)s.keys - 1);
         if (s.window) {
             // skipped tiles begin with the item whose window begins `sink_tiles` tiles on
             const int64_t off = (int64_t)first + 1 - s.window - (int64_t)s.sink_tiles() * s.keys;
-            const int64_t from = off < 0 ? (-off + s.step - 1) / s.step : 0;
-            if (from < p) sum -= line_sum((uint32_t)(p - from), (uint32_t)s.keys, (uint32_t)s.step, (uint32_t)(off + from * s.step));
+            const int64_t from = off >= 0 ? 0 : off < -(int64_t)n * s.step ? n : (uint32_t)(-off + s.step - 1) / (uint32_t)s.step;
+            if (from < n) sum -= line_sum((uint32_t)(n - from), (uint32_t)s.keys, (uint32_t)s.step, (uint32_t)(off + from * s.step));
         }
-        return sum;
+        return all ? sum + tiles(s, n) : sum;
     }
 };
 
