@@ -15,12 +15,7 @@ struct Four {
     static constexpr int kBit = Half<T>::kIsBf16 ? 3 : 6;                             // of the code's lowest bit
     static constexpr uint32_t kMask = 0x000f000fu << kBit;
 
-    static __device__ __forceinline__ uint32_t fma(uint32_t x, uint32_t s, uint32_t b) {
-        uint32_t y;
-        if (Half<T>::kIsBf16) asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(x), "r"(s), "r"(b));
-        else asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(x), "r"(s), "r"(b));
-        return y;
-    }
+    static __device__ __forceinline__ uint32_t fma(uint32_t x, uint32_t s, uint32_t b) { return fma2x16<T>(x, s, b); }
     // 1 + c / 16 of the codes at bits 4 kPlace of each half
     template <int kPlace>
     static __device__ __forceinline__ uint32_t ones(uint32_t word) {

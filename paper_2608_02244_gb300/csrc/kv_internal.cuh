@@ -62,6 +62,15 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// x * y + z of both halves, rounded once
+template <typename T>
+__device__ __forceinline__ uint32_t fma2x16(uint32_t x, uint32_t y, uint32_t z) {
+    uint32_t r;
+    if (Half<T>::kIsBf16) asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(y), "r"(z));
+    else asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(y), "r"(z));
+    return r;
+}
+
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -185,6 +194,7 @@ struct PromptArgs {
     int32_t n_blocks, shift, n_kv_heads, group;
     // by launch_prompt: rows of a tile for each token, tokens of a tile, and how many such parts a key head's queries make
     int32_t rows_of_token, tokens_of_tile, parts;
+    int32_t q_wide, out_wide;     // rows of q and out lie at multiples of 32 bytes
     float *part_o;                // [blocks][2][rows of an item][head_dim]: kPromptRows rows an SM
     float2 *part_ml;              // [blocks][2][rows of an item], as the prefix's
     PromptCut *cut;               // [blocks]

@@ -40,13 +40,33 @@ struct Shape {
     static constexpr int kHalves = D / 64;                       // rows of 128 bytes hold 64 values
     static constexpr int kHalfBytes = 128 * 128;                 // 128 rows of them
     static constexpr int kTileBytes = kHalves * kHalfBytes;
-    static constexpr int kKeyStages = D == 128 ? 3 : 4, kValueStages = D == 128 ? 2 : 4;
+    static constexpr int kKeyStages = D == 128 ? 2 : 4, kValueStages = D == 128 ? 3 : 4;
     static constexpr int kSmem = kGroups * kTileBytes + (kKeyStages + kValueStages) * kTileBytes + 1024;
 };
 
+__device__ __forceinline__ void load32(uint4 &a, uint4 &b, const void *from) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(from) : "memory");
+}
+__device__ __forceinline__ void store32(void *to, uint4 a, uint4 b) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(to), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+}
+
+// Weights are handed over by the block's numbered barriers, which do not lie in shared memory: a look at one that does
+// takes some 400 cycles beside products that read shared memory at its full rate.
+enum { kHandOver = 1 };          // + part + 2 row tile
+constexpr int kHandOverThreads = 128 + 32;
+__device__ __forceinline__ void hand_over(int group, int part) {
+    asm volatile("barrier.cta.arrive %0, %1;" ::"r"(kHandOver + part + 2 * group), "n"(kHandOverThreads) : "memory");
+}
+__device__ __forceinline__ void take_over(int group, int part) {
+    asm volatile("barrier.cta.sync %0, %1;" ::"r"(kHandOver + part + 2 * group), "n"(kHandOverThreads) : "memory");
+}
+
 // barriers, in 8-byte words
-enum { kKeyFull = 0, kValueFull = 8, kFree = 4 /* after a stage's full one */, kClean = 16, kScores = 20, kWeights = 22, kRest = 24, kSumsDone = 26,
-       kQueries = 28, kDrain = 30, kItemFull = 31, kItemFree = kItemFull + kItems, kBars = kItemFree + kItems };
+enum { kKeyFull = 0, kValueFull = 8, kFree = 4 /* after a stage's full one */, kClean = 16, kScores = 20, kSumsDone = 22, kQueries = 24, kDrain = 26,
+       kItemFull = 27, kItemFree = kItemFull + kItems, kBars = kItemFree + kItems };
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -65,7 +85,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
     __shared__ uint32_t tmem_base;
     __shared__ int32_t failed_word;
     __shared__ int32_t flag_word[kItems];           // an item's number in the block, plus one, if a value of it was left out
-    volatile int32_t *failed = &failed_word, *flags = flag_word;
+    volatile int32_t *flags = flag_word;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
@@ -87,10 +107,8 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
         for (int i = 0; i < 20; ++i) bar_init(bar(i), 1);
         for (int i = 0; i < 2; ++i) {
             bar_init(bar(kScores + i), 1);
-            bar_init(bar(kWeights + i), 128);
-            bar_init(bar(kRest + i), 128);
             bar_init(bar(kSumsDone + i), 1);
-            bar_init(bar(kQueries + i), 128);
+            bar_init(bar(kQueries + i), 4);
         }
         bar_init(bar(kDrain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -104,7 +122,31 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
     Run run = find_run<kThreads>(g, shape, words);
     fence_after();
     const uint32_t tmem = tmem_base;
-    auto wait = [&](int b, uint32_t phase) { return __all_sync(~0u, bar_wait(bar(b), phase, failed)); };
+    // A wait: false if it, or another, gave up.  The clock, which takes a few hundred cycles to read, is looked at once in
+    // a while only.
+    const uint32_t failed_at = smem_addr(&failed_word);
+    auto wait_lane = [&](int b, uint32_t phase) {
+        uint64_t begin = 0;
+        for (;;) {
+#pragma unroll 1
+            for (int i = 0; i < 16; ++i)
+                if (bar_try(bar(b), phase)) return true;
+            uint32_t others;
+            asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(others) : "r"(failed_at) : "memory");
+            const uint64_t t = now();
+            if (begin == 0) begin = t;
+            if (others || t - begin > kLimit) {
+                asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(failed_at), "r"(1) : "memory");
+                return false;
+            }
+        }
+    };
+    // of a warp: its threads look together, which costs less than one's look that the others wait for
+    auto wait = [&](int b, uint32_t phase) {
+        const bool done = __all_sync(~0u, wait_lane(b, phase));
+        __syncwarp();
+        return done;
+    };
     // item `n` of this block's run, when it has been planned
     auto item_of = [&](int n) -> const Item & { return items[n % kItems]; };
     auto wait_item = [&](int n) { return wait(kItemFull + n % kItems, (uint32_t)(n / kItems) & 1); };
@@ -131,19 +173,24 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             const bool live = live_of(x);
             const T *from = static_cast<const T *>(g.a.q) + (int64_t)(x.start + token) * g.a.q_stride[0] + (int64_t)(x.q_head + member) * g.a.q_stride[1];
             const uint32_t to = q_at + group * S::kTileBytes + row * 128;
-#pragma unroll 1
-            for (int b = 0; b < D / 64; ++b) {
-                uint4 w[8];
+            uint4 w[D / 8];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) w[c] = live ? *reinterpret_cast<const uint4 *>(from + 64 * b + 8 * c) : make_uint4(0, 0, 0, 0);
+            for (int c = 0; c < D / 8; ++c) w[c] = make_uint4(0, 0, 0, 0);
+            // a row a lane: each load touches a line for each, so the fewer the better
+            if (live && g.q_wide) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + b * S::kHalfBytes + ((c ^ (row & 7)) << 4)),
-                                 "r"(w[c].x), "r"(w[c].y), "r"(w[c].z), "r"(w[c].w) : "memory");
+                for (int c = 0; c < D / 8; c += 2) load32(w[c], w[c + 1], from + 8 * c);
+            } else if (live) {
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) w[c] = *reinterpret_cast<const uint4 *>(from + 8 * c);
             }
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + c / 8 * S::kHalfBytes + ((c % 8 ^ (row & 7)) << 4)),
+                             "r"(w[c].x), "r"(w[c].y), "r"(w[c].z), "r"(w[c].w) : "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            fence_before();
-            bar_arrive(bar(kQueries + group));
+            __syncwarp();
+            if (lane == 0) bar_arrive(bar(kQueries + group));
         };
         uint32_t step = 0;
         int item_no = 0;                           // of this group
@@ -162,7 +209,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                     continue;
                 }
                 if (!loaded) load_queries(x);
-                const int count = x.count;
+                const int count = x.count, tile0 = x.tile0, skipped = x.skipped;
                 // The last group to use a tile frees its stages: when it sees its scores, the products of the keys are
                 // done, and those of the tile before's values, which were issued earlier.
                 const bool frees = (group == 1) == two_of(x) && (threadIdx.x & 127) == 0;
@@ -182,7 +229,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c) tmem_load(s[c], s_at + 32 * c);
                     tmem_load_wait();
-                    const int32_t y0 = tile_at(shape, x, j);
+                    const int32_t y0 = PromptRow::tile(shape, skipped, tile0 + j) * kKeys;
                     const int left = seen_end - y0;
                     // rows end at different tokens: the whole warp takes a branch that a row of it needs, since what
                     // follows (loads and stores of TMEM) is the warp's
@@ -242,7 +289,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                         tmem_store(s_at + 32 * h, p);
                         tmem_store_wait();
                         fence_before();
-                        bar_arrive(bar((h ? kRest : kWeights) + group));      // the product starts with the first part
+                        hand_over(group, h);                          // the product starts with the first part
                     }
                     total += (part[0].x + part[0].y) + (part[1].x + part[1].y);
                 }
@@ -285,17 +332,25 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                     }
                 }
                 if (live && whole) {
+                    uint4 w[4];
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        uint32_t w[4];
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t u[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) w[k] = Half<T>::pack(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
-                        *reinterpret_cast<uint4 *>(out + 32 * c + i) = make_uint4(w[0], w[1], w[2], w[3]);
+                        for (int k = 0; k < 4; ++k) u[k] = Half<T>::pack(__uint_as_float(o[8 * i + 2 * k]) * inv, __uint_as_float(o[8 * i + 2 * k + 1]) * inv);
+                        w[i] = make_uint4(u[0], u[1], u[2], u[3]);
+                    }
+                    if (g.out_wide) {
+                        store32(out + 32 * c, w[0], w[1]);
+                        store32(out + 32 * c + 16, w[2], w[3]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(out + 32 * c + 8 * i) = w[i];
                     }
                 } else if (live) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4)
-                        *reinterpret_cast<uint4 *>(g.part_o + at * D + 32 * c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    for (int i = 0; i < 32; i += 8)
+                        store32(g.part_o + at * D + 32 * c + i, make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]), make_uint4(o[i + 4], o[i + 5], o[i + 6], o[i + 7]));
                 }
             }
             if (live && !whole) g.part_ml[at] = make_float2(top, total);
@@ -304,47 +359,67 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             fence_before();       // the next item's first weights, after which its products overwrite these sums, come later
             done_item(n);
         }
+        // the issuing warp's wait for weights has no end of its own
+        if (!ok)
+#pragma unroll
+            for (int h = 0; h < kParts; ++h) {
+                __syncwarp();
+                hand_over(group, h);
+            }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kLoadWarp || warp == kLoadWarp + 1) {
-            // ---- keys by one warp, values by the other: one copy for each cache block (or part of one) of a tile and 64 of its values
+            // ---- keys by one warp, values by the other: one copy for each cache block (or part of one) of a tile and 64 of
+            // its values.  The lanes look up the blocks and one thread issues: issued by several threads at once, each with
+            // its own operands, copies ended with an illegal address in some builds of this kernel.
             const int rows = min(1 << g.shift, kKeys), pieces = kKeys / rows;      // pieces: 1 .. 16
-            const uint32_t piece_bytes = rows * 128;
-            // this lane's part of a tile: piece lane % pieces, and every 32 / pieces-th half
-            const int piece = lane % pieces;
+            const int piece = lane % pieces;                         // whose block this lane looks up
+            const bool one = elect_one();
             constexpr int32_t kNone = INT32_MIN;
             // A ring for each: a stage's turns are one warp's, which cannot be two turns ahead of itself.
             const bool values = warp != kLoadWarp;
             const int stages = values ? S::kValueStages : S::kKeyStages, full = values ? kValueFull : kKeyFull;
             const uint32_t to = ring + (values ? S::kKeyStages * S::kTileBytes : 0);
             const CUtensorMap *map = values ? &vmap : &kmap;
-            int stage = 0, load = 0;                                 // load: fills so far, counted up to `stages`
+            int stage = 0, load = 0, n = 0, j = 0;                   // load: fills so far, counted up to `stages`
             uint32_t turn = 0;
             bool ok = wait_item(0);
-            for (int n = 0; ok && item_of(n).count > 0; ++n) {
-                const Item &x = item_of(n);
-                const int count = x.count, kv = x.kv;
-                for (int j = 0; j < count && ok; ++j) {
-                    const int32_t y = tile_at(shape, x, j) + piece * rows;
-                    // the block's number, if any of the item's queries sees some of this part
-                    int32_t block = kNone;
-                    if (!(x.kind & kDead) && y < x.end && (y + rows > x.low || y < shape.sinks)) block = block_at(g, x.row, y);
-                    ok = __all_sync(~0u, load < stages || bar_wait(bar(full + kFree + stage), turn ^ 1, failed));
-                    if (!ok) break;
-                    if ((uint32_t)block >= (uint32_t)g.n_blocks) {             // not seen, or beyond the cache: zeros
-                        if (block != kNone) report(g.status);
-                        block = g.n_blocks;
-                    }
-                    if (lane == 0) bar_expect(bar(full + stage), S::kTileBytes);
-                    __syncwarp();
-                    for (int half = lane / pieces; half < S::kHalves; half += 32 / pieces)
-                        tma_load(to + stage * S::kTileBytes + half * S::kHalfBytes + piece * piece_bytes, map, bar(full + stage), y & ((1 << g.shift) - 1), half,
-                                 kv, block);
-                    if (load < stages) ++load;
-                    if (++stage == stages) { stage = 0; turn ^= 1; }
+            Item x = item_of(0);
+            int32_t block = kNone, y0 = 0;                           // of the tile that is next
+            // the block's number, if any of the item's queries sees some of this part; asked for one tile ahead
+            auto look = [&]() {
+                y0 = tile_at(shape, x, j);
+                const int32_t y = y0 + piece * rows;
+                block = !(x.kind & kDead) && y < x.end && (y + rows > x.low || y < shape.sinks) ? block_at(g, x.row, y) : kNone;
+            };
+            if (ok && x.count > 0) look();
+            while (ok && x.count > 0) {
+                int32_t from = block;
+                const int kv = x.kv, slot = y0 & ((1 << g.shift) - 1);             // slot: 0 but in blocks larger than a tile
+                if (++j == x.count) {
+                    done_item(n);
+                    ok = wait_item(++n);
+                    x = item_of(n);
+                    j = 0;
                 }
-                done_item(n);
-                ok = ok && wait_item(n + 1);
+                if (ok && x.count > 0) look();
+                if (load == stages) ok = wait(full + kFree + stage, turn ^ 1) && ok;
+                if (!ok) break;
+                if ((uint32_t)from >= (uint32_t)g.n_blocks) {             // not seen, or beyond the cache: zeros
+                    if (from != kNone) report(g.status);
+                    from = g.n_blocks;
+                }
+                if (one) bar_expect(bar(full + stage), S::kTileBytes);
+                for (int p = 0; p < pieces; ++p) {
+                    const int32_t b = __shfl_sync(~0u, from, p);
+                    if (one)
+#pragma unroll
+                        for (int half = 0; half < S::kHalves; ++half)
+                            tma_load(to + stage * S::kTileBytes + half * S::kHalfBytes + p * rows * 128, map, bar(full + stage), slot, half, kv, b);
+                    __syncwarp();
+                }
+                if (load < stages) ++load;
+                if (++stage == stages) { stage = 0; turn ^= 1; }
             }
             // nothing is left in flight, also after a failure: the last fill of each stage
             for (int i = 0; i < load; ++i) {
@@ -385,42 +460,49 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                     const int32_t y0 = tile_at(shape, x, j);
                     if (edge(shape, x, y0)) {
                         const uint32_t tile = ring + (S::kKeyStages + stage) * S::kTileBytes;
-                        bool found = false;
-                        // rows [r0, r1) of the tile; a lane looks at 16 bytes of four rows at a time
-                        auto clean = [&](int r0, int r1) {
-                            for (int row0 = r0; row0 < r1; row0 += 16)
-#pragma unroll 1
-                                for (int half = 0; half < S::kHalves; ++half) {
-                                    const uint32_t from = tile + half * S::kHalfBytes + (lane % 8) * 16;
-                                    uint32_t w[4][4];
+                        // 16 bytes in a row's half: rows r0 + lane / 8, + 4, ...; eight of them are under way together
+                        auto scan = [&](int r0, int r1) {
+                            uint32_t sum[2] = {0, 0};                                  // 0 times a value is 0 if that is finite
+                            for (int half = 0; half < S::kHalves; ++half)
+                                for (int r = r0 + lane / 8; r < r1; r += 32) {
+                                    uint32_t w[8][4];
 #pragma unroll
-                                    for (int u = 0; u < 4; ++u) {
-                                        const int r = min(row0 + 4 * u + lane / 8, r1 - 1);        // the last one more than once
-                                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                                     : "=r"(w[u][0]), "=r"(w[u][1]), "=r"(w[u][2]), "=r"(w[u][3]) : "r"(from + r * 128) : "memory");
-                                    }
+                                    for (int u = 0; u < 8; ++u)                        // the last row more than once
+                                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[u][0]), "=r"(w[u][1]), "=r"(w[u][2]), "=r"(w[u][3])
+                                                     : "r"(tile + half * S::kHalfBytes + min(r + 4 * u, r1 - 1) * 128 + (lane % 8) * 16) : "memory");
 #pragma unroll
-                                    for (int u = 0; u < 4; ++u) {
-                                        const int r = min(row0 + 4 * u + lane / 8, r1 - 1);
-                                        const bool beyond = y0 + r >= end;
-                                        uint32_t bad = 0;
+                                    for (int u = 0; u < 8; ++u)
 #pragma unroll
-                                        for (int k = 0; k < 4; ++k) bad |= not_finite<T>(w[u][k]);
-                                        if (beyond || bad) {
-                                            found = found || !beyond;
-#pragma unroll
-                                            for (int k = 0; k < 4; ++k)                    // not_finite: bits 15 and 31
-                                                w[u][k] = beyond ? 0u : w[u][k] & ~((not_finite<T>(w[u][k]) >> 15) * 0xffffu);
-                                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                                                         ::"r"(from + r * 128), "r"(w[u][0]), "r"(w[u][1]), "r"(w[u][2]), "r"(w[u][3]) : "memory");
-                                        }
-                                    }
+                                        for (int k = 0; k < 4; ++k) sum[k & 1] = fma2x16<T>(w[u][k], 0, sum[k & 1]);
                                 }
+                            return __any_sync(~0u, ((sum[0] | sum[1]) & 0x7fff7fffu) != 0);      // -0 may come of it too
                         };
-                        const int from = min(max(0, x.from - y0), kKeys);                 // a row in both parts is looked at once
-                        clean(max(0, shape.sinks - y0), min(from, x.below - y0));
-                        clean(from, kKeys);
-                        if (found) flags[n % kItems] = n + 1;
+                        auto mend = [&](int r0, int r1) {
+                            for (int i = lane; i < (r1 - r0) * S::kHalves * 32; i += 32) {
+                                const uint32_t at = tile + i / 32 % S::kHalves * S::kHalfBytes + (r0 + i / 32 / S::kHalves) * 128 + lane * 4;
+                                uint32_t w;
+                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
+                                w &= ~((not_finite<T>(w) >> 15) * 0xffffu);            // not_finite: bits 15 and 31
+                                asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(w) : "memory");
+                            }
+                        };
+                        // rows that some query does not see, a row in both parts once, up to those that none sees
+                        const int last = min(max(0, end - y0), kKeys), from = min(max(0, x.from - y0), last);
+                        const int first = max(0, shape.sinks - y0), below = min(from, x.below - y0);
+                        bool found = false;
+                        if (first < below && scan(first, below)) {
+                            mend(first, below);
+                            found = true;
+                        }
+                        if (from < last && scan(from, last)) {
+                            mend(from, last);
+                            found = true;
+                        }
+                        for (int half = 0; half < S::kHalves; ++half)
+                            for (int r = last + lane / 8; r < kKeys; r += 4)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"
+                                             ::"r"(tile + half * S::kHalfBytes + r * 128 + (lane % 8) * 16), "r"(0) : "memory");
+                        if (found && lane == 0) flags[n % kItems] = n + 1;
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                     __syncwarp();
@@ -430,9 +512,10 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             }
         } else if (warp == kIssueWarp) {
             // The whole warp runs this loop, so that addresses stay uniform, and one thread of it issues: with the
-            // products of 64 cycles each, their issue has to take less.
+            // products of 64 cycles each, their issue has to take less.  Operands of products and copies are in registers
+            // that the warp shares: the others wait for that thread each time (__syncwarp), here and in the loaders.
             const bool one = elect_one();
-            uint32_t step[2] = {0, 0}, begun[2] = {0, 0};       // weights taken, items begun so far of each row tile
+            uint32_t begun[2] = {0, 0};                          // items begun so far of each row tile
             // operands differ in their address field alone: low word plus 16-byte steps
             const uint32_t q_lo = (uint32_t)operand(q_at, 16, 1024), k_lo = (uint32_t)operand(ring, 16, 1024);
             const uint32_t v_lo = (uint32_t)operand(ring + S::kKeyStages * S::kTileBytes, S::kHalfBytes, 1024);
@@ -447,6 +530,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                     }
                     commit(bar(kScores + i));
                 }
+                __syncwarp();
             };
             auto sums = [&](int i, int stage, int part, bool add) {
                 const uint32_t b = v_lo + stage * (S::kTileBytes >> 4), a = i * kKeys, d = kSums + i * D;
@@ -456,6 +540,13 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                     for (int k = 0; k < kSteps; ++k)
                         mma_tmem(d, a + (part * kSteps + k) * 8, b + (part * kSteps + k) * (2048 >> 4), high, kSecondWhat, add || part + k > 0);
                 }
+                __syncwarp();
+            };
+            // several barriers in one wait: a lane for each
+            auto wait_each = [&](int b, uint32_t phase) {
+                const bool done = __all_sync(~0u, wait_lane(b, phase));
+                __syncwarp();
+                return done;
             };
             int k_at = 0, v_at = 0;                              // stages of the tile's keys and values, and their turns
             uint32_t k_turn = 0, v_turn = 0;
@@ -480,20 +571,23 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
 #pragma unroll
                     for (int i = 0; i < kGroups; ++i) {
                         if (i >= groups) break;
-                        // one wait for weights and (before the first row tile's) copies: a lane for each barrier
-                        const int what = i == 0 ? lane : 0;
-                        ok = wait(what == 1 ? kValueFull + v_at : what == 2 ? kClean + v_at : kWeights + i, what == 1 || what == 2 ? v_turn : step[i] & 1);
-                        if (!ok) break;
+                        if (i == 0) {        // copies: these have come long ago, mostly; a lane for each barrier
+                            ok = wait_each(lane == 1 ? kClean + v_at : lane == 2 && more ? kKeyFull + k_at : kValueFull + v_at, lane == 2 && more ? k_turn : v_turn);
+                            // a row tile that gives up hands over once more, enough for this tile
+                            uint32_t others;
+                            asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(others) : "r"(failed_at) : "memory");
+                            ok = ok && !__any_sync(~0u, others);
+                            if (!ok) break;
+                        }
+                        take_over(i, 0);
                         fence_after();
                         sums(i, v_at, 0, j > 0);
-                        const bool keys = i == 0 && more && lane == 1;
-                        ok = wait(keys ? kKeyFull + k_at : kRest + i, keys ? k_turn : step[i] & 1);
-                        ++step[i];
-                        if (!ok) break;
+                        take_over(i, 1);
                         fence_after();
                         sums(i, v_at, 1, true);
                         if (more) scores(i, k_at);
                         else if (one) commit(bar(kSumsDone + i));
+                        __syncwarp();
                     }
                     next(v_at, v_turn, S::kValueStages);
                     if (more) next(k_at, k_turn, S::kKeyStages);
@@ -502,7 +596,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             }
             if (!ok) {
                 // products under way still read shared memory and write TMEM
-                *failed = 1;
+                if (lane == 0) asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(failed_at), "r"(1) : "memory");
                 if (one) commit(bar(kDrain));
                 __syncwarp();
                 bar_wait(bar(kDrain), 0);
@@ -511,7 +605,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0 && *failed) atomicOr(g.status, 2);
+    if (threadIdx.x == 0 && failed_word) atomicOr(g.status, 2);
     if (warp == kIssueWarp)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
@@ -540,6 +634,9 @@ cudaError_t launch_prompt(PromptArgs &g, void *encoder, int head_dim, int type, 
     if (head_dim == 256) return launch_prompt_wide(g, type, sms, st);
     CUtensorMap k, v;
     share_rows(g, kRows);
+    auto wide = [](const void *p, const int64_t *stride) { return reinterpret_cast<uintptr_t>(p) % 32 == 0 && (stride[0] | stride[1]) % 16 == 0; };
+    g.q_wide = wide(g.a.q, g.a.q_stride);
+    g.out_wide = wide(g.a.out, g.a.out_stride);
     if (sms > kMostRuns) sms = kMostRuns;
     const int rows = 1 << g.shift < kKeys ? 1 << g.shift : kKeys;
     if (!encode_cache(encoder, &k, g.cache.k, g.cache.k_stride, rows, 1, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||

@@ -160,6 +160,11 @@ __device__ __forceinline__ float log_of(float top, float total) {
     return total > 0.f || total != total ? (top + log2f(total)) * kLn2 : -INFINITY;
 }
 
+// a / b of numbers that are mostly small: 64 bits take a few hundred cycles
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return (a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
 // A block's run of the line: tiles f .. f1 - 1, of which `here` is the first.
 struct Run {
     int64_t tiles, blocks;       // of the line; those with a run
@@ -168,7 +173,7 @@ struct Run {
 };
 
 struct RunWords {
-    int64_t sums[32], rest;
+    int64_t sums[32], rest, each;        // of the row that the run begins in: tiles before it in the row, and of each head
     int32_t row;
 };
 
@@ -180,12 +185,12 @@ __device__ __forceinline__ Run find_run(const PromptArgs &g, const PromptShape &
     const int begin = min(g.a.n_rows, (int)threadIdx.x * per), end = min(g.a.n_rows, begin + per);
     auto work = [&](int i, bool tell) {
         const Row r = row_of(g, i, tell);
-        return H * r.before(s, r.items(s));
+        return r.before(s, r.items(s));
     };
-    int64_t sum = 0;
-    for (int i = begin; i < end; ++i) sum += work(i, blockIdx.x == 0);
+    int64_t sum = 0;             // this thread's rows
+    for (int i = begin; i < end; ++i) sum += H * work(i, blockIdx.x == 0);
     __syncwarp();                // the threads come from loops of different lengths
-    int64_t before = sum;        // this thread's rows
+    int64_t before = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const int64_t p = __shfl_up_sync(~0u, before, d);
@@ -200,17 +205,18 @@ __device__ __forceinline__ Run find_run(const PromptArgs &g, const PromptShape &
         run.tiles += words.sums[w];
     }
     run.blocks = min((int64_t)gridDim.x, run.tiles);
-    run.f = blockIdx.x < run.blocks ? run.tiles * blockIdx.x / run.blocks : run.tiles;
-    run.f1 = blockIdx.x < run.blocks ? run.tiles * (blockIdx.x + 1) / run.blocks : run.tiles;
+    run.f = blockIdx.x < run.blocks ? quotient(run.tiles * blockIdx.x, run.blocks) : run.tiles;
+    run.f1 = blockIdx.x < run.blocks ? quotient(run.tiles * (blockIdx.x + 1), run.blocks) : run.tiles;
     if (run.f < run.f1 && before <= run.f && run.f < before + sum)
         for (int i = begin; i < end; ++i) {
-            const int64_t k = end - begin == 1 ? sum : work(i, false);
-            if (run.f < before + k) {
+            const int64_t each = end - begin == 1 ? quotient(sum, H) : work(i, false);
+            if (run.f < before + H * each) {
                 words.row = i;
                 words.rest = run.f - before;
+                words.each = each;
                 break;
             }
-            before += k;
+            before += H * each;
         }
     __syncthreads();
     return run;
@@ -223,9 +229,8 @@ __device__ __forceinline__ void begin_run(const PromptArgs &g, const PromptShape
     p.row = words.row;
     p.r = row_of(g, p.row, false);
     p.items = p.r.items(s);
-    const int64_t each = p.r.before(s, p.items);
-    p.head = (int)(words.rest / each);
-    const int64_t rest = words.rest - p.head * each;
+    p.head = (int)quotient(words.rest, words.each);
+    const int64_t rest = words.rest - p.head * words.each;
     // the last item that begins at `rest` or before it: 32 places looked at together
     int lo = 0, hi = p.items;
     while (hi - lo > 1) {
@@ -236,7 +241,7 @@ __device__ __forceinline__ void begin_run(const PromptArgs &g, const PromptShape
         lo += k * step;
     }
     p.item = lo;
-    p.j = (int)(rest - p.r.before(s, lo));
+    p.j = (int)(lo ? rest - p.r.before(s, lo) : rest);
 }
 
 // The run's next item, count 0 when there is none.  `writes`: this thread notes the item that the run's end cuts; it
@@ -261,7 +266,7 @@ __device__ __forceinline__ Item take_item(const PromptArgs &g, const PromptShape
     x.below = low_of(s, last);
     x.kind = (x.count == tiles ? kWhole : 0) | (p.j == 0 ? kFirst : 0) | (p.r.dead ? kDead : 0);
     if (writes && x.count < tiles && p.j == 0)           // its pieces are those of the blocks from here on
-        g.cut[blockIdx.x] = {p.row, p.head, p.item, (int)(((run.f + tiles) * run.blocks - 1) / run.tiles)};
+        g.cut[blockIdx.x] = {p.row, p.head, p.item, (int)quotient((run.f + tiles) * run.blocks - 1, run.tiles)};
     run.f += x.count;
     if (run.f < run.f1) next_item(g, s, p);
     return x;
