@@ -53,20 +53,31 @@ __device__ __forceinline__ void store32(void *to, uint4 a, uint4 b) {
                  ::"l"(to), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
 }
 
-// Weights are handed over by the block's numbered barriers, which do not lie in shared memory: a look at one that does
-// takes some 400 cycles beside products that read shared memory at its full rate.
-enum { kHandOver = 1 };          // + part + 2 row tile
-constexpr int kHandOverThreads = 128 + 32;
-__device__ __forceinline__ void hand_over(int group, int part) {
-    asm volatile("barrier.cta.arrive %0, %1;" ::"r"(kHandOver + part + 2 * group), "n"(kHandOverThreads) : "memory");
+// What the issuing warp waits for in every tile comes by the block's numbered barriers, which do not lie in shared memory:
+// a look at one that does takes some 400 cycles beside products that read shared memory at its full rate.  Weights: one
+// barrier for each row tile and part.  Copies that have come and are clean: one of eight, tile after tile, so that two
+// more arrivals than the issuing warp has seen are none too many for one.
+//
+// These waits have no limit, so that they end is up to who arrives.
+// Copies: the planning warp, whose waits have one; when it gives up it arrives for this tile and the next.  The issuing
+// warp, let go, meets the word that says so before it issues the scores after those, and ends.
+// Weights: a row tile's group arrives whenever its scores come, and scores that were issued do come.  It gives up a
+// wait for scores only some time after that word was written, when none can be issued any more.
+enum { kHandOver = 1 /* + part + 2 row tile */, kCopies = 5 /* + tile % 8 */ };
+constexpr int kHandOverThreads = 128 + 32, kCopiesThreads = 64;
+constexpr uint64_t kGrace = 50000000ull;        // nanoseconds
+template <int kThreads>
+__device__ __forceinline__ void numbered_arrive(int id) {
+    asm volatile("barrier.cta.arrive %0, %1;" ::"r"(id), "n"(kThreads) : "memory");
 }
-__device__ __forceinline__ void take_over(int group, int part) {
-    asm volatile("barrier.cta.sync %0, %1;" ::"r"(kHandOver + part + 2 * group), "n"(kHandOverThreads) : "memory");
+template <int kThreads>
+__device__ __forceinline__ void numbered_sync(int id) {
+    asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "n"(kThreads) : "memory");
 }
 
 // barriers, in 8-byte words
-enum { kKeyFull = 0, kValueFull = 8, kFree = 4 /* after a stage's full one */, kClean = 16, kScores = 20, kSumsDone = 22, kQueries = 24, kDrain = 26,
-       kItemFull = 27, kItemFree = kItemFull + kItems, kBars = kItemFree + kItems };
+enum { kKeyFull = 0, kValueFull = 8, kFree = 4 /* after a stage's full one */, kScores = 16, kSumsDone = 18, kQueries = 20, kDrain = 22,
+       kItemFull = 23, kItemFree = kItemFull + kItems, kBars = kItemFree + kItems };
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -104,7 +115,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             bar_init(bar(kItemFull + i), 1);
             bar_init(bar(kItemFree + i), 11);           // the warps that read it
         }
-        for (int i = 0; i < 20; ++i) bar_init(bar(i), 1);
+        for (int i = 0; i < kScores; ++i) bar_init(bar(i), 1);
         for (int i = 0; i < 2; ++i) {
             bar_init(bar(kScores + i), 1);
             bar_init(bar(kSumsDone + i), 1);
@@ -125,19 +136,23 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
     // A wait: false if it, or another, gave up.  The clock, which takes a few hundred cycles to read, is looked at once in
     // a while only.
     const uint32_t failed_at = smem_addr(&failed_word);
+    auto look_failed = [&]() {
+        uint32_t w;
+        asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(w) : "r"(failed_at) : "memory");
+        return w;
+    };
     auto wait_lane = [&](int b, uint32_t phase) {
-        uint64_t begin = 0;
+        uint64_t begin = 0, told = 0;
         for (;;) {
 #pragma unroll 1
             for (int i = 0; i < 16; ++i)
                 if (bar_try(bar(b), phase)) return true;
-            uint32_t others;
-            asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(others) : "r"(failed_at) : "memory");
             const uint64_t t = now();
             if (begin == 0) begin = t;
-            if (others || t - begin > kLimit) {
-                asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(failed_at), "r"(1) : "memory");
-                return false;
+            if (t - begin > kLimit) asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(failed_at), "r"(1) : "memory");
+            if (look_failed()) {
+                if (told == 0) told = t;
+                if (warp >= kLoadWarp || t - told > kGrace) return false;
             }
         }
     };
@@ -289,7 +304,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                         tmem_store(s_at + 32 * h, p);
                         tmem_store_wait();
                         fence_before();
-                        hand_over(group, h);                          // the product starts with the first part
+                        numbered_arrive<kHandOverThreads>(kHandOver + h + 2 * group);        // the product starts with the first part
                     }
                     total += (part[0].x + part[0].y) + (part[1].x + part[1].y);
                 }
@@ -359,13 +374,6 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             fence_before();       // the next item's first weights, after which its products overwrite these sums, come later
             done_item(n);
         }
-        // the issuing warp's wait for weights has no end of its own
-        if (!ok)
-#pragma unroll
-            for (int h = 0; h < kParts; ++h) {
-                __syncwarp();
-                hand_over(group, h);
-            }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kLoadWarp || warp == kLoadWarp + 1) {
@@ -449,7 +457,13 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             };
             for (int i = 0; i < kAhead && ok; ++i) plan();
             int stage = 0;
-            uint32_t turn = 0;
+            // The tile, of the run, whose keys are waited for; with them the values of the one before are handed over.  All are
+            // waited for here, one after another, and given back only after that: no turn of a barrier is taken for another.
+            uint32_t turn = 0, tile = 0, handed = 0;
+            if (ok && item_of(0).count > 0) {
+                ok = wait(kKeyFull, 0);
+                if (ok) numbered_arrive<kCopiesThreads>(kCopies + handed++);
+            }
             for (int n = 0; ok && item_of(n).count > 0; ++n) {
                 plan();
                 const Item &x = item_of(n);
@@ -506,9 +520,18 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                     __syncwarp();
-                    if (lane == 0) bar_arrive(bar(kClean + stage));
+                    // and the next tile's keys
+                    ++tile;
+                    if (j + 1 < count || item_of(n + 1).count > 0) ok = wait(kKeyFull + tile % S::kKeyStages, tile / S::kKeyStages & 1);
+                    if (!ok) break;
+                    numbered_arrive<kCopiesThreads>(kCopies + handed++ % 8);
                     if (++stage == S::kValueStages) { stage = 0; turn ^= 1; }
                 }
+            }
+            if (!ok) {                                           // the issuing warp is let go
+                __syncwarp();
+                numbered_arrive<kCopiesThreads>(kCopies + handed % 8);
+                numbered_arrive<kCopiesThreads>(kCopies + (handed + 1) % 8);
             }
         } else if (warp == kIssueWarp) {
             // The whole warp runs this loop, so that addresses stay uniform, and one thread of it issues: with the
@@ -542,22 +565,16 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                 }
                 __syncwarp();
             };
-            // several barriers in one wait: a lane for each
-            auto wait_each = [&](int b, uint32_t phase) {
-                const bool done = __all_sync(~0u, wait_lane(b, phase));
-                __syncwarp();
-                return done;
-            };
-            int k_at = 0, v_at = 0;                              // stages of the tile's keys and values, and their turns
-            uint32_t k_turn = 0, v_turn = 0;
-            auto next = [](int &at, uint32_t &turn, int stages) {
-                if (++at == stages) { at = 0; turn ^= 1; }
+            int k_at = 0, v_at = 0;                              // stages of the tile's keys and values
+            uint32_t taken = 0;                                  // copies handed over so far: the run's first keys, then its tiles
+            auto next = [](int &at, int stages) {
+                if (++at == stages) at = 0;
             };
             bool ok = tmem_base == 0 && wait_item(0);            // all columns are ours: they begin at 0
+            if (ok && item_of(0).count > 0) numbered_sync<kCopiesThreads>(kCopies + taken++);
             for (int n = 0; ok && item_of(n).count > 0; ++n) {
                 const int count = item_of(n).count, groups = item_of(n).tokens > g.tokens_of_tile ? 2 : 1;
                 done_item(n);
-                ok = wait(kKeyFull + k_at, k_turn);
                 for (int i = 0; i < groups && ok; ++i) {
                     ok = wait(kQueries + i, begun[i]++ & 1);
                     if (!ok) break;
@@ -565,32 +582,28 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                     scores(i, k_at);
                 }
                 if (!ok) break;
-                next(k_at, k_turn, S::kKeyStages);
+                next(k_at, S::kKeyStages);
                 for (int j = 0; j < count && ok; ++j) {
                     const bool more = j + 1 < count;
+                    const uint32_t others = look_failed();       // used when it has come
+                    numbered_sync<kCopiesThreads>(kCopies + taken++ % 8);        // its values, and the next keys
 #pragma unroll
                     for (int i = 0; i < kGroups; ++i) {
                         if (i >= groups) break;
-                        if (i == 0) {        // copies: these have come long ago, mostly; a lane for each barrier
-                            ok = wait_each(lane == 1 ? kClean + v_at : lane == 2 && more ? kKeyFull + k_at : kValueFull + v_at, lane == 2 && more ? k_turn : v_turn);
-                            // a row tile that gives up hands over once more, enough for this tile
-                            uint32_t others;
-                            asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(others) : "r"(failed_at) : "memory");
-                            ok = ok && !__any_sync(~0u, others);
-                            if (!ok) break;
-                        }
-                        take_over(i, 0);
+                        numbered_sync<kHandOverThreads>(kHandOver + 2 * i);
                         fence_after();
                         sums(i, v_at, 0, j > 0);
-                        take_over(i, 1);
+                        numbered_sync<kHandOverThreads>(kHandOver + 1 + 2 * i);
                         fence_after();
                         sums(i, v_at, 1, true);
+                        if (i == 0) ok = !__any_sync(~0u, others);
+                        if (!ok) break;
                         if (more) scores(i, k_at);
                         else if (one) commit(bar(kSumsDone + i));
                         __syncwarp();
                     }
-                    next(v_at, v_turn, S::kValueStages);
-                    if (more) next(k_at, k_turn, S::kKeyStages);
+                    next(v_at, S::kValueStages);
+                    if (more) next(k_at, S::kKeyStages);
                 }
                 ok = ok && wait_item(n + 1);
             }
