@@ -173,8 +173,8 @@ typedef struct {
  * order.  A query sees the tokens up to its own: the last `window` of those (all if
  * window is 0) and the first `sinks`.  out and lse are isjl_kv_attend's formulas.
  * starts, lens and table are as isjl_kv_assign leaves them (starts, lens_out), so
- * that a step is assign, append and prompt.  What q, out and lse hold beyond
- * starts[n_rows] is neither read nor written.
+ * that a step is assign, append and prompt.  What q holds beyond starts[n_rows] does
+ * not matter, what out and lse hold there stays.
  *
  * Reported by isjl_kv_status: a row whose starts do not ascend in 0..n_tokens is
  * skipped, its outputs are left as they were; a row with fewer own tokens than

@@ -184,18 +184,33 @@ void *tensor_map_encoder() {
     return fn;
 }
 
+namespace {
+using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+bool encode(void *encoder, CUtensorMap *map, const void *p, int type, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box) {
+    const cuuint32_t steps[5] = {1, 1, 1, 1, 1};
+    return reinterpret_cast<Encode>(encoder)(
+               map, type == ISJL_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void *>(p), dims, strides,
+               box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+}  // namespace
+
 bool encode_cache(void *encoder, CUtensorMap *map, void *p, const int64_t *stride, int rows, int halves, int n_blocks, int shift,
                   int n_kv_heads, int head_dim, int type) {
-    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     const cuuint64_t dims[5] = {64, (cuuint64_t)1 << shift, (cuuint64_t)head_dim / 64, (cuuint64_t)n_kv_heads, (cuuint64_t)n_blocks};
     const cuuint64_t strides[4] = {2 * (cuuint64_t)stride[1], 128, 2 * (cuuint64_t)stride[2], 2 * (cuuint64_t)stride[0]};
-    const cuuint32_t box[5] = {64, (cuuint32_t)rows, (cuuint32_t)halves, 1, 1}, steps[5] = {1, 1, 1, 1, 1};
-    return reinterpret_cast<Encode>(encoder)(
-               map, type == ISJL_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, p, dims, strides, box,
-               steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint32_t box[5] = {64, (cuuint32_t)rows, (cuuint32_t)halves, 1, 1};
+    return encode(encoder, map, p, type, 5, dims, strides, box);
+}
+
+bool encode_queries(void *encoder, CUtensorMap *map, const void *p, const int64_t *stride, int tokens, int heads, int n_tokens, int n_heads,
+                    int head_dim, int type) {
+    const cuuint64_t dims[4] = {64, (cuuint64_t)head_dim / 64, (cuuint64_t)n_heads, (cuuint64_t)n_tokens};
+    const cuuint64_t strides[3] = {128, 2 * (cuuint64_t)stride[1], 2 * (cuuint64_t)stride[0]};
+    const cuuint32_t box[4] = {64, 1, (cuuint32_t)heads, (cuuint32_t)tokens};
+    return encode(encoder, map, p, type, 4, dims, strides, box);
 }
 
 }  // namespace isjl

@@ -194,7 +194,7 @@ struct PromptArgs {
     int32_t n_blocks, shift, n_kv_heads, group;
     // by launch_prompt: rows of a tile for each token, tokens of a tile, and how many such parts a key head's queries make
     int32_t rows_of_token, tokens_of_tile, parts;
-    int32_t q_wide, out_wide;     // rows of q and out lie at multiples of 32 bytes
+    int32_t out_wide;             // rows of out lie at multiples of 32 bytes
     float *part_o;                // [blocks][2][rows of an item][head_dim]: kPromptRows rows an SM
     float2 *part_ml;              // [blocks][2][rows of an item], as the prefix's
     PromptCut *cut;               // [blocks]

@@ -44,10 +44,6 @@ struct Shape {
     static constexpr int kSmem = kGroups * kTileBytes + (kKeyStages + kValueStages) * kTileBytes + 1024;
 };
 
-__device__ __forceinline__ void load32(uint4 &a, uint4 &b, const void *from) {
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(from) : "memory");
-}
 __device__ __forceinline__ void store32(void *to, uint4 a, uint4 b) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"l"(to), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
@@ -81,7 +77,8 @@ enum { kKeyFull = 0, kValueFull = 8, kFree = 4 /* after a stage's full one */, k
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
-prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
+prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+              const __grid_constant__ CUtensorMap vmap) {
     using S = Shape<D>;
     constexpr bool kBf16 = Half<T>::kIsBf16;
     constexpr int kChunks = kKeys / 32;
@@ -107,6 +104,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
 
     start_next();
     if (threadIdx.x == 0) {
+        tma_prefetch(&qmap);
         tma_prefetch(&kmap);
         tma_prefetch(&vmap);
         failed_word = 0;
@@ -119,7 +117,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
         for (int i = 0; i < 2; ++i) {
             bar_init(bar(kScores + i), 1);
             bar_init(bar(kSumsDone + i), 1);
-            bar_init(bar(kQueries + i), 4);
+            bar_init(bar(kQueries + i), 1);
         }
         bar_init(bar(kDrain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -182,30 +180,18 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
         const int token = group * g.tokens_of_tile + row / g.rows_of_token, member = row % g.rows_of_token;
         auto two_of = [&](const Item &x) { return x.tokens > g.tokens_of_tile; };
         auto live_of = [&](const Item &x) { return row / g.rows_of_token < g.tokens_of_tile && member < x.members && token < x.tokens; };
-        // This thread's row of an item's queries, swizzled as the tensor cores read it.  The products with the queries
-        // before it are done when this group has seen their scores.
+        // An item's queries of this row tile: tokens, each with its query heads, are rows one after another.  Rows behind the
+        // item's tokens hold other queries or anything: their results are nobody's.  The products with the queries before
+        // are done when this group has seen their scores.
         auto load_queries = [&](const Item &x) {
-            const bool live = live_of(x);
-            const T *from = static_cast<const T *>(g.a.q) + (int64_t)(x.start + token) * g.a.q_stride[0] + (int64_t)(x.q_head + member) * g.a.q_stride[1];
-            const uint32_t to = q_at + group * S::kTileBytes + row * 128;
-            uint4 w[D / 8];
+            if ((threadIdx.x & 127) == 0) {
+                bar_expect(bar(kQueries + group), S::kHalves * g.tokens_of_tile * g.rows_of_token * 128);
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) w[c] = make_uint4(0, 0, 0, 0);
-            // a row a lane: each load touches a line for each, so the fewer the better
-            if (live && g.q_wide) {
-#pragma unroll
-                for (int c = 0; c < D / 8; c += 2) load32(w[c], w[c + 1], from + 8 * c);
-            } else if (live) {
-#pragma unroll
-                for (int c = 0; c < D / 8; ++c) w[c] = *reinterpret_cast<const uint4 *>(from + 8 * c);
+                for (int half = 0; half < S::kHalves; ++half)
+                    tma_load4(q_at + group * S::kTileBytes + half * S::kHalfBytes, &qmap, bar(kQueries + group), half, x.q_head,
+                              x.start + group * g.tokens_of_tile);
             }
-#pragma unroll
-            for (int c = 0; c < D / 8; ++c)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + c / 8 * S::kHalfBytes + ((c % 8 ^ (row & 7)) << 4)),
-                             "r"(w[c].x), "r"(w[c].y), "r"(w[c].z), "r"(w[c].w) : "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) bar_arrive(bar(kQueries + group));
         };
         uint32_t step = 0;
         int item_no = 0;                           // of this group
@@ -624,8 +610,8 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
 }
 
 template <int D, typename T>
-cudaError_t launch_of(const PromptArgs &g, const CUtensorMap &k, const CUtensorMap &v, int sms, cudaStream_t st) {
-    const cudaError_t e = launch_kernel(prompt_kernel<D, T>, dim3(sms), kThreads, Shape<D>::kSmem, st, false, g, k, v);
+cudaError_t launch_of(const PromptArgs &g, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, int sms, cudaStream_t st) {
+    const cudaError_t e = launch_kernel(prompt_kernel<D, T>, dim3(sms), kThreads, Shape<D>::kSmem, st, false, g, q, k, v);
     if (e != cudaSuccess) return e;
     return launch_kernel(join_kernel<D, T, kGroups * kRows, kRows, kKeys>, dim3(kJoinBlocks * sms), kJoinThreads, 0, st, true, g, sms);
 }
@@ -645,18 +631,17 @@ cudaError_t prepare_prompt(int head_dim, int type) {
 
 cudaError_t launch_prompt(PromptArgs &g, void *encoder, int head_dim, int type, int sms, cudaStream_t st) {
     if (head_dim == 256) return launch_prompt_wide(g, type, sms, st);
-    CUtensorMap k, v;
+    CUtensorMap q, k, v;
     share_rows(g, kRows);
-    auto wide = [](const void *p, const int64_t *stride) { return reinterpret_cast<uintptr_t>(p) % 32 == 0 && (stride[0] | stride[1]) % 16 == 0; };
-    g.q_wide = wide(g.a.q, g.a.q_stride);
-    g.out_wide = wide(g.a.out, g.a.out_stride);
+    g.out_wide = reinterpret_cast<uintptr_t>(g.a.out) % 32 == 0 && (g.a.out_stride[0] | g.a.out_stride[1]) % 16 == 0;
     if (sms > kMostRuns) sms = kMostRuns;
     const int rows = 1 << g.shift < kKeys ? 1 << g.shift : kKeys;
-    if (!encode_cache(encoder, &k, g.cache.k, g.cache.k_stride, rows, 1, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||
+    if (!encode_queries(encoder, &q, g.a.q, g.a.q_stride, g.tokens_of_tile, g.rows_of_token, g.a.n_tokens, g.n_kv_heads * g.group, head_dim, type) ||
+        !encode_cache(encoder, &k, g.cache.k, g.cache.k_stride, rows, 1, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||
         !encode_cache(encoder, &v, g.cache.v, g.cache.v_stride, rows, 1, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type))
         return cudaErrorInvalidValue;
-    if (type == ISJL_KV_BF16) return head_dim == 64 ? launch_of<64, __nv_bfloat16>(g, k, v, sms, st) : launch_of<128, __nv_bfloat16>(g, k, v, sms, st);
-    return head_dim == 64 ? launch_of<64, __half>(g, k, v, sms, st) : launch_of<128, __half>(g, k, v, sms, st);
+    if (type == ISJL_KV_BF16) return head_dim == 64 ? launch_of<64, __nv_bfloat16>(g, q, k, v, sms, st) : launch_of<128, __nv_bfloat16>(g, q, k, v, sms, st);
+    return head_dim == 64 ? launch_of<64, __half>(g, q, k, v, sms, st) : launch_of<128, __half>(g, q, k, v, sms, st);
 }
 
 }  // namespace isjl

@@ -51,6 +51,10 @@ __device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap *map, ui
     asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
                  ::"r"(to), "l"(map), "r"(bar), "r"(0), "r"(slot), "r"(half), "r"(head), "r"(block) : "memory");
 }
+__device__ __forceinline__ void tma_load4(uint32_t to, const CUtensorMap *map, uint32_t bar, int half, int head, int token) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(to), "l"(map), "r"(bar), "r"(0), "r"(half), "r"(head), "r"(token) : "memory");
+}
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
 // Kernels of one call start while the one before them ends; what waits sees all of its predecessor's writes.
@@ -62,6 +66,11 @@ __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontr
 // (always 0), slot, which 64, head, block.  A block number beyond the cache reads as zeros.
 bool encode_cache(void *encoder, CUtensorMap *map, void *p, const int64_t *stride, int rows, int halves, int n_blocks, int shift,
                   int n_kv_heads, int head_dim, int type);
+// A map of queries for copies of `tokens` tokens, each with `heads` heads, and 64 values of those: rows of 128 bytes,
+// tokens outermost, swizzled by 128.  Coordinates: value in the 64 (always 0), which 64, head, token.  What is beyond
+// the last head or token reads as zeros.
+bool encode_queries(void *encoder, CUtensorMap *map, const void *p, const int64_t *stride, int tokens, int heads, int n_tokens, int n_heads,
+                    int head_dim, int type);
 
 // launch, started while the kernel before it in the stream ends (`early`) or after that
 template <typename... Args>
