@@ -238,14 +238,20 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
         delete kv;
         return ISJL_ERR_CUDA;
     }
+    int warps4 = 0;
+    if (isjl::prepare_attend4(cfg->head_dim, cfg->type, cfg->n_q_heads / cfg->n_kv_heads, kv->sms, &warps4) != cudaSuccess) {
+        cudaGetLastError();
+        delete kv;
+        return ISJL_ERR_CUDA;
+    }
     const bool shares = cfg->head_dim <= 128 && cfg->n_q_heads / cfg->n_kv_heads <= 128;
     const size_t sums = rounded(sizeof(int32_t) * (8 + 4 * (size_t)cfg->max_rows));
     const size_t warps = (size_t)kv->per_sm * kv->sms * isjl::kAttendWarps * (shares ? kFiner : 1);
     const int group = cfg->n_q_heads / cfg->n_kv_heads;
     const size_t items = (size_t)queries * cfg->n_kv_heads * ((group + 15) / 16);
-    const size_t cuts = rounded(sizeof(isjl::CutItem) * (items > warps ? items : warps));
-    // pieces of attend's cut items, 32 rows a warp, or of prompt's
-    const size_t cut_rows = std::max((size_t)32 * warps, (size_t)isjl::kPromptRows * kv->sms);
+    const size_t cuts = rounded(sizeof(isjl::CutItem) * std::max({items, warps, (size_t)warps4}));
+    // pieces of attend's and attend4's cut items, 32 rows a warp, or of prompt's
+    const size_t cut_rows = std::max({32 * warps, (size_t)32 * warps4, (size_t)isjl::kPromptRows * kv->sms});
     const size_t ml = rounded(sizeof(float2) * cut_rows), o = sizeof(float) * cfg->head_dim * cut_rows;
     // pieces of the prefix part: an item of 256 rows lies in at most sms / items + 2 blocks; and the own tokens' part
     const size_t pieces = shares ? (size_t)kv->sms * 256 + 3 * (size_t)queries * cfg->n_q_heads : 0;
@@ -360,8 +366,11 @@ isjl_status isjl_kv_attend4(isjl_kv *kv, const isjl_kv_attend_args *a, const isj
     g.shift = kv->shift;
     g.n_kv_heads = kv->cfg.n_kv_heads;
     g.group = kv->cfg.n_q_heads / kv->cfg.n_kv_heads;
+    g.part_o = kv->d_part_o;
+    g.part_ml = kv->d_part_ml;
+    g.cut = kv->d_cut;
     g.status = kv->d_status;
-    return launched(isjl::launch_attend4(g, kv->cfg.head_dim, kv->cfg.type, static_cast<cudaStream_t>(stream)));
+    return launched(isjl::launch_attend4(g, kv->cfg.head_dim, kv->cfg.type, kv->sms, static_cast<cudaStream_t>(stream)));
 }
 
 isjl_status isjl_kv_prompt(isjl_kv *kv, const isjl_kv_prompt_args *a, const isjl_kv_cache *cache, void *stream) {

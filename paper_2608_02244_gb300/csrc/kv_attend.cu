@@ -16,13 +16,13 @@
 // of 8 + 8 heads of 256 values, 2.1 GB: 354 us, 6.1 TB/s.  More than 16 query heads on a key head read it again for
 // each 16: 256 queries of 16 + 1 heads over 8,192 tokens 214 us, of 64 + 1 heads 706.
 #include "kv_ring.cuh"
+#include "kv_sight.cuh"
 #include "kv_tma.cuh"
 
 namespace isjl {
 namespace {
 
-constexpr int kWarps = kAttendWarps, kThreads = 32 * kWarps, kSlice = 32;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kWarps = kAttendWarps, kThreads = 32 * kWarps;
 
 template <int D>
 struct Shape {
@@ -36,45 +36,9 @@ struct Shape {
     static_assert(kWarps * 16 * kJoinRow * 4 <= kRing, "the joined pieces take the ring's place");
 };
 
-// what a query sees: tokens end - window .. end - 1 and 0 .. sinks - 1, counted from the first token that
-// this kernel reads (the prefix's, or the own ones' where the prefix is done elsewhere)
-struct Sight {
-    int32_t end, lo, head;     // head: slices with first tokens that lie before the window's first slice
-    int32_t slices;            // at least 1: an item without tokens still has a result
-    int32_t row;
-};
-
 __device__ __forceinline__ Sight sight(const AttendArgs &g, int t) {
-    const isjl_kv_attend_args &a = g.a;
-    Sight s;
-    const int32_t x = a.lens[t];
-    s.row = a.rows ? a.rows[t] : t;
-    const int32_t prefix = a.n_prefix_blocks << g.shift;
-    const bool bad = x > 0 && s.row >= 0 && (s.row >= a.n_table_rows || ((x - 1) >> g.shift) >= a.table_width);
-    if (bad) report(g.status);
-    s.end = x <= 0 || s.row < 0 || bad ? 0 : x + (g.line.blocks ? 0 : prefix);
-    s.lo = a.window && s.end > a.window ? s.end - a.window : 0;
-    s.head = min((min(a.sinks, s.lo) + kSlice - 1) / kSlice, s.lo / kSlice);
-    s.slices = max(1, s.head + (s.end + kSlice - 1) / kSlice - s.lo / kSlice);
-    return s;
+    return sight_of(g.a, g.shift, g.line.blocks ? 0 : g.a.n_prefix_blocks << g.shift, g.status, t);
 }
-
-// first token of a query's slice
-__device__ __forceinline__ int32_t slice_start(const Sight &s, int i) {
-    return (i < s.head ? i : s.lo / kSlice + i - s.head) * kSlice;
-}
-
-__device__ __forceinline__ float inverse(float total) { return total > 0.f || total != total ? 1.f / total : 0.f; }
-// the logarithm of a sum of exp2, in the natural base
-__device__ __forceinline__ float log_of(float top, float total) {
-    return total > 0.f || total != total ? (top + log2f(total)) * kLn2 : -INFINITY;
-}
-
-// place on the line of slices
-struct Place {
-    int t, h, i;
-    Sight s;
-};
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, Shape<D>::kBlocks)

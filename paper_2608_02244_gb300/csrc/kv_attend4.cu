@@ -1,0 +1,528 @@
+// kv_attend4.cu -- attention of single queries over a paged cache in 4 bits (isjl_kv_attend4).
+//
+// The line of work is kv_attend.cu's: slices of 32 tokens of each query and key head in order, an equal run of them for
+// each warp of the grid.  A slice's codes and scales come by asynchronous copies of 16 bytes through a ring of the warp's
+// own, keys and values in turn.
+//
+// 5 bits a value leave a token and head 160 bytes at 128 values, which the memory brings an SM in 7 cycles: what bounds
+// the work is the instructions from codes to products.  So
+// - both products take the codes as their left operand, tokens (S^T = K Q^T) and values' places (O^T = V^T P^T) as its
+//   rows, and 8 query heads are the columns: nothing is spent on heads that are not there, and 16 heads use the same
+//   operands twice;
+// - which row is which token and which column of the sum which place of a head is free to choose: a thread takes whole
+//   words of eight codes, a shift and one logical instruction makes a pair of them numbers (kv_four.cuh) and one fused
+//   multiplication and addition their values, in the order in which the instruction wants them;
+// - weights go from the first product's layout to the second's by a transposition in the warp (movmatrix).
+#include "kv_four.cuh"
+#include "kv_sight.cuh"
+
+namespace isjl {
+namespace {
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kJoinThreads = 128;
+
+template <int D, int kTiles>
+struct Shape {
+    static constexpr int kCodes = D / 2, kScales = D / 8;          // bytes of a token's key (or value) in one head
+    static constexpr int kChunks = kCodes / 16;                    // of 16 bytes, of its codes
+    static constexpr int kStageBytes = kSlice * (kCodes + kScales);
+    static constexpr int kStages = 5;                              // of a warp's ring: keys or values of a slice
+    static constexpr int kRing = kWarps * kStages * kStageBytes;
+    static constexpr int kBlocks = D == 256 ? 2 : kTiles == 2 ? 3 : 4;      // per SM
+};
+
+__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+template <int kBytes>
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool real) {
+    if (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(real ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(real ? 8 : 0) : "memory");
+}
+
+// Of each eight tokens, the one in row r of a product's operand: with it and `chunk_at` a warp's loads meet no bank twice,
+// by rows (keys) or by pairs of rows (values).
+__device__ __forceinline__ int token_of(int r) { return r ^ ((r >> 1) & 1); }
+// where 16 bytes of a token's codes lie in a stage
+template <int D>
+__device__ __forceinline__ uint32_t chunk_at(int token, int chunk) {
+    if (D == 64) return (token ^ ((token >> 2) & 1)) * 32 + chunk * 16;
+    if (D == 128) return token * 64 + ((chunk ^ ((token >> 1) & 3)) << 4);
+    return token * 128 + ((chunk ^ (token & 7)) << 4);
+}
+
+// kWords neighbouring words of a stage
+template <int kWords>
+__device__ __forceinline__ void load_words(uint32_t (&w)[kWords], uint32_t at) {
+    if constexpr (kWords == 1) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
+    else if constexpr (kWords == 2) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+    else asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+}
+
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+__device__ __forceinline__ Sight sight(const Attend4Args &g, int t) {
+    return sight_of(g.a, g.shift, g.a.n_prefix_blocks << g.shift, g.status, t);
+}
+
+template <int D, typename T, int kTiles>
+__global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4_kernel(const __grid_constant__ Attend4Args g) {
+    using S = Shape<D, kTiles>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    int32_t *before = reinterpret_cast<int32_t *>(smem + S::kRing);                  // [n + 1] slices before a query
+    __shared__ int32_t warp_sum[kWarps];
+    const isjl_kv_attend_args &a = g.a;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int n = a.n, parts = (g.group + 8 * kTiles - 1) / (8 * kTiles), H = g.n_kv_heads * parts, hq = g.n_kv_heads * g.group;
+    const float scale = a.scale * kLog2e;
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // ---- slices before each query
+    {
+        const int per = (n + kThreads - 1) / kThreads;
+        const int begin = min(n, (int)threadIdx.x * per), end = min(n, begin + per);
+        int32_t sum = 0;
+        for (int t = begin; t < end; ++t) {
+            const int32_t k = sight(g, t).slices;
+            before[t] = k;
+            sum += k;
+        }
+        __syncwarp();                // the threads come from loops of different lengths
+        int32_t inc = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int32_t p = __shfl_up_sync(~0u, inc, d);
+            if (lane >= d) inc += p;
+        }
+        if (lane == 31) warp_sum[warp] = inc;
+        __syncthreads();
+        int32_t base = inc - sum;
+        for (int w = 0; w < warp; ++w) base += warp_sum[w];
+        for (int t = begin; t < end; ++t) {
+            const int32_t k = before[t];
+            before[t] = base;
+            base += k;
+        }
+        if (threadIdx.x == kThreads - 1) before[n] = base;
+        __syncthreads();
+    }
+    const int64_t W = (int64_t)before[n] * H;
+    const int64_t C = min((int64_t)gridDim.x * kWarps, W);               // warps with work
+    const int64_t me = (int64_t)blockIdx.x * kWarps + warp;
+    const int64_t f0 = me < C ? W * me / C : W, f1 = me < C ? W * (me + 1) / C : W;
+    if (lane == 0) g.cut[me].t = -1;
+    if (f0 == f1) return;
+
+    auto advance = [&](Place &p) {
+        if (++p.i < p.s.slices) return;
+        p.i = 0;
+        if (++p.h < H) return;
+        p.h = 0;
+        if (++p.t < n) p.s = sight(g, p.t);
+    };
+    Place here;
+    {
+        int lo = 0, hi = n;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((int64_t)before[mid] * H <= f0) lo = mid; else hi = mid;
+        }
+        here.t = lo;
+        here.s = sight(g, lo);
+        const int64_t rest = f0 - (int64_t)before[lo] * H;
+        here.h = (int)(rest / here.s.slices);
+        here.i = (int)(rest - (int64_t)here.h * here.s.slices);
+    }
+
+    // ---- the ring: keys and values of a slice, one stage each
+    const uint32_t ring = smem_at(smem) + warp * S::kStages * S::kStageBytes;
+    const int rows_shift = min(g.shift, 5), slot_mask = (1 << g.shift) - 1;
+    constexpr int32_t kNone = INT32_MIN;
+    // A lane looks up the block of one part of a slice, one slice ahead of the copies that use it.
+    auto block_of = [&](const Place &p) {
+        const int32_t y = slice_start(p.s, p.i) + (lane << rows_shift);
+        if (lane >= kSlice >> rows_shift || y >= p.s.end || (y + (1 << rows_shift) <= p.s.lo && y >= a.sinks)) return kNone;   // nothing is seen of it
+        const int32_t j = y >> g.shift;
+        return j < a.n_prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - a.n_prefix_blocks)];
+    };
+    Place ahead = here;
+    int64_t ahead_left = f1 - f0;                      // slices whose values are still to be asked for
+    bool ahead_values = false;                         // what is next: keys or values
+    int32_t ahead_block = block_of(ahead);
+    auto feed = [&](int stage) {
+        if (ahead_left > 0) {
+            if (!ahead_values && ahead_block != kNone && (uint32_t)ahead_block >= (uint32_t)g.n_blocks) {
+                report(g.status);                      // beyond the cache: zeros
+                ahead_block = kNone;
+            }
+            __syncwarp();
+            const unsigned char *codes = static_cast<const unsigned char *>(ahead_values ? g.cache.v : g.cache.k);
+            const unsigned char *scales = static_cast<const unsigned char *>(ahead_values ? g.cache.v_scale : g.cache.k_scale);
+            const int64_t *cs = ahead_values ? g.cache.v_stride : g.cache.k_stride, *ss = ahead_values ? g.cache.v_scale_stride : g.cache.k_scale_stride;
+            const int kv = ahead.h / parts, slot0 = slice_start(ahead.s, ahead.i) & slot_mask;
+            const uint32_t to = ring + stage * S::kStageBytes;
+            codes += kv * cs[2];
+            scales += 2 * kv * ss[2];
+#pragma unroll
+            for (int i = 0; i < S::kChunks; ++i) {
+                const int id = 32 * i + lane, token = id / S::kChunks, chunk = id % S::kChunks;
+                const int32_t block = __shfl_sync(~0u, ahead_block, token >> rows_shift);
+                const int64_t from = block != kNone ? block * cs[0] + ((slot0 + token) & slot_mask) * cs[1] + 16 * chunk : 0;
+                copy_async<16>(to + chunk_at<D>(token, chunk), codes + from, block != kNone);
+            }
+            {
+                const int32_t block = __shfl_sync(~0u, ahead_block, lane >> rows_shift);
+                const int64_t from = block != kNone ? 2 * (block * ss[0] + ((slot0 + lane) & slot_mask) * ss[1]) : 0;
+                constexpr int kBytes = S::kScales < 16 ? S::kScales : 16;
+#pragma unroll
+                for (int b = 0; b < S::kScales; b += kBytes) copy_async<kBytes>(to + kSlice * S::kCodes + lane * S::kScales + b, scales + from + b, block != kNone);
+            }
+            ahead_values = !ahead_values;
+            if (!ahead_values && --ahead_left > 0) {
+                advance(ahead);
+                ahead_block = block_of(ahead);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < S::kStages - 1; ++i) feed(i);
+    int at_stage = 0;
+    // the next stage of the ring, when it has come; the one before it, which all have read by now, is fed
+    auto next_stage = [&]() {
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
+        __syncwarp();
+        feed(at_stage == 0 ? S::kStages - 1 : at_stage - 1);
+        const uint32_t at = ring + at_stage * S::kStageBytes;
+        if (++at_stage == S::kStages) at_stage = 0;
+        return at;
+    };
+
+    const int r = lane >> 2, c = lane & 3;             // this lane's row of an operand, and its columns 2 c and 2 c + 1
+    constexpr int kKeyWords = D / 32, kKeyLoad = kKeyWords < 4 ? kKeyWords : 4;        // of codes of a token's key: places c D / 4 ..
+    constexpr int kValueWords = D / 64;                                                // of its value: places r D / 8 ..
+    uint32_t q[kTiles][D / 16][2];
+    float o[kTiles][D / 16][4], m[kTiles][2], l[kTiles][2];     // of heads 2 c and 2 c + 1 of each eight
+    int first = 0, live = 0;                           // query heads of the item
+    auto begin_item = [&]() {
+        const int kv = here.h / parts;
+        first = kv * g.group + (here.h - kv * parts) * 8 * kTiles;
+        live = min(8 * kTiles, (kv + 1) * g.group - first);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            m[t][0] = m[t][1] = -INFINITY;
+            l[t][0] = l[t][1] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[t][i][j] = 0.f;
+            // values c D / 4 .. of head r, as the codes come: i and i + 4 of each eight together
+            const bool is = 8 * t + r < live;
+            const T *from = static_cast<const T *>(a.q) + here.t * a.q_stride[0] + (first + 8 * t + r) * a.q_stride[1] + c * (D / 4);
+#pragma unroll
+            for (int w = 0; w < kKeyWords; ++w) {
+                const uint4 x = is ? *reinterpret_cast<const uint4 *>(from + 8 * w) : make_uint4(0, 0, 0, 0);
+                q[t][2 * w][0] = __byte_perm(x.x, x.z, 0x5410);
+                q[t][2 * w][1] = __byte_perm(x.x, x.z, 0x7632);
+                q[t][2 * w + 1][0] = __byte_perm(x.y, x.w, 0x5410);
+                q[t][2 * w + 1][1] = __byte_perm(x.y, x.w, 0x7632);
+            }
+        }
+    };
+
+    auto slice = [&]() {
+        const int32_t x0 = slice_start(here.s, here.i);
+        const uint32_t keys = next_stage();
+        float s[kTiles][2][4] = {};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {                  // sixteen tokens each
+            const int t0 = 16 * h + token_of(r);       // and the one eight further on
+            uint32_t pair[2][kKeyWords / 4 + (kKeyWords < 4)];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) load_words(pair[e], keys + kSlice * S::kCodes + (t0 + 8 * e) * S::kScales + (D == 64 ? c / 2 * 4 : c * (D / 32)));
+#pragma unroll
+            for (int b = 0; b < kKeyWords / kKeyLoad; ++b) {
+                uint32_t w[2][kKeyLoad];
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    load_words(w[e], keys + chunk_at<D>(t0 + 8 * e, D == 64 ? c / 2 : D == 128 ? c : 2 * c + b) + (D == 64 ? c % 2 * 8 : 0));
+                const uint32_t s2[2] = {Four<T>::scale2(pair[0][b]), Four<T>::scale2(pair[1][b])}, b2[2] = {Four<T>::offset2(pair[0][b]), Four<T>::offset2(pair[1][b])};
+#pragma unroll
+                for (int i = 0; i < kKeyLoad; ++i) {
+                    const int k = 2 * (b * kKeyLoad + i);
+                    const uint32_t x[2][4] = {{Four<T>::fma(Four<T>::template ones<0>(w[0][i]), s2[0], b2[0]), Four<T>::fma(Four<T>::template ones<0>(w[1][i]), s2[1], b2[1]),
+                                               Four<T>::fma(Four<T>::template ones<1>(w[0][i]), s2[0], b2[0]), Four<T>::fma(Four<T>::template ones<1>(w[1][i]), s2[1], b2[1])},
+                                              {Four<T>::fma(Four<T>::template ones<2>(w[0][i]), s2[0], b2[0]), Four<T>::fma(Four<T>::template ones<2>(w[1][i]), s2[1], b2[1]),
+                                               Four<T>::fma(Four<T>::template ones<3>(w[0][i]), s2[0], b2[0]), Four<T>::fma(Four<T>::template ones<3>(w[1][i]), s2[1], b2[1])}};
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) {
+                        Half<T>::mma(s[t][h], x[0], q[t][k][0], q[t][k][1]);
+                        Half<T>::mma(s[t][h], x[1], q[t][k + 1][0], q[t][k + 1][1]);
+                    }
+                }
+            }
+        }
+        const bool edge = x0 + kSlice > here.s.end || x0 < here.s.lo;
+        auto hidden = [&](int32_t y) { return y >= here.s.end || (y < here.s.lo && y >= a.sinks); };
+        if (edge) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (hidden(x0 + 16 * h + 8 * e + token_of(r)))
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) s[t][h][2 * e] = s[t][h][2 * e + 1] = -INFINITY;
+        }
+        __syncwarp();
+        // weights are relative to a maximum that may lag behind by kPass: it is looked for only when one is beyond that
+        uint32_t w[kTiles][2][2];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            float top[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) top[j] = fmaxf(fmaxf(s[t][0][j], s[t][0][2 + j]), fmaxf(s[t][1][j], s[t][1][2 + j])) * scale - Grow<T>::kTop;
+            if (__any_sync(~0u, top[0] > m[t][0] + Grow<T>::kPass || top[1] > m[t][1] + Grow<T>::kPass)) {
+                float fix[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(~0u, top[j], d));
+                    const float next = fmaxf(m[t][j], top[j]);
+                    fix[j] = m[t][j] == next ? 1.f : ex2(m[t][j] - next);
+                    m[t][j] = next;
+                    l[t][j] *= fix[j];
+                }
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[t][i][j] *= fix[j & 1];
+            }
+            const float ref[2] = {m[t][0] == -INFINITY ? 0.f : m[t][0], m[t][1] == -INFINITY ? 0.f : m[t][1]};
+            float sum[2] = {0.f, 0.f};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float u = ex2(fmaf(s[t][h][2 * e], scale, -ref[0])), v = ex2(fmaf(s[t][h][2 * e + 1], scale, -ref[1]));
+                    sum[0] += u;
+                    sum[1] += v;
+                    w[t][h][e] = transposed(Half<T>::pack(u, v));
+                }
+            l[t][0] += sum[0];
+            l[t][1] += sum[1];
+        }
+        const uint32_t values = next_stage();
+        if (edge) {
+            // a weight of 0 does not silence an infinite or undefined value: what is not seen stands for 0
+            if (hidden(x0 + lane))
+                for (int b = 0; b < S::kScales; b += 8)
+                    asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(values + kSlice * S::kCodes + lane * S::kScales + b), "r"(0) : "memory");
+            __syncwarp();
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            // this lane's four tokens: two of each eight
+            uint32_t word[4][kValueWords], s2[2], b2[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                uint32_t pair[2][1];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int token = 16 * h + 8 * e + token_of(2 * c + k);
+                    load_words(word[2 * e + k], values + chunk_at<D>(token, D == 64 ? r / 4 : D == 128 ? r / 2 : r) + (D == 64 ? r % 4 * 4 : D == 128 ? r % 2 * 8 : 0));
+                    load_words(pair[k], values + kSlice * S::kCodes + token * S::kScales + (D == 64 ? r / 4 : D == 128 ? r / 2 : r) * 4);
+                }
+                s2[e] = __byte_perm(pair[0][0], pair[1][0], 0x5410);
+                b2[e] = __byte_perm(pair[0][0], pair[1][0], 0x7632);
+            }
+#pragma unroll
+            for (int i = 0; i < kValueWords; ++i)
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {             // places 0 .. 3 and 4 .. 7 of the word
+                    uint32_t y[2], x[2][4];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        y[e] = __byte_perm(word[2 * e][i], word[2 * e + 1][i], part ? 0x7632 : 0x5410);
+                        x[0][2 * e] = Four<T>::fma(Four<T>::template ones<0>(y[e]), s2[e], b2[e]);
+                        x[0][2 * e + 1] = Four<T>::fma(Four<T>::template ones<1>(y[e]), s2[e], b2[e]);
+                        x[1][2 * e] = Four<T>::fma(Four<T>::template ones<2>(y[e]), s2[e], b2[e]);
+                        x[1][2 * e + 1] = Four<T>::fma(Four<T>::template ones<3>(y[e]), s2[e], b2[e]);
+                    }
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) {
+                        Half<T>::mma(o[t][4 * i + 2 * part], x[0], w[t][h][0], w[t][h][1]);
+                        Half<T>::mma(o[t][4 * i + 2 * part + 1], x[1], w[t][h][0], w[t][h][1]);
+                    }
+                }
+        }
+    };
+
+    // the end of an item in this warp's run, or of the run in it
+    auto end_item = [&](bool begins, bool ends) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[t][j] += __shfl_xor_sync(~0u, l[t][j], d);
+                const int row = 8 * t + 2 * c + j;
+                if (row >= live) continue;
+                if (begins && ends) {
+                    const float inv = inverse(l[t][j]);
+                    T *out = static_cast<T *>(a.out) + here.t * a.out_stride[0] + (first + row) * a.out_stride[1] + r * (D / 8);
+#pragma unroll
+                    for (int i = 0; i < D / 64; ++i) {
+                        uint32_t u[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) u[k] = Half<T>::pack(o[t][4 * i + k][j] * inv, o[t][4 * i + k][2 + j] * inv);
+                        *reinterpret_cast<uint4 *>(out + 8 * i) = make_uint4(u[0], u[1], u[2], u[3]);
+                    }
+                    if (r == 0 && a.lse) a.lse[(int64_t)here.t * hq + first + row] = log_of(m[t][j], l[t][j]);
+                } else {
+                    const int64_t at = (me * 2 + begins) * 16 + row;
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i)
+                        *reinterpret_cast<float4 *>(g.part_o + at * D + r * (D / 8) + 4 * i) =
+                            make_float4(o[t][2 * i][j], o[t][2 * i][2 + j], o[t][2 * i + 1][j], o[t][2 * i + 1][2 + j]);
+                    if (r == 0) g.part_ml[at] = make_float2(m[t][j], l[t][j]);
+                }
+            }
+        __syncwarp();
+    };
+
+    begin_item();
+    for (int64_t f = f0; f < f1; ++f) {
+        slice();
+        const bool ends = here.i + 1 == here.s.slices;
+        if (ends || f + 1 == f1) {
+            const int64_t i0 = (int64_t)before[here.t] * H + (int64_t)here.h * here.s.slices;
+            end_item(i0 >= f0, ends);
+            if (!ends && i0 >= f0 && lane == 0)         // its pieces are those of the warps from here on
+                g.cut[me] = {here.t, here.h, (int)me, (int)(((i0 + here.s.slices) * C - 1) / W)};
+        }
+        if (f + 1 < f1) {
+            advance(here);
+            if (here.i == 0) begin_item();
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+// Joins the pieces of the items that runs' ends cut, a block for the warp in whose run one begins.
+template <int D, typename T, int kTiles>
+__global__ void __launch_bounds__(kJoinThreads) join4_kernel(const __grid_constant__ Attend4Args g) {
+    const isjl_kv_attend_args &a = g.a;
+    const int parts = (g.group + 8 * kTiles - 1) / (8 * kTiles), hq = g.n_kv_heads * g.group;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const CutItem item = g.cut[blockIdx.x];
+    if (item.t < 0) return;
+    const int kv = item.h / parts, from = kv * g.group + (item.h - kv * parts) * 8 * kTiles, rows = min(8 * kTiles, (kv + 1) * g.group - from);
+    for (int x = threadIdx.x; x < rows * (D / 4); x += kJoinThreads) {
+        const int row = x / (D / 4), d = (x % (D / 4)) * 4;
+        float top = -INFINITY, total = 0.f;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        constexpr int kBatch = 8;                           // their loads are under way together
+        for (int w0 = item.first; w0 <= item.last; w0 += kBatch) {
+            float2 ml[kBatch];
+            float4 v[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int w = min(w0 + k, item.last);
+                const int64_t at = ((int64_t)w * 2 + (w == item.first)) * 16 + row;
+                ml[k] = g.part_ml[at];
+                v[k] = *reinterpret_cast<const float4 *>(g.part_o + at * D + d);
+            }
+            float next = top;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) next = fmaxf(next, ml[k].x);
+            const float ref = next == -INFINITY ? 0.f : next, fix = ex2(top - ref);
+            top = next;
+            total *= fix;
+            sum.x *= fix;
+            sum.y *= fix;
+            sum.z *= fix;
+            sum.w *= fix;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (w0 + k > item.last) break;
+                const float p = ex2(ml[k].x - ref);
+                total += ml[k].y * p;
+                sum.x += v[k].x * p;
+                sum.y += v[k].y * p;
+                sum.z += v[k].z * p;
+                sum.w += v[k].w * p;
+            }
+        }
+        const float inv = inverse(total);
+        *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + item.t * a.out_stride[0] + (from + row) * a.out_stride[1] + d) =
+            make_uint2(Half<T>::pack(sum.x * inv, sum.y * inv), Half<T>::pack(sum.z * inv, sum.w * inv));
+        if (d == 0 && a.lse) a.lse[(int64_t)item.t * hq + from + row] = log_of(top, total);
+    }
+}
+
+template <int D, int kTiles>
+size_t smem_of(int n) { return Shape<D, kTiles>::kRing + (size_t)(n + 1) * sizeof(int32_t); }
+
+// a kernel's launch, started while the one before it in the stream ends
+template <typename... Args>
+cudaError_t launch_early(void (*kernel)(Args...), int grid, int threads, size_t smem, cudaStream_t st, bool early, const Args &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = early ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int D, typename T, int kTiles>
+cudaError_t launch_of(const Attend4Args &g, int sms, cudaStream_t st) {
+    const int grid = Shape<D, kTiles>::kBlocks * sms;
+    const cudaError_t e = launch_early(attend4_kernel<D, T, kTiles>, grid, kThreads, smem_of<D, kTiles>(g.a.n), st, false, g);
+    if (e != cudaSuccess) return e;
+    return launch_early(join4_kernel<D, T, kTiles>, grid * kWarps, kJoinThreads, 0, st, true, g);
+}
+
+template <int D, typename T, int kTiles>
+cudaError_t prepare_of(int sms, int *warps) {
+    *warps = Shape<D, kTiles>::kBlocks * sms * kWarps;
+    // the limit belongs to the function, not to a handle: always the largest
+    return cudaFuncSetAttribute(attend4_kernel<D, T, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<D, kTiles>(ISJL_KV_MAX_ROWS));
+}
+
+// 8 query heads at a time, or 16 where a key head has more
+template <int D, typename T>
+cudaError_t prepare_tiles(int group, int sms, int *warps) {
+    return group <= 8 ? prepare_of<D, T, 1>(sms, warps) : prepare_of<D, T, 2>(sms, warps);
+}
+template <int D, typename T>
+cudaError_t launch_tiles(const Attend4Args &g, int sms, cudaStream_t st) {
+    return g.group <= 8 ? launch_of<D, T, 1>(g, sms, st) : launch_of<D, T, 2>(g, sms, st);
+}
+
+}  // namespace
+
+cudaError_t prepare_attend4(int head_dim, int type, int group, int sms, int *warps) {
+    if (type == ISJL_KV_BF16)
+        return head_dim == 64 ? prepare_tiles<64, __nv_bfloat16>(group, sms, warps)
+             : head_dim == 128 ? prepare_tiles<128, __nv_bfloat16>(group, sms, warps) : prepare_tiles<256, __nv_bfloat16>(group, sms, warps);
+    return head_dim == 64 ? prepare_tiles<64, __half>(group, sms, warps)
+         : head_dim == 128 ? prepare_tiles<128, __half>(group, sms, warps) : prepare_tiles<256, __half>(group, sms, warps);
+}
+
+cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, int sms, cudaStream_t st) {
+    if (type == ISJL_KV_BF16)
+        return head_dim == 64 ? launch_tiles<64, __nv_bfloat16>(g, sms, st)
+             : head_dim == 128 ? launch_tiles<128, __nv_bfloat16>(g, sms, st) : launch_tiles<256, __nv_bfloat16>(g, sms, st);
+    return head_dim == 64 ? launch_tiles<64, __half>(g, sms, st)
+         : head_dim == 128 ? launch_tiles<128, __half>(g, sms, st) : launch_tiles<256, __half>(g, sms, st);
+}
+
+}  // namespace isjl

@@ -56,6 +56,12 @@ struct Half<__half> {
     }
 };
 
+// log2 of the growth of a maximum that is let pass, and of the largest weight of the tile that set it
+template <typename T>
+struct Grow {
+    static constexpr float kPass = Half<T>::kIsBf16 ? 8.f : 4.f, kTop = Half<T>::kTop > 0 ? Half<T>::kTop - kPass : 0.f;
+};
+
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -165,21 +171,26 @@ struct AttendArgs {
                                   // [kAttendWarps * grid], or with a prefix all items [n * key heads (parts of them)]
     int32_t *status;
 };
-// ---- attend4, one warp's dot products (kv_simple.cu)
-struct Attend4Args {
-    isjl_kv_attend_args a;
-    isjl_kv_cache4 cache;
-    int32_t n_blocks, shift, n_kv_heads, group;
-    int32_t *status;
-};
-cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, cudaStream_t st);
-
 size_t attend_smem(int head_dim, int n);
 // once for a shape, before its first launch: blocks that fit an SM, and the most queries of a call with which they do
 // (with more, one block less fits: each holds 4 bytes a query)
 cudaError_t prepare_attend(int head_dim, int type, int *blocks, int *queries);
 cudaError_t launch_attend(const AttendArgs &g, void *encoder, int head_dim, int type, int grid, cudaStream_t st);
 
+
+// ---- attend4 (kv_attend4.cu)
+struct Attend4Args {
+    isjl_kv_attend_args a;
+    isjl_kv_cache4 cache;
+    int32_t n_blocks, shift, n_kv_heads, group;
+    float *part_o;                // [warps][2][16][head_dim] pieces of (query, key head) items: one that began earlier, one
+    float2 *part_ml;              // [warps][2][16]           that goes on
+    CutItem *cut;                 // [warps] items that begin in a warp's run and are cut by its end
+    int32_t *status;
+};
+// once for a shape, before its first launch; warps: most of a call
+cudaError_t prepare_attend4(int head_dim, int type, int group, int sms, int *warps);
+cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, int sms, cudaStream_t st);
 
 // ---- prompt (kv_prompt.cu; heads of 256 values: kv_prompt_wide.cu)
 // an item that the end of its block's run cuts; the blocks up to `last` have a piece of it

@@ -5,12 +5,6 @@
 
 namespace isjl {
 
-// log2 of the growth of a maximum that is let pass, and of the largest weight of the tile that set it
-template <typename T>
-struct Grow {
-    static constexpr float kPass = Half<T>::kIsBf16 ? 8.f : 4.f, kTop = Half<T>::kTop > 0 ? Half<T>::kTop - kPass : 0.f;
-};
-
 // shared-memory operand with rows of 128 bytes, swizzled by 128 bytes
 __device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t leading, uint32_t stride) {
     return (uint64_t)((at >> 4) & 0x3fff) | ((uint64_t)((leading >> 4) & 0x3fff) << 16) |
