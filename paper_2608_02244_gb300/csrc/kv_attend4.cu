@@ -19,7 +19,7 @@
 namespace isjl {
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kJoinThreads = 128;
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kJoinThreads = 256;
 
 template <int D, int kTiles>
 struct Shape {
@@ -137,48 +137,57 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         here.i = (int)(rest - (int64_t)here.h * here.s.slices);
     }
 
-    // ---- the ring: keys and values of a slice, one stage each
+    // ---- the ring: keys and values of a slice, one stage each.  A slice is four times eight tokens, each eight in one
+    // block; of the first sixteen lanes each finds where one kind (keys' codes and scales, values' codes and scales) of
+    // one eight lies, and looks up its block a slice ahead of that.
     const uint32_t ring = smem_at(smem) + warp * S::kStages * S::kStageBytes;
-    const int rows_shift = min(g.shift, 5), slot_mask = (1 << g.shift) - 1;
+    const int slot_mask = (1 << g.shift) - 1, kind = (lane >> 2) & 3;
     constexpr int32_t kNone = INT32_MIN;
-    // A lane looks up the block of one part of a slice, one slice ahead of the copies that use it.
     auto block_of = [&](const Place &p) {
-        const int32_t y = slice_start(p.s, p.i) + (lane << rows_shift);
-        if (lane >= kSlice >> rows_shift || y >= p.s.end || (y + (1 << rows_shift) <= p.s.lo && y >= a.sinks)) return kNone;   // nothing is seen of it
+        const int32_t y = slice_start(p.s, p.i) + 8 * (lane & 3);
+        if (y >= p.s.end || (y + 8 <= p.s.lo && y >= a.sinks)) return kNone;           // nothing is seen of it
         const int32_t j = y >> g.shift;
         return j < a.n_prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - a.n_prefix_blocks)];
     };
+    const unsigned char *const kind_base = static_cast<const unsigned char *>(kind == 0 ? g.cache.k : kind == 1 ? g.cache.k_scale : kind == 2 ? g.cache.v : g.cache.v_scale);
+    const int64_t *const kind_stride = kind == 0 ? g.cache.k_stride : kind == 1 ? g.cache.k_scale_stride : kind == 2 ? g.cache.v_stride : g.cache.v_scale_stride;
     Place ahead = here;
-    int64_t ahead_left = f1 - f0;                      // slices whose values are still to be asked for
+    int ahead_left = (int)(f1 - f0);                   // slices whose values are still to be asked for
     bool ahead_values = false;                         // what is next: keys or values
     int32_t ahead_block = block_of(ahead);
+    const unsigned char *eight = nullptr;              // this lane's kind of its eight tokens
+    constexpr int kRows = 32 / S::kChunks;             // tokens that one copy of all lanes brings codes of
+    const uint32_t copy_to = chunk_at<D>(lane / S::kChunks, lane % S::kChunks);
     auto feed = [&](int stage) {
         if (ahead_left > 0) {
-            if (!ahead_values && ahead_block != kNone && (uint32_t)ahead_block >= (uint32_t)g.n_blocks) {
-                report(g.status);                      // beyond the cache: zeros
-                ahead_block = kNone;
+            if (!ahead_values) {
+                bool there = ahead_block != kNone;
+                if (there && (uint32_t)ahead_block >= (uint32_t)g.n_blocks) {
+                    report(g.status);                  // beyond the cache: zeros
+                    there = false;
+                }
+                const int slot = (slice_start(ahead.s, ahead.i) + 8 * (lane & 3)) & slot_mask;
+                const int64_t at = ahead_block * kind_stride[0] + slot * kind_stride[1] + ahead.h / parts * kind_stride[2];
+                eight = there ? kind_base + at * (kind & 1 ? 2 : 1) : nullptr;
+                __syncwarp();
             }
-            __syncwarp();
-            const unsigned char *codes = static_cast<const unsigned char *>(ahead_values ? g.cache.v : g.cache.k);
-            const unsigned char *scales = static_cast<const unsigned char *>(ahead_values ? g.cache.v_scale : g.cache.k_scale);
-            const int64_t *cs = ahead_values ? g.cache.v_stride : g.cache.k_stride, *ss = ahead_values ? g.cache.v_scale_stride : g.cache.k_scale_stride;
-            const int kv = ahead.h / parts, slot0 = slice_start(ahead.s, ahead.i) & slot_mask;
+            const int64_t code_stride = (ahead_values ? g.cache.v_stride : g.cache.k_stride)[1], scale_stride = (ahead_values ? g.cache.v_scale_stride : g.cache.k_scale_stride)[1];
             const uint32_t to = ring + stage * S::kStageBytes;
-            codes += kv * cs[2];
-            scales += 2 * kv * ss[2];
+            const int64_t code_off = lane / S::kChunks % 8 * code_stride + lane % S::kChunks * 16;
+            const int from_lane = ahead_values * 8;
 #pragma unroll
             for (int i = 0; i < S::kChunks; ++i) {
-                const int id = 32 * i + lane, token = id / S::kChunks, chunk = id % S::kChunks;
-                const int32_t block = __shfl_sync(~0u, ahead_block, token >> rows_shift);
-                const int64_t from = block != kNone ? block * cs[0] + ((slot0 + token) & slot_mask) * cs[1] + 16 * chunk : 0;
-                copy_async<16>(to + chunk_at<D>(token, chunk), codes + from, block != kNone);
+                const int which = kRows == 16 ? 2 * i + (lane >> 4) : kRows * i / 8;
+                const unsigned char *from = reinterpret_cast<const unsigned char *>(__shfl_sync(~0u, reinterpret_cast<int64_t>(eight), from_lane + which));
+                const int64_t off = code_off + (kRows == 4 && i % 2 ? 4 * code_stride : 0);
+                copy_async<16>(to + (kRows == 4 && i % 2 ? copy_to ^ 64 : copy_to) + i * kRows * S::kCodes, from ? from + off : kind_base, from != nullptr);
             }
             {
-                const int32_t block = __shfl_sync(~0u, ahead_block, lane >> rows_shift);
-                const int64_t from = block != kNone ? 2 * (block * ss[0] + ((slot0 + lane) & slot_mask) * ss[1]) : 0;
+                const unsigned char *from = reinterpret_cast<const unsigned char *>(__shfl_sync(~0u, reinterpret_cast<int64_t>(eight), from_lane + 4 + (lane >> 3)));
+                const unsigned char *at = from ? from + 2 * ((lane & 7) * scale_stride) : kind_base;
                 constexpr int kBytes = S::kScales < 16 ? S::kScales : 16;
 #pragma unroll
-                for (int b = 0; b < S::kScales; b += kBytes) copy_async<kBytes>(to + kSlice * S::kCodes + lane * S::kScales + b, scales + from + b, block != kNone);
+                for (int b = 0; b < S::kScales; b += kBytes) copy_async<kBytes>(to + kSlice * S::kCodes + lane * S::kScales + b, at + b, from != nullptr);
             }
             ahead_values = !ahead_values;
             if (!ahead_values && --ahead_left > 0) {
@@ -204,6 +213,12 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     const int r = lane >> 2, c = lane & 3;             // this lane's row of an operand, and its columns 2 c and 2 c + 1
     constexpr int kKeyWords = D / 32, kKeyLoad = kKeyWords < 4 ? kKeyWords : 4;        // of codes of a token's key: places c D / 4 ..
     constexpr int kValueWords = D / 64;                                                // of its value: places r D / 8 ..
+    // where this lane's part of the first of each eight tokens' rows is: a key's, and a value's of two tokens
+    const uint32_t key_at = chunk_at<D>(token_of(r), D == 64 ? c / 2 : D == 128 ? c : 2 * c) + (D == 64 ? c % 2 * 8 : 0);
+    const uint32_t key_scale_at = kSlice * S::kCodes + token_of(r) * S::kScales + (D == 64 ? c / 2 * 4 : c * (D / 32));
+    const int value_chunk = D == 64 ? r / 4 : D == 128 ? r / 2 : r, value_rest = D == 64 ? r % 4 * 4 : D == 128 ? r % 2 * 8 : 0;
+    const uint32_t value_at[2] = {chunk_at<D>(token_of(2 * c), value_chunk) + value_rest, chunk_at<D>(token_of(2 * c + 1), value_chunk) + value_rest};
+    const uint32_t value_scale_at[2] = {kSlice * S::kCodes + token_of(2 * c) * S::kScales + value_chunk * 4u, kSlice * S::kCodes + token_of(2 * c + 1) * S::kScales + value_chunk * 4u};
     uint32_t q[kTiles][D / 16][2];
     float o[kTiles][D / 16][4], m[kTiles][2], l[kTiles][2];     // of heads 2 c and 2 c + 1 of each eight
     int first = 0, live = 0;                           // query heads of the item
@@ -239,16 +254,15 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         float s[kTiles][2][4] = {};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {                  // sixteen tokens each
-            const int t0 = 16 * h + token_of(r);       // and the one eight further on
             uint32_t pair[2][kKeyWords / 4 + (kKeyWords < 4)];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) load_words(pair[e], keys + kSlice * S::kCodes + (t0 + 8 * e) * S::kScales + (D == 64 ? c / 2 * 4 : c * (D / 32)));
+            for (int e = 0; e < 2; ++e) load_words(pair[e], keys + key_scale_at + (16 * h + 8 * e) * S::kScales);
 #pragma unroll
             for (int b = 0; b < kKeyWords / kKeyLoad; ++b) {
                 uint32_t w[2][kKeyLoad];
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                    load_words(w[e], keys + chunk_at<D>(t0 + 8 * e, D == 64 ? c / 2 : D == 128 ? c : 2 * c + b) + (D == 64 ? c % 2 * 8 : 0));
+                    load_words(w[e], keys + (b ? key_at ^ 16 : key_at) + (16 * h + 8 * e) * S::kCodes);
                 const uint32_t s2[2] = {Four<T>::scale2(pair[0][b]), Four<T>::scale2(pair[1][b])}, b2[2] = {Four<T>::offset2(pair[0][b]), Four<T>::offset2(pair[1][b])};
 #pragma unroll
                 for (int i = 0; i < kKeyLoad; ++i) {
@@ -331,9 +345,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
                 uint32_t pair[2][1];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const int token = 16 * h + 8 * e + token_of(2 * c + k);
-                    load_words(word[2 * e + k], values + chunk_at<D>(token, D == 64 ? r / 4 : D == 128 ? r / 2 : r) + (D == 64 ? r % 4 * 4 : D == 128 ? r % 2 * 8 : 0));
-                    load_words(pair[k], values + kSlice * S::kCodes + token * S::kScales + (D == 64 ? r / 4 : D == 128 ? r / 2 : r) * 4);
+                    load_words(word[2 * e + k], values + value_at[k] + (16 * h + 8 * e) * S::kCodes);
+                    load_words(pair[k], values + value_scale_at[k] + (16 * h + 8 * e) * S::kScales);
                 }
                 s2[e] = __byte_perm(pair[0][0], pair[1][0], 0x5410);
                 b2[e] = __byte_perm(pair[0][0], pair[1][0], 0x7632);
@@ -420,42 +433,65 @@ __global__ void __launch_bounds__(kJoinThreads) join4_kernel(const __grid_consta
     const CutItem item = g.cut[blockIdx.x];
     if (item.t < 0) return;
     const int kv = item.h / parts, from = kv * g.group + (item.h - kv * parts) * 8 * kTiles, rows = min(8 * kTiles, (kv + 1) * g.group - from);
-    for (int x = threadIdx.x; x < rows * (D / 4); x += kJoinThreads) {
+    // where few rows have many pieces, several threads share them
+    constexpr int kBatch = 8;                               // pieces whose loads are under way together
+    __shared__ float4 part_sum[kJoinThreads];
+    __shared__ float2 part_ml[kJoinThreads];
+    const int units = rows * (D / 4), pieces = item.last - item.first + 1;
+    const int shares = max(1, min(kJoinThreads / units, (pieces + kBatch - 1) / kBatch)), per = (pieces + shares - 1) / shares;
+    for (int x0 = 0; x0 < units; x0 += kJoinThreads) {
+        const int x = x0 + (units < kJoinThreads ? threadIdx.x % units : threadIdx.x), share = units < kJoinThreads ? threadIdx.x / units : 0;
         const int row = x / (D / 4), d = (x % (D / 4)) * 4;
         float top = -INFINITY, total = 0.f;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        constexpr int kBatch = 8;                           // their loads are under way together
-        for (int w0 = item.first; w0 <= item.last; w0 += kBatch) {
-            float2 ml[kBatch];
-            float4 v[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                const int w = min(w0 + k, item.last);
-                const int64_t at = ((int64_t)w * 2 + (w == item.first)) * 16 + row;
-                ml[k] = g.part_ml[at];
-                v[k] = *reinterpret_cast<const float4 *>(g.part_o + at * D + d);
-            }
-            float next = top;
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) next = fmaxf(next, ml[k].x);
-            const float ref = next == -INFINITY ? 0.f : next, fix = ex2(top - ref);
+        auto add = [&](float2 ml, float4 v) {               // relative to top
+            const float p = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+            total += ml.y * p;
+            sum.x += v.x * p;
+            sum.y += v.y * p;
+            sum.z += v.z * p;
+            sum.w += v.w * p;
+        };
+        auto raise = [&](float next) {
+            const float fix = next == top ? 1.f : ex2(top - next);
             top = next;
             total *= fix;
             sum.x *= fix;
             sum.y *= fix;
             sum.z *= fix;
             sum.w *= fix;
+        };
+        const int last = min(item.last, item.first + (share + 1) * per - 1);
+        if (x < units && share < shares)
+            for (int w0 = item.first + share * per; w0 <= last; w0 += kBatch) {
+                float2 ml[kBatch];
+                float4 v[kBatch];
 #pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                if (w0 + k > item.last) break;
-                const float p = ex2(ml[k].x - ref);
-                total += ml[k].y * p;
-                sum.x += v[k].x * p;
-                sum.y += v[k].y * p;
-                sum.z += v[k].z * p;
-                sum.w += v[k].w * p;
+                for (int k = 0; k < kBatch; ++k) {
+                    const int w = min(w0 + k, last);
+                    const int64_t at = ((int64_t)w * 2 + (w == item.first)) * 16 + row;
+                    ml[k] = g.part_ml[at];
+                    v[k] = *reinterpret_cast<const float4 *>(g.part_o + at * D + d);
+                }
+                float next = top;
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) next = fmaxf(next, ml[k].x);
+                raise(next);
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k)
+                    if (w0 + k <= last) add(ml[k], v[k]);
             }
+        if (shares > 1) {                                   // the same for the whole block, and then all units lie in it
+            part_sum[threadIdx.x] = sum;
+            part_ml[threadIdx.x] = make_float2(top, total);
+            __syncthreads();
+            if (share > 0) return;
+            float next = top;
+            for (int k = 1; k < shares; ++k) next = fmaxf(next, part_ml[k * units + threadIdx.x].x);
+            raise(next);
+            for (int k = 1; k < shares; ++k) add(part_ml[k * units + threadIdx.x], part_sum[k * units + threadIdx.x]);
         }
+        if (x >= units || share > 0) continue;
         const float inv = inverse(total);
         *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + item.t * a.out_stride[0] + (from + row) * a.out_stride[1] + d) =
             make_uint2(Half<T>::pack(sum.x * inv, sum.y * inv), Half<T>::pack(sum.z * inv, sum.w * inv));
