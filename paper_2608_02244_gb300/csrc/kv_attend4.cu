@@ -16,6 +16,8 @@
 #include "kv_four.cuh"
 #include "kv_sight.cuh"
 
+#include <type_traits>
+
 namespace isjl {
 namespace {
 
@@ -27,6 +29,7 @@ struct Shape {
     static constexpr int kChunks = kCodes / 16;                    // of 16 bytes, of its codes
     static constexpr int kStageBytes = kSlice * (kCodes + kScales);
     static constexpr int kStages = 5;                              // of a warp's ring: keys or values of a slice
+    static_assert(kStages % 2 == 1, "a slice's keys and values are under way together");
     static constexpr int kRing = kWarps * kStages * kStageBytes;
     static constexpr int kBlocks = D == 256 ? 2 : kTiles == 2 ? 3 : 4;      // per SM
 };
@@ -58,6 +61,12 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[kWords], uint32_t at) {
     else asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
 }
 
+__device__ __forceinline__ const unsigned char *load_pointer(uint32_t at) {
+    uint64_t p;
+    asm volatile("ld.shared.b64 %0, [%1];" : "=l"(p) : "r"(at) : "memory");
+    return reinterpret_cast<const unsigned char *>(p);
+}
+
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     uint32_t y;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -68,12 +77,19 @@ __device__ __forceinline__ Sight sight(const Attend4Args &g, int t) {
     return sight_of(g.a, g.shift, g.a.n_prefix_blocks << g.shift, g.status, t);
 }
 
+// place on the line of slices, with its first token
+struct At : Place {
+    int32_t x, kv;
+};
+
 template <int D, typename T, int kTiles>
 __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4_kernel(const __grid_constant__ Attend4Args g) {
     using S = Shape<D, kTiles>;
     extern __shared__ __align__(128) unsigned char smem[];
     int32_t *before = reinterpret_cast<int32_t *>(smem + S::kRing);                  // [n + 1] slices before a query
     __shared__ int32_t warp_sum[kWarps];
+    __shared__ const unsigned char *eight_at[kWarps][16];
+    __shared__ int64_t eight_stride[kWarps][4][3];
     const isjl_kv_attend_args &a = g.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n = a.n, parts = (g.group + 8 * kTiles - 1) / (8 * kTiles), H = g.n_kv_heads * parts, hq = g.n_kv_heads * g.group;
@@ -116,14 +132,21 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     if (lane == 0) g.cut[me].t = -1;
     if (f0 == f1) return;
 
-    auto advance = [&](Place &p) {
-        if (++p.i < p.s.slices) return;
-        p.i = 0;
-        if (++p.h < H) return;
-        p.h = 0;
-        if (++p.t < n) p.s = sight(g, p.t);
+    auto locate = [&](At &p) {
+        p.kv = p.h / parts;
+        p.x = slice_start(p.s, p.i);
     };
-    Place here;
+    auto advance = [&](At &p) {
+        p.x = ++p.i == p.s.head ? p.s.lo / kSlice * kSlice : p.x + kSlice;
+        if (p.i < p.s.slices) return;
+        p.i = 0;
+        if (++p.h >= H) {
+            p.h = 0;
+            if (++p.t < n) p.s = sight(g, p.t);
+        }
+        locate(p);
+    };
+    At here;
     {
         int lo = 0, hi = n;
         while (hi - lo > 1) {
@@ -135,6 +158,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         const int64_t rest = f0 - (int64_t)before[lo] * H;
         here.h = (int)(rest / here.s.slices);
         here.i = (int)(rest - (int64_t)here.h * here.s.slices);
+        locate(here);
     }
 
     // ---- the ring: keys and values of a slice, one stage each.  A slice is four times eight tokens, each eight in one
@@ -143,54 +167,66 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     const uint32_t ring = smem_at(smem) + warp * S::kStages * S::kStageBytes;
     const int slot_mask = (1 << g.shift) - 1, kind = (lane >> 2) & 3;
     constexpr int32_t kNone = INT32_MIN;
-    auto block_of = [&](const Place &p) {
-        const int32_t y = slice_start(p.s, p.i) + 8 * (lane & 3);
+    auto block_of = [&](const At &p) {
+        const int32_t y = p.x + 8 * (lane & 3);
         if (y >= p.s.end || (y + 8 <= p.s.lo && y >= a.sinks)) return kNone;           // nothing is seen of it
         const int32_t j = y >> g.shift;
         return j < a.n_prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - a.n_prefix_blocks)];
     };
     const unsigned char *const kind_base = static_cast<const unsigned char *>(kind == 0 ? g.cache.k : kind == 1 ? g.cache.k_scale : kind == 2 ? g.cache.v : g.cache.v_scale);
-    const int64_t *const kind_stride = kind == 0 ? g.cache.k_stride : kind == 1 ? g.cache.k_scale_stride : kind == 2 ? g.cache.v_stride : g.cache.v_scale_stride;
-    Place ahead = here;
+    if (lane < 16 && (lane & 3) == 0)
+        for (int i = 0; i < 3; ++i)                    // in bytes
+            eight_stride[warp][kind][i] = (kind == 0 ? g.cache.k_stride : kind == 1 ? g.cache.k_scale_stride : kind == 2 ? g.cache.v_stride : g.cache.v_scale_stride)[i] << (kind & 1);
+    __syncwarp();
+    At ahead = here;
     int ahead_left = (int)(f1 - f0);                   // slices whose values are still to be asked for
-    bool ahead_values = false;                         // what is next: keys or values
     int32_t ahead_block = block_of(ahead);
-    const unsigned char *eight = nullptr;              // this lane's kind of its eight tokens
+    uint32_t ahead_there = 0;                          // which of its eights are read: the others are zeros
     constexpr int kRows = 32 / S::kChunks;             // tokens that one copy of all lanes brings codes of
-    const uint32_t copy_to = chunk_at<D>(lane / S::kChunks, lane % S::kChunks);
-    auto feed = [&](int stage) {
+    const uint32_t copy_to = ring + chunk_at<D>(lane / S::kChunks, lane % S::kChunks);
+    const int64_t code_off[2] = {lane / S::kChunks % 8 * g.cache.k_stride[1] + lane % S::kChunks * 16, lane / S::kChunks % 8 * g.cache.v_stride[1] + lane % S::kChunks * 16};
+    const int64_t scale_off[2] = {2 * (lane & 7) * g.cache.k_scale_stride[1], 2 * (lane & 7) * g.cache.v_scale_stride[1]};
+    const uint32_t eights = smem_at(eight_at[warp]);
+    auto copies = [&](uint32_t stage, auto values, auto all) {
+        constexpr int v = decltype(values)::value;
+        const int64_t half = 4 * (v ? g.cache.v_stride : g.cache.k_stride)[1];
+#pragma unroll
+        for (int i = 0; i < S::kChunks; ++i) {
+            const uint32_t which = kRows == 16 ? 2 * i + (lane >> 4) : kRows * i / 8;
+            copy_async<16>((copy_to + stage + i * kRows * S::kCodes) ^ (kRows == 4 && i % 2 ? 64 : 0), load_pointer(eights + (8 * v + which) * 8) + code_off[v] + (kRows == 4 && i % 2 ? half : 0),
+                           decltype(all)::value || ahead_there >> which & 1);
+        }
+        const uint32_t which = lane >> 3;
+        const unsigned char *from = load_pointer(eights + (8 * v + 4 + which) * 8) + scale_off[v];
+        constexpr int kBytes = S::kScales < 16 ? S::kScales : 16;
+#pragma unroll
+        for (int b = 0; b < S::kScales; b += kBytes)
+            copy_async<kBytes>(ring + stage + kSlice * S::kCodes + lane * S::kScales + b, from + b, decltype(all)::value || ahead_there >> which & 1);
+    };
+    auto feed_keys = [&](uint32_t stage) {
         if (ahead_left > 0) {
-            if (!ahead_values) {
-                bool there = ahead_block != kNone;
-                if (there && (uint32_t)ahead_block >= (uint32_t)g.n_blocks) {
-                    report(g.status);                  // beyond the cache: zeros
-                    there = false;
-                }
-                const int slot = (slice_start(ahead.s, ahead.i) + 8 * (lane & 3)) & slot_mask;
-                const int64_t at = ahead_block * kind_stride[0] + slot * kind_stride[1] + ahead.h / parts * kind_stride[2];
-                eight = there ? kind_base + at * (kind & 1 ? 2 : 1) : nullptr;
-                __syncwarp();
+            bool there = ahead_block != kNone;
+            if (there && (uint32_t)ahead_block >= (uint32_t)g.n_blocks) {
+                report(g.status);                      // beyond the cache: zeros
+                there = false;
             }
-            const int64_t code_stride = (ahead_values ? g.cache.v_stride : g.cache.k_stride)[1], scale_stride = (ahead_values ? g.cache.v_scale_stride : g.cache.k_scale_stride)[1];
-            const uint32_t to = ring + stage * S::kStageBytes;
-            const int64_t code_off = lane / S::kChunks % 8 * code_stride + lane % S::kChunks * 16;
-            const int from_lane = ahead_values * 8;
-#pragma unroll
-            for (int i = 0; i < S::kChunks; ++i) {
-                const int which = kRows == 16 ? 2 * i + (lane >> 4) : kRows * i / 8;
-                const unsigned char *from = reinterpret_cast<const unsigned char *>(__shfl_sync(~0u, reinterpret_cast<int64_t>(eight), from_lane + which));
-                const int64_t off = code_off + (kRows == 4 && i % 2 ? 4 * code_stride : 0);
-                copy_async<16>(to + (kRows == 4 && i % 2 ? copy_to ^ 64 : copy_to) + i * kRows * S::kCodes, from ? from + off : kind_base, from != nullptr);
+            if (lane < 16) {
+                const int slot = (ahead.x + 8 * (lane & 3)) & slot_mask;
+                const int64_t *stride = eight_stride[warp][kind];
+                eight_at[warp][lane] = kind_base + (there ? ahead_block * stride[0] + slot * stride[1] + ahead.kv * stride[2] : 0);
             }
-            {
-                const unsigned char *from = reinterpret_cast<const unsigned char *>(__shfl_sync(~0u, reinterpret_cast<int64_t>(eight), from_lane + 4 + (lane >> 3)));
-                const unsigned char *at = from ? from + 2 * ((lane & 7) * scale_stride) : kind_base;
-                constexpr int kBytes = S::kScales < 16 ? S::kScales : 16;
-#pragma unroll
-                for (int b = 0; b < S::kScales; b += kBytes) copy_async<kBytes>(to + kSlice * S::kCodes + lane * S::kScales + b, at + b, from != nullptr);
-            }
-            ahead_values = !ahead_values;
-            if (!ahead_values && --ahead_left > 0) {
+            ahead_there = __ballot_sync(~0u, there) & 15;
+            __syncwarp();
+            if (ahead_there == 15) copies(stage, std::false_type(), std::true_type());
+            else copies(stage, std::false_type(), std::false_type());
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto feed_values = [&](uint32_t stage) {
+        if (ahead_left > 0) {
+            if (ahead_there == 15) copies(stage, std::true_type(), std::true_type());
+            else copies(stage, std::true_type(), std::false_type());
+            if (--ahead_left > 0) {
                 advance(ahead);
                 ahead_block = block_of(ahead);
             }
@@ -198,15 +234,22 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
-    for (int i = 0; i < S::kStages - 1; ++i) feed(i);
-    int at_stage = 0;
-    // the next stage of the ring, when it has come; the one before it, which all have read by now, is fed
-    auto next_stage = [&]() {
+    for (int i = 0; i < S::kStages - 1; i += 2) {
+        feed_keys(i * S::kStageBytes);
+        feed_values((i + 1) * S::kStageBytes);
+        __syncwarp();
+    }
+    uint32_t at_stage = 0;
+    // the next stage of the ring, when it has come; the one before it, which all have read by now, is fed: when keys are
+    // taken with keys, as an even number of stages is under way
+    auto next_stage = [&](auto values) {
         asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
         __syncwarp();
-        feed(at_stage == 0 ? S::kStages - 1 : at_stage - 1);
-        const uint32_t at = ring + at_stage * S::kStageBytes;
-        if (++at_stage == S::kStages) at_stage = 0;
+        const uint32_t last = (at_stage == 0 ? S::kStages * S::kStageBytes : at_stage) - S::kStageBytes;
+        if (decltype(values)::value) feed_values(last);
+        else feed_keys(last);
+        const uint32_t at = ring + at_stage;
+        at_stage = at_stage == (S::kStages - 1) * S::kStageBytes ? 0 : at_stage + S::kStageBytes;
         return at;
     };
 
@@ -223,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     float o[kTiles][D / 16][4], m[kTiles][2], l[kTiles][2];     // of heads 2 c and 2 c + 1 of each eight
     int first = 0, live = 0;                           // query heads of the item
     auto begin_item = [&]() {
-        const int kv = here.h / parts;
+        const int kv = here.kv;
         first = kv * g.group + (here.h - kv * parts) * 8 * kTiles;
         live = min(8 * kTiles, (kv + 1) * g.group - first);
 #pragma unroll
@@ -249,8 +292,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     };
 
     auto slice = [&]() {
-        const int32_t x0 = slice_start(here.s, here.i);
-        const uint32_t keys = next_stage();
+        const int32_t x0 = here.x;
+        const uint32_t keys = next_stage(std::false_type());
         float s[kTiles][2][4] = {};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {                  // sixteen tokens each
@@ -328,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
             l[t][0] += sum[0];
             l[t][1] += sum[1];
         }
-        const uint32_t values = next_stage();
+        const uint32_t values = next_stage(std::true_type());
         if (edge) {
             // a weight of 0 does not silence an infinite or undefined value: what is not seen stands for 0
             if (hidden(x0 + lane))
@@ -407,16 +450,16 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     };
 
     begin_item();
-    for (int64_t f = f0; f < f1; ++f) {
+    for (int left = (int)(f1 - f0); left > 0; --left) {
         slice();
         const bool ends = here.i + 1 == here.s.slices;
-        if (ends || f + 1 == f1) {
+        if (ends || left == 1) {
             const int64_t i0 = (int64_t)before[here.t] * H + (int64_t)here.h * here.s.slices;
             end_item(i0 >= f0, ends);
             if (!ends && i0 >= f0 && lane == 0)         // its pieces are those of the warps from here on
                 g.cut[me] = {here.t, here.h, (int)me, (int)(((i0 + here.s.slices) * C - 1) / W)};
         }
-        if (f + 1 < f1) {
+        if (left > 1) {
             advance(here);
             if (here.i == 0) begin_item();
         }

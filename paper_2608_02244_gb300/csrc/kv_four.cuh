@@ -21,7 +21,9 @@ struct Four {
     static __device__ __forceinline__ uint32_t ones(uint32_t word) {
         constexpr int kShift = kBit - 4 * kPlace;
         const uint32_t at = kShift >= 0 ? word << (kShift & 31) : word >> (-kShift & 31);
-        return (at & kMask) | kOne;
+        uint32_t x;                  // (at & kMask) | kOne: said in C++ it became two instructions
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x) : "r"(at), "n"(kMask), "r"(kOne));
+        return x;
     }
     // both halves of a scale and offset pair
     static __device__ __forceinline__ uint32_t scale2(uint32_t pair) { return __byte_perm(pair, 0, 0x1010); }
