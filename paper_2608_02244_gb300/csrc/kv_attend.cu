@@ -22,7 +22,7 @@
 namespace isjl {
 namespace {
 
-constexpr int kWarps = kAttendWarps, kThreads = 32 * kWarps;
+constexpr int kWarps = kAttendWarps, kThreads = 32 * kWarps, kSlice = 32;
 
 template <int D>
 struct Shape {
@@ -37,7 +37,7 @@ struct Shape {
 };
 
 __device__ __forceinline__ Sight sight(const AttendArgs &g, int t) {
-    return sight_of(g.a, g.shift, g.line.blocks ? 0 : g.a.n_prefix_blocks << g.shift, g.status, t);
+    return sight_of<kSlice>(g.a, g.shift, g.line.blocks ? 0 : g.a.n_prefix_blocks << g.shift, g.status, t);
 }
 
 template <int D, typename T>
@@ -119,7 +119,7 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     // the number of this lane's block, asked for one slice ahead of the copies that use it and looked at only there
     constexpr int32_t kNone = INT32_MIN;
     auto block_of = [&](const Place &p) {
-        const int32_t y = slice_start(p.s, p.i) + (piece << rows_shift);
+        const int32_t y = slice_start<kSlice>(p.s, p.i) + (piece << rows_shift);
         if (!copies || y >= p.s.end || (y + (1 << rows_shift) <= p.s.lo && y >= a.sinks)) return kNone;   // nothing is seen of it
         const int32_t j = y >> g.shift;
         return j < prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - prefix_blocks)];
@@ -154,7 +154,7 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         if (lane == 0) bar_expect(bar, S::kStageBytes);
         if (copies)
             tma_load(copy_at + stage * S::kStageBytes, ahead_values ? &vmap : &kmap, bar,
-                     slice_start(ahead.s, ahead.i) & ((1 << g.shift) - 1) & ~((1 << rows_shift) - 1), 0, ahead.h / parts, block);
+                     slice_start<kSlice>(ahead.s, ahead.i) & ((1 << g.shift) - 1) & ~((1 << rows_shift) - 1), 0, ahead.h / parts, block);
         ahead_values = !ahead_values;
         if (ahead_values) return;
         if (--ahead_left == 0) return;
@@ -225,7 +225,7 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         value_row[h] = row_at((lane & 7) + ((lane >> 3) & 1) * 8 + 16 * h);
     }
     auto slice = [&]() {
-        const int32_t x = slice_start(here.s, here.i);
+        const int32_t x = slice_start<kSlice>(here.s, here.i);
         const uint32_t keys = next_stage(0);
         float s[4][4] = {};
         {

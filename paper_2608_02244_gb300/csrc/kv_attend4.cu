@@ -1,6 +1,6 @@
 // kv_attend4.cu -- attention of single queries over a paged cache in 4 bits (isjl_kv_attend4).
 //
-// The line of work is kv_attend.cu's: slices of 32 tokens of each query and key head in order, an equal run of them for
+// The line of work is kv_attend.cu's: slices of 32 or 64 tokens of each query and key head in order, an equal run of them for
 // each warp of the grid.  A slice's codes and scales come by asynchronous copies of 16 bytes through a ring of the warp's
 // own, keys and values in turn.
 //
@@ -27,11 +27,12 @@ template <int D, int kTiles>
 struct Shape {
     static constexpr int kCodes = D / 2, kScales = D / 8;          // bytes of a token's key (or value) in one head
     static constexpr int kChunks = kCodes / 16;                    // of 16 bytes, of its codes
+    static constexpr int kSlice = D == 256 ? 32 : 64, kEights = kSlice / 8;        // tokens
     static constexpr int kStageBytes = kSlice * (kCodes + kScales);
-    static constexpr int kStages = 5;                              // of a warp's ring: keys or values of a slice
+    static constexpr int kStages = D == 256 ? 5 : 3;                              // of a warp's ring: keys or values of a slice
     static_assert(kStages % 2 == 1, "a slice's keys and values are under way together");
     static constexpr int kRing = kWarps * kStages * kStageBytes;
-    static constexpr int kBlocks = D == 256 ? 2 : kTiles == 2 ? 3 : 4;      // per SM
+    static constexpr int kBlocks = D == 256 || kTiles == 2 ? 2 : 3;      // per SM
 };
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -73,8 +74,9 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     return y;
 }
 
+template <int kSlice>
 __device__ __forceinline__ Sight sight(const Attend4Args &g, int t) {
-    return sight_of(g.a, g.shift, g.a.n_prefix_blocks << g.shift, g.status, t);
+    return sight_of<kSlice>(g.a, g.shift, g.a.n_prefix_blocks << g.shift, g.status, t);
 }
 
 // place on the line of slices, with its first token
@@ -85,10 +87,11 @@ struct At : Place {
 template <int D, typename T, int kTiles>
 __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4_kernel(const __grid_constant__ Attend4Args g) {
     using S = Shape<D, kTiles>;
+    constexpr int kSlice = S::kSlice, kEights = S::kEights;
     extern __shared__ __align__(128) unsigned char smem[];
     int32_t *before = reinterpret_cast<int32_t *>(smem + S::kRing);                  // [n + 1] slices before a query
     __shared__ int32_t warp_sum[kWarps];
-    __shared__ const unsigned char *eight_at[kWarps][16];
+    __shared__ const unsigned char *eight_at[kWarps][4 * kEights];
     __shared__ int64_t eight_stride[kWarps][4][3];
     const isjl_kv_attend_args &a = g.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -102,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         const int begin = min(n, (int)threadIdx.x * per), end = min(n, begin + per);
         int32_t sum = 0;
         for (int t = begin; t < end; ++t) {
-            const int32_t k = sight(g, t).slices;
+            const int32_t k = sight<kSlice>(g, t).slices;
             before[t] = k;
             sum += k;
         }
@@ -134,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
 
     auto locate = [&](At &p) {
         p.kv = p.h / parts;
-        p.x = slice_start(p.s, p.i);
+        p.x = slice_start<kSlice>(p.s, p.i);
     };
     auto advance = [&](At &p) {
         p.x = ++p.i == p.s.head ? p.s.lo / kSlice * kSlice : p.x + kSlice;
@@ -142,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         p.i = 0;
         if (++p.h >= H) {
             p.h = 0;
-            if (++p.t < n) p.s = sight(g, p.t);
+            if (++p.t < n) p.s = sight<kSlice>(g, p.t);
         }
         locate(p);
     };
@@ -154,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
             if ((int64_t)before[mid] * H <= f0) lo = mid; else hi = mid;
         }
         here.t = lo;
-        here.s = sight(g, lo);
+        here.s = sight<kSlice>(g, lo);
         const int64_t rest = f0 - (int64_t)before[lo] * H;
         here.h = (int)(rest / here.s.slices);
         here.i = (int)(rest - (int64_t)here.h * here.s.slices);
@@ -165,22 +168,23 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     // block; of the first sixteen lanes each finds where one kind (keys' codes and scales, values' codes and scales) of
     // one eight lies, and looks up its block a slice ahead of that.
     const uint32_t ring = smem_at(smem) + warp * S::kStages * S::kStageBytes;
-    const int slot_mask = (1 << g.shift) - 1, kind = (lane >> 2) & 3;
+    const int slot_mask = (1 << g.shift) - 1, kind = (lane / kEights) & 3, my_eight = lane % kEights;
     constexpr int32_t kNone = INT32_MIN;
     auto block_of = [&](const At &p) {
-        const int32_t y = p.x + 8 * (lane & 3);
+        const int32_t y = p.x + 8 * my_eight;
         if (y >= p.s.end || (y + 8 <= p.s.lo && y >= a.sinks)) return kNone;           // nothing is seen of it
         const int32_t j = y >> g.shift;
         return j < a.n_prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - a.n_prefix_blocks)];
     };
     const unsigned char *const kind_base = static_cast<const unsigned char *>(kind == 0 ? g.cache.k : kind == 1 ? g.cache.k_scale : kind == 2 ? g.cache.v : g.cache.v_scale);
-    if (lane < 16 && (lane & 3) == 0)
+    if (lane < 4 * kEights && my_eight == 0)
         for (int i = 0; i < 3; ++i)                    // in bytes
             eight_stride[warp][kind][i] = (kind == 0 ? g.cache.k_stride : kind == 1 ? g.cache.k_scale_stride : kind == 2 ? g.cache.v_stride : g.cache.v_scale_stride)[i] << (kind & 1);
     __syncwarp();
     At ahead = here;
     int ahead_left = (int)(f1 - f0);                   // slices whose values are still to be asked for
     int32_t ahead_block = block_of(ahead);
+    constexpr uint32_t kAll = (1u << kEights) - 1;
     uint32_t ahead_there = 0;                          // which of its eights are read: the others are zeros
     constexpr int kRows = 32 / S::kChunks;             // tokens that one copy of all lanes brings codes of
     const uint32_t copy_to = ring + chunk_at<D>(lane / S::kChunks, lane % S::kChunks);
@@ -191,17 +195,20 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         constexpr int v = decltype(values)::value;
         const int64_t half = 4 * (v ? g.cache.v_stride : g.cache.k_stride)[1];
 #pragma unroll
-        for (int i = 0; i < S::kChunks; ++i) {
+        for (int i = 0; i < S::kChunks * kSlice / 32; ++i) {
             const uint32_t which = kRows == 16 ? 2 * i + (lane >> 4) : kRows * i / 8;
-            copy_async<16>((copy_to + stage + i * kRows * S::kCodes) ^ (kRows == 4 && i % 2 ? 64 : 0), load_pointer(eights + (8 * v + which) * 8) + code_off[v] + (kRows == 4 && i % 2 ? half : 0),
+            copy_async<16>((copy_to + stage + i * kRows * S::kCodes) ^ (kRows == 4 && i % 2 ? 64 : 0), load_pointer(eights + (2 * kEights * v + which) * 8) + code_off[v] + (kRows == 4 && i % 2 ? half : 0),
                            decltype(all)::value || ahead_there >> which & 1);
         }
-        const uint32_t which = lane >> 3;
-        const unsigned char *from = load_pointer(eights + (8 * v + 4 + which) * 8) + scale_off[v];
-        constexpr int kBytes = S::kScales < 16 ? S::kScales : 16;
 #pragma unroll
-        for (int b = 0; b < S::kScales; b += kBytes)
-            copy_async<kBytes>(ring + stage + kSlice * S::kCodes + lane * S::kScales + b, from + b, decltype(all)::value || ahead_there >> which & 1);
+        for (int i = 0; i < kSlice / 32; ++i) {
+            const uint32_t which = 4 * i + (lane >> 3);
+            const unsigned char *from = load_pointer(eights + (2 * kEights * v + kEights + which) * 8) + scale_off[v];
+            constexpr int kBytes = S::kScales < 16 ? S::kScales : 16;
+#pragma unroll
+            for (int b = 0; b < S::kScales; b += kBytes)
+                copy_async<kBytes>(ring + stage + kSlice * S::kCodes + (32 * i + lane) * S::kScales + b, from + b, decltype(all)::value || ahead_there >> which & 1);
+        }
     };
     auto feed_keys = [&](uint32_t stage) {
         if (ahead_left > 0) {
@@ -210,21 +217,21 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
                 report(g.status);                      // beyond the cache: zeros
                 there = false;
             }
-            if (lane < 16) {
-                const int slot = (ahead.x + 8 * (lane & 3)) & slot_mask;
+            if (lane < 4 * kEights) {
+                const int slot = (ahead.x + 8 * my_eight) & slot_mask;
                 const int64_t *stride = eight_stride[warp][kind];
                 eight_at[warp][lane] = kind_base + (there ? ahead_block * stride[0] + slot * stride[1] + ahead.kv * stride[2] : 0);
             }
-            ahead_there = __ballot_sync(~0u, there) & 15;
+            ahead_there = __ballot_sync(~0u, there) & kAll;
             __syncwarp();
-            if (ahead_there == 15) copies(stage, std::false_type(), std::true_type());
+            if (ahead_there == kAll) copies(stage, std::false_type(), std::true_type());
             else copies(stage, std::false_type(), std::false_type());
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     auto feed_values = [&](uint32_t stage) {
         if (ahead_left > 0) {
-            if (ahead_there == 15) copies(stage, std::true_type(), std::true_type());
+            if (ahead_there == kAll) copies(stage, std::true_type(), std::true_type());
             else copies(stage, std::true_type(), std::false_type());
             if (--ahead_left > 0) {
                 advance(ahead);
@@ -294,9 +301,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     auto slice = [&]() {
         const int32_t x0 = here.x;
         const uint32_t keys = next_stage(std::false_type());
-        float s[kTiles][2][4] = {};
+        constexpr int kSixteens = kSlice / 16;
+        float s[kTiles][kSixteens][4] = {};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {                  // sixteen tokens each
+        for (int h = 0; h < kSixteens; ++h) {                  // sixteen tokens each
             uint32_t pair[2][kKeyWords / 4 + (kKeyWords < 4)];
 #pragma unroll
             for (int e = 0; e < 2; ++e) load_words(pair[e], keys + key_scale_at + (16 * h + 8 * e) * S::kScales);
@@ -326,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         auto hidden = [&](int32_t y) { return y >= here.s.end || (y < here.s.lo && y >= a.sinks); };
         if (edge) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < kSixteens; ++h)
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     if (hidden(x0 + 16 * h + 8 * e + token_of(r)))
@@ -335,12 +343,17 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         }
         __syncwarp();
         // weights are relative to a maximum that may lag behind by kPass: it is looked for only when one is beyond that
-        uint32_t w[kTiles][2][2];
+        uint32_t w[kTiles][kSixteens][2];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
             float top[2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) top[j] = fmaxf(fmaxf(s[t][0][j], s[t][0][2 + j]), fmaxf(s[t][1][j], s[t][1][2 + j])) * scale - Grow<T>::kTop;
+            for (int j = 0; j < 2; ++j) {
+                top[j] = fmaxf(s[t][0][j], s[t][0][2 + j]);
+#pragma unroll
+                for (int h = 1; h < kSixteens; ++h) top[j] = fmaxf(top[j], fmaxf(s[t][h][j], s[t][h][2 + j]));
+                top[j] = top[j] * scale - Grow<T>::kTop;
+            }
             if (__any_sync(~0u, top[0] > m[t][0] + Grow<T>::kPass || top[1] > m[t][1] + Grow<T>::kPass)) {
                 float fix[2];
 #pragma unroll
@@ -360,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
             const float ref[2] = {m[t][0] == -INFINITY ? 0.f : m[t][0], m[t][1] == -INFINITY ? 0.f : m[t][1]};
             float sum[2] = {0.f, 0.f};
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < kSixteens; ++h)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float u = ex2(fmaf(s[t][h][2 * e], scale, -ref[0])), v = ex2(fmaf(s[t][h][2 * e + 1], scale, -ref[1]));
@@ -374,13 +387,14 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         const uint32_t values = next_stage(std::true_type());
         if (edge) {
             // a weight of 0 does not silence an infinite or undefined value: what is not seen stands for 0
-            if (hidden(x0 + lane))
-                for (int b = 0; b < S::kScales; b += 8)
-                    asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(values + kSlice * S::kCodes + lane * S::kScales + b), "r"(0) : "memory");
+            for (int i = lane; i < kSlice; i += 32)
+                if (hidden(x0 + i))
+                    for (int b = 0; b < S::kScales; b += 8)
+                        asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(values + kSlice * S::kCodes + i * S::kScales + b), "r"(0) : "memory");
             __syncwarp();
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kSixteens; ++h) {
             // this lane's four tokens: two of each eight
             uint32_t word[4][kValueWords], s2[2], b2[2];
 #pragma unroll

@@ -1,5 +1,5 @@
 // kv_sight.cuh -- the line of work of the attentions of single queries (kv_attend.cu, kv_attend4.cu): for each query, each
-// key head (or part of its query heads), the slices of 32 tokens that it sees.
+// key head (or part of its query heads), the slices of tokens that it sees.
 #pragma once
 
 #include "kv_internal.cuh"
@@ -7,7 +7,6 @@
 namespace isjl {
 namespace {
 
-constexpr int kSlice = 32;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // what a query sees: tokens end - window .. end - 1 and 0 .. sinks - 1, counted from the first token that
@@ -19,6 +18,7 @@ struct Sight {
 };
 
 // prefix: tokens of it that are read before the own ones
+template <int kSlice>
 __device__ __forceinline__ Sight sight_of(const isjl_kv_attend_args &a, int shift, int32_t prefix, int32_t *status, int t) {
     Sight s;
     const int32_t x = a.lens[t];
@@ -33,6 +33,7 @@ __device__ __forceinline__ Sight sight_of(const isjl_kv_attend_args &a, int shif
 }
 
 // first token of a query's slice
+template <int kSlice>
 __device__ __forceinline__ int32_t slice_start(const Sight &s, int i) {
     return (i < s.head ? i : s.lo / kSlice + i - s.head) * kSlice;
 }
