@@ -26,8 +26,11 @@ __device__ __forceinline__ void unpack8(const uint4 &w, float (&x)[8]) {
     }
 }
 
-// The codes of this thread's 8 values of a group, and the group's scale and offset, in T.  The divisions are exact, as
-// their definition has them: 16-bit values lie on borders between codes often.
+// The codes of this thread's 8 values of a group, and the group's scale and offset, in T.  16-bit values lie on borders
+// between codes often, so the quotient d / S, with d = x - B, has to be rounded as the definition has it.  A border is
+// t S with t = 1 + (c + 1/2) / 16, exact in 32 bits, and d is a number of 32 bits in the same or the next binade: where
+// they differ, they do so by more than S 2^-24, and the rounded quotient is on the same side of t.  So an estimate with
+// the reciprocal is put right by d's exact distance from the estimate's value: beyond half a step, or at it and odd.
 template <typename T>
 __device__ __forceinline__ uint32_t codes4(const float (&x)[8], uint32_t *scales) {
     float lo = x[0], hi = x[0];
@@ -49,12 +52,18 @@ __device__ __forceinline__ uint32_t codes4(const float (&x)[8], uint32_t *scales
     fine = fine && s < INFINITY && b > -INFINITY;
     *scales = fine ? Half<T>::pack(s, b) : Half<T>::pack(NAN, NAN);
     uint32_t word = 0;
-    if (fine && s > 0.f)
+    if (fine && s > 0.f) {
+        // a scale below the normal numbers: all of it by 2^64, which changes no quotient
+        const float up = s < 0x1p-100f ? 0x1p64f : 1.f, step = s * up * 0.0625f, inv = __fdividef(1.f, step);
+        constexpr float kWhole = 0x1.8p23f;         // a sum with it is rounded to a whole number, ties to even
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float c = rintf(__fdiv_rn(x[i] - b, s) * 16.f - 16.f);
-            word |= (uint32_t)fminf(fmaxf(c, 0.f), 15.f) << (4 * i);
+            const float d = (x[i] - b) * up, n = fmaf(d, inv, kWhole), off = fabsf(fmaf(kWhole - n, step, d));
+            int c = __float_as_int(n) - __float_as_int(kWhole + 16.f);
+            if (off > step * 0.5f || (off == step * 0.5f && (c & 1))) c += d > (n - kWhole) * step ? 1 : -1;
+            word |= (uint32_t)min(max(c, 0), 15) << (4 * i);
         }
+    }
     return word;
 }
 
@@ -90,16 +99,6 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
         return;
     }
     const int64_t block = slot >> g.shift, place = slot & ((1 << g.shift) - 1);
-    // the token's part of each array: [2] keys and values
-    unsigned char *codes[2];
-    T *scales[2];
-    if (kFour)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t *cs = i ? g.cache4.v_stride : g.cache4.k_stride, *ss = i ? g.cache4.v_scale_stride : g.cache4.k_scale_stride;
-            codes[i] = static_cast<unsigned char *>(i ? g.cache4.v : g.cache4.k) + block * cs[0] + place * cs[1] + 4 * c;
-            scales[i] = static_cast<T *>(i ? g.cache4.v_scale : g.cache4.k_scale) + block * ss[0] + place * ss[1] + c / 4 * 2;
-        }
     T *k_out = static_cast<T *>(g.cache.k) + block * g.cache.k_stride[0] + place * g.cache.k_stride[1];
     T *v_out = static_cast<T *>(g.cache.v) + block * g.cache.v_stride[0] + place * g.cache.v_stride[1];
 
@@ -146,7 +145,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
             unpack8<T>(raw[u], x);
             uint4 w = raw[u];
             if (h0 + u * kHeads < hq + hkv) {        // some of the warps' heads are q or k heads
-                const bool normed = is_k ? a.k_weight != nullptr : a.q_weight != nullptr;
+                // codes are made of y, which for a value head is what came; its 16 bits are kept as they are
+                const bool normed = !(kFour && is_v) && (is_k ? a.k_weight != nullptr : a.q_weight != nullptr), turned = turns && !(kFour && is_v);
                 if (a.q_weight || a.k_weight) {
                     float sum = 0.f, scale[8];
 #pragma unroll
@@ -160,26 +160,32 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
                         for (int i = 0; i < 8; ++i) x[i] *= r * scale[i];
                 }
                 float y[8];
+                if (a.interleaved) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float other = __shfl_sync(~0u, x[i], from);
-                    y[i] = turns ? x[i] * cosv[i] + (a.interleaved ? x[i ^ 1] : other) * sinv[i] : x[i];
+                    for (int i = 0; i < 8; ++i) y[i] = turned ? x[i] * cosv[i] + x[i ^ 1] * sinv[i] : x[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float other = __shfl_sync(~0u, x[i], from);
+                        y[i] = turned ? x[i] * cosv[i] + other * sinv[i] : x[i];
+                    }
                 }
-                if (kFour && is_v) unpack8<T>(raw[u], x);
-                else if (kFour)
+                if (!is_v) w = make_uint4(Half<T>::pack(y[0], y[1]), Half<T>::pack(y[2], y[3]), Half<T>::pack(y[4], y[5]), Half<T>::pack(y[6], y[7]));
+                if (kFour)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[i] = y[i];
-                if (!is_v) w = make_uint4(Half<T>::pack(y[0], y[1]), Half<T>::pack(y[2], y[3]), Half<T>::pack(y[4], y[5]), Half<T>::pack(y[6], y[7]));
             }
             if (kFour && h0 + (u + 1) * kHeads > hq) {      // some of the warps' heads are k or v heads
                 uint32_t pair;
                 __syncwarp();
                 const uint32_t word = codes4<T>(x, &pair);
                 if (h >= hq && h < heads) {
+                    const isjl_kv_cache4 &four = g.cache4;
+                    const int64_t *cs = is_v ? four.v_stride : four.k_stride, *ss = is_v ? four.v_scale_stride : four.k_scale_stride;
                     const int head = is_v ? h - hq - hkv : h - hq;
-                    *reinterpret_cast<uint32_t *>(codes[is_v] + head * (is_v ? g.cache4.v_stride : g.cache4.k_stride)[2]) = word;
+                    *reinterpret_cast<uint32_t *>(static_cast<unsigned char *>(is_v ? four.v : four.k) + block * cs[0] + place * cs[1] + head * cs[2] + 4 * c) = word;
                     if (c % 4 == 0)
-                        *reinterpret_cast<uint32_t *>(scales[is_v] + head * (is_v ? g.cache4.v_scale_stride : g.cache4.k_scale_stride)[2]) = pair;
+                        *reinterpret_cast<uint32_t *>(static_cast<T *>(is_v ? four.v_scale : four.k_scale) + block * ss[0] + place * ss[1] + head * ss[2] + c / 4 * 2) = pair;
                 }
                 if (h >= hq) continue;
             }

@@ -4,43 +4,56 @@
 // 5 bits a value in, 16 out.
 #include "kv_four.cuh"
 
+#include <algorithm>
+
 namespace isjl {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128, kTokens = 8;
 
 template <int D, typename T>
-__global__ void __launch_bounds__(kThreads) read4_kernel(const __grid_constant__ Read4Args g, int tokens_of_block) {
+__global__ void __launch_bounds__(kThreads) read4_kernel(const __grid_constant__ Read4Args g) {
     const isjl_kv_read4_args &a = g.a;
     constexpr int kLanes = D / 8;
-    const int words = 2 * g.n_kv_heads * kLanes;               // of a token
-    const int first = blockIdx.x * tokens_of_block, tokens = min(tokens_of_block, a.n_tokens - first);
-    for (int i = threadIdx.x; i < tokens * words; i += kThreads) {
-        const int t = i / words, j = i - t * words, side = j >= words / 2, c = j % kLanes;
-        const int h = (side ? j - words / 2 : j) / kLanes;
-        const int64_t slot = a.slots[first + t];
+    const int words = 2 * g.n_kv_heads * kLanes, groups = max(1, kThreads / words);        // of a token; tokens side by side
+    const int group = threadIdx.x / words;                     // beyond groups - 1: nothing to do
+    const int64_t first = ((int64_t)blockIdx.x * groups + group) * kTokens;
+    if (words <= kThreads && group >= groups) return;
+    for (int j = words <= kThreads ? threadIdx.x - group * words : threadIdx.x; j < words; j += kThreads) {
+        const int side = j >= words / 2, c = j % kLanes, h = (side ? j - words / 2 : j) / kLanes;
+        const int64_t *cs = side ? g.cache.v_stride : g.cache.k_stride, *ss = side ? g.cache.v_scale_stride : g.cache.k_scale_stride;
+        const unsigned char *codes = static_cast<const unsigned char *>(side ? g.cache.v : g.cache.k) + h * cs[2] + 4 * c;
+        const T *scales = static_cast<const T *>(side ? g.cache.v_scale : g.cache.k_scale) + h * ss[2] + c / 4 * 2;
         const int64_t *to_stride = side ? a.v_stride : a.k_stride;
-        T *to = static_cast<T *>(side ? a.v_out : a.k_out) + (first + t) * to_stride[0] + h * to_stride[1] + 8 * c;
-        uint32_t v[4] = {0, 0, 0, 0};
-        if (slot >= 0 && slot < g.n_slots) {
-            const int64_t block = slot >> g.shift, place = slot & ((1 << g.shift) - 1);
-            const int64_t *cs = side ? g.cache.v_stride : g.cache.k_stride, *ss = side ? g.cache.v_scale_stride : g.cache.k_scale_stride;
-            const uint32_t word = *reinterpret_cast<const uint32_t *>(
-                static_cast<const unsigned char *>(side ? g.cache.v : g.cache.k) + block * cs[0] + place * cs[1] + h * cs[2] + 4 * c);
-            const uint32_t pair = *reinterpret_cast<const uint32_t *>(
-                static_cast<const T *>(side ? g.cache.v_scale : g.cache.k_scale) + block * ss[0] + place * ss[1] + h * ss[2] + c / 4 * 2);
-            Four<T>::values(v, word, pair);
-        } else if (slot >= g.n_slots && j == 0) {
-            report(g.status);
+        T *to = static_cast<T *>(side ? a.v_out : a.k_out) + first * to_stride[0] + h * to_stride[1] + 8 * c;
+        int64_t slot[kTokens];
+        uint32_t word[kTokens], pair[kTokens];
+#pragma unroll
+        for (int u = 0; u < kTokens; ++u) slot[u] = first + u < a.n_tokens ? a.slots[first + u] : -1;
+#pragma unroll
+        for (int u = 0; u < kTokens; ++u) {
+            word[u] = pair[u] = 0;                             // stands for 0
+            if (slot[u] >= g.n_slots) {
+                if (j == 0) report(g.status);
+            } else if (slot[u] >= 0) {
+                const int64_t block = slot[u] >> g.shift, place = slot[u] & ((1 << g.shift) - 1);
+                word[u] = __ldcs(reinterpret_cast<const uint32_t *>(codes + block * cs[0] + place * cs[1]));
+                pair[u] = *reinterpret_cast<const uint32_t *>(scales + block * ss[0] + place * ss[1]);
+            }
         }
-        *reinterpret_cast<uint4 *>(to) = make_uint4(v[0], v[1], v[2], v[3]);
+#pragma unroll
+        for (int u = 0; u < kTokens; ++u) {
+            uint32_t v[4];
+            Four<T>::values(v, word[u], pair[u]);
+            if (first + u < a.n_tokens) __stcs(reinterpret_cast<uint4 *>(to + u * to_stride[0]), make_uint4(v[0], v[1], v[2], v[3]));
+        }
     }
 }
 
 template <int D, typename T>
 cudaError_t launch_of(const Read4Args &g, cudaStream_t st) {
-    const int words = 2 * g.n_kv_heads * (D / 8), per = max(1, 4 * kThreads / words);
-    read4_kernel<D, T><<<(g.a.n_tokens - 1) / per + 1, kThreads, 0, st>>>(g, per);
+    const int words = 2 * g.n_kv_heads * (D / 8), per = kTokens * std::max(1, kThreads / words);
+    read4_kernel<D, T><<<(g.a.n_tokens - 1) / per + 1, kThreads, 0, st>>>(g);
     return cudaGetLastError();
 }
 

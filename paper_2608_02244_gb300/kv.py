@@ -209,19 +209,20 @@ class Decoder:
     def _cache4(self, cache):
         if len(cache) != 4:
             self._bad("a cache in 4 bits is codes of keys and of values, scales of keys and of values")
-        codes, scales, index, steps = self._codes_shape, self._scales_shape, self._index, []
-        for t, shape, dtype, inner in ((cache[0], codes, self.torch.uint8, (1,)), (cache[1], codes, self.torch.uint8, (1,)),
-                                       (cache[2], scales, self.dtype, (2, 1)), (cache[3], scales, self.dtype, (2, 1))):
-            st = t.stride()
-            # the stride of an axis of one element says nothing
-            if t.shape != shape or t.dtype is not dtype or t.get_device() != index or st[-1] != 1 or \
-                    (len(inner) == 2 and st[3] != 2 and shape[3] > 1):
-                self._bad(f"a cache in 4 bits has codes of torch.uint8 {codes} and scales of {self.dtype} {scales} on "
-                          f"{self.device}, a head's next to one another")
-            if shape[0] == 1 or shape[2] == 1:
-                st = [x if n > 1 else 16 for x, n in zip(st, shape)]
-            steps += st[:3]
-        return _CACHE4.pack(*(t.data_ptr() for t in cache), *steps)
+        k, v, ks, vs = cache
+        codes, scales, index, dtype, u8 = self._codes_shape, self._scales_shape, self._index, self.dtype, self.torch.uint8
+        a, b, c, d = k.stride(), v.stride(), ks.stride(), vs.stride()
+        if k.shape != codes or v.shape != codes or ks.shape != scales or vs.shape != scales or \
+                k.dtype is not u8 or v.dtype is not u8 or ks.dtype is not dtype or vs.dtype is not dtype or \
+                k.get_device() != index or v.get_device() != index or ks.get_device() != index or vs.get_device() != index or \
+                a[3] != 1 or b[3] != 1 or c[4] != 1 or d[4] != 1 or (scales[3] > 1 and (c[3] != 2 or d[3] != 2)):
+            self._bad(f"a cache in 4 bits has codes of torch.uint8 {codes} and scales of {dtype} {scales} on {self.device}, "
+                      "a head's next to one another")
+        if codes[0] == 1 or codes[2] == 1:
+            # the stride of an axis of one element says nothing: any valid one
+            a, b, c, d = ([x if n > 1 else 16 for x, n in zip(y, codes)] for y in (a, b, c, d))
+        return _CACHE4.pack(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), a[0], a[1], a[2], b[0], b[1], b[2],
+                            c[0], c[1], c[2], d[0], d[1], d[2])
 
     def _empty(self, stream, shape, dtype):
         """Memory for a result.  The allocator hands out what is free in the order of one stream's
@@ -413,17 +414,23 @@ class Decoder:
     def read4(self, slots, cache, k=None, v=None, stream=None):
         """Keys and values of slots in 16 bits, [tokens, n_kv_heads, head_dim] each: see isjl_kv_read4.  `k` and `v`
         take them if given: any strides but 1 last, such as a cache's own slots."""
-        n = slots.shape[0]
-        shape, args = (n, self.n_kv_heads, self.head_dim), [n, self._ints("slots", slots, (n,), self.torch.int64)]
-        packed, given = self._cache4(cache), (k, v)
-        k, v = (self._empty(stream, shape, self.dtype) if t is None else t for t in given)
-        for t in (k, v):
-            if t.shape != shape or t.dtype is not self.dtype or t.get_device() != self._index or t.stride(2) != 1:
-                self._bad(f"k and v must be {self.dtype} {shape} on {self.device} with stride 1 last")
+        n, dtype, index = slots.shape[0], self.dtype, self._index
+        shape = (n, self.n_kv_heads, self.head_dim)
+        places, packed = self._ints("slots", slots, (n,), self.torch.int64), self._cache4(cache)
+        if k is None:
+            k = self._empty(stream, shape, dtype)
+        if v is None:
+            v = self._empty(stream, shape, dtype)
+        ks, vs = k.stride(), v.stride()
+        if k.shape != shape or v.shape != shape or k.dtype is not dtype or v.dtype is not dtype or \
+                k.get_device() != index or v.get_device() != index or ks[2] != 1 or vs[2] != 1:
+            self._bad(f"k and v must be {dtype} {shape} on {self.device} with stride 1 last")
+        if n <= 1 or shape[1] == 1:
             # the stride of an axis of one element says nothing: any valid one
-            args += [t.data_ptr()] + [x if m > 1 else 8 for x, m in zip(t.stride()[:2], shape)]
+            ks, vs = ([x if m > 1 else 8 for x, m in zip(y, shape)] for y in (ks, vs))
+        args = _READ4.pack(n, places, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1])
         st = self._stream(stream, (slots, *cache, k, v))
-        _check(self._lib.isjl_kv_read4(self.handle, _READ4.pack(*args), packed, st), "isjl_kv_read4")
+        _check(self._lib.isjl_kv_read4(self.handle, args, packed, st), "isjl_kv_read4")
         return k, v
 
     def status(self):
