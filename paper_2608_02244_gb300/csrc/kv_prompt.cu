@@ -316,15 +316,15 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             const int q_head = x.q_head + member;
             T *out = static_cast<T *>(g.a.out) + query * g.a.out_stride[0] + q_head * g.a.out_stride[1];
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
+            for (int c = 0; c < D / 16; ++c) {
+                uint32_t o[16];
                 __syncwarp();
-                tmem_load(o, o_at + 32 * c);
+                tmem_load(o, o_at + 16 * c);
                 tmem_load_wait();
                 if (live && left_out) {
-                    const Spoilt y = spoilt<D, T>(g, shape, x, token, q_head, 32 * c, top, scale);
+                    const Spoilt y = spoilt<D, T, 16>(g, shape, x, token, q_head, 16 * c, top, scale);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
+                    for (int i = 0; i < 16; ++i) {
                         float z = __uint_as_float(o[i]);
                         if (y.plus >> i & 1) z += INFINITY;
                         if (y.minus >> i & 1) z -= INFINITY;
@@ -333,25 +333,24 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                     }
                 }
                 if (live && whole) {
-                    uint4 w[4];
+                    uint4 w[2];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 2; ++i) {
                         uint32_t u[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) u[k] = Half<T>::pack(__uint_as_float(o[8 * i + 2 * k]) * inv, __uint_as_float(o[8 * i + 2 * k + 1]) * inv);
                         w[i] = make_uint4(u[0], u[1], u[2], u[3]);
                     }
                     if (g.out_wide) {
-                        store32(out + 32 * c, w[0], w[1]);
-                        store32(out + 32 * c + 16, w[2], w[3]);
+                        store32(out + 16 * c, w[0], w[1]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(out + 32 * c + 8 * i) = w[i];
+                        for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4 *>(out + 16 * c + 8 * i) = w[i];
                     }
                 } else if (live) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8)
-                        store32(g.part_o + at * D + 32 * c + i, make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]), make_uint4(o[i + 4], o[i + 5], o[i + 6], o[i + 7]));
+                    for (int i = 0; i < 16; i += 8)
+                        store32(g.part_o + at * D + 16 * c + i, make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]), make_uint4(o[i + 4], o[i + 5], o[i + 6], o[i + 7]));
                 }
             }
             if (live && !whole) g.part_ml[at] = make_float2(top, total);

@@ -116,7 +116,7 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
 struct Spoilt {
     uint32_t plus, minus, none;
 };
-template <int D, typename T>
+template <int D, typename T, int kColumns>
 __device__ __forceinline__ Spoilt spoilt(const PromptArgs &g, const PromptShape &s, const Item &x, int32_t token, int32_t q_head, int column, float top,
                                          float scale) {
     Spoilt out = {0, 0, 0};
@@ -131,7 +131,7 @@ __device__ __forceinline__ Spoilt spoilt(const PromptArgs &g, const PromptShape 
             const T *v = static_cast<const T *>(g.cache.v) + block * g.cache.v_stride[0] + slot * g.cache.v_stride[1] + x.kv * g.cache.v_stride[2] + column;
             bool any = false;
 #pragma unroll 1
-            for (int i = 0; i < 16; ++i) any = any || not_finite<T>(reinterpret_cast<const uint32_t *>(v)[i]);
+            for (int i = 0; i < kColumns / 2; ++i) any = any || not_finite<T>(reinterpret_cast<const uint32_t *>(v)[i]);
             if (!any) continue;
             const T *k = static_cast<const T *>(g.cache.k) + block * g.cache.k_stride[0] + slot * g.cache.k_stride[1] + x.kv * g.cache.k_stride[2];
             const T *q = static_cast<const T *>(g.a.q) + (int64_t)(x.start + token) * g.a.q_stride[0] + (int64_t)q_head * g.a.q_stride[1];
@@ -143,7 +143,7 @@ __device__ __forceinline__ Spoilt spoilt(const PromptArgs &g, const PromptShape 
             }
             const bool counts = ex2(dot * scale - (top == -INFINITY ? 0.f : top)) > 0.f;       // 0 times infinity is undefined
 #pragma unroll 1
-            for (int i = 0; i < 32; ++i) {
+            for (int i = 0; i < kColumns; ++i) {
                 const float z = Half<T>::unpack(reinterpret_cast<const uint16_t *>(v)[i]).x;
                 if (z - z == 0.f) continue;
                 if (!counts || z != z) out.none |= 1u << i;

@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) prompt_wide_kernel(const __
             if (spoils)
 #pragma unroll
                 for (int b = 0; b < D / 32; ++b) {
-                    const Spoilt y = spoilt<D, T>(g, shape, x, token[h], q_head[h], 32 * b, m[h], scale);
+                    const Spoilt y = spoilt<D, T, 32>(g, shape, x, token[h], q_head[h], 32 * b, m[h], scale);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int at = 8 * (i / 2) + c2 + (i & 1);

@@ -53,6 +53,10 @@ __device__ __forceinline__ void tmem_load(uint32_t (&v)[32], uint32_t at) {
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : R8(v, 0), R8(v, 8), R8(v, 16), R8(v, 24) : "r"(at));
 }
+__device__ __forceinline__ void tmem_load(uint32_t (&v)[16], uint32_t at) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : R8(v, 0), R8(v, 8) : "r"(at));
+}
 __device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t (&v)[32]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
