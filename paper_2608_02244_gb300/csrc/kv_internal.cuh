@@ -192,7 +192,7 @@ struct Attend4Args {
 cudaError_t prepare_attend4(int head_dim, int type, int group, int sms, int *warps);
 cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, int sms, cudaStream_t st);
 
-// ---- prompt (kv_prompt.cu; heads of 256 values: kv_prompt_wide.cu)
+// ---- prompt (kv_prompt.cu)
 // an item that the end of its block's run cuts; the blocks up to `last` have a piece of it
 struct alignas(16) PromptCut {
     int32_t row, head, item;      // row < 0: none
@@ -214,7 +214,5 @@ struct PromptArgs {
 constexpr int kPromptRows = 512;  // of the pieces of an SM's blocks
 cudaError_t prepare_prompt(int head_dim, int type);   // once for a shape, before its first launch
 cudaError_t launch_prompt(PromptArgs &g, void *encoder, int head_dim, int type, int sms, cudaStream_t st);
-cudaError_t prepare_prompt_wide(int type);
-cudaError_t launch_prompt_wide(PromptArgs &g, int type, int sms, cudaStream_t st);
 
 }  // namespace isjl

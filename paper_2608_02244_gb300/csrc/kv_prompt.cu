@@ -2,9 +2,9 @@
 //
 // The queries of a row's tokens, times the `group` query heads of a key head, are the rows of a matrix: S = Q K^T,
 // O = softmax(S) V, 4 D operations for each row and visible token, on the fifth-generation tensor cores.  An item is
-// two tiles of 128 rows (one with heads of 256 values, whose sums fill half of TMEM) of one key head: a run of
-// neighbouring tokens, each with all of its query heads, so that a tile of keys and values is used by all of them.
-// An item's tiles of 128 tokens (64) end with the tokens that its last query sees.
+// two tiles of 128 rows of one key head: a run of neighbouring tokens, each with all of its query heads, so that a
+// tile of keys and values is used by all of them.  An item's tiles of 128 tokens end with the tokens that its last
+// query sees.
 //
 // Keys and values come by TMA from the cache's blocks through a ring each, one thread issues the products, and each
 // row of a tile is one thread of a group of four warps that takes the row's maximum, exponentials and sum.  Scores
@@ -12,6 +12,10 @@
 // alternate: while the tensor cores work for one, the other's group is at its exponentials.  The sums O stay in TMEM
 // for the whole run and are rescaled only when a row's maximum has grown by more than 2^8 (fp16: 2^4) since the last
 // time; rounding weights to 16 bits is as exact as with the true maximum.
+//
+// Heads of 256 values: one row tile, whose sums take half of TMEM, and tiles of 64 tokens, since 128 rows of queries and
+// five tiles of keys and values fill shared memory.  Its scores have two places in turn, and the next ones are issued
+// before the weights of these are there, so that the tensor cores have work during the exponentials.
 //
 // What a query does not see must not reach its sums, and a weight of 0 does not silence an infinite or undefined
 // value.  In the tiles of which some of the item's queries see a part only, one warp makes zeros of the values that no
@@ -21,27 +25,35 @@
 // The work is a line of (row, key head, item, tile): every block has an equal run of it, wherever prompts end, and one
 // long prompt, many short ones or a few queries over a long cache all keep every SM busy to the end.  Items cut by the
 // runs' ends leave pieces (sum, maximum and total of each row), which a second kernel joins in their order.
+//
+// Measured, 32 + 8 heads of 128 values, bf16: 16,384 tokens 1,335 us (1,645 TFLOP/s, power-limited when it runs for
+// long: 1,440 us), 8 requests of 4,096 785 us (1,400), 32 of 1,024 314 us (875), 64 of 256 119 us; 64 values, 16,384 tokens
+// 1,117 us (985: 128 exponentials a row and tile take the SM 2,048 cycles, the products 1,024); 256 values, 16 + 4 heads,
+// 16,384 tokens 1,630 us (1,350; products a warp at a time, 64 rows an item, took 11,700).  Short prompts are bound by what
+// an item takes beside its tiles: some 3,000 cycles of TMEM loads and 2,000 of stores for its results, during which its
+// own products wait, and the first tile's way through the pipeline.
 #include "kv_prompt.cuh"
 #include "kv_tensor.cuh"
 
 namespace isjl {
 namespace {
 
-constexpr int kRows = 128, kKeys = 128;             // of a row tile, of a token tile
-constexpr int kGroups = 2;                          // row tiles of an item, each with its four warps
-constexpr int kSums = kGroups * kKeys;              // TMEM: scores from 0, sums from here
-constexpr int kParts = kKeys / 64;                  // of a tile's weights, handed over one after another
-constexpr int kThreads = 384;                       // two groups of four warps; the warps that load, issue, and plan and clean
-constexpr int kLoadWarp = 8, kIssueWarp = 10, kPlanWarp = 11;
+constexpr int kRows = 128;                          // of a row tile
 constexpr int kItems = 8, kAhead = 6;               // planned items kept at a time; planned ahead of the values that are cleaned
 
 template <int D>
 struct Shape {
+    static constexpr int kGroups = D == 256 ? 1 : 2;             // row tiles of an item, each with its four warps
+    static constexpr int kKeys = D == 256 ? 64 : 128;            // of a token tile
+    static constexpr int kParts = kKeys / 64;                    // of a tile's weights, handed over one after another
+    static constexpr int kLoadWarp = 4 * kGroups, kIssueWarp = kLoadWarp + 2, kPlanWarp = kLoadWarp + 3;     // plans and cleans
+    static constexpr int kThreads = 128 * kGroups + 128;
+    static constexpr int kSums = 256;                            // TMEM: scores from 0, sums from here
     static constexpr int kHalves = D / 64;                       // rows of 128 bytes hold 64 values
-    static constexpr int kHalfBytes = 128 * 128;                 // 128 rows of them
-    static constexpr int kTileBytes = kHalves * kHalfBytes;
-    static constexpr int kKeyStages = D == 128 ? 2 : 4, kValueStages = D == 128 ? 3 : 4;
-    static constexpr int kSmem = kGroups * kTileBytes + (kKeyStages + kValueStages) * kTileBytes + 1024;
+    static constexpr int kQueryHalf = kRows * 128, kQueryBytes = kHalves * kQueryHalf;
+    static constexpr int kHalfBytes = kKeys * 128, kTileBytes = kHalves * kHalfBytes;
+    static constexpr int kKeyStages = D == 64 ? 4 : 2, kValueStages = D == 64 ? 4 : 3;
+    static constexpr int kSmem = kGroups * kQueryBytes + (kKeyStages + kValueStages) * kTileBytes + 1024;
 };
 
 __device__ __forceinline__ void store32(void *to, uint4 a, uint4 b) {
@@ -76,12 +88,14 @@ enum { kKeyFull = 0, kValueFull = 8, kFree = 4 /* after a stage's full one */, k
        kItemFull = 23, kItemFree = kItemFull + kItems, kBars = kItemFree + kItems };
 
 template <int D, typename T>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Shape<D>::kThreads, 1)
 prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
               const __grid_constant__ CUtensorMap vmap) {
     using S = Shape<D>;
     constexpr bool kBf16 = Half<T>::kIsBf16;
-    constexpr int kChunks = kKeys / 32;
+    constexpr int kGroups = S::kGroups, kKeys = S::kKeys, kParts = S::kParts, kSums = S::kSums, kThreads = S::kThreads;
+    constexpr int kLoadWarp = S::kLoadWarp, kIssueWarp = S::kIssueWarp, kPlanWarp = S::kPlanWarp, kChunks = kKeys / 32;
+    constexpr bool kTwo = kGroups == 2;
     // operand types, 32-bit sums, 128 rows; the first product has a column for each token and both operands along D, the
     // second D columns and its right operand (values, tokens outermost) across
     constexpr uint32_t kTypes = (1u << 4) | (kBf16 ? (1u << 7) | (1u << 10) : 0u) | ((kRows / 16) << 24);
@@ -97,7 +111,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
-    const uint32_t q_at = base, ring = base + kGroups * S::kTileBytes;
+    const uint32_t q_at = base, ring = base + kGroups * S::kQueryBytes;
     const uint32_t bar0 = smem_addr(bars);
     auto bar = [&](int i) { return bar0 + 8 * i; };
     const PromptShape shape = {kKeys, kGroups * g.tokens_of_tile, g.a.window, g.a.sinks};
@@ -111,7 +125,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
         for (int i = 0; i < kItems; ++i) {
             flag_word[i] = 0;
             bar_init(bar(kItemFull + i), 1);
-            bar_init(bar(kItemFree + i), 11);           // the warps that read it
+            bar_init(bar(kItemFree + i), kPlanWarp);        // the warps that read it
         }
         for (int i = 0; i < kScores; ++i) bar_init(bar(i), 1);
         for (int i = 0; i < 2; ++i) {
@@ -171,11 +185,11 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
     // Registers at launch: 384 x 168.  A row's thread holds 128 scores beside its weights, the third group
     // needs few: 256 x 216 + 128 x 72 are the same sum.
     if (warp < kLoadWarp) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        if (kTwo) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ---- the rows of one tile, a thread each
         const int group = warp >> 2, row = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;         // this warp's quarter of the TMEM lanes
-        const uint32_t s_at = tmem + group * kKeys + lanes, o_at = tmem + kSums + group * D + lanes;
+        const uint32_t s_first = tmem + group * kKeys + lanes, o_at = tmem + kSums + group * D + lanes;
         const float scale = g.a.scale * kLog2e;
         const int token = group * g.tokens_of_tile + row / g.rows_of_token, member = row % g.rows_of_token;
         auto two_of = [&](const Item &x) { return x.tokens > g.tokens_of_tile; };
@@ -188,13 +202,17 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                 bar_expect(bar(kQueries + group), S::kHalves * g.tokens_of_tile * g.rows_of_token * 128);
 #pragma unroll
                 for (int half = 0; half < S::kHalves; ++half)
-                    tma_load4(q_at + group * S::kTileBytes + half * S::kHalfBytes, &qmap, bar(kQueries + group), half, x.q_head,
+                    tma_load4(q_at + group * S::kQueryBytes + half * S::kQueryHalf, &qmap, bar(kQueries + group), half, x.q_head,
                               x.start + group * g.tokens_of_tile);
             }
             __syncwarp();
         };
         uint32_t step = 0;
         int item_no = 0;                           // of this group
+        // One row tile: a tile's sums, on the barrier that its number in the run says.  Only the last tile's and the one
+        // before it are asked for: what the barrier had two tiles earlier was done when the last tile's scores came, and
+        // what it has two tiles later waits for weights that are not made yet, so its turn is the one that is meant.
+        auto sums_done = [&](uint32_t t) { return wait(kSumsDone + (t & 1), t >> 1 & 1); };
         int key_stage = 0, value_stage = 0;        // of the keys and values that are freed next
         auto next = [](int &at, int by, int stages) { at = (at + by) % stages; };
         bool ok = wait_item(0), loaded = false;
@@ -212,19 +230,23 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                 if (!loaded) load_queries(x);
                 const int count = x.count, tile0 = x.tile0, skipped = x.skipped;
                 // The last group to use a tile frees its stages: when it sees its scores, the products of the keys are
-                // done, and those of the tile before's values, which were issued earlier.
+                // done, and those of the values that were issued earlier: of the tile before, or with one row tile of the
+                // one before that.
+                constexpr int kBehind = kTwo ? 1 : 2;
+                bool lost = false;
                 const bool frees = (group == 1) == two_of(x) && (threadIdx.x & 127) == 0;
                 const int32_t seen_end = x.kind & kDead ? 0 : x.place + token + 1, low = low_of(shape, x.place + token);
                 for (int j = 0; j < count; ++j, ++step) {
-                    ok = wait(kScores + group, step & 1);
+                    ok = kTwo ? wait(kScores + group, step & 1) : wait(kScores + (step & 1), step >> 1 & 1);
                     if (!ok) break;
                     fence_after();
                     if (frees) {
                         bar_arrive(bar(kKeyFull + kFree + key_stage));
-                        if (j > 0) bar_arrive(bar(kValueFull + kFree + value_stage));
+                        if (j >= kBehind) bar_arrive(bar(kValueFull + kFree + value_stage));
                     }
                     next(key_stage, 1, S::kKeyStages);
-                    if (j > 0) next(value_stage, 1, S::kValueStages);
+                    if (j >= kBehind) next(value_stage, 1, S::kValueStages);
+                    const uint32_t s_at = kTwo ? s_first : s_first + (step & 1) * kKeys;
                     __syncwarp();                     // lanes come from the wait one by one, loads from TMEM are the warp's
                     uint32_t s[kChunks][32];
 #pragma unroll
@@ -262,6 +284,11 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                         const float fix = top == next ? 1.f : ex2(top - next);      // of -infinity too: another row's maximum grew
                         top = next;
                         total *= fix;
+                        // with one row tile these scores were issued before the last sums
+                        if (!kTwo) {
+                            lost = !sums_done(step - 1);
+                            fence_after();
+                        }
 #pragma unroll 1
                         for (int c = 0; c < D / 32; ++c) {
                             uint32_t o[32];
@@ -290,10 +317,13 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                         tmem_store(s_at + 32 * h, p);
                         tmem_store_wait();
                         fence_before();
-                        numbered_arrive<kHandOverThreads>(kHandOver + h + 2 * group);        // the product starts with the first part
+                        // the product starts with the first part
+                        numbered_arrive<kHandOverThreads>(kTwo ? kHandOver + h + 2 * group : kHandOver + (step & 1));
                     }
+                    if (lost) break;                  // not before the issuing warp is let go
                     total += (part[0].x + part[0].y) + (part[1].x + part[1].y);
                 }
+                ok = ok && !lost;
                 if (!ok) break;
             }
             // The next item's queries come in, and their first product is done, while this one's results are written.
@@ -302,29 +332,33 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             const Item &following = item_of(n + 1);
             loaded = following.count > 0 && !(group == 1 && !two_of(following));
             if (loaded) load_queries(following);
-            ok = wait(kSumsDone + group, item_no & 1);
+            ok = kTwo ? wait(kSumsDone + group, item_no & 1) : sums_done(step - 1);
             if (!ok) break;
             fence_after();
             ++item_no;
             const Item &x = item_of(n);
-            if ((group == 1) == two_of(x) && (threadIdx.x & 127) == 0) bar_arrive(bar(kValueFull + kFree + value_stage));
-            next(value_stage, 1, S::kValueStages);
+            for (int i = kTwo ? 1 : min(x.count, 2); i > 0; --i) {
+                if ((group == 1) == two_of(x) && (threadIdx.x & 127) == 0) bar_arrive(bar(kValueFull + kFree + value_stage));
+                next(value_stage, 1, S::kValueStages);
+            }
             const bool left_out = flags[n % kItems] == n + 1, live = live_of(x), whole = x.kind & kWhole;
             const float inv = inverse(total);
             // an item's result, or a piece: the item's first one in the block's second place
             const int64_t query = x.start + token, at = ((int64_t)(2 * blockIdx.x + ((x.kind & kFirst) != 0)) * kGroups + group) * kRows + row;
             const int q_head = x.q_head + member;
             T *out = static_cast<T *>(g.a.out) + query * g.a.out_stride[0] + q_head * g.a.out_stride[1];
+            // Few columns at a time: with 32, 2 to 3% slower in short items, with all under way together 5%, since this code
+            // is fetched anew for each item.
 #pragma unroll 1
-            for (int c = 0; c < D / 16; ++c) {
-                uint32_t o[16];
+            for (int c = 0; c < D / kColumns; ++c) {
+                uint32_t o[kColumns];
                 __syncwarp();
-                tmem_load(o, o_at + 16 * c);
+                tmem_load(o, o_at + kColumns * c);
                 tmem_load_wait();
                 if (live && left_out) {
-                    const Spoilt y = spoilt<D, T, 16>(g, shape, x, token, q_head, 16 * c, top, scale);
+                    const Spoilt y = spoilt<D, T>(g, shape, x, token, q_head, kColumns * c, top, scale);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
+                    for (int i = 0; i < kColumns; ++i) {
                         float z = __uint_as_float(o[i]);
                         if (y.plus >> i & 1) z += INFINITY;
                         if (y.minus >> i & 1) z -= INFINITY;
@@ -342,15 +376,15 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                         w[i] = make_uint4(u[0], u[1], u[2], u[3]);
                     }
                     if (g.out_wide) {
-                        store32(out + 16 * c, w[0], w[1]);
+                        store32(out + kColumns * c, w[0], w[1]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4 *>(out + 16 * c + 8 * i) = w[i];
+                        for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4 *>(out + kColumns * c + 8 * i) = w[i];
                     }
                 } else if (live) {
 #pragma unroll
-                    for (int i = 0; i < 16; i += 8)
-                        store32(g.part_o + at * D + 16 * c + i, make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]), make_uint4(o[i + 4], o[i + 5], o[i + 6], o[i + 7]));
+                    for (int i = 0; i < kColumns; i += 8)
+                        store32(g.part_o + at * D + kColumns * c + i, make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]), make_uint4(o[i + 4], o[i + 5], o[i + 6], o[i + 7]));
                 }
             }
             if (live && !whole) g.part_ml[at] = make_float2(top, total);
@@ -360,7 +394,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             done_item(n);
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (kTwo) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kLoadWarp || warp == kLoadWarp + 1) {
             // ---- keys by one warp, values by the other: one copy for each cache block (or part of one) of a tile and 64 of
             // its values.  The lanes look up the blocks and one thread issues: issued by several threads at once, each with
@@ -528,20 +562,21 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             const uint32_t q_lo = (uint32_t)operand(q_at, 16, 1024), k_lo = (uint32_t)operand(ring, 16, 1024);
             const uint32_t v_lo = (uint32_t)operand(ring + S::kKeyStages * S::kTileBytes, S::kHalfBytes, 1024);
             constexpr uint32_t high = (1024 >> 4) | (1u << 14) | (2u << 29);
-            auto scores = [&](int i, int stage) {
-                const uint32_t a = q_lo + i * (S::kTileBytes >> 4), b = k_lo + stage * (S::kTileBytes >> 4);
+            // of row tile i, into place `to` of two
+            auto scores = [&](int i, int to, int stage) {
+                const uint32_t a = q_lo + i * (S::kQueryBytes >> 4), b = k_lo + stage * (S::kTileBytes >> 4);
                 if (one) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint32_t in = (k % 4) * 32;
-                        mma_smem(i * kKeys, a + (((k / 4) * S::kHalfBytes + in) >> 4), b + (((k / 4) * S::kHalfBytes + in) >> 4), high, kFirstWhat, k > 0);
+                        mma_smem(to * kKeys, a + (((k / 4) * S::kQueryHalf + in) >> 4), b + (((k / 4) * S::kHalfBytes + in) >> 4), high, kFirstWhat, k > 0);
                     }
-                    commit(bar(kScores + i));
+                    commit(bar(kScores + to));
                 }
                 __syncwarp();
             };
-            auto sums = [&](int i, int stage, int part, bool add) {
-                const uint32_t b = v_lo + stage * (S::kTileBytes >> 4), a = i * kKeys, d = kSums + i * D;
+            auto sums = [&](int i, int from, int stage, int part, bool add) {
+                const uint32_t b = v_lo + stage * (S::kTileBytes >> 4), a = from * kKeys, d = kSums + i * D;
                 constexpr int kSteps = 4;                        // of 16 tokens
                 if (one) {
 #pragma unroll
@@ -552,6 +587,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             };
             int k_at = 0, v_at = 0;                              // stages of the tile's keys and values
             uint32_t taken = 0;                                  // copies handed over so far: the run's first keys, then its tiles
+            uint32_t step = 0;                                   // tiles so far
             auto next = [](int &at, int stages) {
                 if (++at == stages) at = 0;
             };
@@ -564,7 +600,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                     ok = wait(kQueries + i, begun[i]++ & 1);
                     if (!ok) break;
                     fence_after();
-                    scores(i, k_at);
+                    scores(i, kTwo ? i : step & 1, k_at);
                 }
                 if (!ok) break;
                 next(k_at, S::kKeyStages);
@@ -572,18 +608,31 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                     const bool more = j + 1 < count;
                     const uint32_t others = look_failed();       // used when it has come
                     numbered_sync<kCopiesThreads>(kCopies + taken++ % 8);        // its values, and the next keys
+                    if (!kTwo) {
+                        // One row tile: the next scores, in the other place, before the weights of these are there.  What lay
+                        // in that place were the weights of the tile before, whose product was issued earlier.
+                        ok = !__any_sync(~0u, others);
+                        if (!ok) break;
+                        if (more) scores(0, (step + 1) & 1, k_at);
+                        numbered_sync<kHandOverThreads>(kHandOver + (step & 1));
+                        fence_after();
+                        sums(0, step & 1, v_at, 0, j > 0);
+                        if (one) commit(bar(kSumsDone + (step & 1)));
+                        __syncwarp();
+                        ++step;
+                    }
 #pragma unroll
-                    for (int i = 0; i < kGroups; ++i) {
+                    for (int i = 0; kTwo && i < kGroups; ++i) {
                         if (i >= groups) break;
                         numbered_sync<kHandOverThreads>(kHandOver + 2 * i);
                         fence_after();
-                        sums(i, v_at, 0, j > 0);
+                        sums(i, i, v_at, 0, j > 0);
                         numbered_sync<kHandOverThreads>(kHandOver + 1 + 2 * i);
                         fence_after();
-                        sums(i, v_at, 1, true);
+                        sums(i, i, v_at, 1, true);
                         if (i == 0) ok = !__any_sync(~0u, others);
                         if (!ok) break;
-                        if (more) scores(i, k_at);
+                        if (more) scores(i, i, k_at);
                         else if (one) commit(bar(kSumsDone + i));
                         __syncwarp();
                     }
@@ -610,9 +659,9 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
 
 template <int D, typename T>
 cudaError_t launch_of(const PromptArgs &g, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, int sms, cudaStream_t st) {
-    const cudaError_t e = launch_kernel(prompt_kernel<D, T>, dim3(sms), kThreads, Shape<D>::kSmem, st, false, g, q, k, v);
+    const cudaError_t e = launch_kernel(prompt_kernel<D, T>, dim3(sms), Shape<D>::kThreads, Shape<D>::kSmem, st, false, g, q, k, v);
     if (e != cudaSuccess) return e;
-    return launch_kernel(join_kernel<D, T, kGroups * kRows, kRows, kKeys>, dim3(kJoinBlocks * sms), kJoinThreads, 0, st, true, g, sms);
+    return launch_kernel(join_kernel<D, T, Shape<D>::kGroups * kRows, kRows, Shape<D>::kKeys>, dim3(kJoinBlocks * sms), kJoinThreads, 0, st, true, g, sms);
 }
 
 template <int D, typename T>
@@ -620,27 +669,32 @@ cudaError_t prepare_of() {
     return cudaFuncSetAttribute(prompt_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem);
 }
 
+template <typename T>
+cudaError_t prepare_dim(int head_dim) {
+    return head_dim == 64 ? prepare_of<64, T>() : head_dim == 128 ? prepare_of<128, T>() : prepare_of<256, T>();
+}
+template <typename T>
+cudaError_t launch_dim(const PromptArgs &g, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, int head_dim, int sms, cudaStream_t st) {
+    return head_dim == 64 ? launch_of<64, T>(g, q, k, v, sms, st) : head_dim == 128 ? launch_of<128, T>(g, q, k, v, sms, st) : launch_of<256, T>(g, q, k, v, sms, st);
+}
+
 }  // namespace
 
 cudaError_t prepare_prompt(int head_dim, int type) {
-    if (head_dim == 256) return prepare_prompt_wide(type);
-    if (type == ISJL_KV_BF16) return head_dim == 64 ? prepare_of<64, __nv_bfloat16>() : prepare_of<128, __nv_bfloat16>();
-    return head_dim == 64 ? prepare_of<64, __half>() : prepare_of<128, __half>();
+    return type == ISJL_KV_BF16 ? prepare_dim<__nv_bfloat16>(head_dim) : prepare_dim<__half>(head_dim);
 }
 
 cudaError_t launch_prompt(PromptArgs &g, void *encoder, int head_dim, int type, int sms, cudaStream_t st) {
-    if (head_dim == 256) return launch_prompt_wide(g, type, sms, st);
     CUtensorMap q, k, v;
     share_rows(g, kRows);
     g.out_wide = reinterpret_cast<uintptr_t>(g.a.out) % 32 == 0 && (g.a.out_stride[0] | g.a.out_stride[1]) % 16 == 0;
     if (sms > kMostRuns) sms = kMostRuns;
-    const int rows = 1 << g.shift < kKeys ? 1 << g.shift : kKeys;
+    const int keys = head_dim == 256 ? Shape<256>::kKeys : Shape<128>::kKeys, rows = 1 << g.shift < keys ? 1 << g.shift : keys;
     if (!encode_queries(encoder, &q, g.a.q, g.a.q_stride, g.tokens_of_tile, g.rows_of_token, g.a.n_tokens, g.n_kv_heads * g.group, head_dim, type) ||
         !encode_cache(encoder, &k, g.cache.k, g.cache.k_stride, rows, 1, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type) ||
         !encode_cache(encoder, &v, g.cache.v, g.cache.v_stride, rows, 1, g.n_blocks, g.shift, g.n_kv_heads, head_dim, type))
         return cudaErrorInvalidValue;
-    if (type == ISJL_KV_BF16) return head_dim == 64 ? launch_of<64, __nv_bfloat16>(g, q, k, v, sms, st) : launch_of<128, __nv_bfloat16>(g, q, k, v, sms, st);
-    return head_dim == 64 ? launch_of<64, __half>(g, q, k, v, sms, st) : launch_of<128, __half>(g, q, k, v, sms, st);
+    return type == ISJL_KV_BF16 ? launch_dim<__nv_bfloat16>(g, q, k, v, head_dim, sms, st) : launch_dim<__half>(g, q, k, v, head_dim, sms, st);
 }
 
 }  // namespace isjl

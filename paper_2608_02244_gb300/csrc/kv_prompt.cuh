@@ -1,6 +1,5 @@
-// kv_prompt.cuh -- what the two kernels of isjl_kv_prompt share: kv_prompt.cu (heads of 64 and 128 values) and
-// kv_prompt_wide.cu (256).  Rows of queries and the items that they make, the run of items that a block has, values that
-// must not spread, and the kernel that joins pieces of items.
+// kv_prompt.cuh -- what stands around isjl_kv_prompt's products (kv_prompt.cu): rows of queries and the items that they
+// make, the run of items that a block has, values that must not spread, and the kernel that joins pieces of items.
 #pragma once
 
 #include "kv_prompt_line.cuh"
@@ -10,6 +9,7 @@ namespace isjl {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kColumns = 16;                        // of a row's sums that are written at a time
 constexpr int kMostRuns = 1024;                     // blocks that have a run, at most
 constexpr int kJoinBlocks = 8, kJoinThreads = 128;  // of the joining kernel, for each SM
 
@@ -111,12 +111,12 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
     return ((w & kExponent) + kLowest) & 0x80008000u;
 }
 
-// Of the values that the sums left out because they are not finite: what they make of 32 columns' sums, a bit each
+// Of the values that the sums left out because they are not finite: what they make of kColumns columns' sums, a bit each
 // (infinite, the other sign's, undefined).  Rare and slow: the row's weights are computed again from the cache.
 struct Spoilt {
     uint32_t plus, minus, none;
 };
-template <int D, typename T, int kColumns>
+template <int D, typename T>
 __device__ __forceinline__ Spoilt spoilt(const PromptArgs &g, const PromptShape &s, const Item &x, int32_t token, int32_t q_head, int column, float top,
                                          float scale) {
     Spoilt out = {0, 0, 0};

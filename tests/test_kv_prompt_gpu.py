@@ -157,6 +157,23 @@ def test_maxima_that_move(dim, dtype, shape):
     check(s)
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 1, 20, 65, 130])
+def test_maxima_that_move_in_short_items(dim, window):
+    """Many items of one to seven tiles in a run, with maxima that grow from tile to tile; the same bits every time."""
+    import torch
+    s = prompts([400] * 30, [0] * 30, 48, 1, dim, 16, seed=2)
+    d = decoder(s)
+    at = torch.arange(400, device="cuda")
+    for row in s["table"].long():
+        b = row[at // 16]
+        s["k"][b, at % 16] = (s["k"][b, at % 16] * (at[:, None, None] / 60)).to(s["k"].dtype)
+    want, lse = check(s, d, window=window)
+    for _ in range(5):
+        out, again = d.prompt(**s, window=window, lse=True)
+        assert torch.equal(out, want) and torch.equal(again, lse)
+
+
 def test_small_weights_count():
     """fp16: thousands of tokens far below the largest score."""
     import torch
