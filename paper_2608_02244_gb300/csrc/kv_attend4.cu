@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         const int32_t y = p.x + 8 * my_eight;
         if (y >= p.s.end || (y + 8 <= p.s.lo && y >= a.sinks)) return kNone;           // nothing is seen of it
         const int32_t j = y >> g.shift;
-        return j < a.n_prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - a.n_prefix_blocks)];
+        return max(j < a.n_prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - a.n_prefix_blocks)], -1);
     };
     const unsigned char *const kind_base = static_cast<const unsigned char *>(kind == 0 ? g.cache.k : kind == 1 ? g.cache.k_scale : kind == 2 ? g.cache.v : g.cache.v_scale);
     if (lane < 4 * kEights && my_eight == 0)

@@ -417,7 +417,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             auto look = [&]() {
                 y0 = tile_at(shape, x, j);
                 const int32_t y = y0 + piece * rows;
-                block = !(x.kind & kDead) && y < x.end && (y + rows > x.low || y < shape.sinks) ? block_at(g, x.row, y) : kNone;
+                block = !(x.kind & kDead) && y < x.end && (y + rows > x.low || y < shape.sinks) ? max(block_at(g, x.row, y), -1) : kNone;
             };
             if (ok && x.count > 0) look();
             while (ok && x.count > 0) {

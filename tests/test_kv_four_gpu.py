@@ -357,6 +357,22 @@ def test_attend_bad_blocks_and_lengths():
     kv_plain.check_attend(out[:3], lse[:3], *kv_plain.attend(s["q"][:3], z[0], z[1], table[:3], s["lens"][:3]))
 
 
+@pytest.mark.parametrize("number", ["n_blocks", -1, 2**31 - 1, -2**31])
+def test_attend_any_bad_block_is_reported(number):
+    """One block number outside the cache, whatever it is: reported, and its tokens read as zeros."""
+    import torch
+    from paper_2608_02244_gb300 import kv
+    s = requests([70], 4, 2, 128, 16, seed=7)
+    d = decoder4(s)
+    last = s["cache"].k.shape[0]
+    s["table"][0, 3] = last if number == "n_blocks" else number
+    out, lse = d.attend4(**s, lse=True)
+    assert d.status() == kv.ISJL_ERR_INVALID_ARG and d.status() == 0
+    z = [torch.cat((x, torch.zeros_like(x[:1]))) for x in kv4_plain.in_16_bits(s["cache"])]
+    table = torch.where((s["table"] < 0) | (s["table"] >= last), last, s["table"])
+    kv_plain.check_attend(out, lse, *kv_plain.attend(s["q"], z[0], z[1], table, s["lens"]))
+
+
 def test_attend_strided_and_given_outputs():
     import torch
     s = requests([70, 5, 300], 6, 2, 64, 16, seed=7)

@@ -284,6 +284,23 @@ def test_bad_rows_and_blocks():
     kv_plain.check_attend(out, lse, want, want_lse, size)
 
 
+@pytest.mark.parametrize("number", ["n_blocks", -1, 2**31 - 1, -2**31])
+def test_any_bad_block_is_reported(number):
+    """One block number outside the cache, whatever it is: reported, and its tokens read as zeros."""
+    import torch
+    from paper_2608_02244_gb300 import kv
+    s = prompts([50], [20], 4, 2, 128, 16, seed=7)
+    d = decoder(s)
+    last = s["k"].shape[0]
+    s["table"][0, 3] = last if number == "n_blocks" else number
+    out, lse = d.prompt(**s, lse=True)
+    assert d.status() == kv.ISJL_ERR_INVALID_ARG and d.status() == 0
+    k, v = (torch.cat((x, torch.zeros_like(x[:1]))) for x in (s["k"], s["v"]))
+    table = torch.where((s["table"] < 0) | (s["table"] >= last), last, s["table"])
+    want, want_lse, size = plain(dict(s, k=k, v=v, table=table))
+    kv_plain.check_attend(out, lse, want, want_lse, size)
+
+
 def test_bad_starts():
     """Rows whose starts descend or leave the queries are skipped, the others are not."""
     import torch
