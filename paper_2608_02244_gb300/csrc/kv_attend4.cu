@@ -169,12 +169,16 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     // one eight lies, and looks up its block a slice ahead of that.
     const uint32_t ring = smem_at(smem) + warp * S::kStages * S::kStageBytes;
     const int slot_mask = (1 << g.shift) - 1, kind = (lane / kEights) & 3, my_eight = lane % kEights;
-    constexpr int32_t kNone = INT32_MIN;
+    // whether something is seen of a lane's eight tokens
+    auto seen_of = [&](const At &p) {
+        const int32_t y = p.x + 8 * my_eight;
+        return y < p.s.end && (y + 8 > p.s.lo || y < a.sinks);
+    };
     auto block_of = [&](const At &p) {
         const int32_t y = p.x + 8 * my_eight;
-        if (y >= p.s.end || (y + 8 <= p.s.lo && y >= a.sinks)) return kNone;           // nothing is seen of it
+        if (!seen_of(p)) return -1;
         const int32_t j = y >> g.shift;
-        return max(j < a.n_prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - a.n_prefix_blocks)], -1);
+        return j < a.n_prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - a.n_prefix_blocks)];
     };
     const unsigned char *const kind_base = static_cast<const unsigned char *>(kind == 0 ? g.cache.k : kind == 1 ? g.cache.k_scale : kind == 2 ? g.cache.v : g.cache.v_scale);
     if (lane < 4 * kEights && my_eight == 0)
@@ -212,11 +216,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     };
     auto feed_keys = [&](uint32_t stage) {
         if (ahead_left > 0) {
-            bool there = ahead_block != kNone;
-            if (there && (uint32_t)ahead_block >= (uint32_t)g.n_blocks) {
-                report(g.status);                      // beyond the cache: zeros
-                there = false;
-            }
+            const bool there = (uint32_t)ahead_block < (uint32_t)g.n_blocks;
+            if (!there && seen_of(ahead)) report(g.status);          // beyond the cache: zeros
             if (lane < 4 * kEights) {
                 const int slot = (ahead.x + 8 * my_eight) & slot_mask;
                 const int64_t *stride = eight_stride[warp][kind];

@@ -402,7 +402,6 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             const int rows = min(1 << g.shift, kKeys), pieces = kKeys / rows;      // pieces: 1 .. 16
             const int piece = lane % pieces;                         // whose block this lane looks up
             const bool one = elect_one();
-            constexpr int32_t kNone = INT32_MIN;
             // A ring for each: a stage's turns are one warp's, which cannot be two turns ahead of itself.
             const bool values = warp != kLoadWarp;
             const int stages = values ? S::kValueStages : S::kKeyStages, full = values ? kValueFull : kKeyFull;
@@ -412,16 +411,19 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             uint32_t turn = 0;
             bool ok = wait_item(0);
             Item x = item_of(0);
-            int32_t block = kNone, y0 = 0;                           // of the tile that is next
+            int32_t block = 0, y0 = 0;                               // of the tile that is next
+            bool seen = false;
             // the block's number, if any of the item's queries sees some of this part; asked for one tile ahead
             auto look = [&]() {
                 y0 = tile_at(shape, x, j);
                 const int32_t y = y0 + piece * rows;
-                block = !(x.kind & kDead) && y < x.end && (y + rows > x.low || y < shape.sinks) ? max(block_at(g, x.row, y), -1) : kNone;
+                seen = !(x.kind & kDead) && y < x.end && (y + rows > x.low || y < shape.sinks);
+                block = seen ? block_at(g, x.row, y) : 0;
             };
             if (ok && x.count > 0) look();
             while (ok && x.count > 0) {
                 int32_t from = block;
+                const bool real = seen;
                 const int kv = x.kv, slot = y0 & ((1 << g.shift) - 1);             // slot: 0 but in blocks larger than a tile
                 if (++j == x.count) {
                     done_item(n);
@@ -432,8 +434,8 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                 if (ok && x.count > 0) look();
                 if (load == stages) ok = wait(full + kFree + stage, turn ^ 1) && ok;
                 if (!ok) break;
-                if ((uint32_t)from >= (uint32_t)g.n_blocks) {             // not seen, or beyond the cache: zeros
-                    if (from != kNone) report(g.status);
+                if (!real || (uint32_t)from >= (uint32_t)g.n_blocks) {    // not seen, or beyond the cache: zeros
+                    if (real) report(g.status);
                     from = g.n_blocks;
                 }
                 if (one) bar_expect(bar(full + stage), S::kTileBytes);
