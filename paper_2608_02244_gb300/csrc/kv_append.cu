@@ -7,7 +7,8 @@
 // 32 + 2 x 8 heads of 128 values 202 us, 6.1 TB/s).
 //
 // A cache in 4 bits: a group of 32 values is four neighbouring threads, whose least and largest value come by two
-// shuffles; each thread makes a word of its eight codes, the first of the four writes scale and offset.
+// shuffles; each thread makes a word of its eight codes, the first of the four writes scale and offset.  Bound by
+// instructions: 20,011 tokens of 28 + 2 x 4 heads of 64 values 40 us, 31 into 16 bits, whose rows in memory are longer.
 #include "kv_internal.cuh"
 
 namespace isjl {

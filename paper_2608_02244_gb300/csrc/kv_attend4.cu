@@ -13,6 +13,11 @@
 //   words of eight codes, a shift and one logical instruction makes a pair of them numbers (kv_four.cuh) and one fused
 //   multiplication and addition their values, in the order in which the instruction wants them;
 // - weights go from the first product's layout to the second's by a transposition in the warp (movmatrix).
+//
+// 512 queries of 64 + 8 heads of 128 values over 1.1 million tokens, 1.6 GB: 338 us, 4.7 TB/s; 690 instructions for 32 tokens
+// of a key head (290 make numbers of codes, 32 are products), issue slots 58% busy, the ALU 51%, the tensor pipe 21%.  128
+// queries over 4,096 tokens with 4 query heads on each of 8 key heads 147 us (4.6 TB/s), 16 on each of 4 106; 256 values, 4
+// on each of 4, 154 (4.4 TB/s).
 #include "kv_four.cuh"
 #include "kv_sight.cuh"
 
@@ -27,7 +32,9 @@ template <int D, int kTiles>
 struct Shape {
     static constexpr int kCodes = D / 2, kScales = D / 8;          // bytes of a token's key (or value) in one head
     static constexpr int kChunks = kCodes / 16;                    // of 16 bytes, of its codes
-    static constexpr int kSlice = D == 256 ? 32 : 64, kEights = kSlice / 8;        // tokens
+    // tokens.  Longer slices have fewer instructions a token around their products: 64 against 32 with 128 values 337 and 381 us
+    // (the case above), with 64 values 98 and 112; with 256 values, where fewer blocks' rings fit, 269 and 155.
+    static constexpr int kSlice = D == 256 ? 32 : 64, kEights = kSlice / 8;
     static constexpr int kStageBytes = kSlice * (kCodes + kScales);
     static constexpr int kStages = D == 256 ? 5 : 3;                              // of a warp's ring: keys or values of a slice
     static_assert(kStages % 2 == 1, "a slice's keys and values are under way together");
@@ -591,7 +598,8 @@ cudaError_t prepare_of(int sms, int *warps) {
     return cudaFuncSetAttribute(attend4_kernel<D, T, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<D, kTiles>(ISJL_KV_MAX_ROWS));
 }
 
-// 8 query heads at a time, or 16 where a key head has more
+// 8 query heads at a time, or 16 where a key head has more, which then is read once for 16: 4 key heads with 16 query heads
+// each, 128 queries over 4,096 tokens, 106 us against 150 in two times 8 (256 values: 278 and 302).
 template <int D, typename T>
 cudaError_t prepare_tiles(int group, int sms, int *warps) {
     return group <= 8 ? prepare_of<D, T, 1>(sms, warps) : prepare_of<D, T, 2>(sms, warps);

@@ -29,7 +29,7 @@
 // Measured, 32 + 8 heads of 128 values, bf16: 16,384 tokens 1,335 us (1,645 TFLOP/s, power-limited when it runs for
 // long: 1,440 us), 8 requests of 4,096 785 us (1,400), 32 of 1,024 314 us (875), 64 of 256 119 us; 64 values, 16,384 tokens
 // 1,117 us (985: 128 exponentials a row and tile take the SM 2,048 cycles, the products 1,024); 256 values, 16 + 4 heads,
-// 16,384 tokens 1,630 us (1,350; products a warp at a time, 64 rows an item, took 11,700).  Short prompts are bound by what
+// 16,384 tokens 1,635 us (1,345; products a warp at a time, 64 rows an item, took 11,700).  Short prompts are bound by what
 // an item takes beside its tiles: some 3,000 cycles of TMEM loads and 2,000 of stores for its results, during which its
 // own products wait, and the first tile's way through the pipeline.
 #include "kv_prompt.cuh"

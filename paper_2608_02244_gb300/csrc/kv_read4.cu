@@ -1,7 +1,8 @@
 // kv_read4.cu -- 16-bit values of slots of a cache in 4 bits (isjl_kv_read4).
 //
-// A thread takes 8 codes (4 bytes) to 8 values (16 bytes); a block has some tokens' keys and values.  Bound by memory:
-// 5 bits a value in, 16 out.
+// A thread takes 8 codes (4 bytes) to 8 values (16 bytes), the same place of eight tokens, whose loads are under way
+// together.  Bound by memory, 5 bits a value in, 16 out: 98,309 tokens of 8 heads of 128 values, 529 MB, 95 us (5.6 TB/s; four
+// tokens a thread 119, sixteen 120).
 #include "kv_four.cuh"
 
 #include <algorithm>
