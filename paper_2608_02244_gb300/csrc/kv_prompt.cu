@@ -46,6 +46,10 @@ struct Shape {
     static constexpr int kGroups = D == 256 ? 1 : 2;             // row tiles of an item, each with its four warps
     static constexpr int kKeys = D == 256 ? 64 : 128;            // of a token tile
     static constexpr int kParts = kKeys / 64;                    // of a tile's weights, handed over one after another
+    // An item's first scores, its results and the masks of its last tile, in tiles, which the runs count with them.  With 0, 2,
+    // 3 and 4 of them one prompt of 16,384 tokens (128 values) took 1,344, 1,223, 1,226 and 1,232 us, 37 ragged ones (64 values)
+    // 172, 135, 145 and 148; with 256 values, 0, 2, 4 and 6: 1,668, 1,555, 1,501 and 1,498 us and, ragged, 161, 122, 111 and 115.
+    static constexpr int kExtra = D == 256 ? 4 : 2;
     static constexpr int kLoadWarp = 4 * kGroups, kIssueWarp = kLoadWarp + 2, kPlanWarp = kLoadWarp + 3;     // plans and cleans
     static constexpr int kThreads = 128 * kGroups + 128;
     static constexpr int kSums = 256;                            // TMEM: scores from 0, sums from here
@@ -114,7 +118,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
     const uint32_t q_at = base, ring = base + kGroups * S::kQueryBytes;
     const uint32_t bar0 = smem_addr(bars);
     auto bar = [&](int i) { return bar0 + 8 * i; };
-    const PromptShape shape = {kKeys, kGroups * g.tokens_of_tile, g.a.window, g.a.sinks};
+    const PromptShape shape = {kKeys, kGroups * g.tokens_of_tile, g.a.window, g.a.sinks, S::kExtra};
 
     start_next();
     if (threadIdx.x == 0) {

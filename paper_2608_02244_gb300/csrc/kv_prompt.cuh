@@ -165,9 +165,10 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
     return (a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
 }
 
-// A block's run of the line: tiles f .. f1 - 1, of which `here` is the first.
+// A block's run of the line: places f .. f1 - 1, of which `here` is the first.  An item's tiles have some places before them
+// that stand for its beginning and end, so that runs of many items have fewer tiles.
 struct Run {
-    int64_t tiles, blocks;       // of the line; those with a run
+    int64_t tiles, blocks;       // places of the line; blocks with a run
     int64_t f, f1;
     Place here;
 };
@@ -251,8 +252,13 @@ __device__ __forceinline__ Item take_item(const PromptArgs &g, const PromptShape
     if (run.f == run.f1) return x;
     Place &p = run.here;
     const int32_t tiles = p.r.tiles(s, p.item), first = p.item * s.step, last = p.r.end(s, p.item) - 1;
-    x.count = (int)min((int64_t)tiles - p.j, run.f1 - run.f);
-    x.tile0 = p.j;
+    const int32_t places = (int32_t)min((int64_t)s.extra + tiles - p.j, run.f1 - run.f);
+    x.tile0 = max(0, p.j - s.extra);
+    x.count = max(0, p.j + places - s.extra) - x.tile0;
+    if (x.count == 0) {                                  // the run ends before the item's first tile
+        run.f = run.f1;
+        return x;
+    }
     x.skipped = p.r.skip(s, p.item);
     x.row = p.row;
     x.kv = p.head / g.parts;
@@ -264,10 +270,10 @@ __device__ __forceinline__ Item take_item(const PromptArgs &g, const PromptShape
     x.low = low_of(s, x.place);
     x.from = p.r.dead ? 0 : x.place + 1;
     x.below = low_of(s, last);
-    x.kind = (x.count == tiles ? kWhole : 0) | (p.j == 0 ? kFirst : 0) | (p.r.dead ? kDead : 0);
-    if (writes && x.count < tiles && p.j == 0)           // its pieces are those of the blocks from here on
-        g.cut[blockIdx.x] = {p.row, p.head, p.item, (int)quotient((run.f + tiles) * run.blocks - 1, run.tiles)};
-    run.f += x.count;
+    x.kind = (x.count == tiles ? kWhole : 0) | (x.tile0 == 0 ? kFirst : 0) | (p.r.dead ? kDead : 0);
+    if (writes && x.count < tiles && x.tile0 == 0)       // its pieces are those of the blocks from here on
+        g.cut[blockIdx.x] = {p.row, p.head, p.item, (int)quotient((run.f - p.j + s.extra + tiles) * run.blocks - 1, run.tiles)};
+    run.f += places;
     if (run.f < run.f1) next_item(g, s, p);
     return x;
 }

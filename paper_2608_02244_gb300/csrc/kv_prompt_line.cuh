@@ -40,6 +40,7 @@ struct PromptShape {
     int32_t keys;              // tokens of a tile
     int32_t step;              // queries of an item
     int32_t window, sinks;     // window 0: all
+    int32_t extra;             // what an item takes beside its tiles, in tiles: places of the line in front of them
     ISJL_LINE int32_t sink_tiles() const { return sinks / keys + (sinks % keys != 0); }
 };
 
@@ -65,11 +66,11 @@ struct PromptRow {
     }
     // which tile of tokens is an item's j-th
     static ISJL_LINE int32_t tile(const PromptShape &s, int32_t skipped, int32_t j) { return j < s.sink_tiles() ? j : j + skipped; }
-    // tiles of the items before p, p <= items
+    // places of the line of the items before p, p <= items
     ISJL_LINE int64_t before(const PromptShape &s, int32_t p) const {
         const bool all = p > 0 && p == items(s);           // the last item may be a shorter one
         const int32_t n = all ? p - 1 : p;
-        int64_t sum = line_sum((uint32_t)n, (uint32_t)s.keys, (uint32_t)s.step, (uint32_t)first + (uint32_t)s.step + (uint32_t)s.keys - 1);
+        int64_t sum = (int64_t)p * s.extra + line_sum((uint32_t)n, (uint32_t)s.keys, (uint32_t)s.step, (uint32_t)first + (uint32_t)s.step + (uint32_t)s.keys - 1);
         if (s.window) {
             // skipped tiles begin with the item whose window begins `sink_tiles` tiles on
             const int64_t off = (int64_t)first + 1 - s.window - (int64_t)s.sink_tiles() * s.keys;

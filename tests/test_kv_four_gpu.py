@@ -357,6 +357,12 @@ def test_attend_bad_blocks_and_lengths():
     kv_plain.check_attend(out[:3], lse[:3], *kv_plain.attend(s["q"][:3], z[0], z[1], table[:3], s["lens"][:3]))
 
 
+@pytest.mark.parametrize("hq,hkv,dim", [(100, 100, 64), (700, 700, 64), (1024, 1024, 64), (1024, 256, 64), (305, 305, 256), (1000, 8, 64)])
+def test_attend_many_heads(hq, hkv, dim):
+    """Key heads in numbers that do not divide the grid's warps."""
+    check_attend4(requests([70, 0, 200, 1, 33], hq, hkv, dim, 16, seed=hkv))
+
+
 @pytest.mark.parametrize("number", ["n_blocks", -1, 2**31 - 1, -2**31])
 def test_attend_any_bad_block_is_reported(number):
     """One block number outside the cache, whatever it is: reported, and its tokens read as zeros."""

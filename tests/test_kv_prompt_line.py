@@ -30,6 +30,7 @@ int main() {
         s.step = (s.keys == 128 ? 2 : 1) * (128 / rows);
         s.window = rnd(2) ? 0 : 1 + size(12);
         s.sinks = s.window && rnd(2) ? size(9) : 0;
+        s.extra = rnd(2) ? 0 : rnd(6);
         PromptRow r;
         r.count = 1 + size(11);
         r.first = rnd(2) ? 0 : size(13);
@@ -54,22 +55,22 @@ int main() {
             }
             if (at != want.size() || got.back() != want.back()) { printf("lacks a tile\n"); return 1; }
             if (got.size() > want.size() + 1) { printf("%zu tiles for %zu\n", got.size(), want.size()); return 1; }
-            sum += r.tiles(s, p);
+            sum += s.extra + r.tiles(s, p);
             ++checked;
         }
         if (r.before(s, r.items(s)) != sum) { printf("all\n"); return 1; }
     }
     // the largest numbers: no sum wraps
-    PromptShape s = {128, 256, 0, 0};
+    PromptShape s = {128, 256, 0, 0, 3};
     PromptRow r = {2147483647 - 255 - 5, 5};
     int64_t want = 0;
-    for (int p = 0; p < r.items(s); ++p) want += r.tiles(s, p);
+    for (int p = 0; p < r.items(s); ++p) want += s.extra + r.tiles(s, p);
     if (r.before(s, r.items(s)) != want) { printf("largest %ld %ld\n", (long)r.before(s, r.items(s)), (long)want); return 1; }
     s.window = 70000; s.sinks = 1000; want = 0;
-    for (int p = 0; p < r.items(s); ++p) want += r.tiles(s, p);
+    for (int p = 0; p < r.items(s); ++p) want += s.extra + r.tiles(s, p);
     if (r.before(s, r.items(s)) != want) { printf("largest with a window\n"); return 1; }
     r.first = 2147483647 - 255 - 1000; r.count = 1000; s.window = 2147483647 - 300; s.step = 2; want = 0;
-    for (int p = 0; p < r.items(s); ++p) want += r.tiles(s, p);
+    for (int p = 0; p < r.items(s); ++p) want += s.extra + r.tiles(s, p);
     if (r.before(s, r.items(s)) != want) { printf("largest place\n"); return 1; }
     printf("checked\n");
     return checked > 10000 ? 0 : 1;
