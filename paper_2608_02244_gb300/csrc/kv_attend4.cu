@@ -18,9 +18,9 @@
 //   multiplication and addition their values, in the order in which the instruction wants them;
 // - weights go from the first product's layout to the second's by a transposition in the warp (movmatrix).
 //
-// 512 queries of 64 + 8 heads of 128 values over 1.1 million tokens, 1.6 GB: 338 us, 4.7 TB/s; 690 instructions for 32 tokens
+// 512 queries of 64 + 8 heads of 128 values over 1.1 million tokens, 1.6 GB: 333 us, 4.8 TB/s; 690 instructions for 32 tokens
 // of a key head (290 make numbers of codes, 32 are products), issue slots 58% busy, the ALU 51%, the tensor pipe 21%.  128
-// queries over 4,096 tokens with 4 query heads on each of 8 key heads 147 us (4.6 TB/s), 16 on each of 4 106; 256 values, 4
+// queries over 4,096 tokens with 4 query heads on each of 8 key heads 150 us (4.5 TB/s), 16 on each of 4 106; 256 values, 4
 // on each of 4, 154 (4.4 TB/s).
 #include "kv_four.cuh"
 #include "kv_sight.cuh"

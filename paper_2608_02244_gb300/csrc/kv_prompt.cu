@@ -23,15 +23,16 @@
 // end, from the cache.
 //
 // The work is a line of (row, key head, item, tile): every block has an equal run of it, wherever prompts end, and one
-// long prompt, many short ones or a few queries over a long cache all keep every SM busy to the end.  Items cut by the
+// long prompt, many short ones or a few queries over a long cache all keep every SM busy to the end.  What an item takes
+// beside its tiles counts as some tiles more.  Items cut by the
 // runs' ends leave pieces (sum, maximum and total of each row), which a second kernel joins in their order.
 //
-// Measured, 32 + 8 heads of 128 values, bf16: 16,384 tokens 1,335 us (1,645 TFLOP/s, power-limited when it runs for
-// long: 1,440 us), 8 requests of 4,096 785 us (1,400), 32 of 1,024 314 us (875), 64 of 256 119 us; 64 values, 16,384 tokens
-// 1,117 us (985: 128 exponentials a row and tile take the SM 2,048 cycles, the products 1,024); 256 values, 16 + 4 heads,
-// 16,384 tokens 1,635 us (1,345; products a warp at a time, 64 rows an item, took 11,700).  Short prompts are bound by what
-// an item takes beside its tiles: some 3,000 cycles of TMEM loads and 2,000 of stores for its results, during which its
-// own products wait, and the first tile's way through the pipeline.
+// Measured, 32 + 8 heads of 128 values, bf16: 16,384 tokens 1,205 to 1,225 us (1,800 TFLOP/s; power-limited when it runs
+// for long: 1,360 us), 8 requests of 4,096 737 us (1,490), 32 of 1,024 306 us (900), 64 of 256 115 us; 64 values, 16,384 tokens
+// 1,047 us (1,050: 128 exponentials a row and tile take the SM 2,048 cycles, the products 1,024); 256 values, 16 + 4 heads,
+// 16,384 tokens 1,500 to 1,590 us (1,400; products a warp at a time, 64 rows an item, took 11,700).  Short prompts are bound
+// by what an item takes beside its tiles: 4,000 cycles for its results (TMEM loads and stores, during which its rows'
+// threads do nothing else), 2,000 until the next item's first weights, 1,200 for the masks of its last tile.
 #include "kv_prompt.cuh"
 #include "kv_tensor.cuh"
 

@@ -402,7 +402,7 @@ class Decoder:
     # ---- a cache in 4 bits ---------------------------------------------------
     def cache4(self):
         """A new cache in 4 bits whose tokens stand for zeros, each block's heads outermost in memory: a head's
-        codes and scales of a block then lie next to one another, which is the fastest order to read."""
+        codes and scales of a block then lie next to one another, in whole lines of memory for attend4."""
         n, bs, heads, _ = self._cache_shape
 
         def zeros(dtype, *inner):
