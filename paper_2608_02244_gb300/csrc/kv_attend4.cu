@@ -171,9 +171,9 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         here.x = slice_start<kSlice>(here.s, here.i);
     }
 
-    // ---- the ring: keys and values of a slice, one stage each.  A slice is four times eight tokens, each eight in one
-    // block; of the first sixteen lanes each finds where one kind (keys' codes and scales, values' codes and scales) of
-    // one eight lies, and looks up its block a slice ahead of that.
+    // ---- the ring: keys and values of a slice, one stage each.  A slice is four or eight times eight tokens, each eight in
+    // one block; a lane for each eight and kind (keys' codes and scales, values' codes and scales) finds where it lies, and
+    // looks up its block a slice ahead of that.
     const uint32_t ring = smem_at(smem) + warp * S::kStages * S::kStageBytes;
     const int slot_mask = (1 << g.shift) - 1, kind = (lane / kEights) & 3, my_eight = lane % kEights;
     // whether something is seen of a lane's eight tokens

@@ -112,7 +112,6 @@ cudaError_t launch_append(const AppendArgs &a, int head_dim, int type, int sms, 
 cudaError_t launch_append4(const AppendArgs &a, int head_dim, int type, int sms, cudaStream_t st);
 
 // ---- read4 (kv_read4.cu)
-constexpr int kGroup4 = 32;       // values of a group of a cache in 4 bits
 struct Read4Args {
     isjl_kv_read4_args a;
     isjl_kv_cache4 cache;
@@ -177,7 +176,6 @@ size_t attend_smem(int head_dim, int n);
 cudaError_t prepare_attend(int head_dim, int type, int *blocks, int *queries);
 cudaError_t launch_attend(const AttendArgs &g, void *encoder, int head_dim, int type, int grid, cudaStream_t st);
 
-
 // ---- attend4 (kv_attend4.cu)
 struct Attend4Args {
     isjl_kv_attend_args a;
@@ -185,7 +183,7 @@ struct Attend4Args {
     int32_t n_blocks, shift, n_kv_heads, group;
     float *part_o;                // [warps][2][16][head_dim] pieces of (query, key head) items: one that began earlier, one
     float2 *part_ml;              // [warps][2][16]           that goes on
-    CutItem *cut;                 // [warps] items that begin in a warp's run and are cut by its end
+    CutItem *cut;                 // [warps] items that begin in a warp's run and are cut by its end; first and last are teams
     int32_t *status;
 };
 // once for a shape, before its first launch; warps: most of a call
