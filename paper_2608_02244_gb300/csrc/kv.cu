@@ -356,6 +356,8 @@ isjl_status isjl_kv_read4(isjl_kv *kv, const isjl_kv_read4_args *a, const isjl_k
 
 isjl_status isjl_kv_attend4(isjl_kv *kv, const isjl_kv_attend_args *a, const isjl_kv_cache4 *cache, void *stream) {
     if (!attend_ok(kv, a) || !cache4_ok(kv, cache)) return ISJL_ERR_INVALID_ARG;
+    // each query has a place of the line beside its slices
+    if (a->n * ((((int64_t)a->table_width + a->n_prefix_blocks) << kv->shift) / 32 + 3) > INT32_MAX) return ISJL_ERR_INVALID_ARG;
     if (a->n == 0) return ISJL_OK;
     isjl::Attend4Args g;
     std::memset(&g, 0, sizeof(g));

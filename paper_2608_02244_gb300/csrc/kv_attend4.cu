@@ -1,7 +1,7 @@
 // kv_attend4.cu -- attention of single queries over a paged cache in 4 bits (isjl_kv_attend4).
 //
 // The work is a line of slices of 32 or 64 tokens of each query.  The grid's warps are teams, a warp for each key head, and
-// every team has an equal run of the line, wherever requests end.  A team's warps go over the same tokens at about the same
+// every team has an equal run of the line, wherever requests end, with what a query takes beside its slices counted in.  A team's warps go over the same tokens at about the same
 // time, each by itself: where a token's heads lie side by side in memory, they share lines of it, of which a head's codes
 // and scales are a part only (with a run of one head's slices for each warp, 128 queries over 4,096 tokens of 8 heads took
 // 320 us in that order and 148 with a block's heads apart).  A slice's codes and scales come by asynchronous copies of 16
@@ -18,7 +18,7 @@
 //   multiplication and addition their values, in the order in which the instruction wants them;
 // - weights go from the first product's layout to the second's by a transposition in the warp (movmatrix).
 //
-// 512 queries of 64 + 8 heads of 128 values over 1.1 million tokens, 1.6 GB: 333 us, 4.8 TB/s; 690 instructions for 32 tokens
+// 512 queries of 64 + 8 heads of 128 values over 1.1 million tokens, 1.6 GB: 329 us, 4.8 TB/s; 690 instructions for 32 tokens
 // of a key head (290 make numbers of codes, 32 are products), issue slots 58% busy, the ALU 51%, the tensor pipe 21%.  128
 // queries over 4,096 tokens with 4 query heads on each of 8 key heads 150 us (4.5 TB/s), 16 on each of 4 106; 256 values, 4
 // on each of 4, 154 (4.4 TB/s).
@@ -32,6 +32,10 @@ namespace isjl {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kJoinThreads = 256;
+// A query's beginning and end, in slices, which the runs count with them: places of the line in front of its slices.  With 0,
+// 1 and 2 of them 256 queries of 1 to 6,144 tokens (32 + 8 heads of 128 values) took 92.4, 88.7 and 90.7 us, 512 of up to 8,192
+// (64 + 8 heads) 336, 329 and 331.
+constexpr int kExtra = 1;
 
 template <int D, int kTiles>
 struct Shape {
@@ -103,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     using S = Shape<D, kTiles>;
     constexpr int kSlice = S::kSlice, kEights = S::kEights;
     extern __shared__ __align__(128) unsigned char smem[];
-    int32_t *before = reinterpret_cast<int32_t *>(smem + S::kRing);                  // [n + 1] slices before a query
+    int32_t *before = reinterpret_cast<int32_t *>(smem + S::kRing);                  // [n + 1] places before a query
     __shared__ int32_t warp_sum[kWarps];
     __shared__ const unsigned char *eight_at[kWarps][4 * kEights];
     __shared__ int64_t eight_stride[kWarps][4][3];
@@ -113,13 +117,13 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     const float scale = a.scale * kLog2e;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    // ---- slices before each query
+    // ---- places of the line before each query
     {
         const int per = (n + kThreads - 1) / kThreads;
         const int begin = min(n, (int)threadIdx.x * per), end = min(n, begin + per);
         int32_t sum = 0;
         for (int t = begin; t < end; ++t) {
-            const int32_t k = sight<kSlice>(g, t).slices;
+            const int32_t k = sight<kSlice>(g, t).slices + kExtra;
             before[t] = k;
             sum += k;
         }
@@ -158,18 +162,24 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
         if (++p.t < n) p.s = sight<kSlice>(g, p.t);
         p.x = slice_start<kSlice>(p.s, 0);
     };
-    At here;
-    {
+    // the query that place f of the line is one of
+    auto query_at = [&](int64_t f) {
         int lo = 0, hi = n;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (before[mid] <= f0) lo = mid; else hi = mid;
+            if (before[mid] <= f) lo = mid; else hi = mid;
         }
-        here.t = lo;
-        here.s = sight<kSlice>(g, lo);
-        here.i = (int)(f0 - before[lo]);
-        here.x = slice_start<kSlice>(here.s, here.i);
-    }
+        return lo;
+    };
+    // slices before place f
+    auto slices_before = [&](int64_t f, int t) { return before[t] - (int64_t)kExtra * t + max((int64_t)0, f - before[t] - kExtra); };
+    At here;
+    here.t = query_at(f0);
+    const int slices = (int)(slices_before(f1, f1 == W ? n - 1 : query_at(f1)) - slices_before(f0, here.t));
+    if (slices == 0) return;
+    here.s = sight<kSlice>(g, here.t);
+    here.i = max(0, (int)(f0 - before[here.t]) - kExtra);
+    here.x = slice_start<kSlice>(here.s, here.i);
 
     // ---- the ring: keys and values of a slice, one stage each.  A slice is four or eight times eight tokens, each eight in
     // one block; a lane for each eight and kind (keys' codes and scales, values' codes and scales) finds where it lies, and
@@ -193,7 +203,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
             eight_stride[warp][kind][i] = (kind == 0 ? g.cache.k_stride : kind == 1 ? g.cache.k_scale_stride : kind == 2 ? g.cache.v_stride : g.cache.v_scale_stride)[i] << (kind & 1);
     __syncwarp();
     At ahead = here;
-    int ahead_left = (int)(f1 - f0);                   // slices whose values are still to be asked for
+    int ahead_left = slices;                           // slices whose values are still to be asked for
     int32_t ahead_block = block_of(ahead);
     constexpr uint32_t kAll = (1u << kEights) - 1;
     uint32_t ahead_there = 0;                          // which of its eights are read: the others are zeros
@@ -471,14 +481,15 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     };
 
     begin_item();
-    for (int left = (int)(f1 - f0); left > 0; --left) {
+    int begun = here.i;                                // the slice that this warp's part of the item begins with
+    for (int left = slices; left > 0; --left) {
         slice();
         const bool ends = here.i + 1 == here.s.slices;
         if (ends || left == 1) {
-            const int64_t i0 = before[here.t];
-            end_item(i0 >= f0, ends);
-            if (!ends && i0 >= f0 && lane == 0)         // its pieces are those of the teams from here on
-                g.cut[me] = {here.t, head, (int)team, (int)(((i0 + here.s.slices) * C - 1) / W)};
+            end_item(begun == 0, ends);
+            if (!ends && begun == 0 && lane == 0)       // its pieces are those of the teams from here on
+                g.cut[me] = {here.t, head, (int)team, (int)(((int64_t)before[here.t + 1] * C - 1) / W)};
+            begun = 0;
         }
         if (left > 1) {
             advance(here);

@@ -113,6 +113,9 @@ int main() {
         SAME(isjl_kv_attend4(&h, &a, nullptr, nullptr), bad);
         a = good; a.n = 5; SAME(isjl_kv_attend4(&h, &a, &c4, nullptr), bad);
         a = good; a.n_table_rows = 0; SAME(isjl_kv_attend4(&h, &a, &c4, nullptr), bad);
+        h.cfg.max_rows = 4096;                     // slices, and a place for each query, are counted in 32 bits
+        a = good; a.n = a.n_table_rows = 4096; a.table_width = 1048570; SAME(isjl_kv_attend4(&h, &a, &c4, nullptr), bad);
+        h.cfg.max_rows = 4;
         a = good; a.table_width = 1 << 27; SAME(isjl_kv_attend4(&h, &a, &c4, nullptr), bad);
         a = good; a.n_prefix_blocks = 1; SAME(isjl_kv_attend4(&h, &a, &c4, nullptr), bad);
         a = good; a.scale = -1.f; SAME(isjl_kv_attend4(&h, &a, &c4, nullptr), bad);
