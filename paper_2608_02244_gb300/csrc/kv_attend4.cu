@@ -4,7 +4,7 @@
 // every team has an equal run of the line, wherever requests end, with what a query takes beside its slices counted in.  A team's warps go over the same tokens at about the same
 // time, each by itself: where a token's heads lie side by side in memory, they share lines of it, of which a head's codes
 // and scales are a part only (with a run of one head's slices for each warp, 128 queries over 4,096 tokens of 8 heads took
-// 320 us in that order and 148 with a block's heads apart).  A slice's codes and scales come by asynchronous copies of 16
+// 320 us in that order and 148 with a block's heads apart; now 151 and 148).  A slice's codes and scales come by asynchronous copies of 16
 // bytes through a ring of the warp's own, keys and values in turn.  Items cut by the runs' ends leave pieces, which a second
 // kernel joins in their order.
 //
@@ -20,8 +20,8 @@
 //
 // 512 queries of 64 + 8 heads of 128 values over 1.1 million tokens, 1.6 GB: 329 us, 4.8 TB/s; 690 instructions for 32 tokens
 // of a key head (290 make numbers of codes, 32 are products), issue slots 58% busy, the ALU 51%, the tensor pipe 21%.  128
-// queries over 4,096 tokens with 4 query heads on each of 8 key heads 150 us (4.5 TB/s), 16 on each of 4 106; 256 values, 4
-// on each of 4, 154 (4.4 TB/s).
+// queries over 4,096 tokens with 4 query heads on each of 8 key heads 148 us (4.5 TB/s), 16 on each of 4 106; 256 values, 4
+// on each of 4, 151 (4.5 TB/s).
 #include "kv_four.cuh"
 #include "kv_sight.cuh"
 
@@ -613,14 +613,18 @@ cudaError_t prepare_of(int sms, int *warps) {
 }
 
 // 8 query heads at a time, or 16 where a key head has more, which then is read once for 16: 4 key heads with 16 query heads
-// each, 128 queries over 4,096 tokens, 106 us against 150 in two times 8 (256 values: 278 and 302).
+// each, 128 queries over 4,096 tokens, 106 us against 150 in two times 8.  Not with 256 values, where 16 heads' sums do not
+// fit the registers: 306 us against 286.
+template <int D>
+bool sixteen(int group) { return D < 256 && group > 8; }
+
 template <int D, typename T>
 cudaError_t prepare_tiles(int group, int sms, int *warps) {
-    return group <= 8 ? prepare_of<D, T, 1>(sms, warps) : prepare_of<D, T, 2>(sms, warps);
+    return sixteen<D>(group) ? prepare_of<D, T, D < 256 ? 2 : 1>(sms, warps) : prepare_of<D, T, 1>(sms, warps);
 }
 template <int D, typename T>
 cudaError_t launch_tiles(const Attend4Args &g, int sms, cudaStream_t st) {
-    return g.group <= 8 ? launch_of<D, T, 1>(g, sms, st) : launch_of<D, T, 2>(g, sms, st);
+    return sixteen<D>(g.group) ? launch_of<D, T, D < 256 ? 2 : 1>(g, sms, st) : launch_of<D, T, 1>(g, sms, st);
 }
 
 }  // namespace
