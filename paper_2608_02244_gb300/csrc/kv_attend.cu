@@ -106,21 +106,20 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
         if (++p.t < n) p.s = sight(g, p.t);
     };
 
-    // ---- the ring: keys and values of a slice, one stage each.  A lane has one copy of a stage: the rows of one
-    // of the slice's blocks, or all of them where the block is larger.
+    // ---- the ring: keys and values of a slice, one stage each.  A copy is the rows of one of the slice's blocks, or all of
+    // them where the block is larger; a lane for each looks up its block, and one thread issues them.
     const uint32_t ring = smem_addr(smem) + warp * S::kStages * S::kStageBytes;
     const int32_t prefix_blocks = g.line.blocks ? 0 : a.n_prefix_blocks;
-    const int rows_shift = min(g.shift, 5), piece = lane;
-    const bool copies = piece < (kSlice >> rows_shift);
+    const int rows_shift = min(g.shift, 5), piece = lane, pieces = kSlice >> rows_shift;     // pieces: 1, 2 or 4
+    const bool looks = piece < pieces, one = elect_one();
     const uint32_t half_bytes = 128u << rows_shift;                    // a copy's rows of 64 values
-    const uint32_t copy_at = ring + piece * S::kHalves * half_bytes;
     // where a row lies in a stage
     auto row_at = [&](int row) { return (row >> rows_shift) * S::kHalves * half_bytes + (row & ((1 << rows_shift) - 1)) * 128; };
     // the number of this lane's block, asked for one slice ahead of the copies that use it and looked at only there
     constexpr int32_t kNone = INT32_MIN;
     auto block_of = [&](const Place &p) {
         const int32_t y = slice_start<kSlice>(p.s, p.i) + (piece << rows_shift);
-        if (!copies || y >= p.s.end || (y + (1 << rows_shift) <= p.s.lo && y >= a.sinks)) return kNone;   // nothing is seen of it
+        if (!looks || y >= p.s.end || (y + (1 << rows_shift) <= p.s.lo && y >= a.sinks)) return kNone;   // nothing is seen of it
         const int32_t j = y >> g.shift;
         return j < prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - prefix_blocks)];
     };
@@ -151,10 +150,14 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
             if (block != kNone) report(g.status);
             block = g.n_blocks;
         }
-        if (lane == 0) bar_expect(bar, S::kStageBytes);
-        if (copies)
-            tma_load(copy_at + stage * S::kStageBytes, ahead_values ? &vmap : &kmap, bar,
-                     slice_start<kSlice>(ahead.s, ahead.i) & ((1 << g.shift) - 1) & ~((1 << rows_shift) - 1), 0, ahead.h / parts, block);
+        const CUtensorMap *const map = ahead_values ? &vmap : &kmap;
+        const int slot = slice_start<kSlice>(ahead.s, ahead.i) & ((1 << g.shift) - 1) & ~((1 << rows_shift) - 1), kv = ahead.h / parts;
+        if (one) bar_expect(bar, S::kStageBytes);
+        for (int p = 0; p < pieces; ++p) {
+            const int32_t b = __shfl_sync(~0u, block, p);
+            if (one) tma_load(ring + stage * S::kStageBytes + p * S::kHalves * half_bytes, map, bar, slot, 0, kv, b);
+        }
+        __syncwarp();
         ahead_values = !ahead_values;
         if (ahead_values) return;
         if (--ahead_left == 0) return;

@@ -232,11 +232,12 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kLoadWarp || warp == kLoadWarp + 1) {
-            // ---- keys by one warp, values by the other: one copy for each cache block (or part of one) of a tile and 64 of its values
+            // ---- keys by one warp, values by the other: one copy for each cache block (or part of one) of a tile and 64 of
+            // its values.  The lanes look up the blocks and one thread issues.
             const int rows = min(1 << g.shift, kKeys), pieces = kKeys / rows;      // pieces: 1 .. 16
             const uint32_t piece_bytes = rows * 128;
-            // this lane's part of a tile: piece lane % pieces, and every 32 / pieces-th half
-            const int piece = lane % pieces;
+            const int piece = lane % pieces;                         // whose block this lane looks up
+            const bool one = elect_one();
             constexpr int32_t kNone = INT32_MIN;
             auto block_of = [&](int j) {
                 const int token = j * kKeys + piece * rows;
@@ -257,7 +258,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                 int coming = block_of(j0);                             // asked for one tile ahead
                 for (int j = j0; j < j0 + count && ok; ++j) {
                     int block = coming;
-                    const int slot = (j * kKeys + piece * rows) & ((1 << g.shift) - 1);
+                    const int slot = j * kKeys & ((1 << g.shift) - 1);             // 0 but in blocks larger than a tile
                     if (j + 1 < j0 + count) coming = block_of(j + 1);
                     if ((uint32_t)block >= (uint32_t)g.n_blocks) {                 // beyond the prefix or the cache: zeros
                         if (block != kNone) report(g.status);
@@ -265,11 +266,15 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                     }
                     ok = __all_sync(~0u, load < stages || bar_wait(bar(full + kFree + stage), turn ^ 1, failed));
                     if (!ok) break;
-                    if (lane == 0) bar_expect(bar(full + stage), S::kTileBytes);
-                    __syncwarp();
-                    for (int half = lane / pieces; half < S::kHalves; half += 32 / pieces)
-                        tma_load(to + stage * S::kTileBytes + half * S::kHalfBytes + piece * piece_bytes, map, bar(full + stage), slot, half,
-                                 head, block);
+                    if (one) bar_expect(bar(full + stage), S::kTileBytes);
+                    for (int p = 0; p < pieces; ++p) {
+                        const int32_t b = __shfl_sync(~0u, block, p);
+                        if (one)
+#pragma unroll
+                            for (int half = 0; half < S::kHalves; ++half)
+                                tma_load(to + stage * S::kTileBytes + half * S::kHalfBytes + p * piece_bytes, map, bar(full + stage), slot, half, head, b);
+                        __syncwarp();
+                    }
                     ++load;
                     if (++stage == stages) { stage = 0; turn ^= 1; }
                 }
@@ -278,7 +283,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
             for (int i = max(0, load - stages); i < load; ++i) bar_wait(bar(full + i % stages), (i / stages) & 1, nullptr);
         } else if (warp == kIssueWarp) {
             // The whole warp runs this loop, so that addresses stay uniform, and one thread of it issues: with the
-            // products of 64 cycles each, their issue has to take less.
+            // products of 64 cycles each, their issue has to take less.  The others wait for that thread each time.
             const bool one = elect_one();
             uint32_t step[2] = {0, 0}, begun[2] = {0, 0};       // weights taken, items begun so far of each row tile
             bool ok = tmem_base == 0;                            // all columns are ours: they begin at 0
@@ -296,6 +301,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                     }
                     commit(bar(kScores + i));
                 }
+                __syncwarp();
             };
             auto sums = [&](int i, int stage, int half, bool add) {
                 const uint32_t b = v_lo + stage * (S::kTileBytes >> 4), a = i * 128, d = 256 + i * 128;
@@ -305,6 +311,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                     for (int k = 0; k < kSteps; ++k)
                         mma_tmem(d, a + (half * kSteps + k) * 8, b + (half * kSteps + k) * (2048 >> 4), high, kSecond, add || half + k > 0);
                 }
+                __syncwarp();
             };
             auto wait = [&](int b, uint32_t phase) { ok = ok && __all_sync(~0u, bar_wait(bar(b), phase, failed)); };
             int k_at = 0, v_at = 0;                              // stages of the tile's keys and values, and their turns
@@ -342,6 +349,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                         sums(i, v_at, 1, true);
                         if (more) scores(i, k_at);
                         else if (one) commit(bar(kSums + i));
+                        __syncwarp();
                     }
                     next(v_at, v_turn, S::kValueStages);
                     if (more) next(k_at, k_turn, S::kKeyStages);

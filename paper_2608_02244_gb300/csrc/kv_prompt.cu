@@ -402,8 +402,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
         if (kTwo) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kLoadWarp || warp == kLoadWarp + 1) {
             // ---- keys by one warp, values by the other: one copy for each cache block (or part of one) of a tile and 64 of
-            // its values.  The lanes look up the blocks and one thread issues: issued by several threads at once, each with
-            // its own operands, copies ended with an illegal address in some builds of this kernel.
+            // its values.  The lanes look up the blocks and one thread issues.
             const int rows = min(1 << g.shift, kKeys), pieces = kKeys / rows;      // pieces: 1 .. 16
             const int piece = lane % pieces;                         // whose block this lane looks up
             const bool one = elect_one();

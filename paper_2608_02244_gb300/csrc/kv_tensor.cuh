@@ -22,11 +22,6 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b, uin
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n}"
                  ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(what), "r"((int)add) : "memory");
 }
-__device__ __forceinline__ bool elect_one() {
-    uint32_t mine;
-    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(mine));
-    return mine != 0;
-}
 __device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }

@@ -47,6 +47,16 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t phase, volatile 
     return true;
 }
 
+// true for one thread of a whole warp
+__device__ __forceinline__ bool elect_one() {
+    uint32_t mine;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(mine));
+    return mine != 0;
+}
+
+// Copies are issued by one thread of a warp, between points where the whole warp is together: the lanes bring the block
+// numbers by shuffles, the other operands are the same for all.  Issued by several threads, each with operands of its own,
+// they ended with an illegal address in some builds of kv_prompt.cu; nothing in the source says which builds would.
 __device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap *map, uint32_t bar, int slot, int half, int head, int block) {
     asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
                  ::"r"(to), "l"(map), "r"(bar), "r"(0), "r"(slot), "r"(half), "r"(head), "r"(block) : "memory");
