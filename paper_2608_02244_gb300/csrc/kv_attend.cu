@@ -116,10 +116,12 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     // where a row lies in a stage
     auto row_at = [&](int row) { return (row >> rows_shift) * S::kHalves * half_bytes + (row & ((1 << rows_shift) - 1)) * 128; };
     // the number of this lane's block, asked for one slice ahead of the copies that use it and looked at only there
-    constexpr int32_t kNone = INT32_MIN;
+    // whether something is seen of that block's part, as it is asked for
+    bool ahead_seen = false;
     auto block_of = [&](const Place &p) {
         const int32_t y = slice_start<kSlice>(p.s, p.i) + (piece << rows_shift);
-        if (!looks || y >= p.s.end || (y + (1 << rows_shift) <= p.s.lo && y >= a.sinks)) return kNone;   // nothing is seen of it
+        ahead_seen = looks && y < p.s.end && (y + (1 << rows_shift) > p.s.lo || y < a.sinks);
+        if (!ahead_seen) return -1;
         const int32_t j = y >> g.shift;
         return j < prefix_blocks ? a.prefix[j] : a.table[(int64_t)p.s.row * a.table_width + (j - prefix_blocks)];
     };
@@ -141,13 +143,13 @@ attend_kernel(const __grid_constant__ AttendArgs g, const __grid_constant__ CUte
     Place ahead = here;
     int64_t ahead_left = f1 - f0;                      // slices whose values are still to be asked for
     bool ahead_values = false;                         // what is next: keys or values
-    int32_t ahead_block = f0 < f1 ? block_of(ahead) : kNone;
+    int32_t ahead_block = f0 < f1 ? block_of(ahead) : -1;
     auto feed = [&](int stage) {
         if (ahead_left == 0) return;
         const uint32_t bar = bar0 + 8 * stage;
         int32_t block = ahead_block;
-        if ((uint32_t)block >= (uint32_t)g.n_blocks) {                 // beyond the cache: zeros
-            if (block != kNone) report(g.status);
+        if ((uint32_t)block >= (uint32_t)g.n_blocks) {                 // not seen, or beyond the cache: zeros
+            if (ahead_seen) report(g.status);
             block = g.n_blocks;
         }
         const CUtensorMap *const map = ahead_values ? &vmap : &kmap;

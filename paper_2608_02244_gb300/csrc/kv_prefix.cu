@@ -238,11 +238,8 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
             const uint32_t piece_bytes = rows * 128;
             const int piece = lane % pieces;                         // whose block this lane looks up
             const bool one = elect_one();
-            constexpr int32_t kNone = INT32_MIN;
-            auto block_of = [&](int j) {
-                const int token = j * kKeys + piece * rows;
-                return token < g.tokens ? g.prefix[token >> g.shift] : kNone;
-            };
+            auto seen = [&](int j) { return j * kKeys + piece * rows < g.tokens; };      // of tile j
+            auto block_of = [&](int j) { return seen(j) ? g.prefix[(j * kKeys + piece * rows) >> g.shift] : -1; };
             // A ring for each: a stage's turns are one warp's, which cannot be two turns ahead of itself.
             const bool values = warp != kLoadWarp;
             const int stages = values ? S::kValueStages : S::kKeyStages, full = values ? kValueFull : kKeyFull;
@@ -261,7 +258,7 @@ prefix_kernel(const __grid_constant__ PrefixArgs g, const __grid_constant__ CUte
                     const int slot = j * kKeys & ((1 << g.shift) - 1);             // 0 but in blocks larger than a tile
                     if (j + 1 < j0 + count) coming = block_of(j + 1);
                     if ((uint32_t)block >= (uint32_t)g.n_blocks) {                 // beyond the prefix or the cache: zeros
-                        if (block != kNone) report(g.status);
+                        if (seen(j)) report(g.status);
                         block = g.n_blocks;
                     }
                     ok = __all_sync(~0u, load < stages || bar_wait(bar(full + kFree + stage), turn ^ 1, failed));
