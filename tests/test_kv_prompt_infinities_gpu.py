@@ -91,3 +91,14 @@ def test_infinities_in_items_in_pieces(counts, before, hq, hkv, dim, dtype):
               (row, b + n // 2, 0, 8, math.inf)])
     s = prompts(counts, before, hq, hkv, dim, 32, dtype, seed=5)
     check(s, [(row, b - 4000 + (n + 1) // 2, 0, 5, math.inf), (row, b, 0, 6, -math.inf)], window=4000)
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, "float16"), (128, "bfloat16"), (128, "float16"), (256, "bfloat16")])
+@pytest.mark.parametrize("sight", SIGHTS)
+def test_infinities_in_whole_items(dim, dtype, sight):
+    """So many items that most lie whole in a block's run."""
+    rows = 160
+    s = prompts([300, 40] * (rows // 2), [50, 0] * (rows // 2), 4, 2, dim, 16, dtype, seed=6)
+    check(s, [x for row in range(0, rows, 2) for x in ((row, 51 + row, row // 2 % 2, 5, math.inf), (row, 60 + row, 1, dim - 1, -math.inf),
+                                                       (row, 225, 0, 7, math.inf), (row, 230, 0, 7, -math.inf),
+                                                       (row + 1, row // 4, 1, 33, math.inf))], **sight)
