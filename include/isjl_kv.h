@@ -147,7 +147,8 @@ typedef struct {
  * the query is the last of them.  Of the P + x it sees the last `window` (all if
  * window is 0) and the first `sinks`.  With s = scale * q . k over those,
  * out = sum exp(s) v / sum exp(s) and lse = log(sum exp(s)).  A query with
- * lens[t] <= 0 or rows[t] < 0 sees nothing: out 0, lse -infinity. */
+ * lens[t] <= 0 or rows[t] < 0 sees nothing: out 0, lse -infinity.  out may be q
+ * itself (its strides then q's). */
 typedef struct {
     int32_t n;                   /* queries, 0..max_rows */
     int32_t n_table_rows;
@@ -174,7 +175,8 @@ typedef struct {
  * window is 0) and the first `sinks`.  out and lse are isjl_kv_attend's formulas.
  * starts, lens and table are as isjl_kv_assign leaves them (starts, lens_out), so
  * that a step is assign, append and prompt.  What q holds beyond starts[n_rows] does
- * not matter, what out and lse hold there stays.
+ * not matter, what out and lse hold there stays.  out may be q itself (its strides
+ * then q's).
  *
  * Reported by isjl_kv_status: a row whose starts do not ascend in 0..n_tokens is
  * skipped, its outputs are left as they were; a row with fewer own tokens than

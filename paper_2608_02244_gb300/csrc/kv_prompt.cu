@@ -352,6 +352,30 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
             const int64_t query = x.start + token, at = ((int64_t)(2 * blockIdx.x + ((x.kind & kFirst) != 0)) * kGroups + group) * kRows + row;
             const int q_head = x.q_head + member;
             T *out = static_cast<T *>(g.a.out) + query * g.a.out_stride[0] + q_head * g.a.out_stride[1];
+            // what was left out, all of it before any result is written: weights are computed from q, which out may be
+            if (left_out) {
+#pragma unroll 1
+                for (int c = 0; c < D / kSpoilt; ++c) {
+                    uint32_t o[kSpoilt];
+                    __syncwarp();
+                    tmem_load(o, o_at + kSpoilt * c);
+                    tmem_load_wait();
+                    if (live) {
+                        const Spoilt y = spoilt<D, T>(g, shape, x, token, q_head, kSpoilt * c, top, scale);
+#pragma unroll
+                        for (int i = 0; i < kSpoilt; ++i) {
+                            float z = __uint_as_float(o[i]);
+                            if (y.plus >> i & 1) z += INFINITY;
+                            if (y.minus >> i & 1) z -= INFINITY;
+                            if (y.none >> i & 1) z = NAN;
+                            o[i] = __float_as_uint(z);
+                        }
+                    }
+                    __syncwarp();
+                    tmem_store(o_at + kSpoilt * c, o);
+                }
+                tmem_store_wait();
+            }
             // Few columns at a time: with 32, 2 to 3% slower in short items, with all under way together 5%, since this code
             // is fetched anew for each item.
 #pragma unroll 1
@@ -360,17 +384,6 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                 __syncwarp();
                 tmem_load(o, o_at + kColumns * c);
                 tmem_load_wait();
-                if (live && left_out) {
-                    const Spoilt y = spoilt<D, T>(g, shape, x, token, q_head, kColumns * c, top, scale);
-#pragma unroll
-                    for (int i = 0; i < kColumns; ++i) {
-                        float z = __uint_as_float(o[i]);
-                        if (y.plus >> i & 1) z += INFINITY;
-                        if (y.minus >> i & 1) z -= INFINITY;
-                        if (y.none >> i & 1) z = NAN;
-                        o[i] = __float_as_uint(z);
-                    }
-                }
                 if (live && whole) {
                     uint4 w[2];
 #pragma unroll

@@ -10,6 +10,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kColumns = 16;                        // of a row's sums that are written at a time
+constexpr int kSpoilt = 32;                         // of a row's sums that values not finite are added to at a time
 constexpr int kMostRuns = 1024;                     // blocks that have a run, at most
 constexpr int kJoinBlocks = 8, kJoinThreads = 128;  // of the joining kernel, for each SM
 
@@ -111,7 +112,7 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
     return ((w & kExponent) + kLowest) & 0x80008000u;
 }
 
-// Of the values that the sums left out because they are not finite: what they make of kColumns columns' sums, a bit each
+// Of the values that the sums left out because they are not finite: what they make of kSpoilt columns' sums, a bit each
 // (infinite, the other sign's, undefined).  Rare and slow: the row's weights are computed again from the cache.
 struct Spoilt {
     uint32_t plus, minus, none;
@@ -131,7 +132,7 @@ __device__ __forceinline__ Spoilt spoilt(const PromptArgs &g, const PromptShape 
             const T *v = static_cast<const T *>(g.cache.v) + block * g.cache.v_stride[0] + slot * g.cache.v_stride[1] + x.kv * g.cache.v_stride[2] + column;
             bool any = false;
 #pragma unroll 1
-            for (int i = 0; i < kColumns / 2; ++i) any = any || not_finite<T>(reinterpret_cast<const uint32_t *>(v)[i]);
+            for (int i = 0; i < kSpoilt / 2; ++i) any = any || not_finite<T>(reinterpret_cast<const uint32_t *>(v)[i]);
             if (!any) continue;
             const T *k = static_cast<const T *>(g.cache.k) + block * g.cache.k_stride[0] + slot * g.cache.k_stride[1] + x.kv * g.cache.k_stride[2];
             const T *q = static_cast<const T *>(g.a.q) + (int64_t)(x.start + token) * g.a.q_stride[0] + (int64_t)q_head * g.a.q_stride[1];
@@ -143,7 +144,7 @@ __device__ __forceinline__ Spoilt spoilt(const PromptArgs &g, const PromptShape 
             }
             const bool counts = ex2(dot * scale - (top == -INFINITY ? 0.f : top)) > 0.f;       // 0 times infinity is undefined
 #pragma unroll 1
-            for (int i = 0; i < kColumns; ++i) {
+            for (int i = 0; i < kSpoilt; ++i) {
                 const float z = Half<T>::unpack(reinterpret_cast<const uint16_t *>(v)[i]).x;
                 if (z - z == 0.f) continue;
                 if (!counts || z != z) out.none |= 1u << i;
