@@ -12,6 +12,7 @@ struct isjl_kv {
     int device = 0;                      // whose memory and kernels these are: calls with another one current are refused
     int sms = 0, shift = 0;
     int per_sm = 0, full = 0;            // the attention's blocks of an SM, with at most `full` queries
+    int per_sm4 = 0, full4 = 0;          // attend4's
     // one allocation: the status word, then the workspaces of assign and attend
     unsigned char *d_work = nullptr;
     int32_t *d_status = nullptr;
@@ -239,7 +240,8 @@ isjl_status isjl_kv_create(const isjl_kv_config *cfg, isjl_kv **out) {
         return ISJL_ERR_CUDA;
     }
     int warps4 = 0;
-    if (isjl::prepare_attend4(cfg->head_dim, cfg->type, cfg->n_q_heads / cfg->n_kv_heads, kv->sms, &warps4) != cudaSuccess) {
+    if (isjl::prepare_attend4(cfg->head_dim, cfg->type, cfg->n_q_heads / cfg->n_kv_heads, kv->sms, &kv->per_sm4, &kv->full4, &warps4) !=
+            cudaSuccess || kv->per_sm4 < 1) {
         cudaGetLastError();
         delete kv;
         return ISJL_ERR_CUDA;
@@ -372,7 +374,8 @@ isjl_status isjl_kv_attend4(isjl_kv *kv, const isjl_kv_attend_args *a, const isj
     g.part_ml = kv->d_part_ml;
     g.cut = kv->d_cut;
     g.status = kv->d_status;
-    return launched(isjl::launch_attend4(g, kv->cfg.head_dim, kv->cfg.type, kv->sms, static_cast<cudaStream_t>(stream)));
+    const int grid = kv->sms * (a->n <= kv->full4 || kv->per_sm4 == 1 ? kv->per_sm4 : kv->per_sm4 - 1);
+    return launched(isjl::launch_attend4(g, kv->cfg.head_dim, kv->cfg.type, grid, static_cast<cudaStream_t>(stream)));
 }
 
 isjl_status isjl_kv_prompt(isjl_kv *kv, const isjl_kv_prompt_args *a, const isjl_kv_cache *cache, void *stream) {

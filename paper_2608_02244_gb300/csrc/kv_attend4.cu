@@ -574,10 +574,6 @@ __global__ void __launch_bounds__(kJoinThreads) join4_kernel(const __grid_consta
     }
 }
 
-// what fits the SMs at a time, and a warp for each of 1024 heads at least
-template <int D, int kTiles>
-int grid_of(int sms) { return std::max(Shape<D, kTiles>::kBlocks * sms, 1024 / kWarps); }
-
 template <int D, int kTiles>
 size_t smem_of(int n) { return Shape<D, kTiles>::kRing + (size_t)(n + 1) * sizeof(int32_t); }
 
@@ -597,19 +593,34 @@ cudaError_t launch_early(void (*kernel)(Args...), int grid, int threads, size_t 
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// Blocks: what fits the SMs at a time, and a warp for each head (or part of one) at least.  Runs are equal, so blocks that
+// begin when others have ended cost a second time: 4,096 queries of 400 tokens (32 + 8 heads of 128 values), of whose places
+// two blocks hold all that an SM has, 584 us, and 693 with a grid of three; 256 values, one block, 727 and 735 with two.
 template <int D, typename T, int kTiles>
-cudaError_t launch_of(const Attend4Args &g, int sms, cudaStream_t st) {
-    const int grid = grid_of<D, kTiles>(sms);
+cudaError_t launch_of(const Attend4Args &g, int grid, cudaStream_t st) {
+    const int heads = g.n_kv_heads * ((g.group + 8 * kTiles - 1) / (8 * kTiles));
+    grid = std::max(grid, (heads + kWarps - 1) / kWarps);
     const cudaError_t e = launch_early(attend4_kernel<D, T, kTiles>, grid, kThreads, smem_of<D, kTiles>(g.a.n), st, false, g);
     if (e != cudaSuccess) return e;
     return launch_early(join4_kernel<D, T, kTiles>, grid * kWarps, kJoinThreads, 0, st, true, g);
 }
 
 template <int D, typename T, int kTiles>
-cudaError_t prepare_of(int sms, int *warps) {
-    *warps = grid_of<D, kTiles>(sms) * kWarps;
+cudaError_t prepare_of(int sms, int *blocks, int *queries, int *warps) {
+    const auto kernel = attend4_kernel<D, T, kTiles>;
     // the limit belongs to the function, not to a handle: always the largest
-    return cudaFuncSetAttribute(attend4_kernel<D, T, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<D, kTiles>(ISJL_KV_MAX_ROWS));
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<D, kTiles>(ISJL_KV_MAX_ROWS));
+    int lo = 1, hi = ISJL_KV_MAX_ROWS + 1, per = 0;
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(blocks, kernel, kThreads, smem_of<D, kTiles>(1));
+    *blocks = std::min(*blocks, Shape<D, kTiles>::kBlocks);
+    while (e == cudaSuccess && hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kThreads, smem_of<D, kTiles>(mid));
+        if (per >= *blocks) lo = mid; else hi = mid;
+    }
+    *queries = lo;
+    *warps = std::max(*blocks * sms * kWarps, 1024);
+    return e;
 }
 
 // 8 query heads at a time, or 16 where a key head has more, which then is read once for 16: 4 key heads with 16 query heads
@@ -619,30 +630,30 @@ template <int D>
 bool sixteen(int group) { return D < 256 && group > 8; }
 
 template <int D, typename T>
-cudaError_t prepare_tiles(int group, int sms, int *warps) {
-    return sixteen<D>(group) ? prepare_of<D, T, D < 256 ? 2 : 1>(sms, warps) : prepare_of<D, T, 1>(sms, warps);
+cudaError_t prepare_tiles(int group, int sms, int *blocks, int *queries, int *warps) {
+    return sixteen<D>(group) ? prepare_of<D, T, D < 256 ? 2 : 1>(sms, blocks, queries, warps) : prepare_of<D, T, 1>(sms, blocks, queries, warps);
 }
 template <int D, typename T>
-cudaError_t launch_tiles(const Attend4Args &g, int sms, cudaStream_t st) {
-    return sixteen<D>(g.group) ? launch_of<D, T, D < 256 ? 2 : 1>(g, sms, st) : launch_of<D, T, 1>(g, sms, st);
+cudaError_t launch_tiles(const Attend4Args &g, int grid, cudaStream_t st) {
+    return sixteen<D>(g.group) ? launch_of<D, T, D < 256 ? 2 : 1>(g, grid, st) : launch_of<D, T, 1>(g, grid, st);
 }
 
 }  // namespace
 
-cudaError_t prepare_attend4(int head_dim, int type, int group, int sms, int *warps) {
+cudaError_t prepare_attend4(int head_dim, int type, int group, int sms, int *blocks, int *queries, int *warps) {
     if (type == ISJL_KV_BF16)
-        return head_dim == 64 ? prepare_tiles<64, __nv_bfloat16>(group, sms, warps)
-             : head_dim == 128 ? prepare_tiles<128, __nv_bfloat16>(group, sms, warps) : prepare_tiles<256, __nv_bfloat16>(group, sms, warps);
-    return head_dim == 64 ? prepare_tiles<64, __half>(group, sms, warps)
-         : head_dim == 128 ? prepare_tiles<128, __half>(group, sms, warps) : prepare_tiles<256, __half>(group, sms, warps);
+        return head_dim == 64 ? prepare_tiles<64, __nv_bfloat16>(group, sms, blocks, queries, warps)
+             : head_dim == 128 ? prepare_tiles<128, __nv_bfloat16>(group, sms, blocks, queries, warps) : prepare_tiles<256, __nv_bfloat16>(group, sms, blocks, queries, warps);
+    return head_dim == 64 ? prepare_tiles<64, __half>(group, sms, blocks, queries, warps)
+         : head_dim == 128 ? prepare_tiles<128, __half>(group, sms, blocks, queries, warps) : prepare_tiles<256, __half>(group, sms, blocks, queries, warps);
 }
 
-cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, int sms, cudaStream_t st) {
+cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, int grid, cudaStream_t st) {
     if (type == ISJL_KV_BF16)
-        return head_dim == 64 ? launch_tiles<64, __nv_bfloat16>(g, sms, st)
-             : head_dim == 128 ? launch_tiles<128, __nv_bfloat16>(g, sms, st) : launch_tiles<256, __nv_bfloat16>(g, sms, st);
-    return head_dim == 64 ? launch_tiles<64, __half>(g, sms, st)
-         : head_dim == 128 ? launch_tiles<128, __half>(g, sms, st) : launch_tiles<256, __half>(g, sms, st);
+        return head_dim == 64 ? launch_tiles<64, __nv_bfloat16>(g, grid, st)
+             : head_dim == 128 ? launch_tiles<128, __nv_bfloat16>(g, grid, st) : launch_tiles<256, __nv_bfloat16>(g, grid, st);
+    return head_dim == 64 ? launch_tiles<64, __half>(g, grid, st)
+         : head_dim == 128 ? launch_tiles<128, __half>(g, grid, st) : launch_tiles<256, __half>(g, grid, st);
 }
 
 }  // namespace isjl

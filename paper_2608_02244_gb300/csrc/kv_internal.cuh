@@ -186,9 +186,9 @@ struct Attend4Args {
     CutItem *cut;                 // [warps] items that begin in a warp's run and are cut by its end; first and last are teams
     int32_t *status;
 };
-// once for a shape, before its first launch; warps: most of a call
-cudaError_t prepare_attend4(int head_dim, int type, int group, int sms, int *warps);
-cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, int sms, cudaStream_t st);
+// once for a shape, before its first launch: as prepare_attend; warps: most of a call
+cudaError_t prepare_attend4(int head_dim, int type, int group, int sms, int *blocks, int *queries, int *warps);
+cudaError_t launch_attend4(const Attend4Args &g, int head_dim, int type, int grid, cudaStream_t st);
 
 // ---- prompt (kv_prompt.cu)
 // an item that the end of its block's run cuts; the blocks up to `last` have a piece of it
