@@ -24,6 +24,7 @@
 // on each of 4, 151 (4.5 TB/s).
 #include "kv_four.cuh"
 #include "kv_sight.cuh"
+#include "kv_tma.cuh"
 
 #include <algorithm>
 #include <type_traits>
@@ -50,8 +51,6 @@ struct Shape {
     static constexpr int kRing = kWarps * kStages * kStageBytes;
     static constexpr int kBlocks = D == 256 || kTiles == 2 ? 2 : 3;      // per SM
 };
-
-__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 template <int kBytes>
 __device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool real) {
@@ -116,7 +115,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     const int n = a.n, parts = (g.group + 8 * kTiles - 1) / (8 * kTiles), H = g.n_kv_heads * parts, hq = g.n_kv_heads * g.group;
     const float scale = a.scale * kLog2e;
 
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    start_next();
     // ---- places of the line before each query
     {
         const int per = (n + kThreads - 1) / kThreads;
@@ -184,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     // ---- the ring: keys and values of a slice, one stage each.  A slice is four or eight times eight tokens, each eight in
     // one block; a lane for each eight and kind (keys' codes and scales, values' codes and scales) finds where it lies, and
     // looks up its block a slice ahead of that.
-    const uint32_t ring = smem_at(smem) + warp * S::kStages * S::kStageBytes;
+    const uint32_t ring = smem_addr(smem) + warp * S::kStages * S::kStageBytes;
     const int slot_mask = (1 << g.shift) - 1, kind = (lane / kEights) & 3, my_eight = lane % kEights;
     // whether something is seen of a lane's eight tokens
     auto seen_of = [&](const At &p) {
@@ -211,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kTiles>::kBlocks)) attend4
     const uint32_t copy_to = ring + chunk_at<D>(lane / S::kChunks, lane % S::kChunks);
     const int64_t code_off[2] = {lane / S::kChunks % 8 * g.cache.k_stride[1] + lane % S::kChunks * 16, lane / S::kChunks % 8 * g.cache.v_stride[1] + lane % S::kChunks * 16};
     const int64_t scale_off[2] = {2 * (lane & 7) * g.cache.k_scale_stride[1], 2 * (lane & 7) * g.cache.v_scale_stride[1]};
-    const uint32_t eights = smem_at(eight_at[warp]);
+    const uint32_t eights = smem_addr(eight_at[warp]);
     auto copies = [&](uint32_t stage, auto values, auto all) {
         constexpr int v = decltype(values)::value;
         const int64_t half = 4 * (v ? g.cache.v_stride : g.cache.k_stride)[1];
@@ -504,7 +503,7 @@ template <int D, typename T, int kTiles>
 __global__ void __launch_bounds__(kJoinThreads) join4_kernel(const __grid_constant__ Attend4Args g) {
     const isjl_kv_attend_args &a = g.a;
     const int parts = (g.group + 8 * kTiles - 1) / (8 * kTiles), H = g.n_kv_heads * parts, hq = g.n_kv_heads * g.group;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_for_previous();
     const CutItem item = g.cut[blockIdx.x];
     if (item.t < 0) return;
     const int kv = item.h / parts, from = kv * g.group + (item.h - kv * parts) * 8 * kTiles, rows = min(8 * kTiles, (kv + 1) * g.group - from);
@@ -577,22 +576,6 @@ __global__ void __launch_bounds__(kJoinThreads) join4_kernel(const __grid_consta
 template <int D, int kTiles>
 size_t smem_of(int n) { return Shape<D, kTiles>::kRing + (size_t)(n + 1) * sizeof(int32_t); }
 
-// a kernel's launch, started while the one before it in the stream ends
-template <typename... Args>
-cudaError_t launch_early(void (*kernel)(Args...), int grid, int threads, size_t smem, cudaStream_t st, bool early, const Args &...args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = early ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 // Blocks: what fits the SMs at a time, and a warp for each head (or part of one) at least.  Runs are equal, so blocks that
 // begin when others have ended cost a second time: 4,096 queries of 400 tokens (32 + 8 heads of 128 values), of whose places
 // two blocks hold all that an SM has, 584 us, and 693 with a grid of three; 256 values, one block, 727 and 735 with two.
@@ -600,9 +583,9 @@ template <int D, typename T, int kTiles>
 cudaError_t launch_of(const Attend4Args &g, int grid, cudaStream_t st) {
     const int heads = g.n_kv_heads * ((g.group + 8 * kTiles - 1) / (8 * kTiles));
     grid = std::max(grid, (heads + kWarps - 1) / kWarps);
-    const cudaError_t e = launch_early(attend4_kernel<D, T, kTiles>, grid, kThreads, smem_of<D, kTiles>(g.a.n), st, false, g);
+    const cudaError_t e = launch_kernel(attend4_kernel<D, T, kTiles>, grid, kThreads, smem_of<D, kTiles>(g.a.n), st, false, g);
     if (e != cudaSuccess) return e;
-    return launch_early(join4_kernel<D, T, kTiles>, grid * kWarps, kJoinThreads, 0, st, true, g);
+    return launch_kernel(join4_kernel<D, T, kTiles>, grid * kWarps, kJoinThreads, 0, st, true, g);
 }
 
 template <int D, typename T, int kTiles>

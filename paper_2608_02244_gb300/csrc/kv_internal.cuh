@@ -62,10 +62,19 @@ struct Grow {
     static constexpr float kPass = Half<T>::kIsBf16 ? 8.f : 4.f, kTop = Half<T>::kTop > 0 ? Half<T>::kTop - kPass : 0.f;
 };
 
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// 1 over a sum of weights, 0 where there were none
+__device__ __forceinline__ float inverse(float total) { return total > 0.f || total != total ? 1.f / total : 0.f; }
+// the logarithm of a sum of exp2, in the natural base
+__device__ __forceinline__ float log_of(float top, float total) {
+    return total > 0.f || total != total ? (top + log2f(total)) * kLn2 : -INFINITY;
 }
 
 // x * y + z of both halves, rounded once

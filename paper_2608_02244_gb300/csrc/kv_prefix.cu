@@ -32,7 +32,6 @@ namespace {
 constexpr int kRows = 128, kKeys = 128;        // of a row tile, of a token tile
 constexpr int kThreads = 384;                  // two groups of four warps; the loading and the issuing warp's group
 constexpr int kLoadWarp = 8, kIssueWarp = 10;
-constexpr float kLog2e = 1.4426950408889634f;
 
 template <int D>
 struct Shape {

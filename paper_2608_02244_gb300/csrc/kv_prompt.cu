@@ -240,7 +240,7 @@ prompt_kernel(const __grid_constant__ PromptArgs g, const __grid_constant__ CUte
                 constexpr int kBehind = kTwo ? 1 : 2;
                 bool lost = false;
                 const bool frees = (group == 1) == two_of(x) && (threadIdx.x & 127) == 0;
-                const int32_t seen_end = x.kind & kDead ? 0 : x.place + token + 1, low = low_of(shape, x.place + token);
+                const int32_t seen_end = x.kind & kDead ? 0 : x.place + token + 1, low = PromptRow::low(shape, x.place + token);
                 for (int j = 0; j < count; ++j, ++step) {
                     ok = kTwo ? wait(kScores + group, step & 1) : wait(kScores + (step & 1), step >> 1 & 1);
                     if (!ok) break;

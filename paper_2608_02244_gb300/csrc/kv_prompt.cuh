@@ -8,7 +8,6 @@
 namespace isjl {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kColumns = 16;                        // of a row's sums that are written at a time
 constexpr int kSpoilt = 32;                         // of a row's sums that values not finite are added to at a time
 constexpr int kMostRuns = 1024;                     // blocks that have a run, at most
@@ -102,8 +101,6 @@ __device__ __forceinline__ bool edge(const PromptShape &s, const Item &x, int32_
     return y0 + s.keys > x.from || (y0 < x.below && y0 + s.keys > s.sinks);
 }
 __device__ __forceinline__ bool edge_token(const PromptShape &s, const Item &x, int32_t y) { return y >= x.from || (y < x.below && y >= s.sinks); }
-// the first place of the window of a query
-__device__ __forceinline__ int32_t low_of(const PromptShape &s, int32_t place) { return s.window && place >= s.window ? place + 1 - s.window : 0; }
 
 // whether one of a word's two 16-bit numbers is infinite or undefined: its exponent's bits are all set
 template <typename T>
@@ -121,7 +118,7 @@ template <int D, typename T>
 __device__ __forceinline__ Spoilt spoilt(const PromptArgs &g, const PromptShape &s, const Item &x, int32_t token, int32_t q_head, int column, float top,
                                          float scale) {
     Spoilt out = {0, 0, 0};
-    const int32_t place = x.place + token, low = low_of(s, place);
+    const int32_t place = x.place + token, low = PromptRow::low(s, place);
     for (int32_t j = 0; j < x.count; ++j) {
         const int32_t y0 = tile_at(s, x, j);
         if (!edge(s, x, y0)) continue;
@@ -153,12 +150,6 @@ __device__ __forceinline__ Spoilt spoilt(const PromptArgs &g, const PromptShape 
         }
     }
     return out;
-}
-
-__device__ __forceinline__ float inverse(float total) { return total > 0.f || total != total ? 1.f / total : 0.f; }
-// the logarithm of a sum of exp2, in the natural base
-__device__ __forceinline__ float log_of(float top, float total) {
-    return total > 0.f || total != total ? (top + log2f(total)) * kLn2 : -INFINITY;
 }
 
 // a / b of numbers that are mostly small: 64 bits take a few hundred cycles
@@ -268,9 +259,9 @@ __device__ __forceinline__ Item take_item(const PromptArgs &g, const PromptShape
     x.tokens = min(p.r.count - first, s.step);
     x.place = p.r.first + first;
     x.end = last + 1;
-    x.low = low_of(s, x.place);
+    x.low = PromptRow::low(s, x.place);
     x.from = p.r.dead ? 0 : x.place + 1;
-    x.below = low_of(s, last);
+    x.below = PromptRow::low(s, last);
     x.kind = (x.count == tiles ? kWhole : 0) | (x.tile0 == 0 ? kFirst : 0) | (p.r.dead ? kDead : 0);
     if (writes && x.count < tiles && x.tile0 == 0)       // its pieces are those of the blocks from here on
         g.cut[blockIdx.x] = {p.row, p.head, p.item, (int)quotient((run.f - p.j + s.extra + tiles) * run.blocks - 1, run.tiles)};

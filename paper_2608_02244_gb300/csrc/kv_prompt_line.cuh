@@ -54,7 +54,7 @@ struct PromptRow {
         return first + (int32_t)(last < count ? last : count);
     }
     // the first place of a query's window
-    ISJL_LINE int32_t low(const PromptShape &s, int32_t place) const { return s.window && place >= s.window ? place + 1 - s.window : 0; }
+    static ISJL_LINE int32_t low(const PromptShape &s, int32_t place) { return s.window && place >= s.window ? place + 1 - s.window : 0; }
     // tiles between the first tokens' and the window's that none of item p's queries sees
     ISJL_LINE int32_t skip(const PromptShape &s, int32_t p) const {
         const int32_t t = low(s, first + p * s.step) / s.keys - s.sink_tiles();

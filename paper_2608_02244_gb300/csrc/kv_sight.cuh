@@ -7,8 +7,6 @@
 namespace isjl {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
 // what a query sees: tokens end - window .. end - 1 and 0 .. sinks - 1, counted from the first token that
 // this kernel reads (the prefix's, or the own ones' where the prefix is done elsewhere)
 struct Sight {
@@ -36,12 +34,6 @@ __device__ __forceinline__ Sight sight_of(const isjl_kv_attend_args &a, int shif
 template <int kSlice>
 __device__ __forceinline__ int32_t slice_start(const Sight &s, int i) {
     return (i < s.head ? i : s.lo / kSlice + i - s.head) * kSlice;
-}
-
-__device__ __forceinline__ float inverse(float total) { return total > 0.f || total != total ? 1.f / total : 0.f; }
-// the logarithm of a sum of exp2, in the natural base
-__device__ __forceinline__ float log_of(float top, float total) {
-    return total > 0.f || total != total ? (top + log2f(total)) * kLn2 : -INFINITY;
 }
 
 // place on the line of slices

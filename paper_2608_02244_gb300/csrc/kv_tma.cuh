@@ -1,4 +1,5 @@
-// kv_tma.cuh -- barriers in shared memory and copies of cache blocks by TMA, for kv_attend.cu and kv_prefix.cu.
+// kv_tma.cuh -- barriers in shared memory, copies of cache blocks and queries by TMA (kv_attend.cu, kv_prefix.cu, kv_prompt.cu),
+// and launches (kv_attend4.cu too).
 #pragma once
 
 #include <cuda.h>
