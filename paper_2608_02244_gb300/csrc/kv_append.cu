@@ -54,12 +54,14 @@ __device__ __forceinline__ uint32_t codes4(const float (&x)[8], uint32_t *scales
     *scales = fine ? Half<T>::pack(s, b) : Half<T>::pack(NAN, NAN);
     uint32_t word = 0;
     if (fine && s > 0.f) {
-        // a scale below the normal numbers: all of it by 2^64, which changes no quotient
-        const float up = s < 0x1p-100f ? 0x1p64f : 1.f, step = s * up * 0.0625f, inv = __fdividef(1.f, step);
+        // A scale below the normal numbers: all of it by 2^64, which changes no quotient.  So do large ones by 2^-4, for
+        // distances d of which 32 bits hold no number.
+        const float up = s < 0x1p-100f ? 0x1p64f : s > 0x1p100f ? 0x1p-4f : 1.f, step = s * up * 0.0625f, inv = __fdividef(1.f, step);
+        const float from = -b * up;
         constexpr float kWhole = 0x1.8p23f;         // a sum with it is rounded to a whole number, ties to even
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float d = (x[i] - b) * up, n = fmaf(d, inv, kWhole), off = fabsf(fmaf(kWhole - n, step, d));
+            const float d = fmaf(x[i], up, from), n = fmaf(d, inv, kWhole), off = fabsf(fmaf(kWhole - n, step, d));
             int c = __float_as_int(n) - __float_as_int(kWhole + 16.f);
             if (off > step * 0.5f || (off == step * 0.5f && (c & 1))) c += d > (n - kWhole) * step ? 1 : -1;
             word |= (uint32_t)min(max(c, 0), 15) << (4 * i);
