@@ -152,7 +152,8 @@ typedef struct {
 typedef struct {
     int32_t n;                   /* queries, 0..max_rows */
     int32_t n_table_rows;
-    int32_t table_width;         /* table_width * block_size + prefix <= 2^31 - 256, and n times that < 2^36 */
+    int32_t table_width;         /* table_width * block_size + prefix, T, is at most 2^31 - 256, and n (T + 64) < 2^36
+                                    (isjl_kv_attend4: n (T + 96)) */
     int32_t n_prefix_blocks;     /* >= 0 */
     int32_t window;              /* >= 0 */
     int32_t sinks;               /* >= 0, used with a window */
@@ -217,8 +218,8 @@ typedef struct {
  *     S / 32 + u (2 |lo| + 4 S)
  * of x (and T's smallest positive number), where u is T's unit roundoff (2^-8 for bf16,
  * 2^-11 for fp16).  A group with an infinite or
- * undefined value has S = B = NaN and stands for NaN; so does, in fp16, one whose S or
- * B is beyond the type (never with values within +-20,000). */
+ * undefined value has S = B = NaN and stands for NaN; so does one whose S or B is
+ * beyond the type (never with values within +-20,000 in fp16, +-10^38 in bf16). */
 typedef struct {
     void *k;
     void *v;

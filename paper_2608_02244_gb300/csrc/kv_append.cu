@@ -202,7 +202,10 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
 
 // Measured, 32 against 128 threads: 2,048 tokens of 32 + 2 x 8 heads of 128 values 15.5 and 12.6 us, 4,096 tokens 21.0 and
 // 22.1, 49,152 tokens 201 and 226; with 28 + 2 x 4 heads of 64 values 5.9 and 6.4 at 2,048 tokens, 5.2 and 4.1 at 1,024.
-// The rule goes by tokens alone and is that of the larger ones: with the smaller ones it loses 0.5 us at 2,048.
+// The rule goes by tokens alone and is that of the larger ones: with the smaller ones it loses 0.5 us at 2,048.  4-bit caches
+// have the same rule, measured inside a graph (an empty one takes 8.8 us): with the larger heads 20.3 and 13.0 us at 1,024
+// tokens, 23.0 and 20.7 at 2,048, 29.2 and 29.2 at 3,584, 128 and 137 at 20,011; with the smaller ones 10.5 and 9.2 at 1,024,
+// 11.2 and 13.0 at 2,048, 13.5 and 18.6 at 3,584, 49 and 79 at 20,011: there it loses 2 to 5 us from 2,048 to 3,647.
 int many_tokens(int sms) { return 24 * sms; }
 
 // A token is a block.  Few tokens: four warps each, which halve its latency.  Many: a warp each, for more of them under

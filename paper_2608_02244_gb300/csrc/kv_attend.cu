@@ -11,9 +11,9 @@
 // kernel joins in their order.  Joining them here, by the last of an item's warps to arrive, took a fence and an
 // atomic under full memory load: 10 to 20 us of stall against 3 us of a small kernel that starts as this one ends.
 //
-// 512 queries of 64 + 8 heads of 128 values, 4 GB of keys and values: 627 us, 6.5 TB/s; 256 queries, 670 MB: 121 us,
+// 512 queries of 64 + 8 heads of 128 values, 4 GB of keys and values: 637 us, 6.4 TB/s; 256 queries, 670 MB: 121 us,
 // 5.5 TB/s (6 us until the rings are full, and SMs that end up to 15% apart).  The tensor pipe is 18% busy.  64 queries
-// of 8 + 8 heads of 256 values, 2.1 GB: 354 us, 6.1 TB/s.  More than 16 query heads on a key head read it again for
+// of 8 + 8 heads of 256 values, 2.1 GB: 356 us, 6.0 TB/s.  More than 16 query heads on a key head read it again for
 // each 16: 256 queries of 16 + 1 heads over 8,192 tokens 214 us, of 64 + 1 heads 706.
 #include "kv_ring.cuh"
 #include "kv_sight.cuh"

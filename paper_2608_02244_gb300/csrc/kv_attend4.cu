@@ -1,12 +1,12 @@
 // kv_attend4.cu -- attention of single queries over a paged cache in 4 bits (isjl_kv_attend4).
 //
 // The work is a line of slices of 32 or 64 tokens of each query.  The grid's warps are teams, a warp for each key head, and
-// every team has an equal run of the line, wherever requests end, with what a query takes beside its slices counted in.  A team's warps go over the same tokens at about the same
-// time, each by itself: where a token's heads lie side by side in memory, they share lines of it, of which a head's codes
-// and scales are a part only (with a run of one head's slices for each warp, 128 queries over 4,096 tokens of 8 heads took
-// 320 us in that order and 148 with a block's heads apart; now 151 and 148).  A slice's codes and scales come by asynchronous copies of 16
-// bytes through a ring of the warp's own, keys and values in turn.  Items cut by the runs' ends leave pieces, which a second
-// kernel joins in their order.
+// every team has an equal run of the line, wherever requests end, with what a query takes beside its slices counted in.  A
+// team's warps go over the same tokens at about the same time, each by itself: where a token's heads lie side by side in
+// memory, they share lines of it, of which a head's codes and scales are a part only (with a run of one head's slices for
+// each warp, 128 queries over 4,096 tokens of 8 heads took 320 us in that order and 148 with a block's heads apart; now 151
+// and 148).  A slice's codes and scales come by asynchronous copies of 16 bytes through a ring of the warp's own, keys and
+// values in turn.  Items cut by the runs' ends leave pieces, which a second kernel joins in their order.
 //
 // 5 bits a value leave a token and head 160 bytes at 128 values, which the memory brings an SM in 7 cycles: what bounds
 // the work is the instructions from codes to products.  So
@@ -18,10 +18,17 @@
 //   multiplication and addition their values, in the order in which the instruction wants them;
 // - weights go from the first product's layout to the second's by a transposition in the warp (movmatrix).
 //
-// 512 queries of 64 + 8 heads of 128 values over 1.1 million tokens, 1.6 GB: 329 us, 4.8 TB/s; 690 instructions for 32 tokens
-// of a key head (290 make numbers of codes, 32 are products), issue slots 58% busy, the ALU 51%, the tensor pipe 21%.  128
-// queries over 4,096 tokens with 4 query heads on each of 8 key heads 148 us (4.5 TB/s), 16 on each of 4 106; 256 values, 4
-// on each of 4, 151 (4.5 TB/s).
+// The weights are rounded to 16 bits for the second product, as its instruction takes them, each by at most half a step of
+// itself; their sum is of the unrounded ones, and scores, maxima, sums and pieces have 32 bits.
+//
+// 512 queries of 64 + 8 heads of 128 values over 1.23 million tokens, 1.58 GB: 329 us, 4.8 TB/s; 690 instructions for 32
+// tokens of a key head (290 make numbers of codes, 32 are products; the rest are the copies, each with a pointer from shared
+// memory and its 64-bit sum, the softmax of eight columns whatever the number of heads, the weights' transposition and the
+// ring's turns), issue slots 58% busy, the ALU 51%, the tensor pipe 21%.  128 queries over 4,096 tokens with 4 query heads on
+// each of 8 key heads 148 us (4.5 TB/s), 16 on each of 4 106; 256 values, 4 on each of 4, 151 (4.5 TB/s).
+//
+// A prefix that the requests share is read and decoded by every query: 64 queries of 32 + 8 heads over 8,192 tokens of it and
+// 256 of their own 147 us, 512 over 2,048 308.
 #include "kv_four.cuh"
 #include "kv_sight.cuh"
 #include "kv_tma.cuh"

@@ -102,3 +102,15 @@ def test_infinities_in_whole_items(dim, dtype, sight):
     check(s, [x for row in range(0, rows, 2) for x in ((row, 51 + row, row // 2 % 2, 5, math.inf), (row, 60 + row, 1, dim - 1, -math.inf),
                                                        (row, 225, 0, 7, math.inf), (row, 230, 0, 7, -math.inf),
                                                        (row + 1, row // 4, 1, 33, math.inf))], **sight)
+
+
+@pytest.mark.parametrize("hq,hkv,dim", [(1, 1, 64), (2, 2, 128), (4, 1, 128), (1, 1, 256)])
+@pytest.mark.parametrize("sight", [dict(), dict(window=700, sinks=3)])
+def test_all_values_undefined(hq, hkv, dim, sight):
+    """The slowest that such values can be, in the longest items: a result all the same, and no wait that gives up."""
+    s = prompts([2048, 300], [700, 0], hq, hkv, dim, 16, seed=8)
+    s["v"].fill_(math.nan)
+    d = decoder(s)
+    out, lse = d.prompt(**s, lse=True, **sight)
+    assert d.status() == 0
+    assert out.isnan().all() and lse.isfinite().all()
